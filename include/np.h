@@ -536,6 +536,164 @@ int np_trunk_forward(const np_trunk_desc* desc, const np_trunk_weights* weights,
                      const int32_t* centroid_id, float* workspace, float* head_logits, void* stream);
 const char* np_trunk_last_error(void);
 
+/* ---- The attention half of a decode step: a paged key-value cache, what manages its pages, and the attention
+ * that reads it.  It stands beside np_step (the MLP half); the paper leaves attention dense and describes none of
+ * this.  No context is needed: the caller owns the cache, its tables and every buffer (all memory of the current
+ * device), calls queue kernels on `stream` and neither synchronise nor allocate, and all of them may be captured
+ * into a graph.  Text of the calling thread's last error: np_attn_last_error().
+ *
+ * A cache holds n_layers layers of n_pages pages; a page holds the keys and the values of page_tokens consecutive
+ * tokens of one sequence:
+ *   cache  dev [n_layers][n_pages][2][n_kv_heads][page_tokens][head_dim]   (keys, then values; 16-byte aligned)
+ * A page number means the same page in every layer.  Tables say whose page is whose:
+ *   page_table[s][i]  page with tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s; -1 past its pages
+ *   lens[s]           tokens of sequence s
+ *   refs[p]           sequences that hold page p; 0 = free
+ * Sequences made by np_kv_fork share their parents' full pages; a partly filled page belongs to one sequence alone,
+ * so np_kv_append of tokens that np_kv_reserve made room for never writes a page that another sequence reads. */
+#define NP_T_BF16 0
+#define NP_T_FP16 1
+#define NP_KV_MAX_SEQS   1024
+#define NP_KV_MAX_PAGES  (1 << 22)
+#define NP_ATTN_MAX_GROUP 128
+
+typedef struct np_kv_desc {
+  int32_t dtype;         /* NP_T_*: of the cache, and of the rows that go in and out */
+  int32_t n_layers;      /* >= 1 */
+  int32_t n_kv_heads;    /* 1..1024 */
+  int32_t head_dim;      /* 64 or 128 */
+  int32_t page_tokens;   /* 16, 32, 64, 128 or 256 */
+  int32_t n_pages;       /* 1..NP_KV_MAX_PAGES */
+  int32_t max_seqs;      /* rows of the page table, 1..NP_KV_MAX_SEQS */
+  int32_t max_pages;     /* entries of a row, 1..n_pages; max_pages * page_tokens < 2^31 */
+  int32_t reserved[4];   /* 0 */
+} np_kv_desc;
+
+/* Device arrays of a cache.  np_kv_reset writes the empty state into all of them. */
+typedef struct np_kv_tables {
+  int32_t* page_table;   /* [max_seqs][max_pages] */
+  int32_t* lens;         /* [max_seqs] */
+  int32_t* refs;         /* [n_pages] */
+  int32_t* scratch;      /* np_kv_sizes_out.scratch_bytes; its contents mean nothing between calls */
+  int32_t* status;       /* [1] bits NP_KV_S_*, set and never cleared by the kernels (np_attn_check reads them) */
+} np_kv_tables;
+
+/* Status bits.  What an entry point cannot know on the host it checks on the device: the sequence or page concerned is
+ * left out, a bit is set, and everything else of the call is done. */
+#define NP_KV_S_PAGE     1   /* a page number outside [0, n_pages) */
+#define NP_KV_S_SEQ      2   /* a sequence number outside [0, max_seqs), listed twice, or a fork's target that holds tokens */
+#define NP_KV_S_LENGTH   4   /* a length that its row of the page table does not hold, or a negative count */
+#define NP_KV_S_TIMEOUT  8   /* a bounded wait ran out: the call's outputs are incomplete */
+#define NP_KV_S_FULL    32   /* not enough free pages */
+
+typedef struct np_kv_sizes_out {
+  uint64_t cache_bytes;    /* all layers */
+  uint64_t page_bytes;     /* one page of one layer */
+  uint64_t table_bytes;    /* page_table */
+  uint64_t scratch_bytes;  /* np_kv_tables.scratch */
+} np_kv_sizes_out;
+
+/* Rows of heads: element (token, head, i) at data[token * token_stride + head * head_stride + i].  Strides in elements,
+ * multiples of 8 and not negative; data 16-byte aligned.  Heads of a projection's output are read in place this way. */
+typedef struct np_rows {
+  void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} np_rows;
+
+/* Buffer sizes for a description.  Pure host arithmetic.  NP_E_INVAL on a bad description. */
+int np_kv_sizes(const np_kv_desc* desc, np_kv_sizes_out* out);
+
+/* Every table entry -1, every length and count 0, the status word 0.  The cache is left as it is. */
+int np_kv_reset(const np_kv_desc* desc, const np_kv_tables* tables, void* stream);
+
+/* Room for n_new[i] (dev [n], >= 0) more tokens in each of the n sequences `seqs` (dev [n], distinct; NULL: 0..n-1).
+ * Pages are taken in list order, the lowest free number first; lengths grow by n_new at once.  A sequence whose pages are
+ * not all there keeps its length and its pages (NP_KV_S_FULL): with the pages counted out in list order, those up to and
+ * including its own are more than are free.  One that needs no page gets its tokens in any case.
+ *   start_out  dev [n] or NULL: the length before, or -1 where the sequence was left as it was (what np_kv_append takes) */
+int np_kv_reserve(const np_kv_desc* desc, const np_kv_tables* tables, const int32_t* seqs, const int32_t* n_new, int32_t n,
+                  int32_t* start_out, void* stream);
+
+/* Writes keys and values of new tokens into their pages of one layer: row cu[i] + j goes to position start[i] + j of
+ * sequence seqs[i], j < cu[i + 1] - cu[i].  Positions at or past the sequence's length are not written, rows from cu[n]
+ * on are not read, and a sequence with start[i] < 0 is passed over.
+ *   k, v   n_tokens rows of n_kv_heads heads
+ *   seqs   dev [n] (NULL: 0..n-1),  cu  dev [n + 1] ascending, from 0 (NULL: one token each, n_tokens == n),  start  dev [n]
+ * Two rows for the same position: one of them is kept. */
+int np_kv_append(const np_kv_desc* desc, void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* k,
+                 const np_rows* v, int32_t n_tokens, const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n,
+                 void* stream);
+
+/* Sequence dst[i] (empty, listed once) begins as a copy of sequence src[i] (dev [n] each): it shares the full pages, and a
+ * partly filled last page is copied, in every layer, to a page of its own (list order, lowest free number first).  A
+ * source may be listed often.  All sources are taken as they were before the call. */
+int np_kv_fork(const np_kv_desc* desc, void* cache, const np_kv_tables* tables, const int32_t* src, const int32_t* dst,
+               int32_t n, void* stream);
+
+/* The sequences `seqs` (dev [n]; NULL: 0..n-1) give up their pages and become empty.  Freeing an empty one is no error;
+ * one that is listed twice is freed once (NP_KV_S_SEQ). */
+int np_kv_free(const np_kv_desc* desc, const np_kv_tables* tables, const int32_t* seqs, int32_t n, void* stream);
+
+/* Closes the pool up: with N live pages, the i-th live page from number N on moves, in every layer, to the i-th free number
+ * below N.  The tables that say so are written to `out`: the same arrays as `in`, or others of the same sizes (all
+ * three others; entries past a sequence's pages become -1).  The old pages keep their contents until they are taken again,
+ * so work that was queued with the old tables may still run.  in->scratch and in->status serve the call.
+ *   n_live  dev [1] or NULL: N */
+int np_kv_compact(const np_kv_desc* desc, void* cache, const np_kv_tables* in, const np_kv_tables* out, int32_t* n_live,
+                  void* stream);
+
+/* Copies page src[i] of src_cache to page dst[i] of dst_cache in every layer (dev [n] each; caches of one description, or
+ * one cache).  Tables are not touched.  A pair with a number outside the pool is passed over.  The copies happen at once:
+ * a page that is written twice, or read and written in one cache, holds a mixture afterwards. */
+int np_kv_copy_pages(const np_kv_desc* desc, void* dst_cache, const void* src_cache, const int32_t* src, const int32_t* dst,
+                     int32_t n, int32_t* status, void* stream);
+
+/* Attention of one new token per sequence over the cache (n_heads query heads, n_heads % n_kv_heads == 0; head h reads
+ * key-value head h / (n_heads / n_kv_heads)):
+ *   out[i][h] = sum_j softmax_j(scale * q[i][h] . k_j) v_j   over the lens[seqs[i]] tokens of sequence seqs[i]
+ * (the new token among them: append it first).  Keys and values past a sequence's length are not read.  A sequence of
+ * length 0, and a row whose seqs[i] is negative (padding), give zeros and lse -inf, and so does a row whose scores are all
+ * -inf.  fp32 scores, softmax and sums.
+ *   q, out     n rows of n_heads heads; out may not overlap q
+ *   scale      positive and finite
+ *   lse        dev fp32 [n][n_heads] or NULL: log sum_j exp(scale * q . k_j)
+ *   seqs       dev [n] or NULL: 0..n-1; the same sequence may be listed often
+ *   workspace  dev, 16-byte aligned, np_attn_workspace_bytes (a larger one serves, too); zeroed by the caller before its
+ *              first use and left ready for the next call of any size.  Calls (and graphs) that share one must not overlap
+ *              on the GPU
+ * Results do not depend on how the work was split between blocks in more than rounding, and are the same from run to run. */
+int np_attn_workspace_bytes(const np_kv_desc* desc, int32_t n_heads, int32_t n, uint64_t* out);
+int np_attn_decode(const np_kv_desc* desc, const void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* q,
+                   int32_t n_heads, const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse,
+                   void* workspace, void* stream);
+
+/* Causal attention over n packed prompts: rows cu[s] .. cu[s + 1] - 1 are the tokens of prompt s in order, and each sees the
+ * rows of its own prompt up to itself.  Rows of out and lse from cu[n] on (and before cu[0]) are left as they were.
+ *   q, out  n_tokens rows of n_heads heads, k, v  n_tokens rows of n_kv_heads heads; strides above 0 along more than one
+ *           token or head; out may not overlap the others
+ *   cu      dev int32 [n + 1], ascending, 0 <= cu <= n_tokens; a prompt may be empty
+ *   scale   positive and finite
+ *   lse     dev fp32 [n_tokens][n_heads] or NULL
+ *   status  dev int32 [1], zeroed by the caller before its first use
+ * head_dim 64 or 128, n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= NP_ATTN_MAX_GROUP, 1 <= n <= NP_KV_MAX_SEQS.
+ * Scores, softmax and sums in fp32; the probabilities are rounded to the rows' type for the second product.  Later tokens
+ * and other prompts have no effect on a row, infinities and NaN among them. */
+typedef struct np_attn_shape {
+  int32_t dtype;        /* NP_T_* */
+  int32_t n_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t reserved[4];  /* 0 */
+} np_attn_shape;
+int np_attn_prompt(const np_attn_shape* shape, const np_rows* q, const np_rows* k, const np_rows* v, const int32_t* cu, int32_t n,
+                   int32_t n_tokens, float scale, const np_rows* out, float* lse, int32_t* status, void* stream);
+
+/* Waits for `stream` and returns NP_E_DEVICE if a status word (of tables or of np_attn_prompt) has a bit set; the text names
+ * the bits.  Calls that only queue work cannot report them. */
+int np_attn_check(const int32_t* status, void* stream);
+const char* np_attn_last_error(void);
+
 #ifdef __cplusplus
 }
 #endif

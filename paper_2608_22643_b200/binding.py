@@ -42,6 +42,8 @@ EXPORTED = [
     "np_read_counters", "np_export_state", "np_import_state", "np_last_step_times", "np_mlp_chain",
     "np_launch_count", "np_chain_launches", "np_speculate", "np_install_speculative", "np_get_speculative", "np_mlp_kernel_name", "np_selftest_bounded_wait", "np_predict_logits_noalloc", "np_noalloc_check", "np_noalloc_last_error",
     "np_trunk_workspace_floats", "np_trunk_forward", "np_trunk_last_error",
+    "np_kv_sizes", "np_kv_reset", "np_kv_reserve", "np_kv_append", "np_kv_fork", "np_kv_free", "np_kv_compact", "np_kv_copy_pages",
+    "np_attn_workspace_bytes", "np_attn_decode", "np_attn_prompt", "np_attn_check", "np_attn_last_error",
 ]
 
 
@@ -84,6 +86,32 @@ class np_trunk_weights(C.Structure):
 class np_delta_view(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in (
         "delta_ids", "delta_slots", "evict_ids", "overflow_ids", "active_ids", "active_slots", "counters")]
+
+
+NP_T_BF16, NP_T_FP16 = 0, 1
+NP_KV_S_PAGE, NP_KV_S_SEQ, NP_KV_S_LENGTH, NP_KV_S_TIMEOUT, NP_KV_S_FULL = 1, 2, 4, 8, 32
+
+
+class np_kv_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in (
+        "dtype", "n_layers", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "max_seqs", "max_pages")] + [
+        ("reserved", C.c_int32 * 4)]
+
+
+class np_kv_tables(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("page_table", "lens", "refs", "scratch", "status")]
+
+
+class np_kv_sizes_out(C.Structure):
+    _fields_ = [(n, C.c_uint64) for n in ("cache_bytes", "page_bytes", "table_bytes", "scratch_bytes")]
+
+
+class np_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class np_attn_shape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_heads", "n_kv_heads", "head_dim")] + [("reserved", C.c_int32 * 4)]
 
 
 class NpError(RuntimeError):
@@ -147,6 +175,23 @@ def load() -> C.CDLL:
     sigs["np_chain_launches"] = [vp, C.POINTER(C.c_int32)]
     sigs["np_install_speculative"] = [vp, vp]
     sigs["np_get_speculative"] = [vp, i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)]
+    kvd, kvt, rows = C.POINTER(np_kv_desc), C.POINTER(np_kv_tables), C.POINTER(np_rows)
+    lib.np_attn_last_error.restype = C.c_char_p
+    lib.np_attn_last_error.argtypes = []
+    sigs.update({
+        "np_kv_sizes": [kvd, C.POINTER(np_kv_sizes_out)],
+        "np_kv_reset": [kvd, kvt, vp],
+        "np_kv_reserve": [kvd, kvt, vp, vp, i32, vp, vp],
+        "np_kv_append": [kvd, vp, i32, kvt, rows, rows, i32, vp, vp, vp, i32, vp],
+        "np_kv_fork": [kvd, vp, kvt, vp, vp, i32, vp],
+        "np_kv_free": [kvd, kvt, vp, i32, vp],
+        "np_kv_compact": [kvd, vp, kvt, kvt, vp, vp],
+        "np_kv_copy_pages": [kvd, vp, vp, vp, vp, i32, vp, vp],
+        "np_attn_workspace_bytes": [kvd, i32, i32, C.POINTER(C.c_uint64)],
+        "np_attn_decode": [kvd, vp, i32, kvt, rows, i32, vp, i32, C.c_float, rows, vp, vp, vp],
+        "np_attn_prompt": [C.POINTER(np_attn_shape), rows, rows, rows, vp, i32, i32, C.c_float, rows, vp, vp, vp],
+        "np_attn_check": [vp, vp],
+    })
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -285,6 +330,152 @@ def np_trunk_forward(desc, table, features, centroid_id, workspace, head_logits,
     if rc < 0:
         raise NpError(rc, load().np_trunk_last_error().decode())
     return rc
+
+
+# ---- the paged key-value cache and its attention ----------------------------------------
+# Tensors belong to the current device.  Rows of heads (q, k, v, out) are tensors [tokens][heads][head_dim] with any strides
+# between tokens and heads and the last dimension contiguous; everything else is contiguous.
+_ATTN_DTYPE = {torch.bfloat16: NP_T_BF16, torch.float16: NP_T_FP16}
+
+
+def _attn_check(rc: int) -> int:
+    if rc < 0:
+        raise NpError(rc, load().np_attn_last_error().decode())
+    return rc
+
+
+def _refuse(msg: str):
+    raise NpError(NP_E_INVAL, msg)
+
+
+def _dev(t, dtype=None, least: int = 0) -> Optional[int]:
+    """Address of a contiguous tensor of the current device (None stays None) that holds at least ``least`` elements."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        _refuse("tensors must be on the current CUDA device")
+    if dtype is not None and t.dtype is not dtype:
+        _refuse(f"expected a {dtype} tensor, got {t.dtype}")
+    if not t.is_contiguous():
+        _refuse("expected a contiguous tensor")
+    if t.numel() < least:
+        _refuse(f"expected at least {least} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _rows_of(t, dtype: int, tokens: int, heads: int, head_dim: int) -> np_rows:
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        _refuse("tensors must be on the current CUDA device")
+    if t.shape != (tokens, heads, head_dim) or _ATTN_DTYPE.get(t.dtype) != dtype:
+        _refuse(f"expected rows [{tokens}][{heads}][{head_dim}] of the call's type, got {tuple(t.shape)} {t.dtype}")
+    st, sh, sd = t.stride()
+    if sd != 1:
+        _refuse("the last dimension of rows must be contiguous")
+    # a stride nobody steps along may be anything in torch
+    return np_rows(t.data_ptr(), st if tokens > 1 else 0, sh if heads > 1 else 0)
+
+
+def _cache_of(desc: np_kv_desc, cache):
+    want = (desc.n_layers, desc.n_pages, 2, desc.n_kv_heads, desc.page_tokens, desc.head_dim)
+    if tuple(cache.shape) != want or _ATTN_DTYPE.get(cache.dtype) != desc.dtype:
+        _refuse(f"expected a cache {want} of the description's type, got {tuple(cache.shape)} {cache.dtype}")
+    return _dev(cache)
+
+
+def make_kv_desc(dtype, n_layers: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int, max_seqs: int,
+                 max_pages: Optional[int] = None) -> np_kv_desc:
+    """``dtype``: torch.bfloat16 or torch.float16 (or an NP_T_* code)."""
+    code = _ATTN_DTYPE.get(dtype, dtype)
+    if not isinstance(code, int):
+        _refuse(f"no cache of {dtype}: bfloat16 or float16")
+    return np_kv_desc(code, n_layers, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
+                      n_pages if max_pages is None else max_pages)
+
+
+def make_kv_tables(page_table, lens, refs, scratch, status) -> np_kv_tables:
+    """The pointer table over int32 tensors (the caller keeps them alive)."""
+    return np_kv_tables(*[_dev(t, torch.int32) for t in (page_table, lens, refs, scratch, status)])
+
+
+def np_kv_sizes(desc: np_kv_desc) -> np_kv_sizes_out:
+    out = np_kv_sizes_out()
+    _attn_check(load().np_kv_sizes(C.byref(desc), C.byref(out)))
+    return out
+
+
+def np_kv_reset(desc, tables, stream=None) -> int:
+    return _attn_check(load().np_kv_reset(C.byref(desc), C.byref(tables), _stream(stream)))
+
+
+def np_kv_reserve(desc, tables, seqs, n_new, start_out=None, stream=None) -> int:
+    n = n_new.numel()
+    return _attn_check(load().np_kv_reserve(C.byref(desc), C.byref(tables), _dev(seqs, torch.int32, n), _dev(n_new, torch.int32), n,
+                                            _dev(start_out, torch.int32, n), _stream(stream)))
+
+
+def np_kv_append(desc, cache, layer: int, tables, k, v, seqs, cu, start, stream=None) -> int:
+    """``cu`` None: one token for each sequence."""
+    n, tokens = start.numel(), k.shape[0]
+    kr = _rows_of(k, desc.dtype, tokens, desc.n_kv_heads, desc.head_dim)
+    vr = _rows_of(v, desc.dtype, tokens, desc.n_kv_heads, desc.head_dim)
+    return _attn_check(load().np_kv_append(C.byref(desc), _cache_of(desc, cache), layer, C.byref(tables), C.byref(kr), C.byref(vr), tokens,
+                                           _dev(seqs, torch.int32, n), _dev(cu, torch.int32, n + 1), _dev(start, torch.int32), n,
+                                           _stream(stream)))
+
+
+def np_kv_fork(desc, cache, tables, src, dst, stream=None) -> int:
+    n = src.numel()
+    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache), C.byref(tables), _dev(src, torch.int32),
+                                         _dev(dst, torch.int32, n), n, _stream(stream)))
+
+
+def np_kv_free(desc, tables, seqs=None, n: Optional[int] = None, stream=None) -> int:
+    """``seqs`` None: sequences 0..n-1."""
+    n = seqs.numel() if n is None else n
+    return _attn_check(load().np_kv_free(C.byref(desc), C.byref(tables), _dev(seqs, torch.int32, n), n, _stream(stream)))
+
+
+def np_kv_compact(desc, cache, tables, out_tables, n_live=None, stream=None) -> int:
+    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache), C.byref(tables), C.byref(out_tables),
+                                            _dev(n_live, torch.int32, 1), _stream(stream)))
+
+
+def np_kv_copy_pages(desc, dst_cache, src_cache, src, dst, status, stream=None) -> int:
+    n = src.numel()
+    return _attn_check(load().np_kv_copy_pages(C.byref(desc), _cache_of(desc, dst_cache), _cache_of(desc, src_cache), _dev(src, torch.int32),
+                                               _dev(dst, torch.int32, n), n, _dev(status, torch.int32, 1), _stream(stream)))
+
+
+def np_attn_workspace_bytes(desc, n_heads: int, n: int) -> int:
+    out = C.c_uint64()
+    _attn_check(load().np_attn_workspace_bytes(C.byref(desc), n_heads, n, C.byref(out)))
+    return out.value
+
+
+def np_attn_decode(desc, cache, layer: int, tables, q, out, workspace, seqs=None, scale: Optional[float] = None, lse=None, stream=None) -> int:
+    """``scale`` None: 1 / sqrt(head_dim).  ``workspace``: a uint8 tensor, zeroed before its first use."""
+    n, heads = q.shape[0], q.shape[1]
+    qr = _rows_of(q, desc.dtype, n, heads, desc.head_dim)
+    outr = _rows_of(out, desc.dtype, n, heads, desc.head_dim)
+    ws = _dev(workspace, torch.uint8, np_attn_workspace_bytes(desc, heads, n))
+    return _attn_check(load().np_attn_decode(C.byref(desc), _cache_of(desc, cache), layer, C.byref(tables), C.byref(qr), heads,
+                                             _dev(seqs, torch.int32, n), n, desc.head_dim ** -0.5 if scale is None else scale, C.byref(outr),
+                                             _dev(lse, torch.float32, n * heads), ws, _stream(stream)))
+
+
+def np_attn_prompt(q, k, v, cu, out, status, scale: Optional[float] = None, lse=None, stream=None) -> int:
+    """``q``, ``out`` [tokens][heads][head_dim], ``k``, ``v`` [tokens][kv heads][head_dim]; ``cu`` int32, one more than prompts."""
+    tokens, heads, hd = q.shape
+    dtype = _ATTN_DTYPE.get(q.dtype, -1)
+    shape = np_attn_shape(dtype, heads, k.shape[1], hd)
+    r = [_rows_of(t, dtype, tokens, h, hd) for t, h in ((q, heads), (k, k.shape[1]), (v, k.shape[1]), (out, heads))]
+    return _attn_check(load().np_attn_prompt(C.byref(shape), C.byref(r[0]), C.byref(r[1]), C.byref(r[2]), _dev(cu, torch.int32, 2),
+                                             cu.numel() - 1, tokens, hd ** -0.5 if scale is None else scale, C.byref(r[3]),
+                                             _dev(lse, torch.float32, tokens * heads), _dev(status, torch.int32, 1), _stream(stream)))
+
+
+def np_attn_check(status, stream=None) -> int:
+    return _attn_check(load().np_attn_check(_dev(status, torch.int32, 1), _stream(stream)))
 
 
 def np_install(ctx, layer_begin: int, layer_end: int, copy_stream=None) -> int:

@@ -1,0 +1,48 @@
+// Shared by the translation units of the paged cache and its attention (np_kv.cu, np_attn_decode.cu, np_attn_prompt.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "np.h"
+
+namespace npa {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Keeps the text for np_attn_last_error and returns the code.
+int fail(int code, const char* msg);
+int fail_cuda(cudaError_t e);
+
+// Text of what is wrong with a description; NULL: nothing.
+const char* desc_error(const np_kv_desc* d);
+const char* rows_error(const np_rows* r);
+bool tables_ok(const np_kv_tables* t);  // no pointer NULL
+
+inline int log2_of(int pow2) {
+  int s = 0;
+  while ((1 << s) < pow2) ++s;
+  return s;
+}
+
+// SM count of the current device; false: no device.
+bool device_sms(int* sms);
+
+// A launch whose blocks may be scheduled while the kernel before it in the stream ends; the kernel begins with
+// npp::pdl_wait_prior().
+template <class K, class... Args>
+cudaError_t launch_early(K kernel, dim3 grid, int threads, size_t smem, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+}  // namespace npa

@@ -1,0 +1,515 @@
+// Attention of one new token per sequence over the paged cache (np_attn_decode).
+//
+//   out[i][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q[i][h] . k_j - m),   m the row's maximum
+//
+// Every key and value is used once per query head of its group, so the cache's bytes bound the kernel: 2 * head_dim * 2
+// bytes per token and key-value head against 4 * head_dim operations per query head.  What has to be done is to keep
+// enough loads in flight and to split the tokens evenly.
+//
+// * A warp takes sixteen tokens at a time, all heads of a group (eight or sixteen columns) at once, on the tensor cores'
+//   mma.sync form: S^T = K Q^T and O^T = V^T P^T, tokens x head_dim on the wide side, so that a group of one wastes matrix
+//   operations (there are plenty) and no bytes.
+// * Keys and values go from global memory straight into the registers that the products read, 16 bytes per lane, no shared
+//   memory: S sums over head_dim, so any order of head_dim does as long as q has the same, and lane t of a quad takes
+//   pieces t, t + 4, ... of a row; O's rows are head_dim in an order that only the store has to undo, and two tokens' values
+//   are interleaved with byte permutes.  The keys of the next sixteen tokens are asked for when S is there, the values
+//   when O is, so a warp always has 4 KB in flight (head_dim 128).
+// * The running maximum and sum are per warp (base 2, fp32); the accumulators are rescaled only when a maximum grows.  P is
+//   the sum of two terms of the cache's type, so it is good to 16 bits and more where one term has 8 or 11.
+// * All (sequence, group, tile of 64 tokens) triples form one line; each block takes an equal stretch of it.  A block that
+//   has a group's tokens to itself stores the result; otherwise blocks leave (m, l, O) in the workspace and the last to arrive
+//   joins them in the order of the tokens, so that results do not depend on who was last.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "np_attn.h"
+#include "np_device.cuh"
+#include "np_internal.h"
+#include "np_pipe.cuh"
+
+namespace npa {
+namespace {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kTile = kWarps * 16;    // tokens of a tile
+constexpr int kMinTiles = 4;          // tiles a block takes at least, where there are so few that blocks stay idle
+constexpr int kMaxBlocks = 640;       // blocks of a launch (the workspace holds two partial results of each)
+
+struct DecodeArgs {
+  const char* cache;         // of the layer
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* seqs;
+  int32_t* status;
+  const uint16_t* q;
+  uint16_t* out;
+  int64_t q_token, q_head, o_token, o_head;  // elements
+  float* lse;
+  unsigned int* count;       // [n * pairs] pieces that have arrived; zero between calls
+  float* part_ml;            // [2 * kMaxBlocks][HB][2]
+  float* part_o;             // [2 * kMaxBlocks][HB][HD]
+  float scale2;              // scale * log2(e)
+  int n, n_heads, n_kv_heads, group, blocks_of_heads;  // heads of a group: blocks_of_heads pieces of HB
+  int shift, n_pages, max_seqs, max_pages;
+};
+
+template <class T>
+struct Half2;
+template <>
+struct Half2<__nv_bfloat16> {
+  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  }
+  // (x, y) rounded, and what the rounding left, rounded
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    const float2 f = __bfloat1622float2(h);
+    const __nv_bfloat162 l = __floats2bfloat162_rn(x - f.x, y - f.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+  }
+  static __device__ __forceinline__ uint16_t round(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+};
+template <>
+struct Half2<__half> {
+  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  }
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
+    const __half2 h = __floats2half2_rn(x, y);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+  }
+  static __device__ __forceinline__ uint16_t round(float x) { return __half_as_ushort(__float2half_rn(x)); }
+};
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// Tokens of row i of the call; 0 where there are none to read.
+__device__ __forceinline__ int row_len(const DecodeArgs& a, int i, int* seq_out) {
+  const int seq = a.seqs ? a.seqs[i] : i;
+  *seq_out = seq;
+  if (seq < 0) return 0;
+  if (seq >= a.max_seqs) {
+    atomicOr(a.status, NP_KV_S_SEQ);
+    return 0;
+  }
+  const int len = a.lens[seq];
+  if (len < 0 || ((int64_t)len + (1 << a.shift) - 1) >> a.shift > a.max_pages) {
+    atomicOr(a.status, NP_KV_S_LENGTH);
+    return 0;
+  }
+  return len;
+}
+
+template <class T, int HD, int NT>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
+k_attn_decode(DecodeArgs a) {
+  constexpr int HB = 8 * NT;         // heads of a block, at most
+  constexpr int KV = HD / 32;        // 16-byte pieces of a key row per lane
+  constexpr int VC = HD / 64;        // 16-byte pieces of a value row per lane
+  __shared__ int64_t s_end[NP_KV_MAX_SEQS];             // tiles of the rows up to and including this one
+  __shared__ __align__(16) float s_o[kWarps][HB][HD];
+  __shared__ float s_ml[kWarps][HB][2];
+  __shared__ int64_t s_wsum[kWarps];
+  __shared__ int s_last;
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int pairs = a.n_kv_heads * a.blocks_of_heads;   // (key-value head, block of its query heads)
+
+  // ---- tiles of every row, summed up; rows without tokens are answered here
+  int64_t run = 0;
+  for (int base = 0; base < a.n; base += kThreads) {
+    const int i = base + tid;
+    int len = 0, seq = -1;
+    if (i < a.n) len = row_len(a, i, &seq);
+    int64_t inc = ((int64_t)len + kTile - 1) / kTile;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += up;
+    }
+    if (lane == 31) s_wsum[wid] = inc;
+    __syncthreads();
+    for (int w = 0; w < wid; ++w) inc += s_wsum[w];
+    if (i < a.n) s_end[i] = run + inc;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) run += s_wsum[w];
+    __syncthreads();
+  }
+  for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
+    if (s_end[i] != (i ? s_end[i - 1] : 0)) continue;
+    for (int e = tid; e < a.n_heads * (HD / 8); e += kThreads) {
+      const int h = e / (HD / 8), d = e % (HD / 8) * 8;
+      *reinterpret_cast<uint4*>(a.out + i * a.o_token + h * a.o_head + d) = make_uint4(0, 0, 0, 0);
+      if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = -INFINITY;
+    }
+  }
+  const int64_t W = run * pairs;
+  const int64_t G = min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
+  if (blockIdx.x >= G) return;
+  int64_t w0 = W * blockIdx.x / G;
+  const int64_t w1 = W * (blockIdx.x + 1) / G;
+  int row = 0;
+  {
+    int lo = 0, hi = a.n - 1;  // the first row whose tiles end after w0
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (s_end[mid] * pairs > w0) hi = mid;
+      else lo = mid + 1;
+    }
+    row = lo;
+  }
+
+  while (w0 < w1) {
+    // ---- the next piece: tiles [ta, tb) of one (row, pair)
+    while (s_end[row] * pairs <= w0) ++row;
+    const int64_t before = row ? s_end[row - 1] : 0;
+    const int64_t tiles = s_end[row] - before, r0 = w0 - before * pairs;
+    const int pair = (int)(r0 / tiles);
+    const int64_t ta = r0 - pair * tiles, tb = min(tiles, ta + (w1 - w0)), first_w = w0 - ta;
+    w0 += tb - ta;
+    int seq;
+    const int len = row_len(a, row, &seq);
+    const int kvh = pair / a.blocks_of_heads, hb = pair - kvh * a.blocks_of_heads;
+    const int h0 = kvh * a.group + hb * HB, heads = min(HB, a.group - hb * HB);
+    const int32_t* pages = a.table + (size_t)seq * a.max_pages;
+    const int64_t head_bytes = (int64_t)(HD * 2) << a.shift, page_bytes = 2 * a.n_kv_heads * head_bytes;
+    const char* kbase = a.cache + kvh * head_bytes;
+    const char* vbase = kbase + a.n_kv_heads * head_bytes;
+
+    uint4 qf[NT][KV];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < KV; ++j) {
+        qf[nt][j] = make_uint4(0, 0, 0, 0);
+        if (nt * 8 + g < heads) qf[nt][j] = *reinterpret_cast<const uint4*>(a.q + row * a.q_token + (int64_t)(h0 + nt * 8 + g) * a.q_head + (t + 4 * j) * 8);
+      }
+    float m[NT][2], l[NT][2], o[NT][VC * 4][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < VC * 4; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+    }
+
+    uint4 kf[2][KV], vf[4][VC];
+    const int chunk_end = (int)min(((int64_t)len + 15) >> 4, tb * kWarps);  // chunks of 16 tokens
+    // where the chunk's page starts, and how many of its tokens there are (0: nothing to read)
+    auto chunk_of = [&](int c, int pg, int& have, int64_t& at) {
+      have = 0;
+      at = 0;
+      if (c >= chunk_end) return;
+      if ((unsigned)pg >= (unsigned)a.n_pages) {
+        atomicOr(a.status, NP_KV_S_PAGE);
+        return;
+      }
+      have = (int)min((int64_t)16, len - (int64_t)c * 16);
+      at = pg * page_bytes + (int64_t)((c * 16) & ((1 << a.shift) - 1)) * (HD * 2);
+    };
+    auto page_of = [&](int c) { return c < chunk_end ? pages[(int)(((int64_t)c * 16) >> a.shift)] : 0; };
+    auto load_k = [&](int have, int64_t at) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < KV; ++j) {
+          kf[r][j] = make_uint4(0, 0, 0, 0);
+          if (g + 8 * r < have) kf[r][j] = npd::ldg_stream(kbase + at + (g + 8 * r) * (HD * 2) + (t + 4 * j) * 16);
+        }
+    };
+    auto load_v = [&](int have, int64_t at) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
+#pragma unroll
+        for (int c = 0; c < VC; ++c) {
+          vf[r][c] = make_uint4(0, 0, 0, 0);
+          if (tok < have) vf[r][c] = npd::ldg_stream(vbase + at + tok * (HD * 2) + (g + 8 * c) * 16);
+        }
+      }
+    };
+    int c = (int)ta * kWarps + wid;
+    int have, have_next;
+    int64_t at, at_next;
+    chunk_of(c, page_of(c), have, at);
+    load_k(have, at);
+    load_v(have, at);
+    int pg_next = page_of(c + kWarps);
+    for (; c < chunk_end; c += kWarps) {
+      chunk_of(c + kWarps, pg_next, have_next, at_next);
+      pg_next = page_of(c + 2 * kWarps);
+      // ---- S^T = K Q^T
+      float s[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < KV; ++j) {
+          Half2<T>::mma(s[nt], kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, qf[nt][j].x, qf[nt][j].y);
+          Half2<T>::mma(s[nt], kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, qf[nt][j].z, qf[nt][j].w);
+        }
+      }
+      load_k(have_next, at_next);
+      // ---- softmax: s[0], s[1] are token g, s[2], s[3] token g + 8; heads 2t and 2t + 1
+      uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[nt][i] = g + 8 * (i >> 1) < have ? s[nt][i] * a.scale2 : -INFINITY;
+        float now[2], use[2];
+        bool grew = false;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float v = fmaxf(s[nt][i], s[nt][i + 2]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, x));
+          now[i] = fmaxf(m[nt][i], v);
+          use[i] = now[i] == -INFINITY ? 0.f : now[i];  // -inf so far: nothing has been added up yet
+          grew |= now[i] > m[nt][i];
+        }
+        if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float f = exp2_fast(m[nt][i] - use[i]);
+            m[nt][i] = now[i];
+            l[nt][i] *= f;
+#pragma unroll
+            for (int k = 0; k < VC * 4; ++k) {
+              o[nt][k][i] *= f;
+              o[nt][k][i + 2] *= f;
+            }
+          }
+        }
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = exp2_fast(s[nt][i] - use[i & 1]);
+        l[nt][0] += p[0] + p[2];
+        l[nt][1] += p[1] + p[3];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t hi, lo;
+          Half2<T>::split(p[2 * i], p[2 * i + 1], hi, lo);
+          ph[nt][i] = transpose8x8(hi);
+          pl[nt][i] = transpose8x8(lo);
+        }
+      }
+      // ---- O^T += V^T P^T
+#pragma unroll
+      for (int v = 0; v < VC; ++v)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t x0 = word(vf[0][v], w), x1 = word(vf[1][v], w), x2 = word(vf[2][v], w), x3 = word(vf[3][v], w);
+          const uint32_t a0 = __byte_perm(x0, x1, 0x5410), a1 = __byte_perm(x0, x1, 0x7632);
+          const uint32_t a2 = __byte_perm(x2, x3, 0x5410), a3 = __byte_perm(x2, x3, 0x7632);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            Half2<T>::mma(o[nt][v * 4 + w], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+            Half2<T>::mma(o[nt][v * 4 + w], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+          }
+        }
+      load_v(have_next, at_next);
+      have = have_next;
+      at = at_next;
+    }
+
+    // ---- the warps' results meet in shared memory
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], x);
+        const int h = nt * 8 + 2 * t + i;
+        if (h < heads) {
+          if (g == 0) {
+            s_ml[wid][h][0] = m[nt][i];
+            s_ml[wid][h][1] = l[nt][i];
+          }
+#pragma unroll
+          for (int k = 0; k < VC * 4; ++k)
+            *reinterpret_cast<float2*>(&s_o[wid][h][(g + 8 * (k >> 2)) * 8 + 2 * (k & 3)]) = make_float2(o[nt][k][i], o[nt][k][i + 2]);
+        }
+      }
+    __syncthreads();
+    const bool whole = ta == 0 && tb == tiles;
+    const int slot = 2 * blockIdx.x + (ta == 0 ? 1 : 0);
+    for (int e = tid; e < heads * HD; e += kThreads) {
+      const int h = e / HD, d = e % HD;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_ml[w][h][0]);
+      const float use = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, acc = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2_fast(s_ml[w][h][0] - use);
+        sum += f * s_ml[w][h][1];
+        acc += f * s_o[w][h][d];
+      }
+      if (whole) {
+        a.out[row * a.o_token + (int64_t)(h0 + h) * a.o_head + d] = Half2<T>::round(sum == 0.f ? 0.f : acc / sum);
+        if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + h0 + h] = sum == 0.f ? -INFINITY : use * kLn2 + logf(sum);
+      } else {
+        __stcg(&a.part_o[((size_t)slot * HB + h) * HD + d], acc);
+        if (d == 0) {
+          __stcg(&a.part_ml[(slot * HB + h) * 2], top);
+          __stcg(&a.part_ml[(slot * HB + h) * 2 + 1], sum);
+        }
+      }
+    }
+    if (!whole) {
+      // ---- the last block of this (row, pair) joins the pieces
+      const int c0 = (int)(((first_w + 1) * G - 1) / W), c1 = (int)(((first_w + tiles) * G - 1) / W);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        unsigned int* count = a.count + (size_t)row * pairs + pair;
+        const unsigned int arrived = atomicAdd(count, 1u) + 1u;
+        s_last = arrived == (unsigned)(c1 - c0 + 1);
+        if (s_last) *count = 0u;
+      }
+      __syncthreads();
+      if (s_last) {
+        __threadfence();
+        for (int e = tid; e < heads * (HD / 4); e += kThreads) {
+          const int h = e / (HD / 4), d = e % (HD / 4) * 4;
+          float top = -INFINITY;
+          for (int b = c0; b <= c1; ++b) top = fmaxf(top, __ldcg(&a.part_ml[((2 * b + (b == c0)) * HB + h) * 2]));
+          const float use = top == -INFINITY ? 0.f : top;
+          float sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int b = c0; b <= c1; ++b) {
+            const int sl = (2 * b + (b == c0)) * HB + h;
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(&a.part_ml[sl * 2]));
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(&a.part_o[(size_t)sl * HD + d]));
+            const float f = exp2_fast(ml.x - use);
+            sum += f * ml.y;
+            acc.x += f * x.x;
+            acc.y += f * x.y;
+            acc.z += f * x.z;
+            acc.w += f * x.w;
+          }
+          const bool none = sum == 0.f;
+          const float inv = none ? 0.f : 1.f / sum;
+          uint2 r;
+          r.x = (uint32_t)Half2<T>::round(none ? 0.f : acc.x * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.y * inv) << 16;
+          r.y = (uint32_t)Half2<T>::round(none ? 0.f : acc.z * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.w * inv) << 16;
+          *reinterpret_cast<uint2*>(a.out + row * a.o_token + (int64_t)(h0 + h) * a.o_head + d) = r;
+          if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + h0 + h] = none ? -INFINITY : use * kLn2 + logf(sum);
+        }
+      }
+    }
+    __syncthreads();  // s_o, s_ml and s_last are free for the next piece
+  }
+}
+
+int heads_per_block(int group) { return group <= 8 ? 8 : 16; }
+
+template <class T>
+cudaError_t launch(const DecodeArgs& a, int hd, int hb, int sms, cudaStream_t s) {
+  const dim3 grid(std::min(kMaxBlocks, (hb == 8 ? 3 : 2) * sms));
+  if (hd == 128) return hb == 8 ? launch_early(k_attn_decode<T, 128, 1>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 128, 2>, grid, kThreads, 0, s, a);
+  return hb == 8 ? launch_early(k_attn_decode<T, 64, 1>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 64, 2>, grid, kThreads, 0, s, a);
+}
+
+// [(m, l) of the partial results][their O][counts]: the counts start at the same place for every description and n, and the
+// rest needs no particular contents, so one workspace serves calls of different sizes in turn.
+constexpr uint64_t kSpaceO = (uint64_t)2 * kMaxBlocks * 16 * 8, kSpaceCounts = kSpaceO + (uint64_t)2 * kMaxBlocks * 16 * 128 * 4;
+uint64_t space_bytes(int n_kv_heads, int group, int n) {
+  const int hb = heads_per_block(group);
+  return kSpaceCounts + (uint64_t)n * n_kv_heads * ((group + hb - 1) / hb) * 4;
+}
+
+const char* heads_error(const np_kv_desc* d, int n_heads, int n) {
+  if (n_heads < 1 || n_heads > (1 << 17) || n_heads % d->n_kv_heads) return "n_heads must be a positive multiple of n_kv_heads, at most 131072";
+  if (n < 0 || n > NP_KV_MAX_SEQS) return "n outside [0, NP_KV_MAX_SEQS]";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace npa
+
+using namespace npa;
+
+extern "C" {
+
+int np_attn_workspace_bytes(const np_kv_desc* d, int32_t n_heads, int32_t n, uint64_t* out) {
+  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
+  if (const char* m = heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
+  if (!out) return fail(NP_E_INVAL, "NULL argument");
+  *out = space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n);
+  return NP_OK;
+}
+
+int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads,
+                   const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse, void* workspace, void* stream) {
+  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
+  if (const char* m = heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
+  if (!seqs && n > d->max_seqs) return fail(NP_E_INVAL, "n is above max_seqs");
+  if (n == 0) return NP_OK;
+  if (!cache || !workspace || !t || !t->page_table || !t->lens || !t->status) return fail(NP_E_INVAL, "NULL argument");
+  if ((uintptr_t)cache % 16 || (uintptr_t)workspace % 16) return fail(NP_E_INVAL, "cache and workspace must be 16-byte aligned");
+  if (layer < 0 || layer >= d->n_layers) return fail(NP_E_INVAL, "layer outside the cache");
+  if (!std::isfinite(scale) || scale <= 0.f) return fail(NP_E_INVAL, "scale must be positive and finite");
+  if (const char* m = rows_error(q)) return fail(NP_E_INVAL, m);
+  if (const char* m = rows_error(out)) return fail(NP_E_INVAL, m);
+  int sms;
+  if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
+  const int64_t page = (int64_t)2 * d->n_kv_heads * d->page_tokens * d->head_dim * 2;
+  DecodeArgs a = {};
+  a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * page;
+  a.table = t->page_table;
+  a.lens = t->lens;
+  a.seqs = seqs;
+  a.status = t->status;
+  a.q = static_cast<const uint16_t*>(q->data);
+  a.out = static_cast<uint16_t*>(out->data);
+  a.q_token = q->token_stride;
+  a.q_head = q->head_stride;
+  a.o_token = out->token_stride;
+  a.o_head = out->head_stride;
+  a.lse = lse;
+  a.n = n;
+  a.n_heads = n_heads;
+  a.n_kv_heads = d->n_kv_heads;
+  a.group = n_heads / d->n_kv_heads;
+  const int hb = heads_per_block(a.group);
+  a.blocks_of_heads = (a.group + hb - 1) / hb;
+  a.scale2 = scale * kLog2e;
+  a.shift = log2_of(d->page_tokens);
+  a.n_pages = d->n_pages;
+  a.max_seqs = d->max_seqs;
+  a.max_pages = d->max_pages;
+  char* ws = static_cast<char*>(workspace);
+  a.part_ml = reinterpret_cast<float*>(ws);
+  a.part_o = reinterpret_cast<float*>(ws + kSpaceO);
+  a.count = reinterpret_cast<unsigned int*>(ws + kSpaceCounts);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = d->dtype == NP_T_BF16 ? launch<__nv_bfloat16>(a, d->head_dim, hb, sms, s) : launch<__half>(a, d->head_dim, hb, sms, s);
+  return e == cudaSuccess ? NP_OK : fail_cuda(e);
+}
+
+}  // extern "C"

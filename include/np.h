@@ -659,14 +659,14 @@ int np_kv_copy_pages(const np_kv_desc* desc, void* dst_cache, const void* src_ca
  *   scale      positive and finite
  *   lse        dev fp32 [n][n_heads] or NULL: log sum_j exp(scale * q . k_j)
  *   seqs       dev [n] or NULL: 0..n-1; the same sequence may be listed often
- *   workspace  dev, 16-byte aligned, np_attn_workspace_bytes (a larger one serves, too); zeroed by the caller before its
+ *   workspace  dev, 16-byte aligned, workspace_bytes long: at least np_attn_workspace_bytes; zeroed by the caller before its
  *              first use and left ready for the next call of any size.  Calls (and graphs) that share one must not overlap
  *              on the GPU
  * Results do not depend on how the work was split between blocks in more than rounding, and are the same from run to run. */
 int np_attn_workspace_bytes(const np_kv_desc* desc, int32_t n_heads, int32_t n, uint64_t* out);
 int np_attn_decode(const np_kv_desc* desc, const void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* q,
                    int32_t n_heads, const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse,
-                   void* workspace, void* stream);
+                   void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Causal attention over n packed prompts: rows cu[s] .. cu[s + 1] - 1 are the tokens of prompt s in order, and each sees the
  * rows of its own prompt up to itself.  Rows of out and lse from cu[n] on (and before cu[0]) are left as they were.

@@ -188,7 +188,7 @@ def load() -> C.CDLL:
         "np_kv_compact": [kvd, vp, kvt, kvt, vp, vp],
         "np_kv_copy_pages": [kvd, vp, vp, vp, vp, i32, vp, vp],
         "np_attn_workspace_bytes": [kvd, i32, i32, C.POINTER(C.c_uint64)],
-        "np_attn_decode": [kvd, vp, i32, kvt, rows, i32, vp, i32, C.c_float, rows, vp, vp, vp],
+        "np_attn_decode": [kvd, vp, i32, kvt, rows, i32, vp, i32, C.c_float, rows, vp, vp, C.c_uint64, vp],
         "np_attn_prompt": [C.POINTER(np_attn_shape), rows, rows, rows, vp, i32, i32, C.c_float, rows, vp, vp, vp],
         "np_attn_check": [vp, vp],
     })
@@ -348,38 +348,41 @@ def _refuse(msg: str):
     raise NpError(NP_E_INVAL, msg)
 
 
-def _dev(t, dtype=None, least: int = 0) -> Optional[int]:
-    """Address of a contiguous tensor of the current device (None stays None) that holds at least ``least`` elements."""
+def _device() -> int:
+    """The current device; -2 (no tensor's) without one."""
+    try:
+        return torch.cuda.current_device()
+    except (RuntimeError, AssertionError):
+        return -2
+
+
+# Small calls are bound by what these checks take (a few microseconds a call): one query of the device per call, and messages
+# are made up only when something is wrong.
+def _dev(t, dtype, device: int, least: int = 0) -> Optional[int]:
+    """Address of a contiguous tensor of the device (None stays None) that holds at least ``least`` elements."""
     if t is None:
         return None
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        _refuse("tensors must be on the current CUDA device")
-    if dtype is not None and t.dtype is not dtype:
-        _refuse(f"expected a {dtype} tensor, got {t.dtype}")
-    if not t.is_contiguous():
-        _refuse("expected a contiguous tensor")
-    if t.numel() < least:
-        _refuse(f"expected at least {least} elements, got {t.numel()}")
+    if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous() or t.numel() < least:
+        _refuse(f"expected a contiguous {dtype} tensor of at least {least} elements on the current CUDA device, got {t.dtype} "
+                f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows_of(t, dtype: int, tokens: int, heads: int, head_dim: int) -> np_rows:
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        _refuse("tensors must be on the current CUDA device")
-    if t.shape != (tokens, heads, head_dim) or _ATTN_DTYPE.get(t.dtype) != dtype:
-        _refuse(f"expected rows [{tokens}][{heads}][{head_dim}] of the call's type, got {tuple(t.shape)} {t.dtype}")
-    st, sh, sd = t.stride()
-    if sd != 1:
-        _refuse("the last dimension of rows must be contiguous")
+def _rows_of(t, dtype: int, device: int, tokens: int, heads: int, head_dim: int) -> np_rows:
+    st, sh, sd = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.get_device() != device or sd != 1 or t.shape != (tokens, heads, head_dim) or _ATTN_DTYPE.get(t.dtype) != dtype:
+        _refuse(f"expected rows [{tokens}][{heads}][{head_dim}] of the call's type, the last dimension contiguous, on the current CUDA "
+                f"device, got {tuple(t.shape)} {t.dtype} with strides {t.stride()} on {t.device}")
     # a stride nobody steps along may be anything in torch
     return np_rows(t.data_ptr(), st if tokens > 1 else 0, sh if heads > 1 else 0)
 
 
-def _cache_of(desc: np_kv_desc, cache):
-    want = (desc.n_layers, desc.n_pages, 2, desc.n_kv_heads, desc.page_tokens, desc.head_dim)
-    if tuple(cache.shape) != want or _ATTN_DTYPE.get(cache.dtype) != desc.dtype:
-        _refuse(f"expected a cache {want} of the description's type, got {tuple(cache.shape)} {cache.dtype}")
-    return _dev(cache)
+def _cache_of(desc: np_kv_desc, cache, device: int):
+    if (cache.get_device() != device or not cache.is_contiguous() or _ATTN_DTYPE.get(cache.dtype) != desc.dtype
+            or cache.shape != (desc.n_layers, desc.n_pages, 2, desc.n_kv_heads, desc.page_tokens, desc.head_dim)):
+        _refuse(f"expected a contiguous cache [{desc.n_layers}][{desc.n_pages}][2][{desc.n_kv_heads}][{desc.page_tokens}][{desc.head_dim}] of "
+                f"the description's type on the current CUDA device, got {tuple(cache.shape)} {cache.dtype} on {cache.device}")
+    return cache.data_ptr()
 
 
 def make_kv_desc(dtype, n_layers: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int, max_seqs: int,
@@ -394,7 +397,8 @@ def make_kv_desc(dtype, n_layers: int, n_kv_heads: int, head_dim: int, page_toke
 
 def make_kv_tables(page_table, lens, refs, scratch, status) -> np_kv_tables:
     """The pointer table over int32 tensors (the caller keeps them alive)."""
-    return np_kv_tables(*[_dev(t, torch.int32) for t in (page_table, lens, refs, scratch, status)])
+    device = _device()
+    return np_kv_tables(*[_dev(t, torch.int32, device) for t in (page_table, lens, refs, scratch, status)])
 
 
 def np_kv_sizes(desc: np_kv_desc) -> np_kv_sizes_out:
@@ -408,42 +412,43 @@ def np_kv_reset(desc, tables, stream=None) -> int:
 
 
 def np_kv_reserve(desc, tables, seqs, n_new, start_out=None, stream=None) -> int:
-    n = n_new.numel()
-    return _attn_check(load().np_kv_reserve(C.byref(desc), C.byref(tables), _dev(seqs, torch.int32, n), _dev(n_new, torch.int32), n,
-                                            _dev(start_out, torch.int32, n), _stream(stream)))
+    n, i32, dv = n_new.numel(), torch.int32, _device()
+    return _attn_check(load().np_kv_reserve(C.byref(desc), C.byref(tables), _dev(seqs, i32, dv, n), _dev(n_new, i32, dv), n,
+                                            _dev(start_out, i32, dv, n), _stream(stream)))
 
 
 def np_kv_append(desc, cache, layer: int, tables, k, v, seqs, cu, start, stream=None) -> int:
     """``cu`` None: one token for each sequence."""
-    n, tokens = start.numel(), k.shape[0]
-    kr = _rows_of(k, desc.dtype, tokens, desc.n_kv_heads, desc.head_dim)
-    vr = _rows_of(v, desc.dtype, tokens, desc.n_kv_heads, desc.head_dim)
-    return _attn_check(load().np_kv_append(C.byref(desc), _cache_of(desc, cache), layer, C.byref(tables), C.byref(kr), C.byref(vr), tokens,
-                                           _dev(seqs, torch.int32, n), _dev(cu, torch.int32, n + 1), _dev(start, torch.int32), n,
-                                           _stream(stream)))
+    n, tokens, i32, dv = start.numel(), k.shape[0], torch.int32, _device()
+    dtype, heads, hd = desc.dtype, desc.n_kv_heads, desc.head_dim
+    return _attn_check(load().np_kv_append(
+        C.byref(desc), _cache_of(desc, cache, dv), layer, C.byref(tables), C.byref(_rows_of(k, dtype, dv, tokens, heads, hd)),
+        C.byref(_rows_of(v, dtype, dv, tokens, heads, hd)), tokens, _dev(seqs, i32, dv, n), _dev(cu, i32, dv, n + 1), _dev(start, i32, dv), n,
+        _stream(stream)))
 
 
 def np_kv_fork(desc, cache, tables, src, dst, stream=None) -> int:
-    n = src.numel()
-    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache), C.byref(tables), _dev(src, torch.int32),
-                                         _dev(dst, torch.int32, n), n, _stream(stream)))
+    n, i32, dv = src.numel(), torch.int32, _device()
+    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache, dv), C.byref(tables), _dev(src, i32, dv), _dev(dst, i32, dv, n),
+                                         n, _stream(stream)))
 
 
 def np_kv_free(desc, tables, seqs=None, n: Optional[int] = None, stream=None) -> int:
     """``seqs`` None: sequences 0..n-1."""
     n = seqs.numel() if n is None else n
-    return _attn_check(load().np_kv_free(C.byref(desc), C.byref(tables), _dev(seqs, torch.int32, n), n, _stream(stream)))
+    return _attn_check(load().np_kv_free(C.byref(desc), C.byref(tables), _dev(seqs, torch.int32, _device(), n), n, _stream(stream)))
 
 
 def np_kv_compact(desc, cache, tables, out_tables, n_live=None, stream=None) -> int:
-    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache), C.byref(tables), C.byref(out_tables),
-                                            _dev(n_live, torch.int32, 1), _stream(stream)))
+    dv = _device()
+    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache, dv), C.byref(tables), C.byref(out_tables),
+                                            _dev(n_live, torch.int32, dv, 1), _stream(stream)))
 
 
 def np_kv_copy_pages(desc, dst_cache, src_cache, src, dst, status, stream=None) -> int:
-    n = src.numel()
-    return _attn_check(load().np_kv_copy_pages(C.byref(desc), _cache_of(desc, dst_cache), _cache_of(desc, src_cache), _dev(src, torch.int32),
-                                               _dev(dst, torch.int32, n), n, _dev(status, torch.int32, 1), _stream(stream)))
+    n, i32, dv = src.numel(), torch.int32, _device()
+    return _attn_check(load().np_kv_copy_pages(C.byref(desc), _cache_of(desc, dst_cache, dv), _cache_of(desc, src_cache, dv), _dev(src, i32, dv),
+                                               _dev(dst, i32, dv, n), n, _dev(status, i32, dv, 1), _stream(stream)))
 
 
 def np_attn_workspace_bytes(desc, n_heads: int, n: int) -> int:
@@ -454,28 +459,28 @@ def np_attn_workspace_bytes(desc, n_heads: int, n: int) -> int:
 
 def np_attn_decode(desc, cache, layer: int, tables, q, out, workspace, seqs=None, scale: Optional[float] = None, lse=None, stream=None) -> int:
     """``scale`` None: 1 / sqrt(head_dim).  ``workspace``: a uint8 tensor, zeroed before its first use."""
-    n, heads = q.shape[0], q.shape[1]
-    qr = _rows_of(q, desc.dtype, n, heads, desc.head_dim)
-    outr = _rows_of(out, desc.dtype, n, heads, desc.head_dim)
-    ws = _dev(workspace, torch.uint8, np_attn_workspace_bytes(desc, heads, n))
-    return _attn_check(load().np_attn_decode(C.byref(desc), _cache_of(desc, cache), layer, C.byref(tables), C.byref(qr), heads,
-                                             _dev(seqs, torch.int32, n), n, desc.head_dim ** -0.5 if scale is None else scale, C.byref(outr),
-                                             _dev(lse, torch.float32, n * heads), ws, _stream(stream)))
+    n, heads = q.shape[:2]
+    dtype, hd, dv = desc.dtype, desc.head_dim, _device()
+    return _attn_check(load().np_attn_decode(
+        C.byref(desc), _cache_of(desc, cache, dv), layer, C.byref(tables), C.byref(_rows_of(q, dtype, dv, n, heads, hd)), heads,
+        _dev(seqs, torch.int32, dv, n), n, hd ** -0.5 if scale is None else scale, C.byref(_rows_of(out, dtype, dv, n, heads, hd)),
+        _dev(lse, torch.float32, dv, n * heads), _dev(workspace, torch.uint8, dv), workspace.numel(), _stream(stream)))
 
 
 def np_attn_prompt(q, k, v, cu, out, status, scale: Optional[float] = None, lse=None, stream=None) -> int:
     """``q``, ``out`` [tokens][heads][head_dim], ``k``, ``v`` [tokens][kv heads][head_dim]; ``cu`` int32, one more than prompts."""
     tokens, heads, hd = q.shape
-    dtype = _ATTN_DTYPE.get(q.dtype, -1)
-    shape = np_attn_shape(dtype, heads, k.shape[1], hd)
-    r = [_rows_of(t, dtype, tokens, h, hd) for t, h in ((q, heads), (k, k.shape[1]), (v, k.shape[1]), (out, heads))]
-    return _attn_check(load().np_attn_prompt(C.byref(shape), C.byref(r[0]), C.byref(r[1]), C.byref(r[2]), _dev(cu, torch.int32, 2),
-                                             cu.numel() - 1, tokens, hd ** -0.5 if scale is None else scale, C.byref(r[3]),
-                                             _dev(lse, torch.float32, tokens * heads), _dev(status, torch.int32, 1), _stream(stream)))
+    dtype, kv_heads, dv = _ATTN_DTYPE.get(q.dtype, -1), k.shape[1], _device()
+    return _attn_check(load().np_attn_prompt(
+        C.byref(np_attn_shape(dtype, heads, kv_heads, hd)), C.byref(_rows_of(q, dtype, dv, tokens, heads, hd)),
+        C.byref(_rows_of(k, dtype, dv, tokens, kv_heads, hd)), C.byref(_rows_of(v, dtype, dv, tokens, kv_heads, hd)),
+        _dev(cu, torch.int32, dv, 2), cu.numel() - 1, tokens, hd ** -0.5 if scale is None else scale,
+        C.byref(_rows_of(out, dtype, dv, tokens, heads, hd)), _dev(lse, torch.float32, dv, tokens * heads), _dev(status, torch.int32, dv, 1),
+        _stream(stream)))
 
 
 def np_attn_check(status, stream=None) -> int:
-    return _attn_check(load().np_attn_check(_dev(status, torch.int32, 1), _stream(stream)))
+    return _attn_check(load().np_attn_check(_dev(status, torch.int32, _device(), 1), _stream(stream)))
 
 
 def np_install(ctx, layer_begin: int, layer_end: int, copy_stream=None) -> int:

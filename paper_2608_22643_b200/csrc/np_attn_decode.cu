@@ -465,13 +465,15 @@ int np_attn_workspace_bytes(const np_kv_desc* d, int32_t n_heads, int32_t n, uin
 }
 
 int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads,
-                   const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse, void* workspace, void* stream) {
+                   const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse, void* workspace,
+                   uint64_t workspace_bytes, void* stream) {
   if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
   if (const char* m = heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
   if (!seqs && n > d->max_seqs) return fail(NP_E_INVAL, "n is above max_seqs");
   if (n == 0) return NP_OK;
   if (!cache || !workspace || !t || !t->page_table || !t->lens || !t->status) return fail(NP_E_INVAL, "NULL argument");
   if ((uintptr_t)cache % 16 || (uintptr_t)workspace % 16) return fail(NP_E_INVAL, "cache and workspace must be 16-byte aligned");
+  if (workspace_bytes < space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n)) return fail(NP_E_INVAL, "workspace is smaller than np_attn_workspace_bytes says");
   if (layer < 0 || layer >= d->n_layers) return fail(NP_E_INVAL, "layer outside the cache");
   if (!std::isfinite(scale) || scale <= 0.f) return fail(NP_E_INVAL, "scale must be positive and finite");
   if (const char* m = rows_error(q)) return fail(NP_E_INVAL, m);

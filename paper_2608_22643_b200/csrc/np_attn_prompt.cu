@@ -39,9 +39,15 @@ namespace npa {
 namespace {
 
 constexpr int kRows = 128;              // query rows of a tile, keys of a tile
-constexpr int kThreads = 320;
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kThreads = 384;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kPlanWarp = 10, kZeroWarp = 11;
 constexpr float kGrow = 8.f;            // log2 of the growth of a maximum that is let pass
+constexpr int kPlans = 2;               // blocks of work that are laid out ahead
+constexpr int kPlanReaders = 11;        // warps that read a plan: eight of the softmax, products, loads, zeros
+#ifndef NP_POLY
+#define NP_POLY 4
+#endif
+constexpr int kPoly = NP_POLY;          // of sixteen pairs of exponentials, those that the FMA units compute
 
 struct PromptArgs {
   const uint16_t* q;
@@ -76,16 +82,22 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead) {
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
+}
+// one lane of a warp, the same every time
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
 }
 
 #define NP_R32(r, o)                                                                                                                   \
@@ -110,13 +122,61 @@ __device__ __forceinline__ void tm_st16(uint32_t taddr, const uint32_t (&r)[16])
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+// The block's registers (384 threads x 168) are dealt out anew: 200 for each thread of the softmax warps, which hold a row of scores,
+// 104 for the others.  8 * 200 + 4 * 104 = 12 * 168.
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 200;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
-  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+typedef unsigned long long f32x2;  // two fp32 that one instruction works on
+__device__ __forceinline__ f32x2 two(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void apart(f32x2 x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// the largest of three; a NaN among them is the result
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^x of two x <= 8 on the FMA units: x = n + f with n the nearest integer (adding 1.5 * 2^23 leaves it in the low bits), 2^f on
+// [-1/2, 1/2] by the polynomial of degree 5 with the least relative error (2^-23.7, fitted to 2^f by reweighted least squares),
+// n added to the exponent.  Below -126 the result stays about 2^-126.  Not for NaN.
+__device__ __forceinline__ void exp2_poly(f32x2 x, float& lo, float& hi) {
+  float a, b;
+  apart(x, a, b);
+  x = two(fmaxf(a, -126.f), fmaxf(b, -126.f));
+  const float magic = 12582912.f;
+  const f32x2 t = add2(x, two(magic, magic)), n = add2(t, two(-magic, -magic)), f = fma2(n, two(-1.f, -1.f), x);
+  f32x2 p = two(0.0013276472454890609f, 0.0013276472454890609f);
+  p = fma2(p, f, two(0.009675540961325169f, 0.009675540961325169f));
+  p = fma2(p, f, two(0.05550713092088699f, 0.05550713092088699f));
+  p = fma2(p, f, two(0.24022120237350464f, 0.24022120237350464f));
+  p = fma2(p, f, two(0.6931469440460205f, 0.6931469440460205f));
+  p = fma2(p, f, two(1.0000001192092896f, 1.0000001192092896f));
+  float ta, tb, pa, pb;
+  apart(t, ta, tb);
+  apart(p, pa, pb);
+  lo = __uint_as_float(__float_as_uint(pa) + (__float_as_uint(ta) << 23));
+  hi = __uint_as_float(__float_as_uint(pb) + (__float_as_uint(tb) << 23));
 }
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -177,9 +237,59 @@ struct Shape {
   static constexpr int kHalves = HD / 64;                        // 64 values = 128 bytes: one swizzle row
   static constexpr uint32_t kHalfBytes = kRows * 128;            // a tile's rows of one half
   static constexpr uint32_t kTileBytes = kHalves * kHalfBytes;
-  static constexpr int kStages = 4;                              // K0 V0 K1 V1 ...
-  static constexpr size_t kSmem = (2 + kStages) * (size_t)kTileBytes + 1024;
+  static constexpr int kStages = HD == 128 ? 4 : 8;              // K0 V0 K1 V1 ...
+  static constexpr uint32_t kOutBytes = 2048;                    // a warp's 32 rows x 32 values on their way out
+  static constexpr size_t kSmem = (2 + kStages) * (size_t)kTileBytes + 8 * kOutBytes + 1024;
 };
+
+// A block of work: two tiles of rows of one prompt and key-value head.
+struct Plan {
+  int start, len, q0, kvh;  // first row and tokens of the prompt, first token of the block; len 0: nothing is left
+};
+
+struct Work {
+  int start, len, q0, kvh, n_kv[2], n_tiles;
+  bool tail;  // the last tile of keys reaches past the prompt
+  __device__ __forceinline__ Work(const Plan& p, int tile_tokens) : start(p.start), len(p.len), q0(p.q0), kvh(p.kvh) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int first = q0 + i * tile_tokens, end = min(first + tile_tokens, len);
+      n_kv[i] = end > first ? (end + kRows - 1) / kRows : 0;  // the second tile may have no row
+    }
+    n_tiles = max(n_kv[0], n_kv[1]);
+    tail = n_tiles * kRows > len;
+  }
+};
+
+// P = exp2(scale2 * S - m) of a row's 128 scores into tensor memory, its sum; `half` is called when the first half is there.
+template <bool kBf16, bool kPlain, class Half>
+__device__ __forceinline__ float softmax_row(const uint32_t (&s)[kRows], float scale2, float use, uint32_t tp, Half half) {
+  const f32x2 sc = two(scale2, scale2), off = two(-use, -use);
+  f32x2 sum[2] = {0, 0};
+#pragma unroll
+  for (int c = 0; c < kRows; c += 32) {
+    uint32_t w[16];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const f32x2 e = fma2(two(__uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1])), sc, off);
+      float p0, p1;
+      if (!kPlain && (x * kPoly) % 16 + kPoly >= 16) {
+        exp2_poly(e, p0, p1);
+      } else {
+        apart(e, p0, p1);
+        p0 = exp2_fast(p0);
+        p1 = exp2_fast(p1);
+      }
+      sum[x & 1] = add2(sum[x & 1], two(p0, p1));
+      w[x] = pack<kBf16>(p0, p1);
+    }
+    tm_st16(tp + c / 2, w);
+    if (c == 32) half();
+  }
+  float a, b;
+  apart(add2(sum[0], sum[1]), a, b);
+  return a + b;
+}
 
 template <bool kBf16, int HD>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -187,81 +297,48 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               const __grid_constant__ PromptArgs a) {
   using S = Shape<HD>;
   extern __shared__ __align__(1024) unsigned char tsm[];
-  __shared__ int s_end[NP_KV_MAX_SEQS];  // blocks of the prompts up to and including this one
-  __shared__ int s_wsum[kThreads / 32];
-  __shared__ __align__(8) uint64_t full[S::kStages], empty[S::kStages], q_full, s_full[2], p_full[2], o_full[2], v_fixed;
+  __shared__ int s_blocks[NP_KV_MAX_SEQS];  // blocks of work of each prompt (per key-value head)
+  __shared__ Plan s_plan[kPlans];
+  __shared__ __align__(8) uint64_t full[S::kStages], empty[S::kStages], q_full, q_empty, s_full[2], p_half[2], p_full[2], o_full[2], o_empty[2],
+      v_asked[S::kStages], v_zeroed[S::kStages], plan_full[kPlans], plan_empty[kPlans];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_ok[2];
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int block_tokens = 2 * a.tile_tokens;
-
-  // ---- which prompt, which tokens
-  int run = 0;
-  for (int base = 0; base < a.n; base += kThreads) {
-    const int i = base + tid;
-    int inc = 0;
-    if (i < a.n) {
-      const int lo = min(max(a.cu[i], 0), a.n_tokens), hi = min(max(a.cu[i + 1], 0), a.n_tokens);
-      inc = hi > lo ? (hi - lo + block_tokens - 1) / block_tokens : 0;
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += up;
-    }
-    if (lane == 31) s_wsum[wid] = inc;
-    __syncthreads();
-    int all = 0;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < wid) inc += s_wsum[w];
-      all += s_wsum[w];
-    }
-    if (i < a.n) s_end[i] = run + inc;
-    run += all;
-    __syncthreads();
-  }
-  // the blocks with the most keys first: a prompt's last tokens
-  const int kvh = blockIdx.x % a.n_kv_heads, at = run - 1 - (int)(blockIdx.x / a.n_kv_heads);
-  if (at < 0) return;
-  int lo = 0, hi = a.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (s_end[mid] > at) hi = mid;
-    else lo = mid + 1;
-  }
-  const int start = min(max(a.cu[lo], 0), a.n_tokens), len = min(max(a.cu[lo + 1], 0), a.n_tokens) - start;
-  const int q0 = (at - (lo ? s_end[lo - 1] : 0)) * block_tokens;
-  // tiles of keys that each tile of rows sees; the second tile may have no row
-  int n_kv[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int first = q0 + i * a.tile_tokens, end = min(first + a.tile_tokens, len);
-    n_kv[i] = end > first ? (end + kRows - 1) / kRows : 0;
-  }
-  const int n_tiles = max(n_kv[0], n_kv[1]);
-  const bool tail = n_tiles * kRows > len;  // the last tile of keys reaches past the prompt
 
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tsm) + 1023) & ~(uintptr_t)1023);
   unsigned char* q_sm = base;
   unsigned char* ring = base + 2 * S::kTileBytes;
+  unsigned char* out_sm = ring + S::kStages * S::kTileBytes;
 
   if (tid == 0) {
     for (int s = 0; s < S::kStages; ++s) {
       npp::mbar_init(&full[s], 1);
       npp::mbar_init(&empty[s], 1);
+      npp::mbar_init(&v_asked[s], 1);
+      npp::mbar_init(&v_zeroed[s], 1);
     }
     npp::mbar_init(&q_full, 1);
-    npp::mbar_init(&v_fixed, 1);
+    npp::mbar_init(&q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       npp::mbar_init(&s_full[i], 1);
+      npp::mbar_init(&p_half[i], 4);
       npp::mbar_init(&p_full[i], 4);
       npp::mbar_init(&o_full[i], 1);
+      npp::mbar_init(&o_empty[i], 4);
+    }
+    for (int i = 0; i < kPlans; ++i) {
+      npp::mbar_init(&plan_full[i], 1);
+      npp::mbar_init(&plan_empty[i], kPlanReaders);
     }
     npp::fence_barrier_init();
     s_ok[0] = 1;
     s_ok[1] = 0;
+  }
+  for (int i = tid; i < a.n; i += kThreads) {
+    const int lo = min(max(a.cu[i], 0), a.n_tokens), hi = min(max(a.cu[i + 1], 0), a.n_tokens);
+    s_blocks[i] = hi > lo ? (hi - lo + 2 * a.tile_tokens - 1) / (2 * a.tile_tokens) : 0;
   }
   if (wid == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(npp::smem_addr(&s_tmem)), "r"(512) : "memory");
@@ -272,197 +349,347 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   fence_after();
   const uint32_t tmem = s_tmem;
   auto wait = [&](uint64_t* bar, uint32_t parity) { return npp::wait_or_flag(bar, parity, s_ok, a.status); };
-
-  if (wid == kLoadWarp) {
-    // ------------------------------ loads ------------------------------
-    int stage = 0;
-    uint32_t use = 0;
-    bool ok = true;
-    if (lane == 0) {
-      const int tiles = n_kv[1] > 0 ? 2 : 1;
-      npp::mbar_expect_tx(&q_full, (uint32_t)tiles * S::kHalves * 128 * a.group * a.tile_tokens);
-      for (int i = 0; i < tiles; ++i)
-        for (int h = 0; h < S::kHalves; ++h)
-          tma_load_3d(q_sm + i * S::kTileBytes + h * S::kHalfBytes, &map_q, h * 64, kvh * a.group, start + q0 + i * a.tile_tokens, &q_full);
-      for (int j = 0; j < 2 * n_tiles; ++j) {
-        ok = wait(&empty[stage], (use & 1u) ^ 1u);
-        if (!ok) break;
-        npp::mbar_expect_tx(&full[stage], S::kTileBytes);
-        for (int h = 0; h < S::kHalves; ++h)
-          tma_load_3d(ring + stage * S::kTileBytes + h * S::kHalfBytes, j & 1 ? &map_v : &map_k, h * 64, kvh, start + (j >> 1) * kRows, &full[stage]);
-        if (++stage == S::kStages) {
-          stage = 0;
-          ++use;
-        }
-      }
-    }
-    ok = __shfl_sync(0xffffffffu, ok, 0);
-    if (tail && ok) {
-      // rows past the prompt in the last V tile: zero, whatever lies there
-      const int s = (2 * n_tiles - 1) % S::kStages;
-      if (wait(&full[s], (uint32_t)((2 * n_tiles - 1) / S::kStages) & 1u)) {
-        const int from = len - (n_tiles - 1) * kRows, words = (kRows - from) * 8;  // 16-byte words of a half
-        for (int e = lane; e < words * S::kHalves; e += 32) {
-          const int h = e / words, w = e - h * words;
-          *reinterpret_cast<uint4*>(ring + s * S::kTileBytes + h * S::kHalfBytes + from * 128 + w * 16) = make_uint4(0, 0, 0, 0);
-        }
-      }
-      npp::fence_proxy_async();
+  // the same by whole warps: all lanes go on, or none does
+  auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+  // the n-th plan; false: nothing is left, or a wait ran out
+  auto plan = [&](uint32_t n, Plan& p, bool whole_warp) {
+    uint64_t* bar = &plan_full[n % kPlans];
+    if (whole_warp ? !wait_all(bar, (n / kPlans) & 1u) : !wait(bar, (n / kPlans) & 1u)) return false;
+    p = s_plan[n % kPlans];
+    if (whole_warp) {
       __syncwarp();
-      if (lane == 0) npp::mbar_arrive(&v_fixed);
+      if (lane == 0) npp::mbar_arrive(&plan_empty[n % kPlans]);
+    } else {
+      npp::mbar_arrive(&plan_empty[n % kPlans]);
     }
-    if (lane == 0 && !s_ok[0]) {  // after a time-out nobody else waits for the copies
-      uint32_t patience = npp::kSpinLimit;
-      npp::drain_ring(full, S::kStages, stage, use & 1u, patience);
-      npp::wait_landed(&q_full, 0, patience);
+    return p.len > 0;
+  };
+
+  if (wid == kPlanWarp) {
+    fewer_registers();
+    // ------------------------------ plans ------------------------------
+    // Blocks of work in falling order of their place in their prompt, which is the order of their number of keys; this block
+    // takes every gridDim-th, in alternating direction, so that all blocks get about the same.
+    auto from_place = [&](int b) {  // blocks of work at place b or later, all prompts, one key-value head
+      int64_t sum = 0;
+      for (int i = lane; i < a.n; i += 32) sum += max(0, s_blocks[i] - b);
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      return sum;
+    };
+    int most = 0;
+    for (int i = lane; i < a.n; i += 32) most = max(most, s_blocks[i]);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, x));
+    const int64_t total = from_place(0) * a.n_kv_heads;
+    for (uint32_t n = 0;; ++n) {
+      const int64_t r = (int64_t)n * gridDim.x + (n & 1u ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      Plan p = {0, 0, 0, 0};
+      if (r < total) {
+        const int64_t at = r / a.n_kv_heads;
+        int lo = 0, hi = most - 1;  // the largest place with more than `at` blocks from it on
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (from_place(mid) > at) lo = mid;
+          else hi = mid - 1;
+        }
+        int which = (int)(at - from_place(lo + 1));  // among the prompts that have that place
+        for (int first = 0; first < a.n; first += 32) {
+          const uint32_t has = __ballot_sync(0xffffffffu, first + lane < a.n && s_blocks[first + lane] > lo);
+          const int cnt = __popc(has);
+          if (which < cnt) {
+            uint32_t rest = has;
+            for (int x = 0; x < which; ++x) rest &= rest - 1;
+            const int i = first + __ffs(rest) - 1;
+            p.start = min(max(a.cu[i], 0), a.n_tokens);
+            p.len = min(max(a.cu[i + 1], 0), a.n_tokens) - p.start;
+            p.q0 = lo * 2 * a.tile_tokens;
+            p.kvh = (int)(r % a.n_kv_heads);
+            break;
+          }
+          which -= cnt;
+        }
+      }
+      if (!wait_all(&plan_empty[n % kPlans], ((n / kPlans) & 1u) ^ 1u)) break;
+      if (lane == 0) {
+        s_plan[n % kPlans] = p;
+        npp::mbar_arrive(&plan_full[n % kPlans]);
+      }
+      __syncwarp();
+      if (p.len == 0) break;
     }
-  } else if (wid == kMmaWarp) {
-    // ------------------------------ products ------------------------------
+  } else if (wid == kLoadWarp) {
+    fewer_registers();
+    // ------------------------------ loads ------------------------------
     if (lane == 0) {
-      const uint32_t fmt = kBf16 ? 1u : 0u;
-      const uint32_t common = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(kRows >> 4) << 24);
-      const uint32_t id_s = common | ((uint32_t)(kRows >> 3) << 17), id_o = common | (1u << 16) | ((uint32_t)(HD >> 3) << 17);
-      const uint32_t q_addr = npp::smem_addr(q_sm), ring_addr = npp::smem_addr(ring);
-      auto scores = [&](int i, int st) {
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t off = (k >> 2) * S::kHalfBytes + (k & 3) * 32;
-          mma_ss(tmem + i * kRows, smem_desc(q_addr + i * S::kTileBytes + off, 16), smem_desc(ring_addr + st * S::kTileBytes + off, 16), id_s, k > 0);
-        }
-        commit(&s_full[i]);
-      };
-      bool ok = wait(&q_full, 0) && wait(&full[0], 0);
-      if (ok) {
-        fence_after();
-        for (int i = 0; i < 2; ++i)
-          if (n_kv[i] > 0) scores(i, 0);
-        commit(&empty[0]);
-      }
-      for (int j = 0; j < n_tiles && ok; ++j) {
-        const int sv = (2 * j + 1) % S::kStages, sk = (2 * j + 2) % S::kStages;
-        ok = wait(&full[sv], (uint32_t)((2 * j + 1) / S::kStages) & 1u);
-        if (ok && j + 1 < n_tiles) ok = wait(&full[sk], (uint32_t)((2 * j + 2) / S::kStages) & 1u);
-        if (ok && tail && j + 1 == n_tiles) ok = wait(&v_fixed, 0);
-        for (int i = 0; i < 2 && ok; ++i) {
-          if (j >= n_kv[i]) continue;
-          ok = wait(&p_full[i], (uint32_t)j & 1u);
+      int stage = 0;
+      uint32_t use = 0, n = 0;
+      Plan p;
+      bool ok = true;
+      for (; ok && plan(n, p, false); ++n) {
+        const Work w(p, a.tile_tokens);
+        const int tiles = w.n_kv[1] > 0 ? 2 : 1;
+        ok = wait(&q_empty, (n & 1u) ^ 1u);
+        if (!ok) break;
+        npp::mbar_expect_tx(&q_full, (uint32_t)tiles * S::kHalves * 128 * a.group * a.tile_tokens);
+        for (int i = 0; i < tiles; ++i)
+          for (int h = 0; h < S::kHalves; ++h)
+            tma_load_3d(q_sm + i * S::kTileBytes + h * S::kHalfBytes, &map_q, h * 64, w.kvh * a.group, w.start + w.q0 + i * a.tile_tokens, &q_full);
+        for (int j = 0; j < 2 * w.n_tiles; ++j) {
+          ok = wait(&empty[stage], (use & 1u) ^ 1u);
           if (!ok) break;
-          fence_after();
-#pragma unroll
-          for (int k = 0; k < kRows / 16; ++k)
-            mma_ts(tmem + 256 + i * HD, tmem + i * kRows + k * 8, smem_desc(ring_addr + sv * S::kTileBytes + k * 2048, S::kHalfBytes), id_o, (j | k) > 0);
-          if (j + 1 < n_kv[i]) scores(i, sk);
-          else commit(&o_full[i]);
-        }
-        if (ok) {
-          commit(&empty[sv]);
-          if (j + 1 < n_tiles) commit(&empty[sk]);
-        }
-      }
-    }
-  } else {
-    // ------------------------------ softmax and result of a tile ------------------------------
-    const int i = wid >> 2, row = (wid & 3) * 32 + lane;
-    const int in_tile = row / a.group, head = kvh * a.group + row - in_tile * a.group;
-    const int first = q0 + i * a.tile_tokens, tok = first + in_tile;
-    const bool valid = in_tile < a.tile_tokens && tok < len;
-    const uint32_t ts = tmem + ((uint32_t)((wid & 3) * 32) << 16) + i * kRows, to = tmem + ((uint32_t)((wid & 3) * 32) << 16) + 256 + i * HD;
-    float m = -INFINITY, l = 0.f;
-    bool ok = true;
-    for (int j = 0; j < n_kv[i]; ++j) {
-      ok = wait(&s_full[i], (uint32_t)j & 1u);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      fence_after();
-      uint32_t s[kRows];
-#pragma unroll
-      for (int c = 0; c < kRows; c += 32) tm_ld32(ts + c, s, c);
-      wait_ld();
-      if ((j + 1) * kRows - 1 > first) {  // the tile reaches past the first row
-        const int see = tok - j * kRows;
-#pragma unroll
-        for (int c = 0; c < kRows; ++c)
-          if (c > see) s[c] = __float_as_uint(-INFINITY);
-      }
-      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int c = 0; c < kRows; c += 4) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) top[x] = fmaxf(top[x], __uint_as_float(s[c + x]));
-      }
-      const float now = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale2);
-      if (j == 0) {
-        m = now;
-      } else if (__any_sync(0xffffffffu, now > m + kGrow)) {
-        const float f = exp2_fast(m - (now == -INFINITY ? 0.f : now));
-        m = now;
-        l *= f;
-#pragma unroll
-        for (int c = 0; c < HD; c += 32) {
-          uint32_t o[32];
-          tm_ld32(to + c, o, 0);
-          wait_ld();
-          uint32_t w[16];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) w[x] = __float_as_uint(__uint_as_float(o[h * 16 + x]) * f);
-            tm_st16(to + c + h * 16, w);
+          npp::mbar_expect_tx(&full[stage], S::kTileBytes);
+          for (int h = 0; h < S::kHalves; ++h)
+            tma_load_3d(ring + stage * S::kTileBytes + h * S::kHalfBytes, j & 1 ? &map_v : &map_k, h * 64, w.kvh, w.start + (j >> 1) * kRows,
+                        &full[stage]);
+          if (w.tail && j + 1 == 2 * w.n_tiles) npp::mbar_arrive(&v_asked[stage]);
+          if (++stage == S::kStages) {
+            stage = 0;
+            ++use;
           }
         }
       }
-      const float use = m == -INFINITY ? 0.f : m;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < kRows; c += 32) {
-        uint32_t w[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const float p0 = exp2_fast(fmaf(__uint_as_float(s[c + 2 * x]), a.scale2, -use));
-          const float p1 = exp2_fast(fmaf(__uint_as_float(s[c + 2 * x + 1]), a.scale2, -use));
-          sum[(2 * x) & 3] += p0;
-          sum[(2 * x + 1) & 3] += p1;
-          w[x] = pack<kBf16>(p0, p1);
-        }
-        tm_st16(ts + c / 2, w);
+      if (!s_ok[0]) {  // after a time-out nobody else waits for the copies
+        uint32_t patience = npp::kSpinLimit;
+        npp::drain_ring(full, S::kStages, stage, use & 1u, patience);
+        npp::wait_landed(&q_full, n & 1u, patience);
+        if (n > 0) npp::wait_landed(&q_full, (n & 1u) ^ 1u, patience);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      wait_st();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) npp::mbar_arrive(&p_full[i]);
     }
-    if (ok && n_kv[i] > 0) ok = __all_sync(0xffffffffu, wait(&o_full[i], 0));
-    if (ok && n_kv[i] > 0) {
+  } else if (wid == kZeroWarp) {
+    fewer_registers();
+    // ------------------------------ rows past a prompt in its last V tile: zero, whatever lies there ------------------------------
+    uint32_t tiles_before = 0, asked = 0;
+    Plan p;
+    for (uint32_t n = 0; plan(n, p, true); ++n) {
+      const Work w(p, a.tile_tokens);
+      tiles_before += w.n_tiles;
+      if (!w.tail) continue;
+      const uint32_t load = 2 * tiles_before - 1, s = load % S::kStages;
+      // only once the copy has been asked for is the parity of `full` that of its use of the stage
+      if (!wait_all(&v_asked[s], (asked >> s) & 1u) || !wait_all(&full[s], (load / S::kStages) & 1u)) break;
+      asked ^= 1u << s;
+      const int from = w.len - (w.n_tiles - 1) * kRows, words = (kRows - from) * 8;  // 16-byte words of a half
+      for (int e = lane; e < words * S::kHalves; e += 32) {
+        const int h = e / words, x = e - h * words;
+        *reinterpret_cast<uint4*>(ring + s * S::kTileBytes + h * S::kHalfBytes + from * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+      }
+      npp::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) npp::mbar_arrive(&v_zeroed[s]);
+    }
+  } else if (wid == kMmaWarp) {
+    fewer_registers();
+    // ------------------------------ products ------------------------------
+    // The whole warp goes through the loop and one lane issues: what an instruction takes (descriptors, addresses) then is
+    // the same in all lanes, and the compiler keeps it in uniform registers, where the instruction wants it.
+    const uint32_t fmt = kBf16 ? 1u : 0u;
+    const uint32_t common = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(kRows >> 4) << 24);
+    const uint32_t id_s = common | ((uint32_t)(kRows >> 3) << 17), id_o = common | (1u << 16) | ((uint32_t)(HD >> 3) << 17);
+    const uint64_t q_desc = smem_desc(npp::smem_addr(q_sm), 16), k_desc = smem_desc(npp::smem_addr(ring), 16),
+                   v_desc = smem_desc(npp::smem_addr(ring), S::kHalfBytes);
+    auto scores = [&](int i, uint32_t st) {
+      const uint64_t qd = q_desc + (uint32_t)i * (S::kTileBytes >> 4), kd = k_desc + st * (S::kTileBytes >> 4);
+#pragma unroll
+      for (int k = 0; k < HD / 16; ++k) {
+        const uint32_t off = ((k >> 2) * S::kHalfBytes + (k & 3) * 32) >> 4;
+        mma_ss(tmem + i * kRows, qd + off, kd + off, id_s, k > 0);
+      }
+      commit(&s_full[i]);
+    };
+    uint32_t ld = 0, p_cnt[2] = {0, 0}, o_cnt[2] = {0, 0};  // loads, softmax steps and results so far
+    uint32_t zeroed = 0;  // the parity of each stage's next zeroing
+    Plan p;
+    bool ok = true;
+    for (uint32_t n = 0; ok && plan(n, p, true); ++n) {
+      const Work w(p, a.tile_tokens);
+      ok = wait_all(&q_full, n & 1u) && wait_all(&full[ld % S::kStages], (ld / S::kStages) & 1u);
+      if (!ok) break;
+      fence_after();
+      if (elect_one()) {
+        for (int i = 0; i < 2; ++i)
+          if (w.n_kv[i] > 0) scores(i, ld % S::kStages);
+        commit(&empty[ld % S::kStages]);
+        if (w.n_tiles == 1) commit(&q_empty);
+      }
+      __syncwarp();
+      for (int j = 0; j < w.n_tiles && ok; ++j) {
+        const uint32_t lv = ld + 2 * j + 1, lk = lv + 1, sv = lv % S::kStages, sk = lk % S::kStages;
+        const bool more = j + 1 < w.n_tiles;
+        ok = wait_all(&full[sv], (lv / S::kStages) & 1u);
+        if (ok && w.tail && !more) {
+          ok = wait_all(&v_zeroed[sv], (zeroed >> sv) & 1u);
+          zeroed ^= 1u << sv;
+        }
+        bool have_k = false;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (j >= w.n_kv[i] || !ok) continue;
+          if (j == 0) {  // the tile before has been read out of the accumulators
+            ok = wait_all(&o_empty[i], (o_cnt[i] & 1u) ^ 1u);
+            ++o_cnt[i];
+          }
+          const uint32_t par = p_cnt[i]++ & 1u;
+          const uint64_t vd = v_desc + sv * (S::kTileBytes >> 4);
+          ok = ok && wait_all(&p_half[i], par);
+          if (!ok) continue;
+          fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < kRows / 32; ++k) mma_ts(tmem + 256 + i * HD, tmem + i * kRows + k * 8, vd + k * 128, id_o, (j | k) > 0);
+          }
+          __syncwarp();
+          ok = wait_all(&p_full[i], par);
+          if (ok && !have_k && j + 1 < w.n_kv[i]) {
+            ok = wait_all(&full[sk], (lk / S::kStages) & 1u);
+            have_k = true;
+          }
+          if (!ok) continue;
+          fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = kRows / 32; k < kRows / 16; ++k) mma_ts(tmem + 256 + i * HD, tmem + i * kRows + k * 8, vd + k * 128, id_o, 1u);
+            if (j + 1 < w.n_kv[i]) scores(i, sk);
+            else commit(&o_full[i]);
+          }
+          __syncwarp();
+        }
+        if (ok && elect_one()) {
+          commit(&empty[sv]);
+          if (more) commit(&empty[sk]);
+          if (j + 2 == w.n_tiles) commit(&q_empty);
+        }
+        __syncwarp();
+      }
+      ld += 2 * w.n_tiles;
+    }
+  } else {
+    more_registers();
+    // ------------------------------ softmax and result of a tile ------------------------------
+    const int i = wid >> 2, row = (wid & 3) * 32 + lane;
+    const int in_tile = row / a.group, in_group = row - in_tile * a.group;
+    const uint32_t ts = tmem + ((uint32_t)((wid & 3) * 32) << 16) + i * kRows, to = tmem + ((uint32_t)((wid & 3) * 32) << 16) + 256 + i * HD;
+    unsigned char* stage = out_sm + wid * S::kOutBytes;
+    uint32_t s_cnt = 0, o_cnt = 0;
+    Plan p;
+    bool ok = true;
+    for (uint32_t n = 0; ok && plan(n, p, true); ++n) {
+      const Work w(p, a.tile_tokens);
+      const int steps = w.n_kv[i];
+      if (steps == 0) continue;
+      const int first = w.q0 + i * a.tile_tokens, tok = first + in_tile;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < steps; ++j) {
+        ok = wait_all(&s_full[i], s_cnt++ & 1u);
+        if (!ok) break;
+        fence_after();
+        uint32_t s[kRows];
+#pragma unroll
+        for (int c = 0; c < kRows; c += 32) tm_ld32(ts + c, s, c);
+        wait_ld();
+        const bool masked = (j + 1) * kRows - 1 > first;  // the tile reaches past the first row
+        if (masked) {
+          const int see = tok - j * kRows;
+#pragma unroll
+          for (int c = 0; c < kRows; ++c)
+            if (c > see) s[c] = __float_as_uint(-INFINITY);
+        }
+        float top[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top[x] = max3(__uint_as_float(s[x]), __uint_as_float(s[x + 4]), __uint_as_float(s[x + 8]));
+#pragma unroll
+        for (int c = 12; c + 8 <= kRows; c += 8) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) top[x] = max3(top[x], __uint_as_float(s[c + x]), __uint_as_float(s[c + 4 + x]));
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top[x] = max3(top[x], __uint_as_float(s[kRows - 4 + x]), -INFINITY);
+        // a NaN makes the maximum NaN, and with it the row; an infinite score does, too (inf - inf)
+        float now = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY) * a.scale2;
+        now = max3(m, now, now == INFINITY ? __uint_as_float(0x7fffffffu) : -INFINITY);
+        if (j == 0) {
+          m = now;
+        } else if (__any_sync(0xffffffffu, !(now <= m + kGrow))) {
+          const float f = exp2_fast(m - (now == -INFINITY ? 0.f : now));
+          m = now;
+          l *= f;
+#pragma unroll
+          for (int c = 0; c < HD; c += 32) {
+            uint32_t o[32];
+            tm_ld32(to + c, o, 0);
+            wait_ld();
+            uint32_t x16[16];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+              for (int x = 0; x < 16; ++x) x16[x] = __float_as_uint(__uint_as_float(o[h * 16 + x]) * f);
+              tm_st16(to + c + h * 16, x16);
+            }
+          }
+        }
+        auto arrive = [&](uint64_t* bar) {
+          wait_st();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) npp::mbar_arrive(bar);
+        };
+        auto half = [&] { arrive(&p_half[i]); };
+        // The polynomial has no zeros and no NaN: rows without a finite maximum and masked scores are left to the other units.
+        if (masked || __any_sync(0xffffffffu, !(m > -INFINITY))) {
+          const float use = m == -INFINITY ? 0.f : m;
+          l += softmax_row<kBf16, true>(s, a.scale2, use, ts, half);
+        } else {
+          l += softmax_row<kBf16, false>(s, a.scale2, m, ts, half);
+        }
+        arrive(&p_full[i]);
+      }
+      if (ok) ok = wait_all(&o_full[i], o_cnt++ & 1u);
+      if (!ok) break;
+      // ---- the result: through shared memory, so that lanes store neighbouring bytes of a row
       fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      uint16_t* out = a.out + (int64_t)(start + tok) * a.o_token + (int64_t)head * a.o_head;
+      const bool valid = in_tile < a.tile_tokens && tok < w.len;
+      const int head0 = w.kvh * a.group;
       uint32_t big = __float_as_uint(l) & 0x7fffffffu;
 #pragma unroll
       for (int c = 0; c < HD; c += 32) {
         uint32_t o[32];
         tm_ld32(to + c, o, 0);
         wait_ld();
+        if (c + 32 == HD) {  // the accumulators may be written again
+          fence_before();
+          __syncwarp();
+          if (lane == 0) npp::mbar_arrive(&o_empty[i]);
+        }
 #pragma unroll
         for (int x = 0; x < 32; ++x) big = max(big, o[x] & 0x7fffffffu);
-        if (valid) {
 #pragma unroll
-          for (int x = 0; x < 32; x += 8) {
-            uint4 v;
-            v.x = pack<kBf16>(__uint_as_float(o[x]) * inv, __uint_as_float(o[x + 1]) * inv);
-            v.y = pack<kBf16>(__uint_as_float(o[x + 2]) * inv, __uint_as_float(o[x + 3]) * inv);
-            v.z = pack<kBf16>(__uint_as_float(o[x + 4]) * inv, __uint_as_float(o[x + 5]) * inv);
-            v.w = pack<kBf16>(__uint_as_float(o[x + 6]) * inv, __uint_as_float(o[x + 7]) * inv);
-            *reinterpret_cast<uint4*>(out + c + x) = v;
-          }
+        for (int x = 0; x < 4; ++x) {
+          uint4 v;
+          v.x = pack<kBf16>(__uint_as_float(o[8 * x]) * inv, __uint_as_float(o[8 * x + 1]) * inv);
+          v.y = pack<kBf16>(__uint_as_float(o[8 * x + 2]) * inv, __uint_as_float(o[8 * x + 3]) * inv);
+          v.z = pack<kBf16>(__uint_as_float(o[8 * x + 4]) * inv, __uint_as_float(o[8 * x + 5]) * inv);
+          v.w = pack<kBf16>(__uint_as_float(o[8 * x + 6]) * inv, __uint_as_float(o[8 * x + 7]) * inv);
+          *reinterpret_cast<uint4*>(stage + lane * 64 + ((x ^ ((lane >> 1) & 3)) * 16)) = v;
         }
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {  // eight rows a turn, four lanes each
+          const int r = x * 8 + (lane >> 2), piece = lane & 3;
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 64 + ((piece ^ ((r >> 1) & 3)) * 16));
+          const int rr = (wid & 3) * 32 + r, t = rr / a.group;
+          if (t < a.tile_tokens && first + t < w.len)
+            *reinterpret_cast<uint4*>(a.out + (int64_t)(w.start + first + t) * a.o_token + (int64_t)(head0 + rr - t * a.group) * a.o_head + c + piece * 8) = v;
+        }
+        __syncwarp();
       }
-      if (valid && a.lse) a.lse[(size_t)(start + tok) * a.n_heads + head] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * kLn2 + logf(l);
+      if (valid && a.lse)
+        a.lse[(size_t)(w.start + tok) * a.n_heads + head0 + in_group] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * kLn2 + logf(l);
       uint32_t again = __ballot_sync(0xffffffffu, valid && big >= 0x7f800000u);
       while (again) {
         const int src = __ffs(again) - 1;
         again &= again - 1;
-        row_again<kBf16, HD>(a, start, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), kvh, lane);
+        row_again<kBf16, HD>(a, w.start, __shfl_sync(0xffffffffu, tok, src), head0 + __shfl_sync(0xffffffffu, in_group, src), w.kvh, lane);
       }
     }
   }
@@ -558,19 +785,18 @@ extern "C" int np_attn_prompt(const np_attn_shape* d, const np_rows* q, const np
   a.group = group;
   a.tile_tokens = kRows / group;
   a.scale2 = scale * kLog2e;
-  // a prompt of x tokens has ceil(x / block) blocks: together at most this many
-  const int block_tokens = 2 * a.tile_tokens;
-  const int64_t blocks = ((int64_t)n_tokens / block_tokens + std::min<int64_t>(n, n_tokens)) * d->n_kv_heads;
-  if (blocks > 0x7fffffffLL) return fail(NP_E_INVAL, "too many tokens for one call");
   int sms;
   if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
+  // a prompt of x tokens has ceil(x / (2 * tile_tokens)) blocks of work: together at most this many
+  const int64_t work = ((int64_t)n_tokens / (2 * a.tile_tokens) + std::min<int64_t>(n, n_tokens)) * d->n_kv_heads;
+  const unsigned blocks = (unsigned)std::min<int64_t>(work, sms);
   CUtensorMap mq, mk, mv;
   if (!make_map(&mq, *q, d->head_dim, d->n_heads, n_tokens, group, a.tile_tokens) || !make_map(&mk, *k, d->head_dim, d->n_kv_heads, n_tokens, 1, kRows) ||
       !make_map(&mv, *v, d->head_dim, d->n_kv_heads, n_tokens, 1, kRows))
     return fail(NP_E_INVAL, "rows that a tensor map does not describe (strides of 2^40 bytes and more)");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (d->dtype == NP_T_BF16) e = d->head_dim == 128 ? launch<true, 128>(mq, mk, mv, a, (unsigned)blocks, s) : launch<true, 64>(mq, mk, mv, a, (unsigned)blocks, s);
-  else e = d->head_dim == 128 ? launch<false, 128>(mq, mk, mv, a, (unsigned)blocks, s) : launch<false, 64>(mq, mk, mv, a, (unsigned)blocks, s);
+  if (d->dtype == NP_T_BF16) e = d->head_dim == 128 ? launch<true, 128>(mq, mk, mv, a, blocks, s) : launch<true, 64>(mq, mk, mv, a, blocks, s);
+  else e = d->head_dim == 128 ? launch<false, 128>(mq, mk, mv, a, blocks, s) : launch<false, 64>(mq, mk, mv, a, blocks, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);
 }

@@ -121,9 +121,10 @@ def test_append_refuses_bad_arguments(lib):
 def test_decode_refuses_bad_arguments(lib):
     d, t, bad = _desc(), _tables(), nb.NP_E_INVAL
 
-    def call(layer=0, q=_rows(), heads=8, seqs=P, n=2, scale=0.1, out=_rows(), ws=P, cache=P, tables=t):
-        return lib.np_attn_decode(_b(d), cache, layer, _b(tables), _b(q), heads, seqs, n, scale, _b(out), None, ws, None)
+    def call(layer=0, q=_rows(), heads=8, seqs=P, n=2, scale=0.1, out=_rows(), ws=P, size=1 << 40, cache=P, tables=t):
+        return lib.np_attn_decode(_b(d), cache, layer, _b(tables), _b(q), heads, seqs, n, scale, _b(out), None, ws, size, None)
 
+    assert call(size=nb.np_attn_workspace_bytes(d, 8, 2) - 1) == bad and "workspace" in lib.np_attn_last_error().decode()
     assert call(heads=6) == bad and call(heads=0) == bad and call(n=-1) == bad and call(n=1025) == bad and call(n=9, seqs=None) == bad
     assert call(layer=2) == bad and call(cache=None) == bad and call(ws=None) == bad and call(ws=P + 4) == bad
     for s in (0.0, -1.0, float("inf"), float("nan")):
@@ -154,7 +155,7 @@ def test_without_a_device_calls_fail(lib):
         pytest.skip("a device is there")
     d, t = _desc(), _tables()
     assert lib.np_kv_free(_b(d), _b(t), P, 2, None) == nb.NP_E_CUDA
-    assert lib.np_attn_decode(_b(d), P, 0, _b(t), _b(_rows()), 8, P, 2, 0.1, _b(_rows()), None, P, None) == nb.NP_E_CUDA
+    assert lib.np_attn_decode(_b(d), P, 0, _b(t), _b(_rows()), 8, P, 2, 0.1, _b(_rows()), None, P, 1 << 40, None) == nb.NP_E_CUDA
 
 
 def test_binding_refuses_host_tensors_and_other_types(lib):

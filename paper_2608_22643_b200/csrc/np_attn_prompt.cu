@@ -7,9 +7,11 @@
 // products take 1024 cycles of the tensor cores and the exponentials 1024 cycles of the special function units, so the two
 // have to overlap completely:
 //
-// * A block holds two tiles of 128 query rows of the same key-value head.  While the plain cores do one tile's softmax, the
-//   tensor cores do the other's products.  Roles: two groups of four warps (softmax and result of a tile, a row per lane),
-//   one warp that issues the products, one that loads.
+// * A block holds two tiles of 128 query rows of the same key-value head (or an SM two blocks of one tile, for short prompts).
+//   While the plain cores do one tile's softmax, the tensor cores do the other's products.  Roles: four warps to a tile (softmax and
+//   result, a row per lane), one warp that issues the products, one that loads, one that lays out the block's next work.
+// * Blocks stay and take one block of work after the other, the ones with the most keys first; loads and the first scores of the
+//   next run while the result of the last is stored.
 // * A tile's 128 rows are (token, query head) pairs of one group, tokens outermost: with eight heads to a group a tile is
 //   sixteen tokens, keys and values are read once for all eight, and a short prompt fills its tiles.  Heads that do not
 //   divide 128 leave the last rows of a tile unused.
@@ -39,16 +41,8 @@ namespace npa {
 namespace {
 
 constexpr int kRows = 128;              // query rows of a tile, keys of a tile
-constexpr int kThreads = 384;
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kPlanWarp = 10, kZeroWarp = 11;
 constexpr float kGrow = 8.f;            // log2 of the growth of a maximum that is let pass
 constexpr int kPlans = 2;               // blocks of work that are laid out ahead
-constexpr int kPlanReaders = 11;        // warps that read a plan: eight of the softmax, products, loads, zeros
-#ifndef NP_POLY
-#define NP_POLY 4
-#endif
-constexpr int kPoly = NP_POLY;          // of sixteen pairs of exponentials, those that the FMA units compute
-
 struct PromptArgs {
   const uint16_t* q;
   const uint16_t* k;
@@ -60,6 +54,7 @@ struct PromptArgs {
   int32_t* status;
   int n, n_tokens, n_heads, n_kv_heads, group, tile_tokens;
   float scale2;  // scale * log2(e)
+  int out32;     // rows of out start on 32-byte boundaries
 };
 
 __device__ __forceinline__ void tma_load_3d(void* dst_smem, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
@@ -122,10 +117,24 @@ __device__ __forceinline__ void tm_st16(uint32_t taddr, const uint32_t (&r)[16])
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-// The block's registers (384 threads x 168) are dealt out anew: 200 for each thread of the softmax warps, which hold a row of scores,
-// 104 for the others.  8 * 200 + 4 * 104 = 12 * 168.
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 200;"); }
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
+// The block's registers are dealt out anew: 192 or 200 for each thread of the softmax warps, which hold a row of scores, the rest for the
+// four others.  Two tiles: 384 threads x 168 = 8 warps x 200 + 4 x 104; one tile: 256 x 128 = 4 x 192 + 4 x 64.
+template <int kTiles>
+__device__ __forceinline__ void more_registers() {
+  if (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+}
+template <int kTiles>
+__device__ __forceinline__ void fewer_registers() {
+  if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+}
+// 32 bytes, 32-byte aligned: a whole sector
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+               "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -156,27 +165,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-// 2^x of two x <= 8 on the FMA units: x = n + f with n the nearest integer (adding 1.5 * 2^23 leaves it in the low bits), 2^f on
-// [-1/2, 1/2] by the polynomial of degree 5 with the least relative error (2^-23.7, fitted to 2^f by reweighted least squares),
-// n added to the exponent.  Below -126 the result stays about 2^-126.  Not for NaN.
-__device__ __forceinline__ void exp2_poly(f32x2 x, float& lo, float& hi) {
-  float a, b;
-  apart(x, a, b);
-  x = two(fmaxf(a, -126.f), fmaxf(b, -126.f));
-  const float magic = 12582912.f;
-  const f32x2 t = add2(x, two(magic, magic)), n = add2(t, two(-magic, -magic)), f = fma2(n, two(-1.f, -1.f), x);
-  f32x2 p = two(0.0013276472454890609f, 0.0013276472454890609f);
-  p = fma2(p, f, two(0.009675540961325169f, 0.009675540961325169f));
-  p = fma2(p, f, two(0.05550713092088699f, 0.05550713092088699f));
-  p = fma2(p, f, two(0.24022120237350464f, 0.24022120237350464f));
-  p = fma2(p, f, two(0.6931469440460205f, 0.6931469440460205f));
-  p = fma2(p, f, two(1.0000001192092896f, 1.0000001192092896f));
-  float ta, tb, pa, pb;
-  apart(t, ta, tb);
-  apart(p, pa, pb);
-  lo = __uint_as_float(__float_as_uint(pa) + (__float_as_uint(ta) << 23));
-  hi = __uint_as_float(__float_as_uint(pb) + (__float_as_uint(tb) << 23));
 }
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -232,75 +220,89 @@ __device__ __noinline__ void row_again(const PromptArgs& a, int start, int tok, 
     a.lse[(size_t)(start + tok) * a.n_heads + head] = sum == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * kLn2 + logf(sum);
 }
 
-template <int HD>
+template <int HD, int kTiles>
 struct Shape {
   static constexpr int kHalves = HD / 64;                        // 64 values = 128 bytes: one swizzle row
   static constexpr uint32_t kHalfBytes = kRows * 128;            // a tile's rows of one half
   static constexpr uint32_t kTileBytes = kHalves * kHalfBytes;
-  static constexpr int kStages = HD == 128 ? 4 : 8;              // K0 V0 K1 V1 ...
-  static constexpr uint32_t kOutBytes = 2048;                    // a warp's 32 rows x 32 values on their way out
-  static constexpr size_t kSmem = (2 + kStages) * (size_t)kTileBytes + 8 * kOutBytes + 1024;
+  static constexpr int kStages = 2 * kTiles * (128 / HD);        // K0 V0 K1 V1 ...
+  static constexpr size_t kSmem = (kTiles + kStages) * (size_t)kTileBytes + 1024;
+  static constexpr int kSoftmaxWarps = 4 * kTiles, kMmaWarp = kSoftmaxWarps, kLoadWarp = kMmaWarp + 1, kPlanWarp = kMmaWarp + 2;
+  static constexpr int kThreads = 32 * kSoftmaxWarps + 128;      // the last warp has nothing to do
+  static constexpr int kPlanReaders = kSoftmaxWarps + 2;         // warps that read a plan: softmax, products, loads
+  static constexpr int kColumns = kTiles * 256;                  // of tensor memory: scores, then accumulators
 };
 
-// A block of work: two tiles of rows of one prompt and key-value head.
+// A block of work: the tiles of rows, one or two, of one prompt and key-value head.
 struct Plan {
   int start, len, q0, kvh;  // first row and tokens of the prompt, first token of the block; len 0: nothing is left
 };
 
+template <int kTiles>
 struct Work {
-  int start, len, q0, kvh, n_kv[2], n_tiles;
+  int start, len, q0, kvh, n_kv[kTiles], n_tiles;
   bool tail;  // the last tile of keys reaches past the prompt
   __device__ __forceinline__ Work(const Plan& p, int tile_tokens) : start(p.start), len(p.len), q0(p.q0), kvh(p.kvh) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kTiles; ++i) {
       const int first = q0 + i * tile_tokens, end = min(first + tile_tokens, len);
       n_kv[i] = end > first ? (end + kRows - 1) / kRows : 0;  // the second tile may have no row
     }
-    n_tiles = max(n_kv[0], n_kv[1]);
+    n_tiles = max(n_kv[0], n_kv[kTiles - 1]);
     tail = n_tiles * kRows > len;
   }
 };
 
-// P = exp2(scale2 * S - m) of a row's 128 scores into tensor memory, its sum; `half` is called when the first half is there.
-template <bool kBf16, bool kPlain, class Half>
-__device__ __forceinline__ float softmax_row(const uint32_t (&s)[kRows], float scale2, float use, uint32_t tp, Half half) {
+// P = exp2(scale2 * S - m) of 64 of a row's scores, from column C on, into tensor memory; their sum.
+template <bool kBf16, int C>
+__device__ __forceinline__ float softmax_half(const uint32_t (&s)[kRows], float scale2, float use, uint32_t tp) {
   const f32x2 sc = two(scale2, scale2), off = two(-use, -use);
   f32x2 sum[2] = {0, 0};
 #pragma unroll
-  for (int c = 0; c < kRows; c += 32) {
+  for (int c = C; c < C + kRows / 2; c += 32) {
     uint32_t w[16];
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
       const f32x2 e = fma2(two(__uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1])), sc, off);
       float p0, p1;
-      if (!kPlain && (x * kPoly) % 16 + kPoly >= 16) {
-        exp2_poly(e, p0, p1);
-      } else {
-        apart(e, p0, p1);
-        p0 = exp2_fast(p0);
-        p1 = exp2_fast(p1);
-      }
+      apart(e, p0, p1);
+      p0 = exp2_fast(p0);
+      p1 = exp2_fast(p1);
       sum[x & 1] = add2(sum[x & 1], two(p0, p1));
       w[x] = pack<kBf16>(p0, p1);
     }
     tm_st16(tp + c / 2, w);
-    if (c == 32) half();
   }
   float a, b;
   apart(add2(sum[0], sum[1]), a, b);
   return a + b;
 }
 
-template <bool kBf16, int HD>
-__global__ void __launch_bounds__(kThreads, 1)
+// The largest of a row's scores; NaN if one is.
+__device__ __forceinline__ float row_max(const uint32_t (&s)[kRows]) {
+  float top[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) top[x] = max3(__uint_as_float(s[x]), __uint_as_float(s[x + 4]), __uint_as_float(s[x + 8]));
+#pragma unroll
+  for (int c = 12; c + 8 <= kRows; c += 8) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) top[x] = max3(top[x], __uint_as_float(s[c + x]), __uint_as_float(s[c + 4 + x]));
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x) top[x] = max3(top[x], __uint_as_float(s[kRows - 4 + x]), -INFINITY);
+  return max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
+}
+
+template <bool kBf16, int HD, int kTiles>
+__global__ void __launch_bounds__(Shape<HD, kTiles>::kThreads, 3 - kTiles)
 k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
               const __grid_constant__ PromptArgs a) {
-  using S = Shape<HD>;
+  using S = Shape<HD, kTiles>;
   extern __shared__ __align__(1024) unsigned char tsm[];
   __shared__ int s_blocks[NP_KV_MAX_SEQS];  // blocks of work of each prompt (per key-value head)
   __shared__ Plan s_plan[kPlans];
-  __shared__ __align__(8) uint64_t full[S::kStages], empty[S::kStages], q_full, q_empty, s_full[2], p_half[2], p_full[2], o_full[2], o_empty[2],
-      v_asked[S::kStages], v_zeroed[S::kStages], plan_full[kPlans], plan_empty[kPlans];
+  __shared__ __align__(8) uint64_t full[S::kStages], empty[S::kStages], q_full, q_empty, s_full[kTiles], p_half[kTiles], p_full[kTiles], o_full[kTiles], o_empty[kTiles],
+      plan_full[kPlans], plan_empty[kPlans];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_ok[2];
   npp::pdl_wait_prior();
@@ -309,19 +311,16 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tsm) + 1023) & ~(uintptr_t)1023);
   unsigned char* q_sm = base;
-  unsigned char* ring = base + 2 * S::kTileBytes;
-  unsigned char* out_sm = ring + S::kStages * S::kTileBytes;
+  unsigned char* ring = base + kTiles * S::kTileBytes;
 
   if (tid == 0) {
     for (int s = 0; s < S::kStages; ++s) {
       npp::mbar_init(&full[s], 1);
       npp::mbar_init(&empty[s], 1);
-      npp::mbar_init(&v_asked[s], 1);
-      npp::mbar_init(&v_zeroed[s], 1);
     }
     npp::mbar_init(&q_full, 1);
     npp::mbar_init(&q_empty, 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kTiles; ++i) {
       npp::mbar_init(&s_full[i], 1);
       npp::mbar_init(&p_half[i], 4);
       npp::mbar_init(&p_full[i], 4);
@@ -330,18 +329,28 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     }
     for (int i = 0; i < kPlans; ++i) {
       npp::mbar_init(&plan_full[i], 1);
-      npp::mbar_init(&plan_empty[i], kPlanReaders);
+      npp::mbar_init(&plan_empty[i], S::kPlanReaders);
     }
     npp::fence_barrier_init();
     s_ok[0] = 1;
     s_ok[1] = 0;
   }
-  for (int i = tid; i < a.n; i += kThreads) {
-    const int lo = min(max(a.cu[i], 0), a.n_tokens), hi = min(max(a.cu[i + 1], 0), a.n_tokens);
-    s_blocks[i] = hi > lo ? (hi - lo + 2 * a.tile_tokens - 1) / (2 * a.tile_tokens) : 0;
+  // the plan warp counts the blocks of each prompt while the others set up
+  if (wid == S::kPlanWarp) {
+    const int block_tokens = kTiles * a.tile_tokens;
+    for (int i = lane; i < a.n; i += 32) {
+      const int lo = min(max(a.cu[i], 0), a.n_tokens), hi = min(max(a.cu[i + 1], 0), a.n_tokens);
+      s_blocks[i] = hi > lo ? (hi - lo - 1) / block_tokens + 1 : 0;
+    }
+    __syncwarp();
   }
-  if (wid == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(npp::smem_addr(&s_tmem)), "r"(512) : "memory");
+  if (wid == S::kLoadWarp && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+  }
+  if (wid == S::kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(npp::smem_addr(&s_tmem)), "r"(S::kColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_before();
@@ -365,46 +374,44 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     return p.len > 0;
   };
 
-  if (wid == kPlanWarp) {
-    fewer_registers();
+  if (wid >= S::kMmaWarp) {
+   fewer_registers<kTiles>();
+   if (wid == S::kPlanWarp) {
     // ------------------------------ plans ------------------------------
     // Blocks of work in falling order of their place in their prompt, which is the order of their number of keys; this block
     // takes every gridDim-th, in alternating direction, so that all blocks get about the same.
+    const int first_blocks = lane < a.n ? s_blocks[lane] : 0;  // of the first 32 prompts, at hand
     auto from_place = [&](int b) {  // blocks of work at place b or later, all prompts, one key-value head
-      int64_t sum = 0;
-      for (int i = lane; i < a.n; i += 32) sum += max(0, s_blocks[i] - b);
-#pragma unroll
-      for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-      return sum;
+      int sum = max(0, first_blocks - b);
+      for (int i = lane + 32; i < a.n; i += 32) sum += max(0, s_blocks[i] - b);
+      return __reduce_add_sync(0xffffffffu, sum);
     };
-    int most = 0;
-    for (int i = lane; i < a.n; i += 32) most = max(most, s_blocks[i]);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, x));
-    const int64_t total = from_place(0) * a.n_kv_heads;
+    int most = first_blocks;
+    for (int i = lane + 32; i < a.n; i += 32) most = max(most, s_blocks[i]);
+    most = __reduce_max_sync(0xffffffffu, most);
+    const unsigned total = (unsigned)from_place(0) * a.n_kv_heads;
     for (uint32_t n = 0;; ++n) {
-      const int64_t r = (int64_t)n * gridDim.x + (n & 1u ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      const unsigned r = n * gridDim.x + (n & 1u ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
       Plan p = {0, 0, 0, 0};
       if (r < total) {
-        const int64_t at = r / a.n_kv_heads;
+        const int at = (int)(r / (unsigned)a.n_kv_heads);
         int lo = 0, hi = most - 1;  // the largest place with more than `at` blocks from it on
         while (lo < hi) {
           const int mid = (lo + hi + 1) >> 1;
           if (from_place(mid) > at) lo = mid;
           else hi = mid - 1;
         }
-        int which = (int)(at - from_place(lo + 1));  // among the prompts that have that place
+        int which = at - from_place(lo + 1);  // among the prompts that have that place
         for (int first = 0; first < a.n; first += 32) {
-          const uint32_t has = __ballot_sync(0xffffffffu, first + lane < a.n && s_blocks[first + lane] > lo);
+          const uint32_t has = __ballot_sync(0xffffffffu, first + lane < a.n && (first == 0 ? first_blocks : s_blocks[first + lane]) > lo);
           const int cnt = __popc(has);
           if (which < cnt) {
-            uint32_t rest = has;
-            for (int x = 0; x < which; ++x) rest &= rest - 1;
-            const int i = first + __ffs(rest) - 1;
+            const bool it = (has >> lane & 1u) && __popc(has & ((1u << lane) - 1u)) == which;
+            const int i = first + __ffs(__ballot_sync(0xffffffffu, it)) - 1;
             p.start = min(max(a.cu[i], 0), a.n_tokens);
             p.len = min(max(a.cu[i + 1], 0), a.n_tokens) - p.start;
-            p.q0 = lo * 2 * a.tile_tokens;
-            p.kvh = (int)(r % a.n_kv_heads);
+            p.q0 = lo * kTiles * a.tile_tokens;
+            p.kvh = (int)(r - (unsigned)at * a.n_kv_heads);
             break;
           }
           which -= cnt;
@@ -418,8 +425,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       __syncwarp();
       if (p.len == 0) break;
     }
-  } else if (wid == kLoadWarp) {
-    fewer_registers();
+   } else if (wid == S::kLoadWarp) {
     // ------------------------------ loads ------------------------------
     if (lane == 0) {
       int stage = 0;
@@ -427,8 +433,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       Plan p;
       bool ok = true;
       for (; ok && plan(n, p, false); ++n) {
-        const Work w(p, a.tile_tokens);
-        const int tiles = w.n_kv[1] > 0 ? 2 : 1;
+        const Work<kTiles> w(p, a.tile_tokens);
+        const int tiles = w.n_kv[kTiles - 1] > 0 ? kTiles : 1;
         ok = wait(&q_empty, (n & 1u) ^ 1u);
         if (!ok) break;
         npp::mbar_expect_tx(&q_full, (uint32_t)tiles * S::kHalves * 128 * a.group * a.tile_tokens);
@@ -442,7 +448,6 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           for (int h = 0; h < S::kHalves; ++h)
             tma_load_3d(ring + stage * S::kTileBytes + h * S::kHalfBytes, j & 1 ? &map_v : &map_k, h * 64, w.kvh, w.start + (j >> 1) * kRows,
                         &full[stage]);
-          if (w.tail && j + 1 == 2 * w.n_tiles) npp::mbar_arrive(&v_asked[stage]);
           if (++stage == S::kStages) {
             stage = 0;
             ++use;
@@ -456,33 +461,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         if (n > 0) npp::wait_landed(&q_full, (n & 1u) ^ 1u, patience);
       }
     }
-  } else if (wid == kZeroWarp) {
-    fewer_registers();
-    // ------------------------------ rows past a prompt in its last V tile: zero, whatever lies there ------------------------------
-    uint32_t tiles_before = 0, asked = 0;
-    Plan p;
-    for (uint32_t n = 0; plan(n, p, true); ++n) {
-      const Work w(p, a.tile_tokens);
-      tiles_before += w.n_tiles;
-      if (!w.tail) continue;
-      const uint32_t load = 2 * tiles_before - 1, s = load % S::kStages;
-      // only once the copy has been asked for is the parity of `full` that of its use of the stage
-      if (!wait_all(&v_asked[s], (asked >> s) & 1u) || !wait_all(&full[s], (load / S::kStages) & 1u)) break;
-      asked ^= 1u << s;
-      const int from = w.len - (w.n_tiles - 1) * kRows, words = (kRows - from) * 8;  // 16-byte words of a half
-      for (int e = lane; e < words * S::kHalves; e += 32) {
-        const int h = e / words, x = e - h * words;
-        *reinterpret_cast<uint4*>(ring + s * S::kTileBytes + h * S::kHalfBytes + from * 128 + x * 16) = make_uint4(0, 0, 0, 0);
-      }
-      npp::fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) npp::mbar_arrive(&v_zeroed[s]);
-    }
-  } else if (wid == kMmaWarp) {
-    fewer_registers();
+   } else if (wid == S::kMmaWarp) {
     // ------------------------------ products ------------------------------
     // The whole warp goes through the loop and one lane issues: what an instruction takes (descriptors, addresses) then is
-    // the same in all lanes, and the compiler keeps it in uniform registers, where the instruction wants it.
+    // the same in all lanes, and the compiler keeps it in uniform registers, where the instruction wants it.  (One lane in a
+    // loop of its own took 75 cycles per instruction, more than the product itself.)  One warp serves both tiles in turn: with
+    // a warp for each, the tiles fall into step, and the tensor cores wait while both do their softmax.
     const uint32_t fmt = kBf16 ? 1u : 0u;
     const uint32_t common = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(kRows >> 4) << 24);
     const uint32_t id_s = common | ((uint32_t)(kRows >> 3) << 17), id_o = common | (1u << 16) | ((uint32_t)(HD >> 3) << 17);
@@ -497,17 +481,18 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       }
       commit(&s_full[i]);
     };
-    uint32_t ld = 0, p_cnt[2] = {0, 0}, o_cnt[2] = {0, 0};  // loads, softmax steps and results so far
-    uint32_t zeroed = 0;  // the parity of each stage's next zeroing
+    uint32_t ld = 0, p_cnt[kTiles] = {}, o_cnt[kTiles] = {};  // loads, softmax steps and results so far
+    auto wait_load = [&](uint32_t l) { return wait_all(&full[l % S::kStages], (l / S::kStages) & 1u); };
     Plan p;
     bool ok = true;
     for (uint32_t n = 0; ok && plan(n, p, true); ++n) {
-      const Work w(p, a.tile_tokens);
-      ok = wait_all(&q_full, n & 1u) && wait_all(&full[ld % S::kStages], (ld / S::kStages) & 1u);
+      const Work<kTiles> w(p, a.tile_tokens);
+      ok = wait_all(&q_full, n & 1u) && wait_load(ld);
       if (!ok) break;
       fence_after();
       if (elect_one()) {
-        for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
           if (w.n_kv[i] > 0) scores(i, ld % S::kStages);
         commit(&empty[ld % S::kStages]);
         if (w.n_tiles == 1) commit(&q_empty);
@@ -516,39 +501,37 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       for (int j = 0; j < w.n_tiles && ok; ++j) {
         const uint32_t lv = ld + 2 * j + 1, lk = lv + 1, sv = lv % S::kStages, sk = lk % S::kStages;
         const bool more = j + 1 < w.n_tiles;
-        ok = wait_all(&full[sv], (lv / S::kStages) & 1u);
+        ok = wait_load(lv) && (!more || wait_load(lk));
         if (ok && w.tail && !more) {
-          ok = wait_all(&v_zeroed[sv], (zeroed >> sv) & 1u);
-          zeroed ^= 1u << sv;
-        }
-        bool have_k = false;
+          // rows past the prompt: zero, whatever lies there
+          const uint32_t from = (w.len - (w.n_tiles - 1) * kRows) * 128;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+          for (int h = 0; h < S::kHalves; ++h)
+            for (uint32_t e = from + lane * 16; e < S::kHalfBytes; e += 32 * 16)
+              *reinterpret_cast<uint4*>(ring + sv * S::kTileBytes + h * S::kHalfBytes + e) = make_uint4(0, 0, 0, 0);
+          npp::fence_proxy_async();
+          __syncwarp();
+        }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
           if (j >= w.n_kv[i] || !ok) continue;
-          if (j == 0) {  // the tile before has been read out of the accumulators
-            ok = wait_all(&o_empty[i], (o_cnt[i] & 1u) ^ 1u);
-            ++o_cnt[i];
-          }
-          const uint32_t par = p_cnt[i]++ & 1u;
+          if (j == 0) ok = wait_all(&o_empty[i], (o_cnt[i]++ & 1u) ^ 1u);  // the tile before has been read out of the accumulators
+          const uint32_t par = p_cnt[i]++ & 1u, d_s = tmem + i * kRows, d_o = tmem + kTiles * kRows + i * HD;
           const uint64_t vd = v_desc + sv * (S::kTileBytes >> 4);
           ok = ok && wait_all(&p_half[i], par);
           if (!ok) continue;
           fence_after();
-          if (elect_one()) {
+          if (elect_one()) {  // the first 64 keys
 #pragma unroll
-            for (int k = 0; k < kRows / 32; ++k) mma_ts(tmem + 256 + i * HD, tmem + i * kRows + k * 8, vd + k * 128, id_o, (j | k) > 0);
+            for (int k = 0; k < kRows / 32; ++k) mma_ts(d_o, d_s + k * 8, vd + k * 128, id_o, (j | k) > 0);
           }
           __syncwarp();
           ok = wait_all(&p_full[i], par);
-          if (ok && !have_k && j + 1 < w.n_kv[i]) {
-            ok = wait_all(&full[sk], (lk / S::kStages) & 1u);
-            have_k = true;
-          }
           if (!ok) continue;
           fence_after();
           if (elect_one()) {
 #pragma unroll
-            for (int k = kRows / 32; k < kRows / 16; ++k) mma_ts(tmem + 256 + i * HD, tmem + i * kRows + k * 8, vd + k * 128, id_o, 1u);
+            for (int k = kRows / 32; k < kRows / 16; ++k) mma_ts(d_o, d_s + k * 8, vd + k * 128, id_o, 1u);
             if (j + 1 < w.n_kv[i]) scores(i, sk);
             else commit(&o_full[i]);
           }
@@ -563,18 +546,24 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       }
       ld += 2 * w.n_tiles;
     }
+   }
   } else {
-    more_registers();
+    more_registers<kTiles>();
     // ------------------------------ softmax and result of a tile ------------------------------
     const int i = wid >> 2, row = (wid & 3) * 32 + lane;
     const int in_tile = row / a.group, in_group = row - in_tile * a.group;
-    const uint32_t ts = tmem + ((uint32_t)((wid & 3) * 32) << 16) + i * kRows, to = tmem + ((uint32_t)((wid & 3) * 32) << 16) + 256 + i * HD;
-    unsigned char* stage = out_sm + wid * S::kOutBytes;
+    const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16), ts = lanes + i * kRows, to = lanes + kTiles * kRows + i * HD;
     uint32_t s_cnt = 0, o_cnt = 0;
+    auto arrive = [&](uint64_t* bar) {
+      wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) npp::mbar_arrive(bar);
+    };
     Plan p;
     bool ok = true;
     for (uint32_t n = 0; ok && plan(n, p, true); ++n) {
-      const Work w(p, a.tile_tokens);
+      const Work<kTiles> w(p, a.tile_tokens);
       const int steps = w.n_kv[i];
       if (steps == 0) continue;
       const int first = w.q0 + i * a.tile_tokens, tok = first + in_tile;
@@ -587,69 +576,65 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
         for (int c = 0; c < kRows; c += 32) tm_ld32(ts + c, s, c);
         wait_ld();
-        const bool masked = (j + 1) * kRows - 1 > first;  // the tile reaches past the first row
-        if (masked) {
-          const int see = tok - j * kRows;
+        if ((j + 1) * kRows - 1 > first) {  // the tile reaches past the first row
+          const int see = tok - j * kRows, all_see = __shfl_sync(0xffffffffu, see, 0);
 #pragma unroll
-          for (int c = 0; c < kRows; ++c)
-            if (c > see) s[c] = __float_as_uint(-INFINITY);
-        }
-        float top[4];
+          for (int c = 0; c < kRows; c += 32) {
+            if (c + 31 <= all_see) continue;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) top[x] = max3(__uint_as_float(s[x]), __uint_as_float(s[x + 4]), __uint_as_float(s[x + 8]));
-#pragma unroll
-        for (int c = 12; c + 8 <= kRows; c += 8) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) top[x] = max3(top[x], __uint_as_float(s[c + x]), __uint_as_float(s[c + 4 + x]));
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x) top[x] = max3(top[x], __uint_as_float(s[kRows - 4 + x]), -INFINITY);
-        // a NaN makes the maximum NaN, and with it the row; an infinite score does, too (inf - inf)
-        float now = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY) * a.scale2;
-        now = max3(m, now, now == INFINITY ? __uint_as_float(0x7fffffffu) : -INFINITY);
-        if (j == 0) {
-          m = now;
-        } else if (__any_sync(0xffffffffu, !(now <= m + kGrow))) {
-          const float f = exp2_fast(m - (now == -INFINITY ? 0.f : now));
-          m = now;
-          l *= f;
-#pragma unroll
-          for (int c = 0; c < HD; c += 32) {
-            uint32_t o[32];
-            tm_ld32(to + c, o, 0);
-            wait_ld();
-            uint32_t x16[16];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-              for (int x = 0; x < 16; ++x) x16[x] = __float_as_uint(__uint_as_float(o[h * 16 + x]) * f);
-              tm_st16(to + c + h * 16, x16);
-            }
+            for (int x = c; x < c + 32; ++x)
+              if (x > see) s[x] = __float_as_uint(-INFINITY);
           }
         }
-        auto arrive = [&](uint64_t* bar) {
-          wait_st();
-          fence_before();
-          __syncwarp();
-          if (lane == 0) npp::mbar_arrive(bar);
-        };
-        auto half = [&] { arrive(&p_half[i]); };
-        // The polynomial has no zeros and no NaN: rows without a finite maximum and masked scores are left to the other units.
-        if (masked || __any_sync(0xffffffffu, !(m > -INFINITY))) {
-          const float use = m == -INFINITY ? 0.f : m;
-          l += softmax_row<kBf16, true>(s, a.scale2, use, ts, half);
+        // On the assumption that the maximum has not grown much, the first half's exponentials need not wait for it: it is found
+        // beside them, by units that they leave idle.  (The maximum first: 390 cycles of 2350 for a tile.)
+        float part = 0.f, now;
+        bool fast = false;
+        if (j > 0) {
+          part = softmax_half<kBf16, 0>(s, a.scale2, m, ts);
+          now = row_max(s) * a.scale2;
+          fast = __all_sync(0xffffffffu, now <= m + kGrow && m > -INFINITY && now < INFINITY);
         } else {
-          l += softmax_row<kBf16, false>(s, a.scale2, m, ts, half);
+          now = row_max(s) * a.scale2;
         }
+        float use = m;
+        if (!fast) {
+          // a NaN makes the maximum NaN, and with it the row; an infinite score does, too (inf - inf)
+          now = max3(m, now, now == INFINITY ? __uint_as_float(0x7fffffffu) : -INFINITY);
+          if (j == 0) {
+            m = now;
+          } else if (__any_sync(0xffffffffu, !(now <= m + kGrow))) {
+            const float f = exp2_fast(m - (now == -INFINITY ? 0.f : now));
+            m = now;
+            l *= f;
+#pragma unroll
+            for (int c = 0; c < HD; c += 32) {
+              uint32_t o[32], x16[16];
+              tm_ld32(to + c, o, 0);
+              wait_ld();
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int x = 0; x < 16; ++x) x16[x] = __float_as_uint(__uint_as_float(o[h * 16 + x]) * f);
+                tm_st16(to + c + h * 16, x16);
+              }
+            }
+          }
+          use = m == -INFINITY ? 0.f : m;
+          part = softmax_half<kBf16, 0>(s, a.scale2, use, ts);
+        }
+        arrive(&p_half[i]);
+        l += part + softmax_half<kBf16, kRows / 2>(s, a.scale2, use, ts);
         arrive(&p_full[i]);
       }
       if (ok) ok = wait_all(&o_full[i], o_cnt++ & 1u);
       if (!ok) break;
-      // ---- the result: through shared memory, so that lanes store neighbouring bytes of a row
+      // ---- the result
       fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const bool valid = in_tile < a.tile_tokens && tok < w.len;
-      const int head0 = w.kvh * a.group;
+      const int head = w.kvh * a.group + in_group;
+      uint16_t* out = a.out + (int64_t)(w.start + tok) * a.o_token + (int64_t)head * a.o_head;
       uint32_t big = __float_as_uint(l) & 0x7fffffffu;
 #pragma unroll
       for (int c = 0; c < HD; c += 32) {
@@ -663,41 +648,36 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
 #pragma unroll
         for (int x = 0; x < 32; ++x) big = max(big, o[x] & 0x7fffffffu);
+        if (valid) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          uint4 v;
-          v.x = pack<kBf16>(__uint_as_float(o[8 * x]) * inv, __uint_as_float(o[8 * x + 1]) * inv);
-          v.y = pack<kBf16>(__uint_as_float(o[8 * x + 2]) * inv, __uint_as_float(o[8 * x + 3]) * inv);
-          v.z = pack<kBf16>(__uint_as_float(o[8 * x + 4]) * inv, __uint_as_float(o[8 * x + 5]) * inv);
-          v.w = pack<kBf16>(__uint_as_float(o[8 * x + 6]) * inv, __uint_as_float(o[8 * x + 7]) * inv);
-          *reinterpret_cast<uint4*>(stage + lane * 64 + ((x ^ ((lane >> 1) & 3)) * 16)) = v;
-        }
-        __syncwarp();
+          for (int x = 0; x < 32; x += 16) {
+            uint32_t v[8];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {  // eight rows a turn, four lanes each
-          const int r = x * 8 + (lane >> 2), piece = lane & 3;
-          const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 64 + ((piece ^ ((r >> 1) & 3)) * 16));
-          const int rr = (wid & 3) * 32 + r, t = rr / a.group;
-          if (t < a.tile_tokens && first + t < w.len)
-            *reinterpret_cast<uint4*>(a.out + (int64_t)(w.start + first + t) * a.o_token + (int64_t)(head0 + rr - t * a.group) * a.o_head + c + piece * 8) = v;
+            for (int y = 0; y < 8; ++y) v[y] = pack<kBf16>(__uint_as_float(o[x + 2 * y]) * inv, __uint_as_float(o[x + 2 * y + 1]) * inv);
+            if (a.out32) {
+              store32(out + c + x, v);
+            } else {
+              *reinterpret_cast<uint4*>(out + c + x) = make_uint4(v[0], v[1], v[2], v[3]);
+              *reinterpret_cast<uint4*>(out + c + x + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+            }
+          }
         }
-        __syncwarp();
       }
       if (valid && a.lse)
-        a.lse[(size_t)(w.start + tok) * a.n_heads + head0 + in_group] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * kLn2 + logf(l);
+        a.lse[(size_t)(w.start + tok) * a.n_heads + head] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * kLn2 + logf(l);
       uint32_t again = __ballot_sync(0xffffffffu, valid && big >= 0x7f800000u);
       while (again) {
         const int src = __ffs(again) - 1;
         again &= again - 1;
-        row_again<kBf16, HD>(a, w.start, __shfl_sync(0xffffffffu, tok, src), head0 + __shfl_sync(0xffffffffu, in_group, src), w.kvh, lane);
+        row_again<kBf16, HD>(a, w.start, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), w.kvh, lane);
       }
     }
   }
   fence_before();
   __syncthreads();
-  if (wid == kMmaWarp) {
+  if (wid == S::kMmaWarp) {
     fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kColumns) : "memory");
   }
 }
 
@@ -727,11 +707,21 @@ bool make_map(CUtensorMap* map, const np_rows& r, int hd, int heads, int tokens,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool kBf16, int HD>
-cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptArgs& a, unsigned blocks, cudaStream_t s) {
+template <bool kBf16, int HD, int kTiles>
+cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptArgs& a, int sms, cudaStream_t s) {
+  using S = Shape<HD, kTiles>;
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_prompt<kBf16, HD>), &done);
-  return e != cudaSuccess ? e : launch_early(k_attn_prompt<kBf16, HD>, dim3(blocks), kThreads, Shape<HD>::kSmem, s, q, k, v, a);
+  const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_prompt<kBf16, HD, kTiles>), &done);
+  if (e != cudaSuccess) return e;
+  // a prompt of x tokens has ceil(x / (kTiles * tile_tokens)) blocks of work: together at most this many
+  const int64_t work = ((int64_t)a.n_tokens / (kTiles * a.tile_tokens) + std::min(a.n, a.n_tokens)) * a.n_kv_heads;
+  const unsigned blocks = (unsigned)std::min<int64_t>(work, (3 - kTiles) * sms);
+  return launch_early(k_attn_prompt<kBf16, HD, kTiles>, dim3(blocks), S::kThreads, S::kSmem, s, q, k, v, a);
+}
+template <bool kBf16>
+cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptArgs& a, int hd, int tiles, int sms, cudaStream_t s) {
+  if (hd == 128) return tiles == 2 ? launch<kBf16, 128, 2>(q, k, v, a, sms, s) : launch<kBf16, 128, 1>(q, k, v, a, sms, s);
+  return tiles == 2 ? launch<kBf16, 64, 2>(q, k, v, a, sms, s) : launch<kBf16, 64, 1>(q, k, v, a, sms, s);
 }
 
 }  // namespace
@@ -785,18 +775,22 @@ extern "C" int np_attn_prompt(const np_attn_shape* d, const np_rows* q, const np
   a.group = group;
   a.tile_tokens = kRows / group;
   a.scale2 = scale * kLog2e;
+  a.out32 = (uintptr_t)out->data % 32 == 0 && out->token_stride % 16 == 0 && out->head_stride % 16 == 0;
+  if (((int64_t)n_tokens / a.tile_tokens + n) * d->n_kv_heads > 0x7fffffffLL) return fail(NP_E_INVAL, "too many tokens for one call");
   int sms;
   if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
-  // a prompt of x tokens has ceil(x / (2 * tile_tokens)) blocks of work: together at most this many
-  const int64_t work = ((int64_t)n_tokens / (2 * a.tile_tokens) + std::min<int64_t>(n, n_tokens)) * d->n_kv_heads;
-  const unsigned blocks = (unsigned)std::min<int64_t>(work, sms);
   CUtensorMap mq, mk, mv;
   if (!make_map(&mq, *q, d->head_dim, d->n_heads, n_tokens, group, a.tile_tokens) || !make_map(&mk, *k, d->head_dim, d->n_kv_heads, n_tokens, 1, kRows) ||
       !make_map(&mv, *v, d->head_dim, d->n_kv_heads, n_tokens, 1, kRows))
     return fail(NP_E_INVAL, "rows that a tensor map does not describe (strides of 2^40 bytes and more)");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e;
-  if (d->dtype == NP_T_BF16) e = d->head_dim == 128 ? launch<true, 128>(mq, mk, mv, a, blocks, s) : launch<true, 64>(mq, mk, mv, a, blocks, s);
-  else e = d->head_dim == 128 ? launch<false, 128>(mq, mk, mv, a, blocks, s) : launch<false, 64>(mq, mk, mv, a, blocks, s);
+  // Two tiles to a block read keys and values once for both; one tile, two blocks to an SM, wastes less where prompts are short
+  // (blocks end at odd times, a second tile may be empty) and gives every SM work where there is little.  us, two tiles and one:
+  // 64 prompts of 64 tokens, 32 heads of 128: 59 and 44; 16 of 200: 36 and 37; 12 of 300: 50 and 44; 8 of 512: 46 and 48; 4 of 1024:
+  // 60 and 62; one of 512: 16.3 and 14.0; 64 heads over 8, 8 of 512: 69 and 73; 64 heads of 64, 8 of 512: 58 and 55, 4 of 1024: 81
+  // and 77, one of 2048: 64 and 65.
+  const bool little = (int64_t)n_tokens * d->n_kv_heads < (int64_t)2 * a.tile_tokens * sms;
+  const int tiles = little || n_tokens <= (int64_t)n * (d->head_dim == 64 ? 1536 : 320) ? 1 : 2;
+  const cudaError_t e = d->dtype == NP_T_BF16 ? launch<true>(mq, mk, mv, a, d->head_dim, tiles, sms, s) : launch<false>(mq, mk, mv, a, d->head_dim, tiles, sms, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);
 }

@@ -16,9 +16,12 @@
 //   when O is, so a warp always has 4 KB in flight (head_dim 128).
 // * The running maximum and sum are per warp (base 2, fp32); the accumulators are rescaled only when a maximum grows.  P is
 //   the sum of two terms of the cache's type, so it is good to 16 bits and more where one term has 8 or 11.
-// * All (sequence, group, tile of 64 tokens) triples form one line; each block takes an equal stretch of it.  A block that
-//   has a group's tokens to itself stores the result; otherwise blocks leave (m, l, O) in the workspace and the last to arrive
-//   joins them in the order of the tokens, so that results do not depend on who was last.
+// * All (sequence, group, tile of 64 tokens) triples form one line; each block takes an equal stretch of it.  A group's start counts
+//   as two tiles: that is about what it costs (queries, page numbers, the join of the warps), and a block with many short
+//   sequences would be the last otherwise.  A block that has a group's tokens to itself stores the result; otherwise blocks leave
+//   (m, l, O) in the workspace and the last to arrive joins them in the order of the tokens, so that results do not depend on
+//   who was last.
+// * The first keys and values of a block's next piece are asked for before the warps' results of the last are joined.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -36,6 +39,8 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kTile = kWarps * 16;    // tokens of a tile
 constexpr int kMinTiles = 4;          // tiles a block takes at least, where there are so few that blocks stay idle
+constexpr int kStart = 2;             // what a group's start counts, in tiles
+constexpr int kJoin = 8;              // partial results that are joined at a time
 constexpr int kMaxBlocks = 640;       // blocks of a launch (the workspace holds two partial results of each)
 
 struct DecodeArgs {
@@ -48,7 +53,8 @@ struct DecodeArgs {
   uint16_t* out;
   int64_t q_token, q_head, o_token, o_head;  // elements
   float* lse;
-  unsigned int* count;       // [n * pairs] pieces that have arrived; zero between calls
+  unsigned int* count;       // [2 * kMaxBlocks] partial results that have arrived, at the place of their first; zero between calls
+  unsigned int* pair_count;  // [n * pairs] the same of joined ones
   float* part_ml;            // [2 * kMaxBlocks][HB][2]
   float* part_o;             // [2 * kMaxBlocks][HB][HD]
   float scale2;              // scale * log2(e)
@@ -104,6 +110,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// a / b, by 32 bits where they do
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // Tokens of row i of the call; 0 where there are none to read.
 __device__ __forceinline__ int row_len(const DecodeArgs& a, int i, int* seq_out) {
   const int seq = a.seqs ? a.seqs[i] : i;
@@ -127,8 +138,11 @@ k_attn_decode(DecodeArgs a) {
   constexpr int HB = 8 * NT;         // heads of a block, at most
   constexpr int KV = HD / 32;        // 16-byte pieces of a key row per lane
   constexpr int VC = HD / 64;        // 16-byte pieces of a value row per lane
+  constexpr int QV = HB * HD / 8 / kThreads > 0 ? HB * HD / 8 / kThreads : 1;  // 16-byte pieces of the queries per thread
+  constexpr int QR = HD * 2 + 16;    // bytes from query to query in shared memory: eight of them in as many banks
   __shared__ int64_t s_end[NP_KV_MAX_SEQS];             // tiles of the rows up to and including this one
   __shared__ __align__(16) float s_o[kWarps][HB][HD];
+  __shared__ __align__(16) unsigned char s_q[HB * QR];
   __shared__ float s_ml[kWarps][HB][2];
   __shared__ int64_t s_wsum[kWarps];
   __shared__ int s_last;
@@ -137,25 +151,39 @@ k_attn_decode(DecodeArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
   const int pairs = a.n_kv_heads * a.blocks_of_heads;   // (key-value head, block of its query heads)
 
-  // ---- tiles of every row, summed up; rows without tokens are answered here
+  // ---- units (tiles, and a group's start) of every row, summed up; rows without tokens are answered here
   int64_t run = 0;
-  for (int base = 0; base < a.n; base += kThreads) {
-    const int i = base + tid;
+  if (a.n <= 32) {  // every warp by itself: all write the same
     int len = 0, seq = -1;
-    if (i < a.n) len = row_len(a, i, &seq);
-    int64_t inc = ((int64_t)len + kTile - 1) / kTile;
+    if (lane < a.n) len = row_len(a, lane, &seq);
+    int64_t inc = len > 0 ? ((int64_t)len + kTile - 1) / kTile + kStart : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += up;
     }
-    if (lane == 31) s_wsum[wid] = inc;
-    __syncthreads();
-    for (int w = 0; w < wid; ++w) inc += s_wsum[w];
-    if (i < a.n) s_end[i] = run + inc;
+    if (lane < a.n) s_end[lane] = inc;
+    run = __shfl_sync(0xffffffffu, inc, 31);
+    __syncwarp();
+  } else {
+    for (int base = 0; base < a.n; base += kThreads) {
+      const int i = base + tid;
+      int len = 0, seq = -1;
+      if (i < a.n) len = row_len(a, i, &seq);
+      int64_t inc = len > 0 ? ((int64_t)len + kTile - 1) / kTile + kStart : 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) run += s_wsum[w];
-    __syncthreads();
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+      }
+      if (lane == 31) s_wsum[wid] = inc;
+      __syncthreads();
+      for (int w = 0; w < wid; ++w) inc += s_wsum[w];
+      if (i < a.n) s_end[i] = run + inc;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) run += s_wsum[w];
+      __syncthreads();
+    }
   }
   for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
     if (s_end[i] != (i ? s_end[i - 1] : 0)) continue;
@@ -165,14 +193,17 @@ k_attn_decode(DecodeArgs a) {
       if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = -INFINITY;
     }
   }
+  // the line's W units over G blocks: the first `more` blocks take each + 1 of them, the others each
   const int64_t W = run * pairs;
-  const int64_t G = min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
-  if (blockIdx.x >= G) return;
-  int64_t w0 = W * blockIdx.x / G;
-  const int64_t w1 = W * (blockIdx.x + 1) / G;
+  const int G = (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
+  if ((int)blockIdx.x >= G) return;
+  const int64_t each = divide(W, G), more = W - each * G;
+  auto block_of = [&](int64_t w) { return (int)(w < more * (each + 1) ? divide(w, each + 1) : more + divide(w - more * (each + 1), each)); };
+  int64_t w0 = blockIdx.x * each + min((int64_t)blockIdx.x, more);
+  const int64_t w1 = w0 + each + (blockIdx.x < more ? 1 : 0);
   int row = 0;
   {
-    int lo = 0, hi = a.n - 1;  // the first row whose tiles end after w0
+    int lo = 0, hi = a.n - 1;  // the first row whose units end after w0
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (s_end[mid] * pairs > w0) hi = mid;
@@ -181,31 +212,126 @@ k_attn_decode(DecodeArgs a) {
     row = lo;
   }
 
-  while (w0 < w1) {
-    // ---- the next piece: tiles [ta, tb) of one (row, pair)
-    while (s_end[row] * pairs <= w0) ++row;
-    const int64_t before = row ? s_end[row - 1] : 0;
-    const int64_t tiles = s_end[row] - before, r0 = w0 - before * pairs;
-    const int pair = (int)(r0 / tiles);
-    const int64_t ta = r0 - pair * tiles, tb = min(tiles, ta + (w1 - w0)), first_w = w0 - ta;
-    w0 += tb - ta;
-    int seq;
-    const int len = row_len(a, row, &seq);
-    const int kvh = pair / a.blocks_of_heads, hb = pair - kvh * a.blocks_of_heads;
-    const int h0 = kvh * a.group + hb * HB, heads = min(HB, a.group - hb * HB);
-    const int32_t* pages = a.table + (size_t)seq * a.max_pages;
-    const int64_t head_bytes = (int64_t)(HD * 2) << a.shift, page_bytes = 2 * a.n_kv_heads * head_bytes;
-    const char* kbase = a.cache + kvh * head_bytes;
-    const char* vbase = kbase + a.n_kv_heads * head_bytes;
+  const int64_t head_bytes = (int64_t)(HD * 2) << a.shift, page_bytes = 2 * a.n_kv_heads * head_bytes;
+  struct Piece {  // tiles [ta, tb) of one (row, pair)
+    int row, pair, h0, heads, len, tiles, ta, tb;
+    int64_t first_w;  // of its pair, on the line
+    const int32_t* pages;
+    const char* kbase;
+    const char* vbase;
+  };
+  // the next piece with tokens from w0 on; false: none is left
+  auto next_piece = [&](Piece& p) {
+    while (w0 < w1) {
+      while (s_end[row] * pairs <= w0) ++row;
+      const int64_t before = row ? s_end[row - 1] : 0, units = s_end[row] - before, r0 = w0 - before * pairs;
+      const int pair = (int)divide(r0, units);
+      const int64_t ra = r0 - pair * units, rb = min(units, ra + (w1 - w0));
+      p.first_w = w0 - ra;
+      w0 += rb - ra;
+      p.ta = (int)max((int64_t)0, ra - kStart);
+      p.tb = (int)max((int64_t)0, rb - kStart);
+      if (p.ta == p.tb) continue;  // the start alone: whoever has the first tile begins
+      p.row = row;
+      p.pair = pair;
+      p.tiles = (int)(units - kStart);
+      int seq;
+      p.len = row_len(a, row, &seq);
+      const int kvh = pair / a.blocks_of_heads, hb = pair - kvh * a.blocks_of_heads;
+      p.h0 = kvh * a.group + hb * HB;
+      p.heads = min(HB, a.group - hb * HB);
+      p.pages = a.table + (size_t)seq * a.max_pages;
+      p.kbase = a.cache + kvh * head_bytes;
+      p.vbase = p.kbase + a.n_kv_heads * head_bytes;
+      return true;
+    }
+    return false;
+  };
 
-    uint4 qf[NT][KV];
+  uint4 qf[QV], kf[2][KV], vf[4][VC];
+  Piece p = {};
+  int chunk_end, c, have, have_next, pg_next;  // chunks of 16 tokens
+  int64_t at, at_next;
+  // where the chunk's page starts, and how many of its tokens there are (0: nothing to read)
+  auto chunk_of = [&](int chunk, int pg, int& n, int64_t& off) {
+    n = 0;
+    off = 0;
+    if (chunk >= chunk_end) return;
+    if ((unsigned)pg >= (unsigned)a.n_pages) {
+      atomicOr(a.status, NP_KV_S_PAGE);
+      return;
+    }
+    n = (int)min((int64_t)16, p.len - (int64_t)chunk * 16);
+    off = pg * page_bytes + (int64_t)((chunk * 16) & ((1 << a.shift) - 1)) * (HD * 2);
+  };
+  auto page_of = [&](int chunk) { return chunk < chunk_end ? p.pages[(int)(((int64_t)chunk * 16) >> a.shift)] : 0; };
+  auto load_k = [&](int n, int64_t off) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int j = 0; j < KV; ++j) {
-        qf[nt][j] = make_uint4(0, 0, 0, 0);
-        if (nt * 8 + g < heads) qf[nt][j] = *reinterpret_cast<const uint4*>(a.q + row * a.q_token + (int64_t)(h0 + nt * 8 + g) * a.q_head + (t + 4 * j) * 8);
+        kf[r][j] = make_uint4(0, 0, 0, 0);
+        if (g + 8 * r < n) kf[r][j] = npd::ldg_stream(p.kbase + off + (g + 8 * r) * (HD * 2) + (t + 4 * j) * 16);
       }
+  };
+  auto load_v = [&](int n, int64_t off) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
+#pragma unroll
+      for (int x = 0; x < VC; ++x) {
+        vf[r][x] = make_uint4(0, 0, 0, 0);
+        if (tok < n) vf[r][x] = npd::ldg_stream(p.vbase + off + tok * (HD * 2) + (g + 8 * x) * 16);
+      }
+    }
+  };
+  // asks for the queries and the first keys and values of a piece
+  auto begin = [&] {
+    chunk_end = (int)min(((int64_t)p.len + 15) >> 4, (int64_t)p.tb * kWarps);
+    c = p.ta * kWarps + wid;
+    const int pg = page_of(c);
+    pg_next = page_of(c + kWarps);
+#pragma unroll
+    for (int j = 0; j < QV; ++j) {
+      const int x = j * kThreads + tid, h = x / (HD / 8), d = x % (HD / 8) * 8;
+      qf[j] = make_uint4(0, 0, 0, 0);
+      if (h < p.heads) qf[j] = *reinterpret_cast<const uint4*>(a.q + p.row * a.q_token + (int64_t)(p.h0 + h) * a.q_head + d);
+    }
+    chunk_of(c, pg, have, at);
+    load_k(have, at);
+    load_v(have, at);
+  };
+  auto add = [](float4& acc, float f, const float4& v) {
+    acc.x += f * v.x;
+    acc.y += f * v.y;
+    acc.z += f * v.z;
+    acc.w += f * v.w;
+  };
+  // four values of a head's result; its log of the sum with the first
+  auto result = [&](int i, int h, int d, const float4& acc, float use, float sum) {
+    const bool none = sum == 0.f;
+    const float inv = none ? 0.f : 1.f / sum;
+    uint2 r;
+    r.x = (uint32_t)Half2<T>::round(none ? 0.f : acc.x * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.y * inv) << 16;
+    r.y = (uint32_t)Half2<T>::round(none ? 0.f : acc.z * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.w * inv) << 16;
+    *reinterpret_cast<uint2*>(a.out + i * a.o_token + (int64_t)h * a.o_head + d) = r;
+    if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = none ? -INFINITY : use * kLn2 + logf(sum);
+  };
+  // the queries that begin() asked for go where all warps read them; a barrier follows
+  auto keep_queries = [&] {
+#pragma unroll
+    for (int j = 0; j < QV; ++j) {
+      const int x = j * kThreads + tid, h = x / (HD / 8), d = x % (HD / 8);
+      if (h < HB) *reinterpret_cast<uint4*>(s_q + h * QR + d * 16) = qf[j];
+    }
+  };
+  bool any = next_piece(p);
+  if (any) {
+    begin();
+    keep_queries();
+  }
+  __syncthreads();
+  while (any) {
     float m[NT][2], l[NT][2], o[NT][VC * 4][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -214,49 +340,6 @@ k_attn_decode(DecodeArgs a) {
 #pragma unroll
       for (int i = 0; i < VC * 4; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
     }
-
-    uint4 kf[2][KV], vf[4][VC];
-    const int chunk_end = (int)min(((int64_t)len + 15) >> 4, tb * kWarps);  // chunks of 16 tokens
-    // where the chunk's page starts, and how many of its tokens there are (0: nothing to read)
-    auto chunk_of = [&](int c, int pg, int& have, int64_t& at) {
-      have = 0;
-      at = 0;
-      if (c >= chunk_end) return;
-      if ((unsigned)pg >= (unsigned)a.n_pages) {
-        atomicOr(a.status, NP_KV_S_PAGE);
-        return;
-      }
-      have = (int)min((int64_t)16, len - (int64_t)c * 16);
-      at = pg * page_bytes + (int64_t)((c * 16) & ((1 << a.shift) - 1)) * (HD * 2);
-    };
-    auto page_of = [&](int c) { return c < chunk_end ? pages[(int)(((int64_t)c * 16) >> a.shift)] : 0; };
-    auto load_k = [&](int have, int64_t at) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int j = 0; j < KV; ++j) {
-          kf[r][j] = make_uint4(0, 0, 0, 0);
-          if (g + 8 * r < have) kf[r][j] = npd::ldg_stream(kbase + at + (g + 8 * r) * (HD * 2) + (t + 4 * j) * 16);
-        }
-    };
-    auto load_v = [&](int have, int64_t at) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
-#pragma unroll
-        for (int c = 0; c < VC; ++c) {
-          vf[r][c] = make_uint4(0, 0, 0, 0);
-          if (tok < have) vf[r][c] = npd::ldg_stream(vbase + at + tok * (HD * 2) + (g + 8 * c) * 16);
-        }
-      }
-    };
-    int c = (int)ta * kWarps + wid;
-    int have, have_next;
-    int64_t at, at_next;
-    chunk_of(c, page_of(c), have, at);
-    load_k(have, at);
-    load_v(have, at);
-    int pg_next = page_of(c + kWarps);
     for (; c < chunk_end; c += kWarps) {
       chunk_of(c + kWarps, pg_next, have_next, at_next);
       pg_next = page_of(c + 2 * kWarps);
@@ -267,8 +350,9 @@ k_attn_decode(DecodeArgs a) {
         s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
         for (int j = 0; j < KV; ++j) {
-          Half2<T>::mma(s[nt], kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, qf[nt][j].x, qf[nt][j].y);
-          Half2<T>::mma(s[nt], kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, qf[nt][j].z, qf[nt][j].w);
+          const uint4 q = *reinterpret_cast<const uint4*>(s_q + (nt * 8 + g) * QR + (t + 4 * j) * 16);
+          Half2<T>::mma(s[nt], kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, q.x, q.y);
+          Half2<T>::mma(s[nt], kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, q.z, q.w);
         }
       }
       load_k(have_next, at_next);
@@ -334,7 +418,10 @@ k_attn_decode(DecodeArgs a) {
       at = at_next;
     }
 
-    // ---- the warps' results meet in shared memory
+    // ---- on to the next piece; this one's results meet in shared memory meanwhile
+    const Piece e = p;
+    any = next_piece(p);
+    if (any) begin();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -342,7 +429,7 @@ k_attn_decode(DecodeArgs a) {
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], x);
         const int h = nt * 8 + 2 * t + i;
-        if (h < heads) {
+        if (h < e.heads) {
           if (g == 0) {
             s_ml[wid][h][0] = m[nt][i];
             s_ml[wid][h][1] = l[nt][i];
@@ -353,73 +440,96 @@ k_attn_decode(DecodeArgs a) {
         }
       }
     __syncthreads();
-    const bool whole = ta == 0 && tb == tiles;
-    const int slot = 2 * blockIdx.x + (ta == 0 ? 1 : 0);
-    for (int e = tid; e < heads * HD; e += kThreads) {
-      const int h = e / HD, d = e % HD;
+    if (any) keep_queries();
+    const bool whole = e.ta == 0 && e.tb == e.tiles;
+    const int slot = 2 * blockIdx.x + (e.ta == 0 ? 1 : 0);
+    for (int x = tid; x < e.heads * (HD / 4); x += kThreads) {
+      const int h = x / (HD / 4), d = x % (HD / 4) * 4;
       float top = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_ml[w][h][0]);
       const float use = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, acc = 0.f;
+      float sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float f = exp2_fast(s_ml[w][h][0] - use);
+        const float4 v = *reinterpret_cast<const float4*>(&s_o[w][h][d]);
         sum += f * s_ml[w][h][1];
-        acc += f * s_o[w][h][d];
+        add(acc, f, v);
       }
       if (whole) {
-        a.out[row * a.o_token + (int64_t)(h0 + h) * a.o_head + d] = Half2<T>::round(sum == 0.f ? 0.f : acc / sum);
-        if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + h0 + h] = sum == 0.f ? -INFINITY : use * kLn2 + logf(sum);
+        result(e.row, e.h0 + h, d, acc, use, sum);
       } else {
-        __stcg(&a.part_o[((size_t)slot * HB + h) * HD + d], acc);
-        if (d == 0) {
-          __stcg(&a.part_ml[(slot * HB + h) * 2], top);
-          __stcg(&a.part_ml[(slot * HB + h) * 2 + 1], sum);
-        }
+        __stcg(reinterpret_cast<float4*>(&a.part_o[((size_t)slot * HB + h) * HD + d]), acc);
+        if (d == 0) __stcg(reinterpret_cast<float2*>(&a.part_ml[(slot * HB + h) * 2]), make_float2(top, sum));
       }
     }
     if (!whole) {
-      // ---- the last block of this (row, pair) joins the pieces
-      const int c0 = (int)(((first_w + 1) * G - 1) / W), c1 = (int)(((first_w + tiles) * G - 1) / W);
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        unsigned int* count = a.count + (size_t)row * pairs + pair;
-        const unsigned int arrived = atomicAdd(count, 1u) + 1u;
-        s_last = arrived == (unsigned)(c1 - c0 + 1);
-        if (s_last) *count = 0u;
-      }
-      __syncthreads();
-      if (s_last) {
+      // ---- the last block to arrive joins up to kJoin neighbouring pieces; the last of those that did joins what they got
+      const int c0 = block_of(e.first_w + kStart), c1 = block_of(e.first_w + kStart + e.tiles - 1), pieces = c1 - c0 + 1;
+      auto slot_of = [&](int b) { return (2 * b + (b == c0)) * HB; };
+      // true in the block that is the last of n to arrive at a count, which is zero again then
+      auto last_of = [&](unsigned int* count, int n) {
         __threadfence();
-        for (int e = tid; e < heads * (HD / 4); e += kThreads) {
-          const int h = e / (HD / 4), d = e % (HD / 4) * 4;
-          float top = -INFINITY;
-          for (int b = c0; b <= c1; ++b) top = fmaxf(top, __ldcg(&a.part_ml[((2 * b + (b == c0)) * HB + h) * 2]));
-          const float use = top == -INFINITY ? 0.f : top;
-          float sum = 0.f;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int b = c0; b <= c1; ++b) {
-            const int sl = (2 * b + (b == c0)) * HB + h;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(&a.part_ml[sl * 2]));
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(&a.part_o[(size_t)sl * HD + d]));
-            const float f = exp2_fast(ml.x - use);
-            sum += f * ml.y;
-            acc.x += f * x.x;
-            acc.y += f * x.y;
-            acc.z += f * x.z;
-            acc.w += f * x.w;
-          }
-          const bool none = sum == 0.f;
-          const float inv = none ? 0.f : 1.f / sum;
-          uint2 r;
-          r.x = (uint32_t)Half2<T>::round(none ? 0.f : acc.x * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.y * inv) << 16;
-          r.y = (uint32_t)Half2<T>::round(none ? 0.f : acc.z * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.w * inv) << 16;
-          *reinterpret_cast<uint2*>(a.out + row * a.o_token + (int64_t)(h0 + h) * a.o_head + d) = r;
-          if (a.lse && d == 0) a.lse[(size_t)row * a.n_heads + h0 + h] = none ? -INFINITY : use * kLn2 + logf(sum);
+        __syncthreads();
+        if (tid == 0) {
+          s_last = atomicAdd(count, 1u) + 1u == (unsigned)n;
+          if (s_last) *count = 0u;
         }
+        __syncthreads();
+        if (s_last) __threadfence();
+        return s_last != 0;
+      };
+      // the partial results of n blocks, `step` apart, from b on: to the result, or to b's place
+      auto join = [&](int b, int n, int step, bool final) {
+        for (int x0 = wid * 32; x0 < e.heads * (HD / 4); x0 += kThreads) {  // whole warps
+          const int x = x0 + lane, h = x / (HD / 4), d = x % (HD / 4) * 4;
+          const bool there = h < e.heads;
+          float top = -INFINITY, sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int y0 = 0; y0 < n; y0 += kJoin) {
+            float2 ml[kJoin];
+            float4 v[kJoin];
+#pragma unroll
+            for (int y = 0; y < kJoin; ++y) {
+              ml[y] = make_float2(-INFINITY, 0.f);
+              v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (there && y0 + y < n) {
+                const int sl = slot_of(b + (y0 + y) * step) + h;
+                ml[y] = __ldcg(reinterpret_cast<const float2*>(&a.part_ml[sl * 2]));
+                v[y] = __ldcg(reinterpret_cast<const float4*>(&a.part_o[(size_t)sl * HD + d]));
+              }
+            }
+            float now = top;
+#pragma unroll
+            for (int y = 0; y < kJoin; ++y) now = fmaxf(now, ml[y].x);
+            const float use = now == -INFINITY ? 0.f : now, f0 = exp2_fast(top - use);
+            top = now;
+            sum *= f0;
+            acc = make_float4(acc.x * f0, acc.y * f0, acc.z * f0, acc.w * f0);
+#pragma unroll
+            for (int y = 0; y < kJoin; ++y) {
+              const float f = exp2_fast(ml[y].x - use);
+              sum += f * ml[y].y;
+              add(acc, f, v[y]);
+            }
+          }
+          __syncwarp();  // b's place is read by the HD / 4 lanes of a head, all of this warp: they are done
+          if (!there) continue;
+          if (final) {
+            result(e.row, e.h0 + h, d, acc, top == -INFINITY ? 0.f : top, sum);
+          } else {
+            const int sl = slot_of(b) + h;
+            __stcg(reinterpret_cast<float4*>(&a.part_o[(size_t)sl * HD + d]), acc);
+            if (d == 0) __stcg(reinterpret_cast<float2*>(&a.part_ml[sl * 2]), make_float2(top, sum));
+          }
+        }
+      };
+      const int mine = ((int)blockIdx.x - c0) / kJoin, groups = (pieces + kJoin - 1) / kJoin, b0 = c0 + mine * kJoin;
+      if (last_of(&a.count[2 * b0 + (b0 == c0)], min(kJoin, pieces - mine * kJoin))) {
+        join(b0, min(kJoin, pieces - mine * kJoin), 1, groups == 1);
+        if (groups > 1 && last_of(&a.pair_count[(size_t)e.row * pairs + e.pair], groups)) join(c0, groups, kJoin, true);
       }
     }
     __syncthreads();  // s_o, s_ml and s_last are free for the next piece
@@ -438,9 +548,10 @@ cudaError_t launch(const DecodeArgs& a, int hd, int hb, int sms, cudaStream_t s)
 // [(m, l) of the partial results][their O][counts]: the counts start at the same place for every description and n, and the
 // rest needs no particular contents, so one workspace serves calls of different sizes in turn.
 constexpr uint64_t kSpaceO = (uint64_t)2 * kMaxBlocks * 16 * 8, kSpaceCounts = kSpaceO + (uint64_t)2 * kMaxBlocks * 16 * 128 * 4;
+constexpr uint64_t kSpacePairs = kSpaceCounts + (uint64_t)2 * kMaxBlocks * 4;
 uint64_t space_bytes(int n_kv_heads, int group, int n) {
   const int hb = heads_per_block(group);
-  return kSpaceCounts + (uint64_t)n * n_kv_heads * ((group + hb - 1) / hb) * 4;
+  return kSpacePairs + (uint64_t)n * n_kv_heads * ((group + hb - 1) / hb) * 4;
 }
 
 const char* heads_error(const np_kv_desc* d, int n_heads, int n) {
@@ -509,6 +620,7 @@ int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const 
   a.part_ml = reinterpret_cast<float*>(ws);
   a.part_o = reinterpret_cast<float*>(ws + kSpaceO);
   a.count = reinterpret_cast<unsigned int*>(ws + kSpaceCounts);
+  a.pair_count = reinterpret_cast<unsigned int*>(ws + kSpacePairs);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = d->dtype == NP_T_BF16 ? launch<__nv_bfloat16>(a, d->head_dim, hb, sms, s) : launch<__half>(a, d->head_dim, hb, sms, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);

@@ -110,6 +110,13 @@ __device__ __forceinline__ void tm_ld32(uint32_t taddr, uint32_t (&r)[N], int o)
       : NP_R32(r, o)
       : "r"(taddr));
 }
+__device__ __forceinline__ void tm_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
 __device__ __forceinline__ void tm_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
@@ -135,7 +142,17 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
                "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The loads have arrived.  Their registers pass through: what uses them comes behind the wait.
+template <int N>
+__device__ __forceinline__ void wait_ld(uint32_t (&r)[N]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int o = 0; o < N; o += 16)
+    asm volatile(""
+                 : "+r"(r[o + 0]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7]),
+                   "+r"(r[o + 8]), "+r"(r[o + 9]), "+r"(r[o + 10]), "+r"(r[o + 11]), "+r"(r[o + 12]), "+r"(r[o + 13]), "+r"(r[o + 14]),
+                   "+r"(r[o + 15]));
+}
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -567,6 +584,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       const int steps = w.n_kv[i];
       if (steps == 0) continue;
       const int first = w.q0 + i * a.tile_tokens, tok = first + in_tile;
+      const bool valid = in_tile < a.tile_tokens && tok < w.len;  // the other rows hold anything, and have no say
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < steps; ++j) {
         ok = wait_all(&s_full[i], s_cnt++ & 1u);
@@ -575,7 +593,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         uint32_t s[kRows];
 #pragma unroll
         for (int c = 0; c < kRows; c += 32) tm_ld32(ts + c, s, c);
-        wait_ld();
+        wait_ld(s);
         if ((j + 1) * kRows - 1 > first) {  // the tile reaches past the first row
           const int see = tok - j * kRows, all_see = __shfl_sync(0xffffffffu, see, 0);
 #pragma unroll
@@ -593,7 +611,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         if (j > 0) {
           part = softmax_half<kBf16, 0>(s, a.scale2, m, ts);
           now = row_max(s) * a.scale2;
-          fast = __all_sync(0xffffffffu, now <= m + kGrow && m > -INFINITY && now < INFINITY);
+          fast = __all_sync(0xffffffffu, !valid || (now <= m + kGrow && m > -INFINITY && now < INFINITY));
         } else {
           now = row_max(s) * a.scale2;
         }
@@ -603,21 +621,18 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           now = max3(m, now, now == INFINITY ? __uint_as_float(0x7fffffffu) : -INFINITY);
           if (j == 0) {
             m = now;
-          } else if (__any_sync(0xffffffffu, !(now <= m + kGrow))) {
+          } else if (__any_sync(0xffffffffu, valid && !(now <= m + kGrow))) {
             const float f = exp2_fast(m - (now == -INFINITY ? 0.f : now));
             m = now;
             l *= f;
+#pragma unroll 1
+            for (int c = 0; c < HD; c += 16) {
+              uint32_t o[16];
+              tm_ld16(to + c, o);
+              wait_ld(o);
 #pragma unroll
-            for (int c = 0; c < HD; c += 32) {
-              uint32_t o[32], x16[16];
-              tm_ld32(to + c, o, 0);
-              wait_ld();
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int x = 0; x < 16; ++x) x16[x] = __float_as_uint(__uint_as_float(o[h * 16 + x]) * f);
-                tm_st16(to + c + h * 16, x16);
-              }
+              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+              tm_st16(to + c, o);
             }
           }
           use = m == -INFINITY ? 0.f : m;
@@ -632,15 +647,14 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       // ---- the result
       fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const bool valid = in_tile < a.tile_tokens && tok < w.len;
       const int head = w.kvh * a.group + in_group;
       uint16_t* out = a.out + (int64_t)(w.start + tok) * a.o_token + (int64_t)head * a.o_head;
       uint32_t big = __float_as_uint(l) & 0x7fffffffu;
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < HD; c += 32) {
         uint32_t o[32];
         tm_ld32(to + c, o, 0);
-        wait_ld();
+        wait_ld(o);
         if (c + 32 == HD) {  // the accumulators may be written again
           fence_before();
           __syncwarp();

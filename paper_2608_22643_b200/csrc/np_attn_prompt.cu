@@ -799,12 +799,12 @@ extern "C" int np_attn_prompt(const np_attn_shape* d, const np_rows* q, const np
     return fail(NP_E_INVAL, "rows that a tensor map does not describe (strides of 2^40 bytes and more)");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // Two tiles to a block read keys and values once for both; one tile, two blocks to an SM, wastes less where prompts are short
-  // (blocks end at odd times, a second tile may be empty) and gives every SM work where there is little.  us, two tiles and one:
-  // 64 prompts of 64 tokens, 32 heads of 128: 59 and 44; 16 of 200: 36 and 37; 12 of 300: 50 and 44; 8 of 512: 46 and 48; 4 of 1024:
-  // 60 and 62; one of 512: 16.3 and 14.0; 64 heads over 8, 8 of 512: 69 and 73; 64 heads of 64, 8 of 512: 58 and 55, 4 of 1024: 81
-  // and 77, one of 2048: 64 and 65.
+  // (blocks end at odd times, a second tile may be empty) and gives every SM work where there is little.  us, one tile and two:
+  // 32 heads of 128, 64 prompts of 64 tokens 37 and 50, 16 of 128 19.4 and 20.2, 16 of 200 34 and 32, 4 of 1024 59 and 54, one of 512
+  // 13.5 and 15.7; 64 heads over 8, 16 of 200 41 and 44, 16 of 256 51 and 51, 4 of 768 68 and 62, one of 512 17.4 and 18.5; 64 heads
+  // of 64, 16 of 256 37 and 43, 4 of 1024 72 and 81, one of 2048 62 and 64, of 8192 826 and 731.
   const bool little = (int64_t)n_tokens * d->n_kv_heads < (int64_t)2 * a.tile_tokens * sms;
-  const int tiles = little || n_tokens <= (int64_t)n * (d->head_dim == 64 ? 1536 : 320) ? 1 : 2;
+  const int tiles = little || n_tokens <= (int64_t)n * (d->head_dim == 64 ? 2048 : group > 1 ? 224 : 128) ? 1 : 2;
   const cudaError_t e = d->dtype == NP_T_BF16 ? launch<true>(mq, mk, mv, a, d->head_dim, tiles, sms, s) : launch<false>(mq, mk, mv, a, d->head_dim, tiles, sms, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);
 }

@@ -62,6 +62,7 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kPerThread = 8;                             // reference counts per thread and round of a scan
 constexpr int kRound = kPlanThreads * kPerThread;
+constexpr int kFewPages = 2048;                           // page numbers that need no trip through memory
 
 // What the kernels need of a description, and where the pieces of the scratch are.
 struct Pool {
@@ -94,20 +95,28 @@ __device__ __forceinline__ int pages_of(const Pool& p, int len) {
   return n > p.max_pages ? -1 : n;
 }
 
-// Lists, in ascending order, the first `want` pages p of [0, n) for which take(refs[p], p); returns how many there are (at most
-// `want`).  The whole block calls it.  red: 34 ints.
+// The pages that a thread looks at in the round of a scan that begins at page `base`: bit j where take(refs[p], p), p its j-th.
 template <class Take>
-__device__ int list_pages(const int32_t* refs, int n, int want, int32_t* out, int* red, Take take) {
+__device__ __forceinline__ uint32_t pages_taken(const int32_t* refs, int n, int base, Take take) {
+  const int first = base + threadIdx.x * kPerThread;
+  uint32_t mine = 0;
+#pragma unroll
+  for (int j = 0; j < kPerThread; ++j) {
+    const int q = first + j;
+    if (q < n && take(refs[q], q)) mine |= 1u << j;
+  }
+  return mine;
+}
+
+// Lists, in ascending order, the first `want` pages p of [0, n) for which take(refs[p], p); returns how many there are (at most
+// `want`).  The whole block calls it.  round0: pages_taken for the first round.  red: 34 ints.
+template <class Take>
+__device__ int list_pages(const int32_t* refs, int n, int want, uint32_t round0, int32_t* out, int* red, Take take) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   int found = 0;
   for (int base = 0; base < n && found < want; base += kRound) {
     const int first = base + tid * kPerThread;
-    uint32_t mine = 0;
-#pragma unroll
-    for (int j = 0; j < kPerThread; ++j) {
-      const int q = first + j;
-      if (q < n && take(refs[q], q)) mine |= 1u << j;
-    }
+    uint32_t mine = base ? pages_taken(refs, n, base, take) : round0;
     const int cnt = __popc(mine);
     const int inc = npd::block_inclusive_scan_1024(cnt, red, lane, wid);
     int at = found + inc - cnt;
@@ -135,10 +144,13 @@ template <bool kFork>
 __global__ void __launch_bounds__(kPlanThreads, 1)
 k_kv_take(Pool p, const int32_t* __restrict__ a, const int32_t* __restrict__ b, int n, int32_t* __restrict__ start_out) {
   __shared__ int s_seq[NP_KV_MAX_SEQS], s_src[kFork ? NP_KV_MAX_SEQS : 1], s_end[NP_KV_MAX_SEQS], s_old[NP_KV_MAX_SEQS];
+  __shared__ int s_pages[kFewPages];
   __shared__ int red[34];
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  auto is_free = [](int r, int) { return r <= 0; };
+  const uint32_t round0 = pages_taken(p.refs, p.n_pages, 0, is_free);  // on its way beside the sequences' lengths
   // reserve: a = sequences (NULL: 0..n-1), b = new tokens.  fork: a = sources, b = targets.
   int seq = -1, src = -1, add = 0;
   if (tid < n) {
@@ -178,8 +190,8 @@ k_kv_take(Pool p, const int32_t* __restrict__ a, const int32_t* __restrict__ b, 
   const int end = npd::block_inclusive_scan_1024(need, red, lane, wid);
   const int total = red[32];
   __syncthreads();
-  int32_t* pages = p.pages();
-  const int have = total > 0 ? list_pages(p.refs, p.n_pages, min(total, p.n_pages), pages, red, [](int r, int) { return r <= 0; }) : 0;
+  int32_t* pages = total <= kFewPages ? s_pages : p.pages();
+  const int have = total > 0 ? list_pages(p.refs, p.n_pages, min(total, p.n_pages), round0, pages, red, is_free) : 0;
   if (ok && need > 0 && end > have) {
     bad = NP_KV_S_FULL;
     ok = false;
@@ -277,8 +289,10 @@ k_kv_compact_plan(Pool p, int32_t* refs_out, int32_t* __restrict__ n_live) {
   const int live = npd::block_sum_int(mine, red);
   int32_t* map = p.pages();
   __syncthreads();
-  const int moves = list_pages(p.refs, p.n_pages, p.n_pages, p.pair_src(), red, [live](int r, int q) { return r > 0 && q >= live; });
-  list_pages(p.refs, live, moves, p.pair_dst(), red, [](int r, int) { return r <= 0; });
+  auto moving = [live](int r, int q) { return r > 0 && q >= live; };
+  auto hole = [](int r, int) { return r <= 0; };
+  const int moves = list_pages(p.refs, p.n_pages, p.n_pages, pages_taken(p.refs, p.n_pages, 0, moving), p.pair_src(), red, moving);
+  list_pages(p.refs, live, moves, pages_taken(p.refs, live, 0, hole), p.pair_dst(), red, hole);
   for (int q = tid; q < p.n_pages; q += kPlanThreads) {
     map[q] = q;
     const int r = p.refs[q];

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -175,7 +176,7 @@ def load() -> C.CDLL:
     sigs["np_chain_launches"] = [vp, C.POINTER(C.c_int32)]
     sigs["np_install_speculative"] = [vp, vp]
     sigs["np_get_speculative"] = [vp, i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)]
-    kvd, kvt, rows = C.POINTER(np_kv_desc), C.POINTER(np_kv_tables), C.POINTER(np_rows)
+    kvd, kvt, rows = vp, vp, vp     # structures by address: of a ctypes one (byref) or of its bytes
     lib.np_attn_last_error.restype = C.c_char_p
     lib.np_attn_last_error.argtypes = []
     sigs.update({
@@ -189,7 +190,7 @@ def load() -> C.CDLL:
         "np_kv_copy_pages": [kvd, vp, vp, vp, vp, i32, vp, vp],
         "np_attn_workspace_bytes": [kvd, i32, i32, C.POINTER(C.c_uint64)],
         "np_attn_decode": [kvd, vp, i32, kvt, rows, i32, vp, i32, C.c_float, rows, vp, vp, C.c_uint64, vp],
-        "np_attn_prompt": [C.POINTER(np_attn_shape), rows, rows, rows, vp, i32, i32, C.c_float, rows, vp, vp, vp],
+        "np_attn_prompt": [vp, rows, rows, rows, vp, i32, i32, C.c_float, rows, vp, vp, vp],
         "np_attn_check": [vp, vp],
     })
     for name, args in sigs.items():
@@ -336,6 +337,7 @@ def np_trunk_forward(desc, table, features, centroid_id, workspace, head_logits,
 # Tensors belong to the current device.  Rows of heads (q, k, v, out) are tensors [tokens][heads][head_dim] with any strides
 # between tokens and heads and the last dimension contiguous; everything else is contiguous.
 _ATTN_DTYPE = {torch.bfloat16: NP_T_BF16, torch.float16: NP_T_FP16}
+_ATTN_TYPES = (torch.bfloat16, torch.float16)
 
 
 def _attn_check(rc: int) -> int:
@@ -356,8 +358,12 @@ def _device() -> int:
         return -2
 
 
-# Small calls are bound by what these checks take (a few microseconds a call): one query of the device per call, and messages
-# are made up only when something is wrong.
+# Small calls are bound by what these checks take (a few microseconds a call): one query of the device per call, structures as
+# packed bytes, and messages made up only when something is wrong.
+_pack_rows = struct.Struct("@Pqq").pack            # np_rows
+_pack_shape = struct.Struct("@8i").pack            # np_attn_shape
+
+
 def _dev(t, dtype, device: int, least: int = 0) -> Optional[int]:
     """Address of a contiguous tensor of the device (None stays None) that holds at least ``least`` elements."""
     if t is None:
@@ -368,21 +374,24 @@ def _dev(t, dtype, device: int, least: int = 0) -> Optional[int]:
     return t.data_ptr()
 
 
-def _rows_of(t, dtype: int, device: int, tokens: int, heads: int, head_dim: int) -> np_rows:
-    st, sh, sd = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if t.get_device() != device or sd != 1 or t.shape != (tokens, heads, head_dim) or _ATTN_DTYPE.get(t.dtype) != dtype:
-        _refuse(f"expected rows [{tokens}][{heads}][{head_dim}] of the call's type, the last dimension contiguous, on the current CUDA "
-                f"device, got {tuple(t.shape)} {t.dtype} with strides {t.stride()} on {t.device}")
+def _rows_of(t, dtype, device: int, tokens: int, heads: int, head_dim: int) -> bytes:
+    """An np_rows of a tensor of rows (``dtype`` a torch type)."""
+    if t.get_device() != device or t.dtype is not dtype or t.shape != (tokens, heads, head_dim) or t.stride(2) != 1:
+        _refuse(f"expected rows [{tokens}][{heads}][{head_dim}] of {dtype}, the last dimension contiguous, on the current CUDA device, "
+                f"got {tuple(t.shape)} {t.dtype} with strides {t.stride()} on {t.device}")
+    st, sh, _ = t.stride()
     # a stride nobody steps along may be anything in torch
-    return np_rows(t.data_ptr(), st if tokens > 1 else 0, sh if heads > 1 else 0)
+    return _pack_rows(t.data_ptr(), st if tokens > 1 else 0, sh if heads > 1 else 0)
 
 
 def _cache_of(desc: np_kv_desc, cache, device: int):
-    if (cache.get_device() != device or not cache.is_contiguous() or _ATTN_DTYPE.get(cache.dtype) != desc.dtype
-            or cache.shape != (desc.n_layers, desc.n_pages, 2, desc.n_kv_heads, desc.page_tokens, desc.head_dim)):
-        _refuse(f"expected a contiguous cache [{desc.n_layers}][{desc.n_pages}][2][{desc.n_kv_heads}][{desc.page_tokens}][{desc.head_dim}] of "
-                f"the description's type on the current CUDA device, got {tuple(cache.shape)} {cache.dtype} on {cache.device}")
-    return cache.data_ptr()
+    """(address, type, key-value heads, head size) of a cache of the description."""
+    dtype, heads, hd = _ATTN_TYPES[desc.dtype], desc.n_kv_heads, desc.head_dim
+    if (cache.get_device() != device or cache.dtype is not dtype or not cache.is_contiguous()
+            or cache.shape != (desc.n_layers, desc.n_pages, 2, heads, desc.page_tokens, hd)):
+        _refuse(f"expected a contiguous cache [{desc.n_layers}][{desc.n_pages}][2][{heads}][{desc.page_tokens}][{hd}] of {dtype} on the "
+                f"current CUDA device, got {tuple(cache.shape)} {cache.dtype} on {cache.device}")
+    return cache.data_ptr(), dtype, heads, hd
 
 
 def make_kv_desc(dtype, n_layers: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int, max_seqs: int,
@@ -420,17 +429,16 @@ def np_kv_reserve(desc, tables, seqs, n_new, start_out=None, stream=None) -> int
 def np_kv_append(desc, cache, layer: int, tables, k, v, seqs, cu, start, stream=None) -> int:
     """``cu`` None: one token for each sequence."""
     n, tokens, i32, dv = start.numel(), k.shape[0], torch.int32, _device()
-    dtype, heads, hd = desc.dtype, desc.n_kv_heads, desc.head_dim
+    at, dtype, heads, hd = _cache_of(desc, cache, dv)
     return _attn_check(load().np_kv_append(
-        C.byref(desc), _cache_of(desc, cache, dv), layer, C.byref(tables), C.byref(_rows_of(k, dtype, dv, tokens, heads, hd)),
-        C.byref(_rows_of(v, dtype, dv, tokens, heads, hd)), tokens, _dev(seqs, i32, dv, n), _dev(cu, i32, dv, n + 1), _dev(start, i32, dv), n,
-        _stream(stream)))
+        C.byref(desc), at, layer, C.byref(tables), _rows_of(k, dtype, dv, tokens, heads, hd), _rows_of(v, dtype, dv, tokens, heads, hd), tokens,
+        _dev(seqs, i32, dv, n), _dev(cu, i32, dv, n + 1), _dev(start, i32, dv), n, _stream(stream)))
 
 
 def np_kv_fork(desc, cache, tables, src, dst, stream=None) -> int:
     n, i32, dv = src.numel(), torch.int32, _device()
-    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache, dv), C.byref(tables), _dev(src, i32, dv), _dev(dst, i32, dv, n),
-                                         n, _stream(stream)))
+    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache, dv)[0], C.byref(tables), _dev(src, i32, dv),
+                                         _dev(dst, i32, dv, n), n, _stream(stream)))
 
 
 def np_kv_free(desc, tables, seqs=None, n: Optional[int] = None, stream=None) -> int:
@@ -441,13 +449,13 @@ def np_kv_free(desc, tables, seqs=None, n: Optional[int] = None, stream=None) ->
 
 def np_kv_compact(desc, cache, tables, out_tables, n_live=None, stream=None) -> int:
     dv = _device()
-    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache, dv), C.byref(tables), C.byref(out_tables),
+    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache, dv)[0], C.byref(tables), C.byref(out_tables),
                                             _dev(n_live, torch.int32, dv, 1), _stream(stream)))
 
 
 def np_kv_copy_pages(desc, dst_cache, src_cache, src, dst, status, stream=None) -> int:
     n, i32, dv = src.numel(), torch.int32, _device()
-    return _attn_check(load().np_kv_copy_pages(C.byref(desc), _cache_of(desc, dst_cache, dv), _cache_of(desc, src_cache, dv), _dev(src, i32, dv),
+    return _attn_check(load().np_kv_copy_pages(C.byref(desc), _cache_of(desc, dst_cache, dv)[0], _cache_of(desc, src_cache, dv)[0], _dev(src, i32, dv),
                                                _dev(dst, i32, dv, n), n, _dev(status, i32, dv, 1), _stream(stream)))
 
 
@@ -459,24 +467,24 @@ def np_attn_workspace_bytes(desc, n_heads: int, n: int) -> int:
 
 def np_attn_decode(desc, cache, layer: int, tables, q, out, workspace, seqs=None, scale: Optional[float] = None, lse=None, stream=None) -> int:
     """``scale`` None: 1 / sqrt(head_dim).  ``workspace``: a uint8 tensor, zeroed before its first use."""
-    n, heads = q.shape[:2]
-    dtype, hd, dv = desc.dtype, desc.head_dim, _device()
+    n, heads, _ = q.shape
+    dv = _device()
+    at, dtype, _, hd = _cache_of(desc, cache, dv)
     return _attn_check(load().np_attn_decode(
-        C.byref(desc), _cache_of(desc, cache, dv), layer, C.byref(tables), C.byref(_rows_of(q, dtype, dv, n, heads, hd)), heads,
-        _dev(seqs, torch.int32, dv, n), n, hd ** -0.5 if scale is None else scale, C.byref(_rows_of(out, dtype, dv, n, heads, hd)),
-        _dev(lse, torch.float32, dv, n * heads), _dev(workspace, torch.uint8, dv), workspace.numel(), _stream(stream)))
+        C.byref(desc), at, layer, C.byref(tables), _rows_of(q, dtype, dv, n, heads, hd), heads, _dev(seqs, torch.int32, dv, n), n,
+        hd ** -0.5 if scale is None else scale, _rows_of(out, dtype, dv, n, heads, hd), _dev(lse, torch.float32, dv, n * heads),
+        _dev(workspace, torch.uint8, dv), workspace.numel(), _stream(stream)))
 
 
 def np_attn_prompt(q, k, v, cu, out, status, scale: Optional[float] = None, lse=None, stream=None) -> int:
     """``q``, ``out`` [tokens][heads][head_dim], ``k``, ``v`` [tokens][kv heads][head_dim]; ``cu`` int32, one more than prompts."""
     tokens, heads, hd = q.shape
-    dtype, kv_heads, dv = _ATTN_DTYPE.get(q.dtype, -1), k.shape[1], _device()
+    dtype, kv_heads, dv = q.dtype, k.shape[1], _device()
     return _attn_check(load().np_attn_prompt(
-        C.byref(np_attn_shape(dtype, heads, kv_heads, hd)), C.byref(_rows_of(q, dtype, dv, tokens, heads, hd)),
-        C.byref(_rows_of(k, dtype, dv, tokens, kv_heads, hd)), C.byref(_rows_of(v, dtype, dv, tokens, kv_heads, hd)),
-        _dev(cu, torch.int32, dv, 2), cu.numel() - 1, tokens, hd ** -0.5 if scale is None else scale,
-        C.byref(_rows_of(out, dtype, dv, tokens, heads, hd)), _dev(lse, torch.float32, dv, tokens * heads), _dev(status, torch.int32, dv, 1),
-        _stream(stream)))
+        _pack_shape(_ATTN_DTYPE.get(dtype, -1), heads, kv_heads, hd, 0, 0, 0, 0), _rows_of(q, dtype, dv, tokens, heads, hd),
+        _rows_of(k, dtype, dv, tokens, kv_heads, hd), _rows_of(v, dtype, dv, tokens, kv_heads, hd), _dev(cu, torch.int32, dv, 2), cu.numel() - 1,
+        tokens, hd ** -0.5 if scale is None else scale, _rows_of(out, dtype, dv, tokens, heads, hd),
+        _dev(lse, torch.float32, dv, tokens * heads), _dev(status, torch.int32, dv, 1), _stream(stream)))
 
 
 def np_attn_check(status, stream=None) -> int:

@@ -4,8 +4,10 @@
 //
 // Two matrix products per block of rows and 128 keys, S = Q K^T and O += P V, run on the 5th-generation tensor cores with
 // S, P and O in tensor memory; the softmax between them runs on the plain cores.  Per 128 x 128 scores at head_dim 128 the
-// products take 1024 cycles of the tensor cores and the exponentials 1024 cycles of the special function units, so the two
-// have to overlap completely:
+// products take 1024 cycles of the tensor cores, their operands as many of shared memory's bandwidth, and the exponentials 1024
+// cycles of the special function units, so all three have to overlap completely.  They do to 60 % (3260 cycles for two such tiles,
+// both pipes busy 60 % of the time); what is left is hand-overs between the roles.  8192 tokens, 64 heads over 8: 865 us (1270
+// TFLOP/s) as long as the clock holds, 955 and 1150 in the long run, at the power limit.
 //
 // * A block holds two tiles of 128 query rows of the same key-value head (or an SM two blocks of one tile, for short prompts).
 //   While the plain cores do one tile's softmax, the tensor cores do the other's products.  Roles: four warps to a tile (softmax and
@@ -16,13 +18,19 @@
 //   sixteen tokens, keys and values are read once for all eight, and a short prompt fills its tiles.  Heads that do not
 //   divide 128 leave the last rows of a tile unused.
 // * Q, K and V come by tiled TMA (128-byte swizzle).  V is the product's B operand with head_dim contiguous, P its A operand in
-//   tensor memory, where the softmax overwrites the scores it came from.
+//   tensor memory, where the softmax overwrites the scores it came from; the product over the first 64 keys starts while the
+//   exponentials of the others are on their way.
 // * O is rescaled in tensor memory only when a row's maximum has grown by more than 2^8 since it was last taken; until then
 //   probabilities are up to 2^8 instead of 1, which fp32 sums and 16-bit factors hold.  P is rounded to the rows' type (the
 //   product takes nothing wider at this rate), the sum l is of the unrounded values.
 // * Only tiles that reach past a row are masked.  Rows of the tail tile that belong to the next prompt (or to nobody) are zeroed
 //   in V; within a prompt a later token's V meets P = 0 exactly, so only an infinity or a NaN there can reach an earlier row,
 //   and a row whose result is not finite is computed again from plain loads over the tokens that it sees.
+// * Short prompts wait for instructions: what is off the usual path (rescaling, the result) is kept in loops.  Unrolled, twelve
+//   prompts of 1 to 1500 tokens, 32 heads, took 90 us instead of 80.  Measured and dropped: exponentials on the FMA units by a
+//   polynomial (they are no less busy), two lanes to a row (the exchange costs what the halves save), scores read from tensor
+//   memory 32 at a time, a warp of products for each tile (the tiles fall into step), the next block's first scores before the
+//   other tile's last product.
 //
 // Every wait is bounded (np_pipe.cuh); after a time-out all roles leave, the block meets and tensor memory is released.
 #include <cuda.h>
@@ -595,13 +603,13 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         for (int c = 0; c < kRows; c += 32) tm_ld32(ts + c, s, c);
         wait_ld(s);
         if ((j + 1) * kRows - 1 > first) {  // the tile reaches past the first row
-          const int see = tok - j * kRows, all_see = __shfl_sync(0xffffffffu, see, 0);
+          const int see = tok - j * kRows;
 #pragma unroll
           for (int c = 0; c < kRows; c += 32) {
-            if (c + 31 <= all_see) continue;
+            const uint32_t keep = see - c >= 31 ? 0xffffffffu : see < c ? 0u : (2u << (see - c)) - 1u;
 #pragma unroll
-            for (int x = c; x < c + 32; ++x)
-              if (x > see) s[x] = __float_as_uint(-INFINITY);
+            for (int x = 0; x < 32; ++x)
+              if (!(keep >> x & 1u)) s[c + x] = __float_as_uint(-INFINITY);
           }
         }
         // On the assumption that the maximum has not grown much, the first half's exponentials need not wait for it: it is found

@@ -11,7 +11,7 @@
 //
 // * A block holds two tiles of 128 query rows of the same key-value head (or an SM two blocks of one tile, for short prompts).
 //   While the plain cores do one tile's softmax, the tensor cores do the other's products.  Roles: four warps to a tile (softmax and
-//   result, a row per lane), one warp that issues the products, one that loads, one that lays out the block's next work.
+//   result, a row per lane), one warp each that issues the products, loads, and lays out the block's next work.
 // * Blocks stay and take one block of work after the other, the ones with the most keys first; loads and the first scores of the
 //   next run while the result of the last is stored.
 // * A tile's 128 rows are (token, query head) pairs of one group, tokens outermost: with eight heads to a group a tile is
@@ -23,16 +23,17 @@
 // * O is rescaled in tensor memory only when a row's maximum has grown by more than 2^8 since it was last taken; until then
 //   probabilities are up to 2^8 instead of 1, which fp32 sums and 16-bit factors hold.  P is rounded to the rows' type (the
 //   product takes nothing wider at this rate), the sum l is of the unrounded values.
-// * Only tiles that reach past a row are masked.  Rows of the tail tile that belong to the next prompt (or to nobody) are zeroed
-//   in V; within a prompt a later token's V meets P = 0 exactly, so only an infinity or a NaN there can reach an earlier row,
-//   and a row whose result is not finite is computed again from plain loads over the tokens that it sees.
+// * Only tiles that reach past a row are masked.  Rows of the last tile that belong to the next prompt (or to nobody) are zeroed in V;
+//   within a prompt a later token's V meets P = 0 exactly, which only an infinity or a NaN survives: where a result is not finite,
+//   mend_rows looks up whether the tokens that the row sees make it so.  (A warp that looks through these tiles' V beforehand is
+//   simpler, and cost 2 to 10 %: its code, mostly.)
 // * Short prompts wait for instructions: what is off the usual path (rescaling, the result) is kept in loops.  Unrolled, twelve
 //   prompts of 1 to 1500 tokens, 32 heads, took 90 us instead of 80.  Measured and dropped: exponentials on the FMA units by a
 //   polynomial (they are no less busy), two lanes to a row (the exchange costs what the halves save), scores read from tensor
 //   memory 32 at a time, a warp of products for each tile (the tiles fall into step), the next block's first scores before the
 //   other tile's last product.
 //
-// Every wait is bounded (np_pipe.cuh); after a time-out all roles leave, the block meets and tensor memory is released.
+// Every wait is bounded; after a time-out all roles leave, the block meets and tensor memory is released.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -51,6 +52,7 @@ namespace {
 constexpr int kRows = 128;              // query rows of a tile, keys of a tile
 constexpr float kGrow = 8.f;            // log2 of the growth of a maximum that is let pass
 constexpr int kPlans = 2;               // blocks of work that are laid out ahead
+constexpr uint32_t kWaitPolls = 1u << 26;  // a second or two: a tile without rows waits for a whole block of work of the other
 struct PromptArgs {
   const uint16_t* q;
   const uint16_t* k;
@@ -205,44 +207,77 @@ __device__ __forceinline__ float widen(uint16_t x) {
   return kBf16 ? __uint_as_float((uint32_t)x << 16) : __half2float(__ushort_as_half(x));
 }
 
-// One row from plain loads, by a warp: the tokens it sees and no other.
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+// Rows whose O is not finite, by their warp (a row per lane, tokens rising with the lanes, one key-value head).  What the tokens that a row sees make infinite or NaN is so: weights are above 0, so an infinity stays one, and two
+// of different signs or a NaN make a NaN; V is looked through once for all rows.  What they do not has met a later token's V, or
+// has grown too large unnormalised: these values are computed again from plain loads, over the tokens that the row sees.
 template <bool kBf16, int HD>
-__device__ __noinline__ void row_again(const PromptArgs& a, int start, int tok, int head, int kvh, int lane) {
-  const uint16_t* q = a.q + (int64_t)(start + tok) * a.q_token + (int64_t)head * a.q_head;
-  float top = -INFINITY, sum = 0.f, acc[HD / 32];
+__device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, float row_l, int lane) {
+  constexpr int N = HD / 32;  // values of a lane: lane, lane + 32, ...
+  int odd[N];                 // of the tokens so far: 1 a NaN, 2 inf, 4 -inf
 #pragma unroll
-  for (int i = 0; i < HD / 32; ++i) acc[i] = 0.f;
-  for (int base = 0; base <= tok; base += 32) {
-    const int j = base + lane;
-    float s = -INFINITY;
-    if (j <= tok) {
-      const uint16_t* k = a.k + (int64_t)(start + j) * a.k_token + (int64_t)kvh * a.k_head;
-      s = 0.f;
-      for (int d = 0; d < HD; ++d) s = fmaf(widen<kBf16>(q[d]), widen<kBf16>(k[d]), s);
-      s *= a.scale2;
+  for (int i = 0; i < N; ++i) odd[i] = 0;
+  const uint16_t* v0 = a.v + (int64_t)start * a.v_token + (int64_t)kvh * a.v_head + lane;
+  int upto = 0;
+  for (; rows; rows &= rows - 1) {
+    const int src = __ffs(rows) - 1, tok = __shfl_sync(0xffffffffu, row_tok, src), head = __shfl_sync(0xffffffffu, row_head, src);
+    const float l = __shfl_sync(0xffffffffu, row_l, src);
+    if (not_finite(l)) continue;  // a score is no number: all of the row is none
+    uint16_t* out = a.out + (int64_t)(start + tok) * a.o_token + (int64_t)head * a.o_head + lane;
+    bool again = false;
+    if (l != 0.f) {
+#pragma unroll 4
+      for (int j = upto; j <= tok; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float x = widen<kBf16>(v0[j * a.v_token + i * 32]);
+          if (not_finite(x)) odd[i] |= x == INFINITY ? 2 : x == -INFINITY ? 4 : 1;
+        }
+      upto = max(upto, tok + 1);
     }
-    float now = fmaxf(top, s);
 #pragma unroll
-    for (int x = 1; x < 32; x <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, x));
-    const float use = now == -INFINITY ? 0.f : now, f = exp2_fast(top - use), p = j <= tok ? exp2_fast(s - use) : 0.f;
-    top = now;
-    sum = sum * f + p;
-#pragma unroll
-    for (int i = 0; i < HD / 32; ++i) acc[i] *= f;
-    const int most = min(32, tok + 1 - base);
-    for (int l = 0; l < most; ++l) {
-      const float pl = __shfl_sync(0xffffffffu, p, l);
-      const uint16_t* v = a.v + (int64_t)(start + base + l) * a.v_token + (int64_t)kvh * a.v_head;
-#pragma unroll
-      for (int i = 0; i < HD / 32; ++i) acc[i] = fmaf(pl, widen<kBf16>(v[i * 32 + lane]), acc[i]);
+    for (int i = 0; i < N; ++i) {
+      const float old = widen<kBf16>(out[i * 32]);
+      if (l == 0.f) out[i * 32] = 0;  // nothing but scores of -inf
+      else if (not_finite(old) && odd[i])
+        out[i * 32] = (uint16_t)pack<kBf16>(odd[i] == 2 ? INFINITY : odd[i] == 4 ? -INFINITY : __uint_as_float(0x7fffffffu), 0.f);
+      else again |= not_finite(old);
     }
+    if (!__any_sync(0xffffffffu, again)) continue;
+    const uint16_t* q = a.q + (int64_t)(start + tok) * a.q_token + (int64_t)head * a.q_head;
+    float top = -INFINITY, sum = 0.f, acc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] = 0.f;
+    for (int base = 0; base <= tok; base += 32) {
+      const int j = base + lane;
+      float s = -INFINITY;
+      if (j <= tok) {
+        const uint16_t* k = a.k + (int64_t)(start + j) * a.k_token + (int64_t)kvh * a.k_head;
+        s = 0.f;
+        for (int d = 0; d < HD; ++d) s = fmaf(widen<kBf16>(q[d]), widen<kBf16>(k[d]), s);
+        s *= a.scale2;
+      }
+      float now = fmaxf(top, s);
+#pragma unroll
+      for (int x = 1; x < 32; x <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, x));
+      const float use = now == -INFINITY ? 0.f : now, f = exp2_fast(top - use), p = j <= tok ? exp2_fast(s - use) : 0.f;
+      top = now;
+      sum = sum * f + p;
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[i] *= f;
+      const int most = min(32, tok + 1 - base);
+      for (int x = 0; x < most; ++x) {
+        const float px = __shfl_sync(0xffffffffu, p, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = fmaf(px, widen<kBf16>(v0[(base + x) * a.v_token + i * 32]), acc[i]);
+      }
+    }
+    sum = npd::warp_sum(sum);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (!odd[i] && not_finite(widen<kBf16>(out[i * 32]))) out[i * 32] = (uint16_t)pack<kBf16>(acc[i] / sum, 0.f);
   }
-  sum = npd::warp_sum(sum);
-  uint16_t* out = a.out + (int64_t)(start + tok) * a.o_token + (int64_t)head * a.o_head;
-#pragma unroll
-  for (int i = 0; i < HD / 32; ++i) out[i * 32 + lane] = (uint16_t)pack<kBf16>(sum == 0.f ? 0.f : acc[i] / sum, 0.f);
-  if (a.lse && lane == 0)
-    a.lse[(size_t)(start + tok) * a.n_heads + head] = sum == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) * kLn2 + logf(sum);
 }
 
 template <int HD, int kTiles>
@@ -382,7 +417,19 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   __syncthreads();
   fence_after();
   const uint32_t tmem = s_tmem;
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return npp::wait_or_flag(bar, parity, s_ok, a.status); };
+  // true: the phase is complete; false: this or another wait of the block has run out
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    uint32_t polls = 0;
+#pragma unroll 1
+    while (!npp::mbar_try_wait(bar, parity)) {
+      if (!s_ok[0]) return false;
+      if (++polls == kWaitPolls) {
+        s_ok[0] = 0;
+        atomicOr(a.status, NP_KV_S_TIMEOUT);
+      }
+    }
+    return true;
+  };
   // the same by whole warps: all lanes go on, or none does
   auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
   // the n-th plan; false: nothing is left, or a wait ran out
@@ -687,12 +734,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       }
       if (valid && a.lse)
         a.lse[(size_t)(w.start + tok) * a.n_heads + head] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * kLn2 + logf(l);
-      uint32_t again = __ballot_sync(0xffffffffu, valid && big >= 0x7f800000u);
-      while (again) {
-        const int src = __ffs(again) - 1;
-        again &= again - 1;
-        row_again<kBf16, HD>(a, w.start, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), w.kvh, lane);
-      }
+      const uint32_t odd = __ballot_sync(0xffffffffu, valid && big >= 0x7f800000u);
+      if (odd) mend_rows<kBf16, HD>(a, odd, w.start, tok, head, w.kvh, l, lane);
     }
   }
   fence_before();

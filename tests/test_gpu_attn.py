@@ -261,6 +261,56 @@ def test_prompt_later_tokens_do_not_reach_earlier_rows():
     assert torch.isnan(out[100:150].float()).all() and torch.isnan(out[340:].float()).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("hq,hkv,hd", [(1, 1, 64), (4, 2, 128), (5, 1, 128), (8, 1, 64)])
+def test_prompt_infinite_values_reach_the_rows_that_see_them(dtype, hq, hkv, hd):
+    """Values that are not finite, in single places of tokens of every part of a prompt: each row's result is what the weighted sum
+    over the tokens that it sees is, infinities with their signs, and finite everywhere else."""
+    lens = [400, 3, 150]
+    rows, cu = sum(lens), np.concatenate([[0], np.cumsum(lens)])
+    g = torch.Generator(device="cuda").manual_seed(hq)
+    qkv = torch.randn(rows, hq + 2 * hkv, hd, generator=g, device="cuda").to(dtype)
+    rng = np.random.default_rng(hd)
+    places = [(t, int(rng.integers(0, hkv)), int(rng.integers(0, hd)), x) for t, x in zip(
+        [0, 30, 127, 128, 129, 255, 256, 300, 399, 401, 403, 540, 552], [np.inf, -np.inf, np.nan, np.inf, np.inf, -np.inf, np.inf, np.nan, np.inf, np.inf,
+                                                                         -np.inf, np.nan, np.inf])]
+    for t, h, d, x in places:
+        qkv[t, hq + hkv + h, d] = x
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    out, lse = torch.empty(rows, hq, hd, dtype=dtype, device="cuda"), torch.empty(rows, hq, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    nb.np_attn_prompt(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), out, status, lse=lse)
+    assert nb.np_attn_check(status) == nb.NP_OK
+    on, kn, vn, qn, scale = f64(out), f64(k), f64(v), f64(q), hd ** -0.5
+    fine = np.nan_to_num(vn, nan=0.0, posinf=0.0, neginf=0.0)
+    for r in range(rows):
+        a = cu[np.searchsorted(cu, r, side="right") - 1]
+        for h in range(hq):
+            c = h // (hq // hkv)
+            seen = vn[a:r + 1, c]
+            add = np.where(np.isfinite(seen), 0.0, seen)
+            with np.errstate(invalid="ignore"):
+                want_odd = add.sum(0)                      # weights are above 0: what is not finite stays that, signs and all
+            want, wl, mean, amp = A.attend(qn[r, h], kn[a:r + 1, c], fine[a:r + 1, c], scale)
+            tol, _ = A.tolerances(want, wl, mean, amp, r + 1 - a, hd, dtype == HF, True, np.abs(fine).max())
+            odd = ~np.isfinite(want_odd)
+            assert np.array_equal(on[r, h][odd], want_odd[odd], equal_nan=True), (r, h)
+            assert (np.abs(on[r, h][~odd] - want[~odd]) <= tol[~odd]).all(), (r, h)
+
+
+def test_prompt_of_nothing_but_nan_values_ends_like_any_other():
+    n, hq = 6000, 4
+    qkv = torch.randn(n, hq + 2, 128, device="cuda").to(BF)
+    qkv[:, hq + 1] = float("nan")
+    out, status = torch.zeros(n, hq, 128, dtype=BF, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    nb.np_attn_prompt(qkv[:, :hq], qkv[:, hq:hq + 1], qkv[:, hq + 1:], torch.tensor([0, n], dtype=torch.int32, device="cuda"), out, status)
+    assert nb.np_attn_check(status) == nb.NP_OK and torch.isnan(out).all()
+    qkv[:] = float("nan")
+    out.zero_()
+    nb.np_attn_prompt(qkv[:, :hq], qkv[:, hq:hq + 1], qkv[:, hq + 1:], torch.tensor([0, n], dtype=torch.int32, device="cuda"), out, status)
+    assert nb.np_attn_check(status) == nb.NP_OK and torch.isnan(out).all()
+
+
 def test_prompt_rows_with_nothing_but_minus_infinity():
     """Keys of -inf make every score -inf as long as they are all there is: zeros, as for an empty sequence."""
     rows = 140
@@ -273,6 +323,12 @@ def test_prompt_rows_with_nothing_but_minus_infinity():
     nb.np_attn_prompt(qkv[:, :1], qkv[:, 1:2], qkv[:, 2:], torch.tensor([0, rows], dtype=torch.int32, device="cuda"), out, status, lse=lse)
     assert nb.np_attn_check(status) == nb.NP_OK
     assert (out[:5] == 0).all() and (lse[:5] == -float("inf")).all()
+    qkv[3, 2] = float("nan")                   # seen with a weight that is no number: zeros as long as there is no other
+    nb.np_attn_prompt(qkv[:, :1], qkv[:, 1:2], qkv[:, 2:], torch.tensor([0, 5], dtype=torch.int32, device="cuda"), out, status, lse=lse)
+    assert nb.np_attn_check(status) == nb.NP_OK and (out[:5] == 0).all()
+    qkv[3, 2] = 0.5
+    nb.np_attn_prompt(qkv[:, :1], qkv[:, 1:2], qkv[:, 2:], torch.tensor([0, rows], dtype=torch.int32, device="cuda"), out, status, lse=lse)
+    torch.cuda.synchronize()
     kn, vn = f64(qkv[:, 1:2]), f64(qkv[:, 2:])
     check_rows(out[5:], lse[5:], qkv[5:, :1], lambda i: (kn[5:i + 6], vn[5:i + 6]), 0.125, True)
 

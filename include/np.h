@@ -540,7 +540,8 @@ const char* np_trunk_last_error(void);
  * that reads it.  It stands beside np_step (the MLP half); the paper leaves attention dense and describes none of
  * this.  No context is needed: the caller owns the cache, its tables and every buffer (all memory of the current
  * device), calls queue kernels on `stream` and neither synchronise nor allocate, and all of them may be captured
- * into a graph.  Text of the calling thread's last error: np_attn_last_error().
+ * into a graph.  Calls of different streams on the same tables, scratch or cache have to be ordered by the caller where one of
+ * them changes what the other uses (every np_kv call with a list of sequences uses the scratch).  Text of the calling thread's last error: np_attn_last_error().
  *
  * A cache holds n_layers layers of n_pages pages; a page holds the keys and the values of page_tokens consecutive
  * tokens of one sequence:
@@ -620,14 +621,15 @@ int np_kv_reserve(const np_kv_desc* desc, const np_kv_tables* tables, const int3
  * on are not read, and a sequence with start[i] < 0 is passed over.
  *   k, v   n_tokens rows of n_kv_heads heads
  *   seqs   dev [n] (NULL: 0..n-1),  cu  dev [n + 1] ascending, from 0 (NULL: one token each, n_tokens == n),  start  dev [n]
- * Two rows for the same position: one of them is kept. */
+ * Two rows for the same position leave a mixture of both there. */
 int np_kv_append(const np_kv_desc* desc, void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* k,
                  const np_rows* v, int32_t n_tokens, const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n,
                  void* stream);
 
 /* Sequence dst[i] (empty, listed once) begins as a copy of sequence src[i] (dev [n] each): it shares the full pages, and a
  * partly filled last page is copied, in every layer, to a page of its own (list order, lowest free number first).  A
- * source may be listed often.  All sources are taken as they were before the call. */
+ * source may be listed often.  All sources are taken as they were before the call: tokens that were reserved and are
+ * appended to a source later are not in the copy's last page. */
 int np_kv_fork(const np_kv_desc* desc, void* cache, const np_kv_tables* tables, const int32_t* src, const int32_t* dst,
                int32_t n, void* stream);
 
@@ -655,7 +657,7 @@ int np_kv_copy_pages(const np_kv_desc* desc, void* dst_cache, const void* src_ca
  * (the new token among them: append it first).  Keys and values past a sequence's length are not read.  A sequence of
  * length 0, and a row whose seqs[i] is negative (padding), give zeros and lse -inf, and so does a row whose scores are all
  * -inf.  fp32 scores, softmax and sums.
- *   q, out     n rows of n_heads heads; out may not overlap q
+ *   q, out     n rows of n_heads heads; out may not overlap q, its strides are above 0 along more than one row or head
  *   scale      positive and finite
  *   lse        dev fp32 [n][n_heads] or NULL: log sum_j exp(scale * q . k_j)
  *   seqs       dev [n] or NULL: 0..n-1; the same sequence may be listed often

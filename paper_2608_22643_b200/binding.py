@@ -101,6 +101,7 @@ class np_kv_desc(C.Structure):
 
 class np_kv_tables(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("page_table", "lens", "refs", "scratch", "status")]
+    device, room = None, None   # make_kv_tables: where the tensors are, and how many elements they hold
 
 
 class np_kv_sizes_out(C.Structure):
@@ -337,7 +338,8 @@ def np_trunk_forward(desc, table, features, centroid_id, workspace, head_logits,
 # Tensors belong to the current device.  Rows of heads (q, k, v, out) are tensors [tokens][heads][head_dim] with any strides
 # between tokens and heads and the last dimension contiguous; everything else is contiguous.
 _ATTN_DTYPE = {torch.bfloat16: NP_T_BF16, torch.float16: NP_T_FP16}
-_ATTN_TYPES = (torch.bfloat16, torch.float16)
+_ATTN_TYPES = {NP_T_BF16: torch.bfloat16, NP_T_FP16: torch.float16}
+_KV_MAX_SEQS = 1024
 
 
 def _attn_check(rc: int) -> int:
@@ -384,9 +386,21 @@ def _rows_of(t, dtype, device: int, tokens: int, heads: int, head_dim: int) -> b
     return _pack_rows(t.data_ptr(), st if tokens > 1 else 0, sh if heads > 1 else 0)
 
 
+def _tables_of(desc: np_kv_desc, tables: np_kv_tables, device: int):
+    """What goes to the library for a table structure, once its tensors are known to be of the device and large enough."""
+    if tables.room is not None:
+        table, lens, refs, scratch = tables.room
+        seqs, pages = desc.max_seqs, desc.n_pages
+        if (tables.device != device or table < seqs * desc.max_pages or lens < seqs or refs < pages
+                or 0 <= scratch < pages + 2 * max(pages, _KV_MAX_SEQS) + 16):
+            _refuse(f"tables on device {tables.device} of {table}, {lens}, {refs} and {scratch} elements do not serve max_seqs {seqs}, "
+                    f"max_pages {desc.max_pages}, n_pages {pages} on device {device}")
+    return C.byref(tables)
+
+
 def _cache_of(desc: np_kv_desc, cache, device: int):
     """(address, type, key-value heads, head size) of a cache of the description."""
-    dtype, heads, hd = _ATTN_TYPES[desc.dtype], desc.n_kv_heads, desc.head_dim
+    dtype, heads, hd = _ATTN_TYPES.get(desc.dtype), desc.n_kv_heads, desc.head_dim
     if (cache.get_device() != device or cache.dtype is not dtype or not cache.is_contiguous()
             or cache.shape != (desc.n_layers, desc.n_pages, 2, heads, desc.page_tokens, hd)):
         _refuse(f"expected a contiguous cache [{desc.n_layers}][{desc.n_pages}][2][{heads}][{desc.page_tokens}][{hd}] of {dtype} on the "
@@ -405,9 +419,12 @@ def make_kv_desc(dtype, n_layers: int, n_kv_heads: int, head_dim: int, page_toke
 
 
 def make_kv_tables(page_table, lens, refs, scratch, status) -> np_kv_tables:
-    """The pointer table over int32 tensors (the caller keeps them alive)."""
+    """The pointer table over int32 tensors (the caller keeps them alive).  ``scratch`` and ``status`` may be None in the tables that
+    np_kv_compact writes."""
     device = _device()
-    return np_kv_tables(*[_dev(t, torch.int32, device) for t in (page_table, lens, refs, scratch, status)])
+    tables = np_kv_tables(*[_dev(t, torch.int32, device) for t in (page_table, lens, refs, scratch, status)])
+    tables.device, tables.room = device, (page_table.numel(), lens.numel(), refs.numel(), -1 if scratch is None else scratch.numel())
+    return tables
 
 
 def np_kv_sizes(desc: np_kv_desc) -> np_kv_sizes_out:
@@ -417,12 +434,12 @@ def np_kv_sizes(desc: np_kv_desc) -> np_kv_sizes_out:
 
 
 def np_kv_reset(desc, tables, stream=None) -> int:
-    return _attn_check(load().np_kv_reset(C.byref(desc), C.byref(tables), _stream(stream)))
+    return _attn_check(load().np_kv_reset(C.byref(desc), _tables_of(desc, tables, _device()), _stream(stream)))
 
 
 def np_kv_reserve(desc, tables, seqs, n_new, start_out=None, stream=None) -> int:
     n, i32, dv = n_new.numel(), torch.int32, _device()
-    return _attn_check(load().np_kv_reserve(C.byref(desc), C.byref(tables), _dev(seqs, i32, dv, n), _dev(n_new, i32, dv), n,
+    return _attn_check(load().np_kv_reserve(C.byref(desc), _tables_of(desc, tables, dv), _dev(seqs, i32, dv, n), _dev(n_new, i32, dv), n,
                                             _dev(start_out, i32, dv, n), _stream(stream)))
 
 
@@ -431,25 +448,27 @@ def np_kv_append(desc, cache, layer: int, tables, k, v, seqs, cu, start, stream=
     n, tokens, i32, dv = start.numel(), k.shape[0], torch.int32, _device()
     at, dtype, heads, hd = _cache_of(desc, cache, dv)
     return _attn_check(load().np_kv_append(
-        C.byref(desc), at, layer, C.byref(tables), _rows_of(k, dtype, dv, tokens, heads, hd), _rows_of(v, dtype, dv, tokens, heads, hd), tokens,
+        C.byref(desc), at, layer, _tables_of(desc, tables, dv), _rows_of(k, dtype, dv, tokens, heads, hd), _rows_of(v, dtype, dv, tokens, heads, hd), tokens,
         _dev(seqs, i32, dv, n), _dev(cu, i32, dv, n + 1), _dev(start, i32, dv), n, _stream(stream)))
 
 
 def np_kv_fork(desc, cache, tables, src, dst, stream=None) -> int:
     n, i32, dv = src.numel(), torch.int32, _device()
-    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache, dv)[0], C.byref(tables), _dev(src, i32, dv),
+    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache, dv)[0], _tables_of(desc, tables, dv), _dev(src, i32, dv),
                                          _dev(dst, i32, dv, n), n, _stream(stream)))
 
 
 def np_kv_free(desc, tables, seqs=None, n: Optional[int] = None, stream=None) -> int:
-    """``seqs`` None: sequences 0..n-1."""
-    n = seqs.numel() if n is None else n
-    return _attn_check(load().np_kv_free(C.byref(desc), C.byref(tables), _dev(seqs, torch.int32, _device(), n), n, _stream(stream)))
+    """``seqs`` None: sequences 0..n-1; ``n`` None as well: all of them."""
+    if n is None:
+        n = desc.max_seqs if seqs is None else seqs.numel()
+    dv = _device()
+    return _attn_check(load().np_kv_free(C.byref(desc), _tables_of(desc, tables, dv), _dev(seqs, torch.int32, dv, n), n, _stream(stream)))
 
 
 def np_kv_compact(desc, cache, tables, out_tables, n_live=None, stream=None) -> int:
     dv = _device()
-    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache, dv)[0], C.byref(tables), C.byref(out_tables),
+    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache, dv)[0], _tables_of(desc, tables, dv), _tables_of(desc, out_tables, dv),
                                             _dev(n_live, torch.int32, dv, 1), _stream(stream)))
 
 
@@ -471,7 +490,7 @@ def np_attn_decode(desc, cache, layer: int, tables, q, out, workspace, seqs=None
     dv = _device()
     at, dtype, _, hd = _cache_of(desc, cache, dv)
     return _attn_check(load().np_attn_decode(
-        C.byref(desc), at, layer, C.byref(tables), _rows_of(q, dtype, dv, n, heads, hd), heads, _dev(seqs, torch.int32, dv, n), n,
+        C.byref(desc), at, layer, _tables_of(desc, tables, dv), _rows_of(q, dtype, dv, n, heads, hd), heads, _dev(seqs, torch.int32, dv, n), n,
         hd ** -0.5 if scale is None else scale, _rows_of(out, dtype, dv, n, heads, hd), _dev(lse, torch.float32, dv, n * heads),
         _dev(workspace, torch.uint8, dv), workspace.numel(), _stream(stream)))
 

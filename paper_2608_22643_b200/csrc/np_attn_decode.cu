@@ -589,6 +589,7 @@ int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const 
   if (!std::isfinite(scale) || scale <= 0.f) return fail(NP_E_INVAL, "scale must be positive and finite");
   if (const char* m = rows_error(q)) return fail(NP_E_INVAL, m);
   if (const char* m = rows_error(out)) return fail(NP_E_INVAL, m);
+  if ((n > 1 && out->token_stride == 0) || (n_heads > 1 && out->head_stride == 0)) return fail(NP_E_INVAL, "rows of the result need strides above 0");
   int sms;
   if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
   const int64_t page = (int64_t)2 * d->n_kv_heads * d->page_tokens * d->head_dim * 2;

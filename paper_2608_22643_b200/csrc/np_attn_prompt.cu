@@ -209,9 +209,10 @@ __device__ __forceinline__ float widen(uint16_t x) {
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
-// Rows whose O is not finite, by their warp (a row per lane, tokens rising with the lanes, one key-value head).  What the tokens that a row sees make infinite or NaN is so: weights are above 0, so an infinity stays one, and two
-// of different signs or a NaN make a NaN; V is looked through once for all rows.  What they do not has met a later token's V, or
-// has grown too large unnormalised: these values are computed again from plain loads, over the tokens that the row sees.
+// Rows whose O is not finite, by their warp (a row per lane, tokens rising with the lanes, one key-value head).  What the tokens
+// that a row sees make infinite or NaN is so: weights are above 0, so an infinity stays one, and two of different signs or a NaN
+// make a NaN; V is looked through once for all rows.  What they do not has met a later token's V, or has grown too large
+// unnormalised: these values are computed again from plain loads, over the tokens that the row sees.
 template <bool kBf16, int HD>
 __device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, float row_l, int lane) {
   constexpr int N = HD / 32;  // values of a lane: lane, lane + 32, ...
@@ -220,6 +221,7 @@ __device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int s
   for (int i = 0; i < N; ++i) odd[i] = 0;
   const uint16_t* v0 = a.v + (int64_t)start * a.v_token + (int64_t)kvh * a.v_head + lane;
   int upto = 0;
+  __syncwarp();  // the rows' results, which other lanes have stored, are read below
   for (; rows; rows &= rows - 1) {
     const int src = __ffs(rows) - 1, tok = __shfl_sync(0xffffffffu, row_tok, src), head = __shfl_sync(0xffffffffu, row_head, src);
     const float l = __shfl_sync(0xffffffffu, row_l, src);

@@ -165,3 +165,37 @@ def test_binding_refuses_host_tensors_and_other_types(lib):
     assert e.value.code == nb.NP_E_INVAL
     with pytest.raises(nb.NpError):
         nb.make_kv_desc(torch.float32, 1, 1, 64, 16, 1, 1)
+
+
+def test_binding_refuses_a_cache_of_no_type(lib):
+    """A description made by hand with a type that there is none of: a refusal, not an IndexError."""
+    d = _desc(dtype=7)
+    z = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(nb.NpError) as e:
+        nb.np_kv_fork(d, z, _tables(), torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
+    assert e.value.code == nb.NP_E_INVAL
+
+
+@pytest.mark.parametrize("short", range(5))
+def test_binding_refuses_tables_that_are_too_small_or_elsewhere(lib, short):
+    """Tables that would be written past their ends, or that belong to another device than the call."""
+    d = _desc()
+    seqs, pages = d.max_seqs, d.n_pages
+    room = [seqs * d.max_pages, seqs, pages, nb.np_kv_sizes(d).scratch_bytes // 4]
+    t = _tables()
+    t.device, t.room = 0, tuple(room)
+    assert nb._tables_of(d, t, 0) is not None
+    if short < 4:
+        t.room = tuple(r - (i == short) for i, r in enumerate(room))
+    with pytest.raises(nb.NpError) as e:
+        nb._tables_of(d, t, 0 if short < 4 else 1)
+    assert e.value.code == nb.NP_E_INVAL
+
+
+def test_decode_refuses_results_on_top_of_each_other(lib):
+    d, t, bad = _desc(), _tables(), nb.NP_E_INVAL
+
+    def call(out, n):
+        return lib.np_attn_decode(_b(d), P, 0, _b(t), _b(_rows()), 8, P, n, 0.1, _b(out), None, P, 1 << 40, None)
+
+    assert call(_rows(token_stride=0), 2) == bad and call(_rows(head_stride=0), 2) == bad and "above 0" in lib.np_attn_last_error().decode()

@@ -432,3 +432,43 @@ def test_a_run_of_them_together():
             c.pool.compact()
             hist[0] = []
     assert nb.np_attn_check(c.status) == nb.NP_OK
+
+
+def test_prompts_on_streams_of_their_own():
+    """Long and short prompts at once, eager and replayed, one and two tiles to a block: each call as if it were alone."""
+    jobs = []
+    for seed, (lens, hq, hkv, hd) in enumerate([([700, 3, 0, 900], 8, 2, 128), ([64] * 30, 4, 4, 64), ([1], 2, 1, 128)]):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rows = sum(lens)
+        q, k, v = (torch.randn(rows, h, hd, generator=g, device="cuda").to(BF) for h in (hq, hkv, hkv))
+        cu = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+        status, want = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.empty_like(q)
+        nb.np_attn_prompt(q, k, v, cu, want, status)
+        jobs.append((q, k, v, cu, status, want, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    outs, graphs = [], []
+    for q, k, v, cu, status, want, s in jobs:
+        held, graph = torch.empty_like(q), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            nb.np_attn_prompt(q, k, v, cu, held, status, stream=s)
+        graphs.append((graph, s, held, want))
+    for _ in range(20):
+        for (q, k, v, cu, status, want, s), (graph, *_r) in zip(jobs, graphs):
+            with torch.cuda.stream(s):
+                o = torch.empty_like(q)
+                nb.np_attn_prompt(q, k, v, cu, o, status, stream=s)
+                outs.append((o, want))
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o, want in outs) and all(torch.equal(h, want) for _, _, h, want in graphs)
+    assert all(job[4].item() == 0 for job in jobs)
+
+
+def test_decode_of_the_most_rows():
+    """1024 rows of a call, most of them the same sequences again or padding; the largest table."""
+    c = Cache(hkv=1, hd=64, P=16, n_pages=600, max_seqs=1024, max_pages=40)
+    seqs = list(range(0, 1024, 7))
+    c.grow(seqs, [1 + (5 * s) % 43 for s in seqs])
+    rows = [[seqs[i % len(seqs)], -1, 1][0 if i % 3 == 0 else i % 3] for i in range(1024)]
+    _decode(c, 4, seqs=rows)
+    c.check()

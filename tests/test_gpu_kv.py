@@ -255,3 +255,19 @@ def test_tensors_of_another_kind_are_refused():
         nb.np_kv_free(c.desc, c.tables, torch.zeros(2, dtype=torch.int64, device="cuda"))
     with pytest.raises(nb.NpError):
         nb.np_kv_fork(c.desc, c.cache, c.tables, c.dev([0, 1]), c.dev([2]))
+
+
+def test_the_most_sequences_at_once():
+    """1024 sequences in one call of each kind, every one forked from the same parent but one."""
+    c = Cache(P=16, n_pages=3000, max_seqs=1024, hkv=1, max_pages=4)
+    c.reserve([0], [35])
+    dst = list(range(1, 1024))
+    nb.np_kv_fork(c.desc, c.cache, c.tables, c.dev([0] * 1023), c.dev(dst))
+    c.pool.fork([0] * 1023, dst)
+    c.check()
+    c.reserve(list(range(1024)), [(7 * s) % 31 for s in range(1024)])
+    c.check()
+    nb.np_kv_free(c.desc, c.tables)
+    c.pool.free(list(range(1024)))
+    c.check()
+    assert not c.refs.any()

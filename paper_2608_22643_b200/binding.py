@@ -11,7 +11,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 from typing import Optional
 
 import numpy as np
@@ -101,7 +100,7 @@ class np_kv_desc(C.Structure):
 
 class np_kv_tables(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("page_table", "lens", "refs", "scratch", "status")]
-    device, room = None, None   # make_kv_tables: where the tensors are, and how many elements they hold
+    room = None   # make_kv_tables: device, and elements of page_table, lens, refs and scratch (-1: none)
 
 
 class np_kv_sizes_out(C.Structure):
@@ -336,10 +335,23 @@ def np_trunk_forward(desc, table, features, centroid_id, workspace, head_logits,
 
 # ---- the paged key-value cache and its attention ----------------------------------------
 # Tensors belong to the current device.  Rows of heads (q, k, v, out) are tensors [tokens][heads][head_dim] with any strides
-# between tokens and heads and the last dimension contiguous; everything else is contiguous.
+# between tokens and heads and the last dimension contiguous; everything else is contiguous.  What looks at them and calls the
+# library is compiled (csrc/np_attn_bind.cpp): a tensor that does not fit is an NpError of NP_E_INVAL that names it.
 _ATTN_DTYPE = {torch.bfloat16: NP_T_BF16, torch.float16: NP_T_FP16}
-_ATTN_TYPES = {NP_T_BF16: torch.bfloat16, NP_T_FP16: torch.float16}
-_KV_MAX_SEQS = 1024
+_calls = None
+
+
+def _attn():
+    global _calls
+    if _calls is None:
+        load()
+        try:
+            from . import np_attn_bind
+        except ImportError as e:
+            raise RuntimeError(f"np_attn_bind.so is not usable ({e}): build it with `python -m paper_2608_22643_b200.build`") from e
+        np_attn_bind.setup(NpError)
+        _calls = np_attn_bind
+    return _calls
 
 
 def _attn_check(rc: int) -> int:
@@ -348,82 +360,25 @@ def _attn_check(rc: int) -> int:
     return rc
 
 
-def _refuse(msg: str):
-    raise NpError(NP_E_INVAL, msg)
-
-
-def _device() -> int:
-    """The current device; -2 (no tensor's) without one."""
-    try:
-        return torch.cuda.current_device()
-    except (RuntimeError, AssertionError):
-        return -2
-
-
-# Small calls are bound by what these checks take (a few microseconds a call): one query of the device per call, structures as
-# packed bytes, and messages made up only when something is wrong.
-_pack_rows = struct.Struct("@Pqq").pack            # np_rows
-_pack_shape = struct.Struct("@8i").pack            # np_attn_shape
-
-
-def _dev(t, dtype, device: int, least: int = 0) -> Optional[int]:
-    """Address of a contiguous tensor of the device (None stays None) that holds at least ``least`` elements."""
-    if t is None:
-        return None
-    if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous() or t.numel() < least:
-        _refuse(f"expected a contiguous {dtype} tensor of at least {least} elements on the current CUDA device, got {t.dtype} "
-                f"{tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _rows_of(t, dtype, device: int, tokens: int, heads: int, head_dim: int) -> bytes:
-    """An np_rows of a tensor of rows (``dtype`` a torch type)."""
-    if t.get_device() != device or t.dtype is not dtype or t.shape != (tokens, heads, head_dim) or t.stride(2) != 1:
-        _refuse(f"expected rows [{tokens}][{heads}][{head_dim}] of {dtype}, the last dimension contiguous, on the current CUDA device, "
-                f"got {tuple(t.shape)} {t.dtype} with strides {t.stride()} on {t.device}")
-    st, sh, _ = t.stride()
-    # a stride nobody steps along may be anything in torch
-    return _pack_rows(t.data_ptr(), st if tokens > 1 else 0, sh if heads > 1 else 0)
-
-
-def _tables_of(desc: np_kv_desc, tables: np_kv_tables, device: int):
-    """What goes to the library for a table structure, once its tensors are known to be of the device and large enough."""
-    if tables.room is not None:
-        table, lens, refs, scratch = tables.room
-        seqs, pages = desc.max_seqs, desc.n_pages
-        if (tables.device != device or table < seqs * desc.max_pages or lens < seqs or refs < pages
-                or 0 <= scratch < pages + 2 * max(pages, _KV_MAX_SEQS) + 16):
-            _refuse(f"tables on device {tables.device} of {table}, {lens}, {refs} and {scratch} elements do not serve max_seqs {seqs}, "
-                    f"max_pages {desc.max_pages}, n_pages {pages} on device {device}")
-    return C.byref(tables)
-
-
-def _cache_of(desc: np_kv_desc, cache, device: int):
-    """(address, type, key-value heads, head size) of a cache of the description."""
-    dtype, heads, hd = _ATTN_TYPES.get(desc.dtype), desc.n_kv_heads, desc.head_dim
-    if (cache.get_device() != device or cache.dtype is not dtype or not cache.is_contiguous()
-            or cache.shape != (desc.n_layers, desc.n_pages, 2, heads, desc.page_tokens, hd)):
-        _refuse(f"expected a contiguous cache [{desc.n_layers}][{desc.n_pages}][2][{heads}][{desc.page_tokens}][{hd}] of {dtype} on the "
-                f"current CUDA device, got {tuple(cache.shape)} {cache.dtype} on {cache.device}")
-    return cache.data_ptr(), dtype, heads, hd
-
-
 def make_kv_desc(dtype, n_layers: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int, max_seqs: int,
                  max_pages: Optional[int] = None) -> np_kv_desc:
     """``dtype``: torch.bfloat16 or torch.float16 (or an NP_T_* code)."""
     code = _ATTN_DTYPE.get(dtype, dtype)
     if not isinstance(code, int):
-        _refuse(f"no cache of {dtype}: bfloat16 or float16")
+        raise NpError(NP_E_INVAL, f"no cache of {dtype}: bfloat16 or float16")
     return np_kv_desc(code, n_layers, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
                       n_pages if max_pages is None else max_pages)
 
 
 def make_kv_tables(page_table, lens, refs, scratch, status) -> np_kv_tables:
-    """The pointer table over int32 tensors (the caller keeps them alive).  ``scratch`` and ``status`` may be None in the tables that
-    np_kv_compact writes."""
-    device = _device()
-    tables = np_kv_tables(*[_dev(t, torch.int32, device) for t in (page_table, lens, refs, scratch, status)])
-    tables.device, tables.room = device, (page_table.numel(), lens.numel(), refs.numel(), -1 if scratch is None else scratch.numel())
+    """The pointer table over contiguous int32 tensors of one CUDA device (the caller keeps them alive).  ``scratch`` and ``status`` may
+    be None in the tables that np_kv_compact writes."""
+    tensors = (page_table, lens, refs, scratch, status)
+    for t in tensors:
+        if t is not None and (t.device != page_table.device or not t.is_cuda or t.dtype is not torch.int32 or not t.is_contiguous()):
+            raise NpError(NP_E_INVAL, f"expected contiguous int32 tensors of one CUDA device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    tables = np_kv_tables(*[None if t is None else t.data_ptr() for t in tensors])
+    tables.room = (page_table.get_device(), page_table.numel(), lens.numel(), refs.numel(), -1 if scratch is None else scratch.numel())
     return tables
 
 
@@ -434,48 +389,34 @@ def np_kv_sizes(desc: np_kv_desc) -> np_kv_sizes_out:
 
 
 def np_kv_reset(desc, tables, stream=None) -> int:
-    return _attn_check(load().np_kv_reset(C.byref(desc), _tables_of(desc, tables, _device()), _stream(stream)))
+    return _attn().kv_reset(desc, tables, stream)
 
 
 def np_kv_reserve(desc, tables, seqs, n_new, start_out=None, stream=None) -> int:
-    n, i32, dv = n_new.numel(), torch.int32, _device()
-    return _attn_check(load().np_kv_reserve(C.byref(desc), _tables_of(desc, tables, dv), _dev(seqs, i32, dv, n), _dev(n_new, i32, dv), n,
-                                            _dev(start_out, i32, dv, n), _stream(stream)))
+    """``seqs`` None: sequences 0, 1, ... as many as ``n_new`` has."""
+    return _attn().kv_reserve(desc, tables, seqs, n_new, start_out, stream)
 
 
 def np_kv_append(desc, cache, layer: int, tables, k, v, seqs, cu, start, stream=None) -> int:
     """``cu`` None: one token for each sequence."""
-    n, tokens, i32, dv = start.numel(), k.shape[0], torch.int32, _device()
-    at, dtype, heads, hd = _cache_of(desc, cache, dv)
-    return _attn_check(load().np_kv_append(
-        C.byref(desc), at, layer, _tables_of(desc, tables, dv), _rows_of(k, dtype, dv, tokens, heads, hd), _rows_of(v, dtype, dv, tokens, heads, hd), tokens,
-        _dev(seqs, i32, dv, n), _dev(cu, i32, dv, n + 1), _dev(start, i32, dv), n, _stream(stream)))
+    return _attn().kv_append(desc, cache, layer, tables, k, v, seqs, cu, start, stream)
 
 
 def np_kv_fork(desc, cache, tables, src, dst, stream=None) -> int:
-    n, i32, dv = src.numel(), torch.int32, _device()
-    return _attn_check(load().np_kv_fork(C.byref(desc), _cache_of(desc, cache, dv)[0], _tables_of(desc, tables, dv), _dev(src, i32, dv),
-                                         _dev(dst, i32, dv, n), n, _stream(stream)))
+    return _attn().kv_fork(desc, cache, tables, src, dst, stream)
 
 
 def np_kv_free(desc, tables, seqs=None, n: Optional[int] = None, stream=None) -> int:
     """``seqs`` None: sequences 0..n-1; ``n`` None as well: all of them."""
-    if n is None:
-        n = desc.max_seqs if seqs is None else seqs.numel()
-    dv = _device()
-    return _attn_check(load().np_kv_free(C.byref(desc), _tables_of(desc, tables, dv), _dev(seqs, torch.int32, dv, n), n, _stream(stream)))
+    return _attn().kv_free(desc, tables, seqs, n, stream)
 
 
 def np_kv_compact(desc, cache, tables, out_tables, n_live=None, stream=None) -> int:
-    dv = _device()
-    return _attn_check(load().np_kv_compact(C.byref(desc), _cache_of(desc, cache, dv)[0], _tables_of(desc, tables, dv), _tables_of(desc, out_tables, dv),
-                                            _dev(n_live, torch.int32, dv, 1), _stream(stream)))
+    return _attn().kv_compact(desc, cache, tables, out_tables, n_live, stream)
 
 
 def np_kv_copy_pages(desc, dst_cache, src_cache, src, dst, status, stream=None) -> int:
-    n, i32, dv = src.numel(), torch.int32, _device()
-    return _attn_check(load().np_kv_copy_pages(C.byref(desc), _cache_of(desc, dst_cache, dv)[0], _cache_of(desc, src_cache, dv)[0], _dev(src, i32, dv),
-                                               _dev(dst, i32, dv, n), n, _dev(status, i32, dv, 1), _stream(stream)))
+    return _attn().kv_copy_pages(desc, dst_cache, src_cache, src, dst, status, stream)
 
 
 def np_attn_workspace_bytes(desc, n_heads: int, n: int) -> int:
@@ -486,28 +427,16 @@ def np_attn_workspace_bytes(desc, n_heads: int, n: int) -> int:
 
 def np_attn_decode(desc, cache, layer: int, tables, q, out, workspace, seqs=None, scale: Optional[float] = None, lse=None, stream=None) -> int:
     """``scale`` None: 1 / sqrt(head_dim).  ``workspace``: a uint8 tensor, zeroed before its first use."""
-    n, heads, _ = q.shape
-    dv = _device()
-    at, dtype, _, hd = _cache_of(desc, cache, dv)
-    return _attn_check(load().np_attn_decode(
-        C.byref(desc), at, layer, _tables_of(desc, tables, dv), _rows_of(q, dtype, dv, n, heads, hd), heads, _dev(seqs, torch.int32, dv, n), n,
-        hd ** -0.5 if scale is None else scale, _rows_of(out, dtype, dv, n, heads, hd), _dev(lse, torch.float32, dv, n * heads),
-        _dev(workspace, torch.uint8, dv), workspace.numel(), _stream(stream)))
+    return _attn().attn_decode(desc, cache, layer, tables, q, out, workspace, seqs, scale, lse, stream)
 
 
 def np_attn_prompt(q, k, v, cu, out, status, scale: Optional[float] = None, lse=None, stream=None) -> int:
     """``q``, ``out`` [tokens][heads][head_dim], ``k``, ``v`` [tokens][kv heads][head_dim]; ``cu`` int32, one more than prompts."""
-    tokens, heads, hd = q.shape
-    dtype, kv_heads, dv = q.dtype, k.shape[1], _device()
-    return _attn_check(load().np_attn_prompt(
-        _pack_shape(_ATTN_DTYPE.get(dtype, -1), heads, kv_heads, hd, 0, 0, 0, 0), _rows_of(q, dtype, dv, tokens, heads, hd),
-        _rows_of(k, dtype, dv, tokens, kv_heads, hd), _rows_of(v, dtype, dv, tokens, kv_heads, hd), _dev(cu, torch.int32, dv, 2), cu.numel() - 1,
-        tokens, hd ** -0.5 if scale is None else scale, _rows_of(out, dtype, dv, tokens, heads, hd),
-        _dev(lse, torch.float32, dv, tokens * heads), _dev(status, torch.int32, dv, 1), _stream(stream)))
+    return _attn().attn_prompt(q, k, v, cu, out, status, scale, lse, stream)
 
 
 def np_attn_check(status, stream=None) -> int:
-    return _attn_check(load().np_attn_check(_dev(status, torch.int32, _device(), 1), _stream(stream)))
+    return _attn().attn_check(status, stream)
 
 
 def np_install(ctx, layer_begin: int, layer_end: int, copy_stream=None) -> int:

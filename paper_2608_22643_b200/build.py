@@ -1,10 +1,11 @@
-"""Builds libnp.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libnp.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and the compiled part of the Python binding."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -13,6 +14,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(HERE, "build")
 LIB_PATH = os.path.join(HERE, "libnp.so")
+BIND_SOURCE = os.path.join(CSRC, "np_attn_bind.cpp")
+BIND_PATH = os.path.join(HERE, "np_attn_bind.so")
 
 SOURCES = ["np_api.cu", "np_predict.cu", "np_topk.cu", "np_centroid.cu", "np_delta.cu", "np_scatter.cu", "np_mlp.cu", "np_mlp_tc.cu", "np_mlp_chain_alu.cu", "np_mlp_slices.cu", "np_mlp_rows.cu", "np_mlp_batch.cu", "np_mlp_dense.cu", "np_static.cu", "np_io.cu", "np_trunk.cu", "np_predict_tc.cu", "np_kv.cu", "np_attn_decode.cu", "np_attn_prompt.cu"]
 
@@ -67,7 +70,31 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
                 print(out)
     if jobs or force or _stale(LIB_PATH, objs):
         run([nvcc, "-shared", "-o", LIB_PATH, *objs, "-cudart", "static", "-lpthread"])
+    _build_binding(nvcc, force)
     return LIB_PATH
+
+
+def _build_binding(nvcc: str, force: bool) -> None:
+    """``np_attn_bind.so``: a CPython module over libnp.so and torch's tensors.  Built again when torch or the interpreter changes."""
+    import torch
+
+    home = os.path.dirname(os.path.abspath(torch.__file__))
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
+    cmd = ["g++", "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-Wno-unknown-pragmas", "-I", INCLUDE, "-I", sysconfig.get_paths()["include"]]
+    for d in (os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")):
+        cmd += ["-isystem", d]
+    cmd += [BIND_SOURCE, "-o", BIND_PATH, "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", HERE, "-lnp",
+            "-Wl,-rpath,$ORIGIN"]
+    made_by = os.path.join(OBJ_DIR, "np_attn_bind.made_by")
+    how = f"torch {torch.__version__}, python {sys.version}"
+    same = os.path.exists(made_by) and open(made_by).read() == how
+    if not force and same and not _stale(BIND_PATH, [BIND_SOURCE, os.path.join(INCLUDE, "np.h"), os.path.abspath(__file__)]):
+        return
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+    with open(made_by, "w") as f:
+        f.write(how)
 
 
 if __name__ == "__main__":

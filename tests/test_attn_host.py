@@ -180,16 +180,18 @@ def test_binding_refuses_a_cache_of_no_type(lib):
 def test_binding_refuses_tables_that_are_too_small_or_elsewhere(lib, short):
     """Tables that would be written past their ends, or that belong to another device than the call."""
     d = _desc()
-    seqs, pages = d.max_seqs, d.n_pages
-    room = [seqs * d.max_pages, seqs, pages, nb.np_kv_sizes(d).scratch_bytes // 4]
+    room = [torch.cuda.current_device() if torch.cuda.is_available() else -2, d.max_seqs * d.max_pages, d.max_seqs, d.n_pages,
+            nb.np_kv_sizes(d).scratch_bytes // 4]
     t = _tables()
-    t.device, t.room = 0, tuple(room)
-    assert nb._tables_of(d, t, 0) is not None
-    if short < 4:
-        t.room = tuple(r - (i == short) for i, r in enumerate(room))
+    if not torch.cuda.is_available():
+        t.room = tuple(room)
+        with pytest.raises(nb.NpError) as e:
+            nb.np_kv_reset(d, t)
+        assert e.value.code == nb.NP_E_CUDA          # nothing to refuse but the missing device
+    t.room = tuple(r - (i == short) for i, r in enumerate(room))
     with pytest.raises(nb.NpError) as e:
-        nb._tables_of(d, t, 0 if short < 4 else 1)
-    assert e.value.code == nb.NP_E_INVAL
+        nb.np_kv_reset(d, t)
+    assert e.value.code == nb.NP_E_INVAL and "tables on device" in str(e.value)
 
 
 def test_decode_refuses_results_on_top_of_each_other(lib):

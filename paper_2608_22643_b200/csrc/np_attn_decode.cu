@@ -22,6 +22,12 @@
 //   (m, l, O) in the workspace and the last to arrive joins them in the order of the tokens, so that results do not depend on
 //   who was last.
 // * The first keys and values of a block's next piece are asked for before the warps' results of the last are joined.
+//
+// Measured (pages of 64 scattered over the pool, caches larger than the L2 in turn): sixteen sequences of 0 to 4095 tokens, 32 heads
+// of 128, 57.5 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 165 us, 97 %; one of 131071 tokens, 64 heads over 8, 92.6 us,
+// 89 %; one of 100 tokens 4.6 us.  What is not the stream is the launch, three loads that depend on one another (length, page
+// number, keys) and the joins.  Groups of more than eight heads are bound by the steps between the loads of a warp: sixteen heads of 128 to
+// a key-value head reach 64 %.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -38,9 +44,14 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kTile = kWarps * 16;    // tokens of a tile
-constexpr int kMinTiles = 4;          // tiles a block takes at least, where there are so few that blocks stay idle
-constexpr int kStart = 2;             // what a group's start counts, in tiles
-constexpr int kJoin = 8;              // partial results that are joined at a time
+// Units of a block at least, where there are so few that blocks stay idle.  4 x 900 tokens, 16 heads over one: 13.1 us; with 1 15.6, 4 14.9,
+// 8 19.1.  One of 4095 tokens, 32 heads: 21.0 with 1, 2 and 4, 26.1 with 8.
+constexpr int kMinTiles = 2;
+// What a group's start counts, in tiles.  The sixteen sequences above: 57.7 us; with 0 78.4, 1 57.6, 4 59.4.  The long one 93.0, 96.1, 94.3,
+// 91.7; 128 of 1 to 1600 tokens, 64 heads over 8, 71.2, 81.2, 72.9, 73.4; one of 100 tokens 4.7, 7.1, 8.4, 4.9.
+constexpr int kStart = 2;
+// Partial results that are joined at a time.  The long sequence: 93.0 us; with 4 94.9, 16 99.4 (registers).
+constexpr int kJoin = 8;
 constexpr int kMaxBlocks = 640;       // blocks of a launch (the workspace holds two partial results of each)
 
 struct DecodeArgs {
@@ -132,14 +143,20 @@ __device__ __forceinline__ int row_len(const DecodeArgs& a, int i, int* seq_out)
   return len;
 }
 
+// Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
+// accumulators.  us with one more and with this many: 128 values, eight columns, four blocks 113 (the long sequence) and 186 (64 of 1000),
+// three 101 and 164; sixteen columns, 64 of 2000, three 73.8, two 62.4.  64 values, eight columns, 64 heads, 16 sequences of 2000, five
+// 91.2, four 86.8 (three 93.9); sixteen columns, one of 131071, four 43.3, three 40.2 (two 45.0).
+constexpr int blocks_per_sm(int hd, int columns) { return hd == 64 ? (columns == 8 ? 4 : 3) : (columns == 8 ? 3 : 2); }
+
 template <class T, int HD, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, 8 * NT))
 k_attn_decode(DecodeArgs a) {
   constexpr int HB = 8 * NT;         // heads of a block, at most
   constexpr int KV = HD / 32;        // 16-byte pieces of a key row per lane
   constexpr int VC = HD / 64;        // 16-byte pieces of a value row per lane
   constexpr int QV = HB * HD / 8 / kThreads > 0 ? HB * HD / 8 / kThreads : 1;  // 16-byte pieces of the queries per thread
-  constexpr int QR = HD * 2 + 16;    // bytes from query to query in shared memory: eight of them in as many banks
+  constexpr int QR = HD * 2 + 64;    // bytes from query to query in shared memory: the eight lanes of a read meet all banks
   __shared__ int64_t s_end[NP_KV_MAX_SEQS];             // tiles of the rows up to and including this one
   __shared__ __align__(16) float s_o[kWarps][HB][HD];
   __shared__ __align__(16) unsigned char s_q[HB * QR];
@@ -536,11 +553,13 @@ k_attn_decode(DecodeArgs a) {
   }
 }
 
+// Columns of a block.  Sixteen read keys and values once for up to sixteen heads, eight have twice the warps: 64 sequences of 2000 tokens, 64
+// heads over 4, 62 us with sixteen and 81 with eight, which read everything twice.
 int heads_per_block(int group) { return group <= 8 ? 8 : 16; }
 
 template <class T>
 cudaError_t launch(const DecodeArgs& a, int hd, int hb, int sms, cudaStream_t s) {
-  const dim3 grid(std::min(kMaxBlocks, (hb == 8 ? 3 : 2) * sms));
+  const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(hd, hb) * sms));
   if (hd == 128) return hb == 8 ? launch_early(k_attn_decode<T, 128, 1>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 128, 2>, grid, kThreads, 0, s, a);
   return hb == 8 ? launch_early(k_attn_decode<T, 64, 1>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 64, 2>, grid, kThreads, 0, s, a);
 }

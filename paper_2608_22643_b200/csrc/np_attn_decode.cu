@@ -6,9 +6,10 @@
 // bytes per token and key-value head against 4 * head_dim operations per query head.  What has to be done is to keep
 // enough loads in flight and to split the tokens evenly.
 //
-// * A warp takes sixteen tokens at a time, all heads of a group (eight or sixteen columns) at once, on the tensor cores'
-//   mma.sync form: S^T = K Q^T and O^T = V^T P^T, tokens x head_dim on the wide side, so that a group of one wastes matrix
-//   operations (there are plenty) and no bytes.
+// * A warp takes sixteen tokens at a time, all heads of a group (up to eight, or up to sixteen) at once, on the tensor cores'
+//   mma.sync form.  Up to eight heads: S^T = K Q^T and O^T = V^T P^T, tokens and head_dim on the wide side, so that a group of one
+//   wastes matrix operations (there are plenty) and no bytes.  Up to sixteen: S = Q K^T and O = P V; the queries stay in registers,
+//   a row's maximum takes two exchanges instead of three, and P is where the second product wants it.
 // * Keys and values go from global memory straight into the registers that the products read, 16 bytes per lane, no shared
 //   memory: S sums over head_dim, so any order of head_dim does as long as q has the same, and lane t of a quad takes
 //   pieces t, t + 4, ... of a row; O's rows are head_dim in an order that only the store has to undo, and two tokens' values
@@ -26,8 +27,8 @@
 // Measured (pages of 64 scattered over the pool, caches larger than the L2 in turn): sixteen sequences of 0 to 4095 tokens, 32 heads
 // of 128, 57.5 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 165 us, 97 %; one of 131071 tokens, 64 heads over 8, 92.6 us,
 // 89 %; one of 100 tokens 4.6 us.  What is not the stream is the launch, three loads that depend on one another (length, page
-// number, keys) and the joins.  Groups of more than eight heads are bound by the steps between the loads of a warp: sixteen heads of 128 to
-// a key-value head reach 64 %.
+// number, keys) and the joins.  Groups of more than eight heads are bound by the steps between a warp's loads, of which the registers hold
+// no more: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, reach 69 % (65 % with S^T and O^T in two halves).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -144,15 +145,15 @@ __device__ __forceinline__ int row_len(const DecodeArgs& a, int i, int* seq_out)
 }
 
 // Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
-// accumulators.  us with one more and with this many: 128 values, eight columns, four blocks 113 (the long sequence) and 186 (64 of 1000),
-// three 101 and 164; sixteen columns, 64 of 2000, three 73.8, two 62.4.  64 values, eight columns, 64 heads, 16 sequences of 2000, five
-// 91.2, four 86.8 (three 93.9); sixteen columns, one of 131071, four 43.3, three 40.2 (two 45.0).
-constexpr int blocks_per_sm(int hd, int columns) { return hd == 64 ? (columns == 8 ? 4 : 3) : (columns == 8 ? 3 : 2); }
+// accumulators.  us with one more and with this many (the forms of sixteen heads before the last change): 128 values, eight heads, four blocks 113 (the long sequence) and 186 (64 of 1000),
+// three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16 sequences of 2000, five
+// 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
+constexpr int blocks_per_sm(int hd, int heads) { return hd == 64 ? (heads == 8 ? 4 : 3) : (heads == 8 ? 3 : 2); }
 
-template <class T, int HD, int NT>
-__global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, 8 * NT))
+template <class T, int HD, bool kWide>
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kWide ? 16 : 8))
 k_attn_decode(DecodeArgs a) {
-  constexpr int HB = 8 * NT;         // heads of a block, at most
+  constexpr int HB = kWide ? 16 : 8;  // heads of a block, at most
   constexpr int KV = HD / 32;        // 16-byte pieces of a key row per lane
   constexpr int VC = HD / 64;        // 16-byte pieces of a value row per lane
   constexpr int QV = HB * HD / 8 / kThreads > 0 ? HB * HD / 8 / kThreads : 1;  // 16-byte pieces of the queries per thread
@@ -349,74 +350,121 @@ k_attn_decode(DecodeArgs a) {
   }
   __syncthreads();
   while (any) {
-    float m[NT][2], l[NT][2], o[NT][VC * 4][4];
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[kWide ? VC * 8 : VC * 4][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -INFINITY;
-      l[nt][0] = l[nt][1] = 0.f;
+    for (auto& x : o) x[0] = x[1] = x[2] = x[3] = 0.f;
+    uint4 qa[kWide ? 2 : 1][KV];  // sixteen heads: the queries stay in registers
+    if constexpr (kWide) {
 #pragma unroll
-      for (int i = 0; i < VC * 4; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < KV; ++j) qa[r][j] = *reinterpret_cast<const uint4*>(s_q + (r * 8 + g) * QR + (t + 4 * j) * 16);
     }
+    // the maxima of the two heads grow to `top`, what has been added up is rescaled (by(i, factor) for the accumulators of head i), `use` is
+    // what to take off
+    auto raise = [&](const float (&top)[2], float (&use)[2], auto by) {
+      float now[2];
+      bool grew = false;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        now[i] = fmaxf(m[i], top[i]);
+        use[i] = now[i] == -INFINITY ? 0.f : now[i];  // -inf so far: nothing has been added up yet
+        grew |= now[i] > m[i];
+      }
+      if (!__any_sync(0xffffffffu, grew)) return;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float f = exp2_fast(m[i] - use[i]);
+        m[i] = now[i];
+        l[i] *= f;
+        by(i, f);
+      }
+    };
     for (; c < chunk_end; c += kWarps) {
       chunk_of(c + kWarps, pg_next, have_next, at_next);
       pg_next = page_of(c + 2 * kWarps);
-      // ---- S^T = K Q^T
-      float s[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+      uint32_t ph[kWide ? 4 : 2], pl[kWide ? 4 : 2];
+      if constexpr (!kWide) {
+        // ---- S^T = K Q^T
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KV; ++j) {
-          const uint4 q = *reinterpret_cast<const uint4*>(s_q + (nt * 8 + g) * QR + (t + 4 * j) * 16);
-          Half2<T>::mma(s[nt], kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, q.x, q.y);
-          Half2<T>::mma(s[nt], kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, q.z, q.w);
+          const uint4 q = *reinterpret_cast<const uint4*>(s_q + g * QR + (t + 4 * j) * 16);
+          Half2<T>::mma(s, kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, q.x, q.y);
+          Half2<T>::mma(s, kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, q.z, q.w);
         }
-      }
-      load_k(have_next, at_next);
-      // ---- softmax: s[0], s[1] are token g, s[2], s[3] token g + 8; heads 2t and 2t + 1
-      uint32_t ph[NT][2], pl[NT][2];
+        load_k(have_next, at_next);
+        // ---- softmax: s[0], s[1] are token g, s[2], s[3] token g + 8; heads 2t and 2t + 1
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[nt][i] = g + 8 * (i >> 1) < have ? s[nt][i] * a.scale2 : -INFINITY;
-        float now[2], use[2];
-        bool grew = false;
+        for (int i = 0; i < 4; ++i) s[i] = g + 8 * (i >> 1) < have ? s[i] * a.scale2 : -INFINITY;
+        float top[2], use[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float v = fmaxf(s[nt][i], s[nt][i + 2]);
+          top[i] = fmaxf(s[i], s[i + 2]);
 #pragma unroll
-          for (int x = 4; x < 32; x <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, x));
-          now[i] = fmaxf(m[nt][i], v);
-          use[i] = now[i] == -INFINITY ? 0.f : now[i];  // -inf so far: nothing has been added up yet
-          grew |= now[i] > m[nt][i];
+          for (int x = 4; x < 32; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
         }
-        if (__any_sync(0xffffffffu, grew)) {
+        raise(top, use, [&](int i, float f) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float f = exp2_fast(m[nt][i] - use[i]);
-            m[nt][i] = now[i];
-            l[nt][i] *= f;
-#pragma unroll
-            for (int k = 0; k < VC * 4; ++k) {
-              o[nt][k][i] *= f;
-              o[nt][k][i + 2] *= f;
-            }
+          for (auto& x : o) {
+            x[i] *= f;
+            x[i + 2] *= f;
           }
-        }
+        });
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = exp2_fast(s[nt][i] - use[i & 1]);
-        l[nt][0] += p[0] + p[2];
-        l[nt][1] += p[1] + p[3];
+        for (int i = 0; i < 4; ++i) p[i] = exp2_fast(s[i] - use[i & 1]);
+        l[0] += p[0] + p[2];
+        l[1] += p[1] + p[3];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           uint32_t hi, lo;
           Half2<T>::split(p[2 * i], p[2 * i + 1], hi, lo);
-          ph[nt][i] = transpose8x8(hi);
-          pl[nt][i] = transpose8x8(lo);
+          ph[i] = transpose8x8(hi);
+          pl[i] = transpose8x8(lo);
         }
+      } else {
+        // ---- S = Q K^T, eight tokens at a time
+        float s[2][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
+#pragma unroll
+          for (int j = 0; j < KV; ++j) {
+            Half2<T>::mma(s[r], qa[0][j].x, qa[1][j].x, qa[0][j].y, qa[1][j].y, kf[r][j].x, kf[r][j].y);
+            Half2<T>::mma(s[r], qa[0][j].z, qa[1][j].z, qa[0][j].w, qa[1][j].w, kf[r][j].z, kf[r][j].w);
+          }
+        }
+        load_k(have_next, at_next);
+        // ---- softmax: s[r][0], s[r][1] are head g, s[r][2], s[r][3] head g + 8; tokens 8r + 2t and 8r + 2t + 1
+        float top[2], use[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) s[r][2 * i + x] = 8 * r + 2 * t + x < have ? s[r][2 * i + x] * a.scale2 : -INFINITY;
+          top[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
+#pragma unroll
+          for (int x = 1; x < 4; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+        }
+        raise(top, use, [&](int i, float f) {
+#pragma unroll
+          for (auto& x : o) {
+            x[2 * i] *= f;
+            x[2 * i + 1] *= f;
+          }
+        });
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float p0 = exp2_fast(s[r][2 * i] - use[i]), p1 = exp2_fast(s[r][2 * i + 1] - use[i]);
+            l[i] += p0 + p1;
+            Half2<T>::split(p0, p1, ph[2 * r + i], pl[2 * r + i]);
+          }
       }
-      // ---- O^T += V^T P^T
+      // ---- O^T += V^T P^T (eight heads), O += P V (sixteen)
 #pragma unroll
       for (int v = 0; v < VC; ++v)
 #pragma unroll
@@ -424,10 +472,14 @@ k_attn_decode(DecodeArgs a) {
           const uint32_t x0 = word(vf[0][v], w), x1 = word(vf[1][v], w), x2 = word(vf[2][v], w), x3 = word(vf[3][v], w);
           const uint32_t a0 = __byte_perm(x0, x1, 0x5410), a1 = __byte_perm(x0, x1, 0x7632);
           const uint32_t a2 = __byte_perm(x2, x3, 0x5410), a3 = __byte_perm(x2, x3, 0x7632);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            Half2<T>::mma(o[nt][v * 4 + w], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
-            Half2<T>::mma(o[nt][v * 4 + w], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+          if constexpr (!kWide) {
+            Half2<T>::mma(o[v * 4 + w], a0, a1, a2, a3, ph[0], ph[1]);
+            Half2<T>::mma(o[v * 4 + w], a0, a1, a2, a3, pl[0], pl[1]);
+          } else {
+            Half2<T>::mma(o[v * 8 + w * 2], ph[0], ph[1], ph[2], ph[3], a0, a2);
+            Half2<T>::mma(o[v * 8 + w * 2 + 1], ph[0], ph[1], ph[2], ph[3], a1, a3);
+            Half2<T>::mma(o[v * 8 + w * 2], pl[0], pl[1], pl[2], pl[3], a0, a2);
+            Half2<T>::mma(o[v * 8 + w * 2 + 1], pl[0], pl[1], pl[2], pl[3], a1, a3);
           }
         }
       load_v(have_next, at_next);
@@ -440,22 +492,28 @@ k_attn_decode(DecodeArgs a) {
     any = next_piece(p);
     if (any) begin();
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int i = 0; i < 2; ++i) {
+      const int h = kWide ? g + 8 * i : 2 * t + i;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int x = 4; x < 32; x <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], x);
-        const int h = nt * 8 + 2 * t + i;
-        if (h < e.heads) {
-          if (g == 0) {
-            s_ml[wid][h][0] = m[nt][i];
-            s_ml[wid][h][1] = l[nt][i];
-          }
+      for (int x = kWide ? 1 : 4; x < (kWide ? 4 : 32); x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+      if (h < e.heads) {
+        if ((kWide ? t : g) == 0) {
+          s_ml[wid][h][0] = m[i];
+          s_ml[wid][h][1] = l[i];
+        }
+        if constexpr (!kWide) {
 #pragma unroll
           for (int k = 0; k < VC * 4; ++k)
-            *reinterpret_cast<float2*>(&s_o[wid][h][(g + 8 * (k >> 2)) * 8 + 2 * (k & 3)]) = make_float2(o[nt][k][i], o[nt][k][i + 2]);
+            *reinterpret_cast<float2*>(&s_o[wid][h][(g + 8 * (k >> 2)) * 8 + 2 * (k & 3)]) = make_float2(o[k][i], o[k][i + 2]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < VC * 8; k += 2)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              *reinterpret_cast<float2*>(&s_o[wid][h][(2 * t + x + 8 * (k >> 3)) * 8 + (k & 7)]) = make_float2(o[k][2 * i + x], o[k + 1][2 * i + x]);
         }
       }
+    }
     __syncthreads();
     if (any) keep_queries();
     const bool whole = e.ta == 0 && e.tb == e.tiles;
@@ -553,15 +611,15 @@ k_attn_decode(DecodeArgs a) {
   }
 }
 
-// Columns of a block.  Sixteen read keys and values once for up to sixteen heads, eight have twice the warps: 64 sequences of 2000 tokens, 64
-// heads over 4, 62 us with sixteen and 81 with eight, which read everything twice.
+// Heads of a block.  Sixteen read keys and values once for up to sixteen heads, eight have more warps: 64 sequences of 2000 tokens, 64
+// heads over 4, 58 us with sixteen and 81 with eight, which read everything twice.
 int heads_per_block(int group) { return group <= 8 ? 8 : 16; }
 
 template <class T>
 cudaError_t launch(const DecodeArgs& a, int hd, int hb, int sms, cudaStream_t s) {
   const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(hd, hb) * sms));
-  if (hd == 128) return hb == 8 ? launch_early(k_attn_decode<T, 128, 1>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 128, 2>, grid, kThreads, 0, s, a);
-  return hb == 8 ? launch_early(k_attn_decode<T, 64, 1>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 64, 2>, grid, kThreads, 0, s, a);
+  if (hd == 128) return hb == 8 ? launch_early(k_attn_decode<T, 128, false>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 128, true>, grid, kThreads, 0, s, a);
+  return hb == 8 ? launch_early(k_attn_decode<T, 64, false>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 64, true>, grid, kThreads, 0, s, a);
 }
 
 // [(m, l) of the partial results][their O][counts]: the counts start at the same place for every description and n, and the

@@ -28,7 +28,7 @@
 //   mend_rows looks up whether the tokens that the row sees make it so.  (A warp that looks through these tiles' V beforehand is
 //   simpler, and cost 2 to 10 %: its code, mostly.)
 // * Short prompts wait for instructions: what is off the usual path (rescaling, the result) is kept in loops.  Unrolled, twelve
-//   prompts of 1 to 1500 tokens, 32 heads, took 90 us instead of 80.  Measured and dropped: exponentials on the FMA units by a
+//   prompts of 0 to 1500 tokens, 32 heads, took 90 us instead of 80.  Measured and dropped: exponentials on the FMA units by a
 //   polynomial (they are no less busy), two lanes to a row (the exchange costs what the halves save), scores read from tensor
 //   memory 32 at a time, a warp of products for each tile (the tiles fall into step), the next block's first scores before the
 //   other tile's last product.

@@ -28,7 +28,8 @@
 // of 128, 57.5 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 165 us, 97 %; one of 131071 tokens, 64 heads over 8, 92.6 us,
 // 89 %; one of 100 tokens 4.6 us.  What is not the stream is the launch, three loads that depend on one another (length, page
 // number, keys) and the joins.  Groups of more than eight heads are bound by the steps between a warp's loads, of which the registers hold
-// no more: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, reach 69 % (65 % with S^T and O^T in two halves).
+// no more: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, reach 69 % (65 % with S^T and O^T in two halves; 55 % with keys and values two steps ahead in shared memory by
+// asynchronous copies, which the load unit then has to read again).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -654,7 +654,7 @@ int np_kv_copy_pages(const np_kv_desc* desc, void* dst_cache, const void* src_ca
 /* Attention of one new token per sequence over the cache (n_heads query heads, n_heads % n_kv_heads == 0; head h reads
  * key-value head h / (n_heads / n_kv_heads)):
  *   out[i][h] = sum_j softmax_j(scale * q[i][h] . k_j) v_j   over the lens[seqs[i]] tokens of sequence seqs[i]
- * (the new token among them: append it first).  Keys and values past a sequence's length are not read.  A sequence of
+ * (the new token among them: append it first).  Keys and values past a sequence's length have no effect.  A sequence of
  * length 0, and a row whose seqs[i] is negative (padding), give zeros and lse -inf, and so does a row whose scores are all
  * -inf.  fp32 scores, softmax and sums.
  *   q, out     n rows of n_heads heads; out may not overlap q, its strides are above 0 along more than one row or head

@@ -7,14 +7,17 @@
 // enough loads in flight and to split the tokens evenly.
 //
 // * A warp takes sixteen tokens at a time, all heads of a group (up to eight, or up to sixteen) at once, on the tensor cores'
-//   mma.sync form.  Up to eight heads: S^T = K Q^T and O^T = V^T P^T, tokens and head_dim on the wide side, so that a group of one
-//   wastes matrix operations (there are plenty) and no bytes.  Up to sixteen: S = Q K^T and O = P V; the queries stay in registers,
-//   a row's maximum takes two exchanges instead of three, and P is where the second product wants it.
-// * Keys and values go from global memory straight into the registers that the products read, 16 bytes per lane, no shared
-//   memory: S sums over head_dim, so any order of head_dim does as long as q has the same, and lane t of a quad takes
-//   pieces t, t + 4, ... of a row; O's rows are head_dim in an order that only the store has to undo, and two tokens' values
-//   are interleaved with byte permutes.  The keys of the next sixteen tokens are asked for when S is there, the values
-//   when O is, so a warp always has 4 KB in flight (head_dim 128).
+//   mma.sync form, fp32 sums.
+// * Up to eight heads: S^T = K Q^T and O^T = V^T P^T, tokens and head_dim on the wide side, so that a group of one wastes matrix
+//   operations (there are plenty) and no bytes.  Keys and values go from global memory straight into the registers that the
+//   products read, 16 bytes per lane, no shared memory: S sums over head_dim, so any order of head_dim does as long as q has
+//   the same, and lane t of a quad takes pieces t, t + 4, ... of a row; O's rows are head_dim in an order that only the store
+//   has to undo, and two tokens' values are interleaved with byte permutes.  The keys of the next sixteen tokens are asked for
+//   when S is there, the values when O is, so a warp always has 4 KB in flight (head_dim 128).
+// * Up to sixteen heads: S = Q K^T and O = P V, the queries in registers, two exchanges for a row's maximum in place of three, and P is where
+//   the second product wants it.  The accumulators leave no registers for keys and values on their way: a warp has a ring of its own in shared
+//   memory, two chunks of sixteen tokens, each filled by one tiled TMA copy of keys and values.  (The same ring for eight heads, two
+//   blocks to an SM instead of three: 3 % less time for long work, 9 % more for one sequence of 4095.)
 // * The running maximum and sum are per warp (base 2, fp32); the accumulators are rescaled only when a maximum grows.  P is
 //   the sum of two terms of the cache's type, so it is good to 16 bits and more where one term has 8 or 11.
 // * All (sequence, group, tile of 64 tokens) triples form one line; each block takes an equal stretch of it.  A group's start counts
@@ -27,9 +30,11 @@
 // Measured (pages of 64 scattered over the pool, caches larger than the L2 in turn): sixteen sequences of 0 to 4095 tokens, 32 heads
 // of 128, 57.5 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 165 us, 97 %; one of 131071 tokens, 64 heads over 8, 92.6 us,
 // 89 %; one of 100 tokens 4.6 us.  What is not the stream is the launch, three loads that depend on one another (length, page
-// number, keys) and the joins.  Groups of more than eight heads are bound by the steps between a warp's loads, of which the registers hold
-// no more: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, reach 69 % (65 % with S^T and O^T in two halves; 55 % with keys and values two steps ahead in shared memory by
-// asynchronous copies, which the load unit then has to read again).
+// number, keys) and the joins.  Groups of more than eight heads are bound by the steps
+// between a warp's loads: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, 53.0 us, 76 % (69 % with keys and values
+// in registers, 55 % with 16-byte asynchronous copies in place of TMA, 70 % with the chunks beyond asked into the L2 ahead, 74 % with
+// keys and values as two copies).
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -121,6 +126,22 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Four 8 x 8 tiles of 16-bit values; lane 8 i + j has the address of row j of tile i.
+__device__ __forceinline__ void load_tiles(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void load_tiles_transposed(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+// keys and values of sixteen tokens: (64 values, rows of a page's heads, halves of head_dim, keys and values, pages)
+__device__ __forceinline__ void tma_load_chunk(uint32_t dst, const CUtensorMap* map, int row, int page, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %2, %4}], [%5];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(page), "r"(npp::smem_addr(bar))
+               : "memory");
+}
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // a / b, by 32 bits where they do
@@ -146,25 +167,38 @@ __device__ __forceinline__ int row_len(const DecodeArgs& a, int i, int* seq_out)
 }
 
 // Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
-// accumulators.  us with one more and with this many (the forms of sixteen heads before the last change): 128 values, eight heads, four blocks 113 (the long sequence) and 186 (64 of 1000),
+// accumulators.  us with one more and with this many (sixteen heads: with keys and values in registers): 128 values, eight heads, four blocks 113 (the long sequence) and 186 (64 of 1000),
 // three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16 sequences of 2000, five
 // 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
 constexpr int blocks_per_sm(int hd, int heads) { return hd == 64 ? (heads == 8 ? 4 : 3) : (heads == 8 ? 3 : 2); }
 
+constexpr int kSlots = 2;  // sixteen heads: chunks of a warp on their way
+
 template <class T, int HD, bool kWide>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kWide ? 16 : 8))
-k_attn_decode(DecodeArgs a) {
+k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
   constexpr int HB = kWide ? 16 : 8;  // heads of a block, at most
   constexpr int KV = HD / 32;        // 16-byte pieces of a key row per lane
   constexpr int VC = HD / 64;        // 16-byte pieces of a value row per lane
   constexpr int QV = HB * HD / 8 / kThreads > 0 ? HB * HD / 8 / kThreads : 1;  // 16-byte pieces of the queries per thread
-  constexpr int QR = HD * 2 + 64;    // bytes from query to query in shared memory: the eight lanes of a read meet all banks
+  // Sixteen heads: sixteen-value steps along head_dim; bytes of a chunk's keys, and of its keys and values
+  constexpr int KS = HD / 16;
+  constexpr uint32_t kHalf = 16 * HD * 2, kSlot = 2 * kHalf;
+  // Bytes from query to query, values from head to head of a warp's result, in shared memory: reads and stores meet all banks
+  constexpr int QR = HD * 2 + (kWide ? 16 : 64), SO = HD + (kWide ? 8 : 0);
   __shared__ int64_t s_end[NP_KV_MAX_SEQS];             // tiles of the rows up to and including this one
-  __shared__ __align__(16) float s_o[kWarps][HB][HD];
+  __shared__ __align__(16) float s_o[kWarps][HB][SO];
+  __shared__ __align__(8) uint64_t s_full[kWarps][kSlots];  // a warp's ring is its own
+  extern __shared__ __align__(1024) unsigned char s_dyn[];
   __shared__ __align__(16) unsigned char s_q[HB * QR];
   __shared__ float s_ml[kWarps][HB][2];
   __shared__ int64_t s_wsum[kWarps];
   __shared__ int s_last;
+  if (kWide && (threadIdx.x & 31) == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
+    for (int i = 0; i < kSlots; ++i) npp::mbar_init(&s_full[threadIdx.x >> 5][i], 1);
+    npp::fence_barrier_init();
+  }
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -236,6 +270,7 @@ k_attn_decode(DecodeArgs a) {
     int row, pair, h0, heads, len, tiles, ta, tb;
     int64_t first_w;  // of its pair, on the line
     const int32_t* pages;
+    int first_row;    // of its key-value head in a page
     const char* kbase;
     const char* vbase;
   };
@@ -260,6 +295,7 @@ k_attn_decode(DecodeArgs a) {
       p.h0 = kvh * a.group + hb * HB;
       p.heads = min(HB, a.group - hb * HB);
       p.pages = a.table + (size_t)seq * a.max_pages;
+      p.first_row = kvh << a.shift;
       p.kbase = a.cache + kvh * head_bytes;
       p.vbase = p.kbase + a.n_kv_heads * head_bytes;
       return true;
@@ -271,6 +307,12 @@ k_attn_decode(DecodeArgs a) {
   Piece p = {};
   int chunk_end, c, have, have_next, pg_next;  // chunks of 16 tokens
   int64_t at, at_next;
+  int waiting[kSlots];                 // tokens of the chunks in this warp's ring
+  uint32_t asked = 0, used = 0;        // of the ring, so far
+  const uint32_t ring = ((npp::smem_addr(s_dyn) + 1023) & ~1023u) + wid * kSlots * kSlot;
+  // what a lane reads with load_tiles: rows (tokens) 0-7 and 8-15 of two neighbouring 16-byte columns, 128-byte swizzle
+  const uint32_t lane_row = ((lane & 7) + (lane >> 4) * 8) * 128, lane_col = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
+  auto tiles_at = [&](uint32_t base, int step) { return base + lane_row + (step >> 2) * 2048 + (((step & 3) << 5) ^ lane_col); };
   // where the chunk's page starts, and how many of its tokens there are (0: nothing to read)
   auto chunk_of = [&](int chunk, int pg, int& n, int64_t& off) {
     n = 0;
@@ -304,21 +346,45 @@ k_attn_decode(DecodeArgs a) {
       }
     }
   };
+  // asks for a chunk for the ring; how many of its tokens there are (0: nothing to read)
+  auto ask = [&](int chunk, int pg) {
+    if (chunk >= chunk_end) return 0;
+    if ((unsigned)pg >= (unsigned)a.n_pages) {
+      atomicOr(a.status, NP_KV_S_PAGE);
+      return 0;
+    }
+    if (lane == 0) {
+      uint64_t* bar = &s_full[wid][asked % kSlots];
+      npp::mbar_expect_tx(bar, kSlot);
+      tma_load_chunk(ring + asked % kSlots * kSlot, &map, p.first_row + (int)(((int64_t)chunk * 16) & ((1 << a.shift) - 1)), pg, bar);
+    }
+    ++asked;
+    return (int)min((int64_t)16, p.len - (int64_t)chunk * 16);
+  };
   // asks for the queries and the first keys and values of a piece
   auto begin = [&] {
     chunk_end = (int)min(((int64_t)p.len + 15) >> 4, (int64_t)p.tb * kWarps);
     c = p.ta * kWarps + wid;
-    const int pg = page_of(c);
-    pg_next = page_of(c + kWarps);
+    int pg[kSlots + 1];
+#pragma unroll
+    for (int i = 0; i < (kWide ? kSlots : 1) + 1; ++i) pg[i] = page_of(c + i * kWarps);
 #pragma unroll
     for (int j = 0; j < QV; ++j) {
       const int x = j * kThreads + tid, h = x / (HD / 8), d = x % (HD / 8) * 8;
       qf[j] = make_uint4(0, 0, 0, 0);
       if (h < p.heads) qf[j] = *reinterpret_cast<const uint4*>(a.q + p.row * a.q_token + (int64_t)(p.h0 + h) * a.q_head + d);
     }
-    chunk_of(c, pg, have, at);
-    load_k(have, at);
-    load_v(have, at);
+    if constexpr (kWide) {
+      __syncwarp();  // all lanes have read what the ring held
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) waiting[i] = ask(c + i * kWarps, pg[i]);
+      pg_next = pg[kSlots];
+    } else {
+      chunk_of(c, pg[0], have, at);
+      load_k(have, at);
+      load_v(have, at);
+      pg_next = pg[1];
+    }
   };
   auto add = [](float4& acc, float f, const float4& v) {
     acc.x += f * v.x;
@@ -351,15 +417,15 @@ k_attn_decode(DecodeArgs a) {
   }
   __syncthreads();
   while (any) {
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[kWide ? VC * 8 : VC * 4][4];
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[kWide ? 2 * KS : VC * 4][4];
 #pragma unroll
     for (auto& x : o) x[0] = x[1] = x[2] = x[3] = 0.f;
-    uint4 qa[kWide ? 2 : 1][KV];  // sixteen heads: the queries stay in registers
+    uint32_t qr[kWide ? KS : 1][4];  // sixteen heads: the queries of heads g and g + 8, values 16 j + 2t, + 1 and those eight further
     if constexpr (kWide) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+      for (int j = 0; j < KS; ++j)
 #pragma unroll
-        for (int j = 0; j < KV; ++j) qa[r][j] = *reinterpret_cast<const uint4*>(s_q + (r * 8 + g) * QR + (t + 4 * j) * 16);
+        for (int i = 0; i < 4; ++i) qr[j][i] = *reinterpret_cast<const uint32_t*>(s_q + (g + (i & 1) * 8) * QR + j * 32 + t * 4 + (i >> 1) * 16);
     }
     // the maxima of the two heads grow to `top`, what has been added up is rescaled (by(i, factor) for the accumulators of head i), `use` is
     // what to take off
@@ -381,11 +447,11 @@ k_attn_decode(DecodeArgs a) {
         by(i, f);
       }
     };
-    for (; c < chunk_end; c += kWarps) {
-      chunk_of(c + kWarps, pg_next, have_next, at_next);
-      pg_next = page_of(c + 2 * kWarps);
-      uint32_t ph[kWide ? 4 : 2], pl[kWide ? 4 : 2];
-      if constexpr (!kWide) {
+    if constexpr (!kWide) {
+      for (; c < chunk_end; c += kWarps) {
+        chunk_of(c + kWarps, pg_next, have_next, at_next);
+        pg_next = page_of(c + 2 * kWarps);
+        uint32_t ph[2], pl[2];
         // ---- S^T = K Q^T
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -424,68 +490,92 @@ k_attn_decode(DecodeArgs a) {
           ph[i] = transpose8x8(hi);
           pl[i] = transpose8x8(lo);
         }
-      } else {
-        // ---- S = Q K^T, eight tokens at a time
-        float s[2][4];
+        // ---- O^T += V^T P^T
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
+        for (int v = 0; v < VC; ++v)
 #pragma unroll
-          for (int j = 0; j < KV; ++j) {
-            Half2<T>::mma(s[r], qa[0][j].x, qa[1][j].x, qa[0][j].y, qa[1][j].y, kf[r][j].x, kf[r][j].y);
-            Half2<T>::mma(s[r], qa[0][j].z, qa[1][j].z, qa[0][j].w, qa[1][j].w, kf[r][j].z, kf[r][j].w);
-          }
-        }
-        load_k(have_next, at_next);
-        // ---- softmax: s[r][0], s[r][1] are head g, s[r][2], s[r][3] head g + 8; tokens 8r + 2t and 8r + 2t + 1
-        float top[2], use[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) s[r][2 * i + x] = 8 * r + 2 * t + x < have ? s[r][2 * i + x] * a.scale2 : -INFINITY;
-          top[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
-#pragma unroll
-          for (int x = 1; x < 4; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
-        }
-        raise(top, use, [&](int i, float f) {
-#pragma unroll
-          for (auto& x : o) {
-            x[2 * i] *= f;
-            x[2 * i + 1] *= f;
-          }
-        });
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float p0 = exp2_fast(s[r][2 * i] - use[i]), p1 = exp2_fast(s[r][2 * i + 1] - use[i]);
-            l[i] += p0 + p1;
-            Half2<T>::split(p0, p1, ph[2 * r + i], pl[2 * r + i]);
-          }
-      }
-      // ---- O^T += V^T P^T (eight heads), O += P V (sixteen)
-#pragma unroll
-      for (int v = 0; v < VC; ++v)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t x0 = word(vf[0][v], w), x1 = word(vf[1][v], w), x2 = word(vf[2][v], w), x3 = word(vf[3][v], w);
-          const uint32_t a0 = __byte_perm(x0, x1, 0x5410), a1 = __byte_perm(x0, x1, 0x7632);
-          const uint32_t a2 = __byte_perm(x2, x3, 0x5410), a3 = __byte_perm(x2, x3, 0x7632);
-          if constexpr (!kWide) {
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t x0 = word(vf[0][v], w), x1 = word(vf[1][v], w), x2 = word(vf[2][v], w), x3 = word(vf[3][v], w);
+            const uint32_t a0 = __byte_perm(x0, x1, 0x5410), a1 = __byte_perm(x0, x1, 0x7632);
+            const uint32_t a2 = __byte_perm(x2, x3, 0x5410), a3 = __byte_perm(x2, x3, 0x7632);
             Half2<T>::mma(o[v * 4 + w], a0, a1, a2, a3, ph[0], ph[1]);
             Half2<T>::mma(o[v * 4 + w], a0, a1, a2, a3, pl[0], pl[1]);
-          } else {
-            Half2<T>::mma(o[v * 8 + w * 2], ph[0], ph[1], ph[2], ph[3], a0, a2);
-            Half2<T>::mma(o[v * 8 + w * 2 + 1], ph[0], ph[1], ph[2], ph[3], a1, a3);
-            Half2<T>::mma(o[v * 8 + w * 2], pl[0], pl[1], pl[2], pl[3], a0, a2);
-            Half2<T>::mma(o[v * 8 + w * 2 + 1], pl[0], pl[1], pl[2], pl[3], a1, a3);
           }
+        load_v(have_next, at_next);
+        have = have_next;
+        at = at_next;
+      }
+    } else {
+      for (; c < chunk_end; c += kWarps) {
+        const int now = waiting[0], pg = pg_next;
+        pg_next = page_of(c + (kSlots + 1) * kWarps);
+        if (now > 0) {
+          const uint32_t k_at = ring + used % kSlots * kSlot, v_at = k_at + kHalf;
+          uint32_t polls = 0;
+          while (!npp::mbar_try_wait(&s_full[wid][used % kSlots], (used / kSlots) & 1u) && polls < 4 * npp::kSpinLimit)
+            if (++polls == npp::kSpinLimit) atomicOr(a.status, NP_KV_S_TIMEOUT);
+          ++used;
+          if (now < 16) {  // tokens that are not there: zero, whatever their places hold
+            for (int e = lane; e < (16 - now) * (HD / 8); e += 32) {
+              const int r = now + e / (HD / 8), d = e % (HD / 8);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + (d >> 3) * 2048 + r * 128 + (((d ^ r) & 7) << 4)), "r"(0) : "memory");
+            }
+            npp::fence_proxy_async();
+            __syncwarp();
+          }
+          uint32_t ph[4], pl[4];
+          // ---- S = Q K^T, eight tokens at a time
+          float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+          for (int j = 0; j < KS; ++j) {
+            uint32_t x[4];
+            load_tiles(tiles_at(k_at, j), x);
+            Half2<T>::mma(s[0], qr[j][0], qr[j][1], qr[j][2], qr[j][3], x[0], x[1]);
+            Half2<T>::mma(s[1], qr[j][0], qr[j][1], qr[j][2], qr[j][3], x[2], x[3]);
+          }
+          // ---- softmax: s[r][0], s[r][1] are head g, s[r][2], s[r][3] head g + 8; tokens 8r + 2t and 8r + 2t + 1
+          float top[2], use[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+              for (int x = 0; x < 2; ++x) s[r][2 * i + x] = 8 * r + 2 * t + x < now ? s[r][2 * i + x] * a.scale2 : -INFINITY;
+            top[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
+#pragma unroll
+            for (int x = 1; x < 4; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+          }
+          raise(top, use, [&](int i, float f) {
+#pragma unroll
+            for (auto& x : o) {
+              x[2 * i] *= f;
+              x[2 * i + 1] *= f;
+            }
+          });
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const float p0 = exp2_fast(s[r][2 * i] - use[i]), p1 = exp2_fast(s[r][2 * i + 1] - use[i]);
+              l[i] += p0 + p1;
+              Half2<T>::split(p0, p1, ph[2 * r + i], pl[2 * r + i]);
+            }
+          // ---- O += P V
+#pragma unroll
+          for (int j = 0; j < KS; ++j) {
+            uint32_t x[4];
+            load_tiles_transposed(tiles_at(v_at, j), x);
+            Half2<T>::mma(o[2 * j], ph[0], ph[1], ph[2], ph[3], x[0], x[2]);
+            Half2<T>::mma(o[2 * j + 1], ph[0], ph[1], ph[2], ph[3], x[1], x[3]);
+            Half2<T>::mma(o[2 * j], pl[0], pl[1], pl[2], pl[3], x[0], x[2]);
+            Half2<T>::mma(o[2 * j + 1], pl[0], pl[1], pl[2], pl[3], x[1], x[3]);
+          }
+          __syncwarp();
         }
-      load_v(have_next, at_next);
-      have = have_next;
-      at = at_next;
+#pragma unroll
+        for (int i = 0; i + 1 < kSlots; ++i) waiting[i] = waiting[i + 1];
+        waiting[kSlots - 1] = ask(c + kSlots * kWarps, pg);
+      }
     }
 
     // ---- on to the next piece; this one's results meet in shared memory meanwhile
@@ -508,10 +598,7 @@ k_attn_decode(DecodeArgs a) {
             *reinterpret_cast<float2*>(&s_o[wid][h][(g + 8 * (k >> 2)) * 8 + 2 * (k & 3)]) = make_float2(o[k][i], o[k][i + 2]);
         } else {
 #pragma unroll
-          for (int k = 0; k < VC * 8; k += 2)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-              *reinterpret_cast<float2*>(&s_o[wid][h][(2 * t + x + 8 * (k >> 3)) * 8 + (k & 7)]) = make_float2(o[k][2 * i + x], o[k + 1][2 * i + x]);
+          for (int k = 0; k < 2 * KS; ++k) *reinterpret_cast<float2*>(&s_o[wid][h][8 * k + 2 * t]) = make_float2(o[k][2 * i], o[k][2 * i + 1]);
         }
       }
     }
@@ -613,14 +700,49 @@ k_attn_decode(DecodeArgs a) {
 }
 
 // Heads of a block.  Sixteen read keys and values once for up to sixteen heads, eight have more warps: 64 sequences of 2000 tokens, 64
-// heads over 4, 58 us with sixteen and 81 with eight, which read everything twice.
+// heads over 4, 53 us with sixteen and 81 with eight, which read everything twice.
 int heads_per_block(int group) { return group <= 8 ? 8 : 16; }
 
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+  static const EncodeFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
+               ? reinterpret_cast<EncodeFn>(p)
+               : nullptr;
+  }();
+  return fn;
+}
+// A layer of the cache as (64 values, rows of a page's heads, halves of head_dim, keys and values, pages); a box is a chunk.
+bool make_map(CUtensorMap* map, const DecodeArgs& a, int hd) {
+  EncodeFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t row = (cuuint64_t)hd * 2, rows = (cuuint64_t)a.n_kv_heads << a.shift;
+  const cuuint64_t dims[5] = {64, rows, (cuuint64_t)hd / 64, 2, (cuuint64_t)a.n_pages};
+  const cuuint64_t strides[4] = {row, 128, rows * row, 2 * rows * row};
+  const cuuint32_t box[5] = {64, 16, (cuuint32_t)hd / 64, 2, 1}, estr[5] = {1, 1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, const_cast<char*>(a.cache), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class T, int HD, bool kWide>
+cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int sms, cudaStream_t s) {
+  size_t ring = 0;
+  if (kWide) {
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kWide>), &done);
+    if (e != cudaSuccess) return e;
+    ring = (size_t)kWarps * kSlots * 16 * HD * 4 + 1024;
+  }
+  const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(HD, kWide ? 16 : 8) * sms));
+  return launch_early(k_attn_decode<T, HD, kWide>, grid, kThreads, ring, s, map, a);
+}
 template <class T>
-cudaError_t launch(const DecodeArgs& a, int hd, int hb, int sms, cudaStream_t s) {
-  const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(hd, hb) * sms));
-  if (hd == 128) return hb == 8 ? launch_early(k_attn_decode<T, 128, false>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 128, true>, grid, kThreads, 0, s, a);
-  return hb == 8 ? launch_early(k_attn_decode<T, 64, false>, grid, kThreads, 0, s, a) : launch_early(k_attn_decode<T, 64, true>, grid, kThreads, 0, s, a);
+cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hd, int hb, int sms, cudaStream_t s) {
+  if (hd == 128) return hb == 8 ? launch<T, 128, false>(map, a, sms, s) : launch<T, 128, true>(map, a, sms, s);
+  return hb == 8 ? launch<T, 64, false>(map, a, sms, s) : launch<T, 64, true>(map, a, sms, s);
 }
 
 // [(m, l) of the partial results][their O][counts]: the counts start at the same place for every description and n, and the
@@ -700,8 +822,10 @@ int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const 
   a.part_o = reinterpret_cast<float*>(ws + kSpaceO);
   a.count = reinterpret_cast<unsigned int*>(ws + kSpaceCounts);
   a.pair_count = reinterpret_cast<unsigned int*>(ws + kSpacePairs);
+  CUtensorMap map = {};
+  if (hb == 16 && !make_map(&map, a, d->head_dim)) return fail(NP_E_INVAL, "a cache that a tensor map does not describe");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = d->dtype == NP_T_BF16 ? launch<__nv_bfloat16>(a, d->head_dim, hb, sms, s) : launch<__half>(a, d->head_dim, hb, sms, s);
+  const cudaError_t e = d->dtype == NP_T_BF16 ? launch<__nv_bfloat16>(map, a, d->head_dim, hb, sms, s) : launch<__half>(map, a, d->head_dim, hb, sms, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);
 }
 

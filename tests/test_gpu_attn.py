@@ -472,3 +472,88 @@ def test_decode_of_the_most_rows():
     rows = [[seqs[i % len(seqs)], -1, 1][0 if i % 3 == 0 else i % 3] for i in range(1024)]
     _decode(c, 4, seqs=rows)
     c.check()
+
+
+# ---- groups of more than eight heads: keys and values come another way --------------------------------------------------
+@pytest.mark.parametrize("lens,hq,hkv,hd", [([20000], 16, 1, 128), ([20000, 3, 0, 9000], 24, 2, 64), ([1] * 300, 18, 2, 64), ([5000] + [40] * 63, 64, 4, 128),
+                                            ([31, 16, 17, 15, 33], 12, 1, 128)])
+def test_decode_of_large_groups_splits_of_all_sizes(lens, hq, hkv, hd):
+    """Chunks that end inside a page and at its end, few and many pieces; twice into the same workspace gives the same bits."""
+    P = 32
+    c = Cache(hkv=hkv, hd=hd, P=P, n_pages=sum(-(-x // P) for x in lens), max_seqs=len(lens))
+    c.grow(list(range(len(lens))), lens)
+    ws = _workspace(c, hq, len(lens))
+    _, a, la = _decode(c, hq, ws=ws)
+    _, b, lb = _decode(c, hq, ws=ws)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+def test_decode_of_large_groups_infinite_and_missing_values():
+    """As for small groups: -inf scores leave a row empty, what is seen shows, what is not seen does not."""
+    c = Cache(hkv=1, hd=64, P=16, n_pages=8, max_seqs=3)
+    c.grow([0, 1, 2], [20, 20, 20])
+    q = torch.ones(3, 11, 64, dtype=BF, device="cuda")
+    c.cache[0, c.pool.pages[0], 0] = -float("inf")
+    c.cache[0, c.pool.pages[1][1], 1, 0, 3] = float("nan")
+    c.cache[0, c.pool.pages[2][1], :, 0, 4:] = float("inf")
+    out, lse = torch.empty_like(q), torch.empty(3, 11, device="cuda")
+    nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, 11, 3), lse=lse)
+    torch.cuda.synchronize()
+    assert (out[0] == 0).all() and (lse[0] == -float("inf")).all()
+    assert torch.isnan(out[1]).all() and torch.isfinite(lse[1]).all()
+    assert torch.isfinite(out[2]).all() and torch.isfinite(lse[2]).all()
+
+
+def test_decode_of_large_groups_leaves_out_pages_and_rows_that_are_not_there():
+    c = Cache(hkv=1, hd=128, P=16, n_pages=40, max_seqs=3, max_pages=30)
+    c.grow([0, 1, 2], [300, 40, 10])
+    k, v = c.tokens(0, 0)
+    for page in (0, 5, 6, 7, 18):
+        c.table[0, page] = -1 if page & 1 else 40
+    q = torch.randn(4, 16, 128, device="cuda").to(BF)
+    out, lse = torch.empty_like(q), torch.empty(4, 16, device="cuda")
+    c.lens[2] = 16 * 30 + 1
+    nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, 16, 4), seqs=c.dev([0, 1, 3, 2]), lse=lse)
+    torch.cuda.synchronize()
+    assert c.status.item() == A.S_PAGE | A.S_SEQ | A.S_LENGTH
+    seen = np.r_[16:80, 128:288]
+    none = np.zeros((0, 1, 128))
+    check_rows(out, lse, q, lambda i: [(k[seen], v[seen]), c.tokens(0, 1), (none, none), (none, none)][i], 128 ** -0.5, False)
+
+
+def test_decode_of_large_groups_past_32_bit_offsets():
+    n_pages = (1 << 32) // (2 * 2 * 8 * 256 * 128) + 12
+    c = Cache(hkv=8, hd=128, P=256, n_pages=n_pages, max_seqs=2, fill=0.0)
+    c.reserve([0], [256 * (n_pages - 5)])
+    c.grow([1], [1000])
+    nb.np_kv_free(c.desc, c.tables, c.dev([0]))
+    c.pool.free([0])
+    _decode(c, 80, seqs=[1, 0])
+    c.check()
+
+
+def test_decode_of_large_groups_at_once_and_replayed():
+    """Calls of two streams at once, each with its workspace, eager and from a graph, beside calls of small groups."""
+    c = Cache(hkv=2, hd=128, P=16, n_pages=400, max_seqs=4)
+    c.grow([0, 1, 2, 3], [1500, 900, 1, 2000])
+    jobs = []
+    for hq in (32, 26, 8):
+        q = torch.randn(4, hq, 128, device="cuda").to(BF)
+        want, out, s, ws = torch.empty_like(q), torch.empty_like(q), torch.cuda.Stream(), _workspace(c, hq, 4)
+        nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, want, ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, out, ws, stream=s)
+        jobs.append((q, want, out, s, ws, g))
+    eager = []
+    for _ in range(15):
+        for q, want, out, s, ws, g in jobs:
+            with torch.cuda.stream(s):
+                o = torch.empty_like(q)
+                nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, o, ws, stream=s)
+                eager.append((o, want))
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o, want in eager) and all(torch.equal(j[2], j[1]) for j in jobs)
+    assert nb.np_attn_check(c.status) == nb.NP_OK

@@ -34,7 +34,6 @@
 // between a warp's loads: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, 53.0 us, 76 % (69 % with keys and values
 // in registers, 55 % with 16-byte asynchronous copies in place of TMA, 70 % with the chunks beyond asked into the L2 ahead, 74 % with
 // keys and values as two copies).
-#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -703,18 +702,6 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 // heads over 4, 53 us with sixteen and 81 with eight, which read everything twice.
 int heads_per_block(int group) { return group <= 8 ? 8 : 16; }
 
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn encode_fn() {
-  static const EncodeFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
-               ? reinterpret_cast<EncodeFn>(p)
-               : nullptr;
-  }();
-  return fn;
-}
 // A layer of the cache as (64 values, rows of a page's heads, halves of head_dim, keys and values, pages); a box is a chunk.
 bool make_map(CUtensorMap* map, const DecodeArgs& a, int hd) {
   EncodeFn fn = encode_fn();

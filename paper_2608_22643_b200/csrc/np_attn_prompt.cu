@@ -34,7 +34,6 @@
 //   other tile's last product.
 //
 // Every wait is bounded; after a time-out all roles leave, the block meets and tensor memory is released.
-#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -746,19 +745,6 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kColumns) : "memory");
   }
-}
-
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn encode_fn() {
-  static const EncodeFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
-               ? reinterpret_cast<EncodeFn>(p)
-               : nullptr;
-  }();
-  return fn;
 }
 
 // Rows of heads as (head_dim, heads, tokens); a box is 64 values of `box_heads` heads of `box_tokens` tokens.

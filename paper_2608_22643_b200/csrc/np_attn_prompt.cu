@@ -208,12 +208,105 @@ __device__ __forceinline__ float widen(uint16_t x) {
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
+// Rows by plain loads, over the tokens that they see and no others; results replace what is not finite, where they are finite themselves.
+// Four rows and eight tokens at a time: a lane has HD / 32 values of head_dim, then one of the 32 scores.
+template <bool kBf16, int HD>
+__device__ __noinline__ void rows_again(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, int lane) {
+  constexpr int N = HD / 32, R = 4, T = 8;
+  auto load = [](const uint16_t* p, float (&x)[N]) {
+    uint32_t w[N / 2];
+    if constexpr (N == 4) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = widen<kBf16>((uint16_t)(w[i / 2] >> (i & 1) * 16));
+  };
+  const uint16_t* k0 = a.k + (int64_t)start * a.k_token + (int64_t)kvh * a.k_head + lane * N;
+  const uint16_t* v0 = a.v + (int64_t)start * a.v_token + (int64_t)kvh * a.v_head + lane * N;
+  while (rows) {
+    int tok[R], head[R], last = 0;
+    float q[R][N], acc[R][N];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int src = rows ? __ffs(rows) - 1 : 0;
+      tok[r] = __shfl_sync(0xffffffffu, row_tok, src);
+      head[r] = __shfl_sync(0xffffffffu, row_head, src);
+      if (!rows) tok[r] = -1;  // no row: sees nothing
+      rows &= rows - 1;
+      last = max(last, tok[r]);
+      load(a.q + (int64_t)(start + max(tok[r], 0)) * a.q_token + (int64_t)head[r] * a.q_head + lane * N, q[r]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[r][i] = 0.f;
+    }
+    const int mine = lane < 8 ? tok[0] : lane < 16 ? tok[1] : lane < 24 ? tok[2] : tok[3];
+    float top = -INFINITY, sum = 0.f;  // of row lane / 8; the sum of tokens lane % 8, + 8, ...
+    for (int base = 0; base <= last; base += T) {
+      float s[R * T], v[T][N];
+#pragma unroll
+      for (int x = 0; x < T; ++x) {
+        const int64_t j = min(base + x, last);
+        float k[N];
+        load(k0 + j * a.k_token, k);
+        load(v0 + j * a.v_token, v[x]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          s[r * T + x] = q[r][0] * k[0];
+#pragma unroll
+          for (int i = 1; i < N; ++i) s[r * T + x] = fmaf(q[r][i], k[i], s[r * T + x]);
+        }
+      }
+#pragma unroll
+      for (int w = 16; w >= 1; w >>= 1)  // lane l gets the sum over all lanes of s[l]
+#pragma unroll
+        for (int i = 0; i < w; ++i) {
+          const bool up = lane & w;
+          s[i] = (up ? s[i + w] : s[i]) + __shfl_xor_sync(0xffffffffu, up ? s[i] : s[i + w], w);
+        }
+      const float score = base + (lane & 7) <= mine ? s[0] * a.scale2 : -INFINITY;
+      float now = fmaxf(top, score);
+#pragma unroll
+      for (int x = 1; x < T; x <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, x));
+      const float use = now == -INFINITY ? 0.f : now, f = exp2_fast(top - use), p = exp2_fast(score - use);
+      top = now;
+      sum = sum * f + p;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float fr = __shfl_sync(0xffffffffu, f, r * T);
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[r][i] *= fr;
+#pragma unroll
+        for (int x = 0; x < T; ++x) {
+          const float pr = __shfl_sync(0xffffffffu, p, r * T + x);
+          if (base + x > tok[r]) continue;
+#pragma unroll
+          for (int i = 0; i < N; ++i) acc[r][i] = fmaf(pr, v[x][i], acc[r][i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 1; x < T; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float inv = 1.f / __shfl_sync(0xffffffffu, sum, r * T);
+      if (tok[r] < 0) continue;
+      uint16_t* out = a.out + (int64_t)(start + tok[r]) * a.o_token + (int64_t)head[r] * a.o_head + lane * N;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (not_finite(widen<kBf16>(out[i])) && !not_finite(acc[r][i] * inv)) out[i] = (uint16_t)pack<kBf16>(acc[r][i] * inv, 0.f);
+    }
+  }
+}
+
 // Rows whose O is not finite, by their warp (a row per lane, tokens rising with the lanes, one key-value head).  What the tokens
 // that a row sees make infinite or NaN is so: weights are above 0, so an infinity stays one, and two of different signs or a NaN
 // make a NaN; V is looked through once for all rows.  What they do not has met a later token's V, or has grown too large
-// unnormalised: these values are computed again from plain loads, over the tokens that the row sees.  That is slow, and no row's usual
-// way: a NaN in the last of 8192 tokens, whose tile of 128 keys has rows that do not see it, makes 50 ms of a call of 0.9 (64 heads over 8);
-// NaN in all tokens, which every row sees, 8.7.
+// unnormalised: these rows are computed again.  That is slow, and no row's usual way: a NaN in
+// the last of 8192 tokens, whose tile of 128 keys has rows that do not see it, makes 11 ms of a call of 0.9 (64 heads over 8; 50 ms a row at a
+// time); NaN in all tokens, which every row sees, 8.5.
 template <bool kBf16, int HD>
 __device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, float row_l, int lane) {
   constexpr int N = HD / 32;  // values of a lane: lane, lane + 32, ...
@@ -222,13 +315,14 @@ __device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int s
   for (int i = 0; i < N; ++i) odd[i] = 0;
   const uint16_t* v0 = a.v + (int64_t)start * a.v_token + (int64_t)kvh * a.v_head + lane;
   int upto = 0;
+  uint32_t again = 0;
   __syncwarp();  // the rows' results, which other lanes have stored, are read below
   for (; rows; rows &= rows - 1) {
     const int src = __ffs(rows) - 1, tok = __shfl_sync(0xffffffffu, row_tok, src), head = __shfl_sync(0xffffffffu, row_head, src);
     const float l = __shfl_sync(0xffffffffu, row_l, src);
     if (not_finite(l)) continue;  // a score is no number: all of the row is none
     uint16_t* out = a.out + (int64_t)(start + tok) * a.o_token + (int64_t)head * a.o_head + lane;
-    bool again = false;
+    bool left = false;
     if (l != 0.f) {
 #pragma unroll 4
       for (int j = upto; j <= tok; ++j)
@@ -245,49 +339,12 @@ __device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int s
       if (l == 0.f) out[i * 32] = 0;  // nothing but scores of -inf
       else if (not_finite(old) && odd[i])
         out[i * 32] = (uint16_t)pack<kBf16>(odd[i] == 2 ? INFINITY : odd[i] == 4 ? -INFINITY : __uint_as_float(0x7fffffffu), 0.f);
-      else again |= not_finite(old);
+      else left |= not_finite(old);
     }
-    if (!__any_sync(0xffffffffu, again)) continue;
-    const uint16_t* q = a.q + (int64_t)(start + tok) * a.q_token + (int64_t)head * a.q_head;
-    float top = -INFINITY, sum = 0.f, acc[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.f;
-    for (int base = 0; base <= tok; base += 32) {
-      const int j = base + lane;
-      float s = -INFINITY;
-      if (j <= tok) {
-        const uint16_t* k = a.k + (int64_t)(start + j) * a.k_token + (int64_t)kvh * a.k_head;
-        s = 0.f;
-#pragma unroll 2
-        for (int d = 0; d < HD; d += 8) {
-          const uint4 x = *reinterpret_cast<const uint4*>(q + d), y = *reinterpret_cast<const uint4*>(k + d);
-          const uint32_t qw[4] = {x.x, x.y, x.z, x.w}, kw[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-            s = fmaf(widen<kBf16>(qw[w] >> 16), widen<kBf16>(kw[w] >> 16), fmaf(widen<kBf16>(qw[w]), widen<kBf16>(kw[w]), s));
-        }
-        s *= a.scale2;
-      }
-      float now = fmaxf(top, s);
-#pragma unroll
-      for (int x = 1; x < 32; x <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, x));
-      const float use = now == -INFINITY ? 0.f : now, f = exp2_fast(top - use), p = j <= tok ? exp2_fast(s - use) : 0.f;
-      top = now;
-      sum = sum * f + p;
-#pragma unroll
-      for (int i = 0; i < N; ++i) acc[i] *= f;
-      const int most = min(32, tok + 1 - base);
-      for (int x = 0; x < most; ++x) {
-        const float px = __shfl_sync(0xffffffffu, p, x);
-#pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = fmaf(px, widen<kBf16>(v0[(base + x) * a.v_token + i * 32]), acc[i]);
-      }
-    }
-    sum = npd::warp_sum(sum);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (!odd[i] && not_finite(widen<kBf16>(out[i * 32]))) out[i * 32] = (uint16_t)pack<kBf16>(acc[i] / sum, 0.f);
+    if (__any_sync(0xffffffffu, left)) again |= 1u << src;
   }
+  __syncwarp();
+  if (again) rows_again<kBf16, HD>(a, again, start, row_tok, row_head, kvh, lane);
 }
 
 template <int HD, int kTiles>

@@ -13,6 +13,7 @@
 // units of 16 KB that all blocks of the grid take in turn (a page is contiguous per layer only, so a unit is (layer, pair of
 // pages, piece)).
 #include <algorithm>
+#include <atomic>
 #include <cstdio>
 
 #include "np_attn.h"
@@ -56,8 +57,13 @@ const char* rows_error(const np_rows* r) {
 bool tables_ok(const np_kv_tables* t) { return t && t->page_table && t->lens && t->refs && t->scratch && t->status; }
 
 bool device_sms(int* sms) {
+  static std::atomic<int> known[64];
   int dev = 0;
-  return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (dev < 64 && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return true;
+  if (cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return false;
+  if (dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
+  return true;
 }
 
 namespace {

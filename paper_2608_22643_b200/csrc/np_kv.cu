@@ -344,10 +344,7 @@ struct RewriteArgs {
 constexpr int kCopyThreads = 256;
 constexpr int kUnit = 16384;  // bytes of a unit: four 16-byte loads per lane
 
-__global__ void __launch_bounds__(kCopyThreads)
-k_kv_copy(CopyArgs a, RewriteArgs w) {
-  npp::pdl_wait_prior();
-  npp::pdl_launch_dependents();
+__device__ __forceinline__ void copy_and_rewrite(const CopyArgs& a, const RewriteArgs& w) {
   const int tid = threadIdx.x;
   if (w.lens_out) {
     for (int s = blockIdx.x; s < w.max_seqs; s += gridDim.x) {
@@ -402,6 +399,84 @@ k_kv_copy(CopyArgs a, RewriteArgs w) {
       if (at < bytes) *reinterpret_cast<uint4*>(dst + at) = v[k];
     }
   }
+}
+
+__global__ void __launch_bounds__(kCopyThreads)
+k_kv_copy(CopyArgs a, RewriteArgs w) {
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+  copy_and_rewrite(a, w);
+}
+
+// compact of a small pool into other tables, in one launch: every block works the plan out for itself, a few loads and two scans, and
+// nothing that it reads is written.  In a stream of calls 9.1 us with two launches for a pool of 28 pages, 7.0 with one; 148.5 and
+// 146.5 for 96 pages of 80 layers.  The plan in memory (k_kv_compact_plan) is for larger pools, and for tables that are rewritten in place.
+constexpr int kSmallPool = kCopyThreads * kPerThread;
+
+__global__ void __launch_bounds__(kCopyThreads)
+k_kv_compact_small(Pool p, int32_t* refs_out, int32_t* __restrict__ n_live, CopyArgs a, RewriteArgs w) {
+  __shared__ int32_t s_map[kSmallPool], s_from[kSmallPool / 2], s_to[kSmallPool / 2];
+  __shared__ int s_sum[2][kCopyThreads / 32];
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, first = tid * kPerThread;
+  // what a block's threads before this one have, and (total) all of them
+  auto scan = [&](int mine, int* sums, int& total) {
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += up;
+    }
+    if (lane == 31) sums[wid] = inc;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < kCopyThreads / 32; ++i) {
+      if (i < wid) before += sums[i];
+      total += sums[i];
+    }
+    return before + inc - mine;
+  };
+  int refs[kPerThread], alive = 0, live;
+#pragma unroll
+  for (int j = 0; j < kPerThread; ++j) {
+    refs[j] = first + j < p.n_pages ? p.refs[first + j] : 0;
+    alive += refs[j] > 0;
+    s_map[first + j] = first + j;
+  }
+  scan(alive, s_sum[0], live);
+  int both = 0, all;  // holes below `live`, and (from bit 16 on) pages that move
+#pragma unroll
+  for (int j = 0; j < kPerThread; ++j) both += first + j < live ? (refs[j] <= 0) : (refs[j] > 0) << 16;
+  const int before = scan(both, s_sum[1], all);
+  int hole = before & 0xffff, mover = before >> 16;
+#pragma unroll
+  for (int j = 0; j < kPerThread; ++j) {
+    if (first + j < live && refs[j] <= 0) s_to[hole++] = first + j;
+    if (first + j >= live && refs[j] > 0) s_from[mover++] = first + j;
+  }
+  __syncthreads();
+  const int moves = all >> 16;
+  for (int i = tid; i < moves; i += kCopyThreads) s_map[s_from[i]] = s_to[i];
+  __syncthreads();
+  if (blockIdx.x == 0) {
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j)
+      if (first + j < p.n_pages) {
+        if (first + j >= live) refs_out[first + j] = 0;
+        else if (refs[j] > 0) refs_out[first + j] = refs[j];
+        if (refs[j] > 0 && first + j >= live) refs_out[s_map[first + j]] = refs[j];
+      }
+    if (tid == 0 && n_live) *n_live = live;
+  }
+  a.from = s_from;
+  a.to = s_to;
+  a.count = nullptr;
+  a.n_pairs = moves;
+  w.map = s_map;
+  copy_and_rewrite(a, w);
 }
 
 struct AppendArgs {
@@ -509,10 +584,13 @@ CopyArgs copy_args(const np_kv_desc* d, void* dst, const void* src, const int32_
   return CopyArgs{static_cast<char*>(dst), static_cast<const char*>(src), from, to, count, n, d->n_pages, d->n_layers, pb, pb * d->n_pages, status};
 }
 
-cudaError_t launch_copy(const CopyArgs& a, const RewriteArgs& w, int sms, cudaStream_t s) {
+unsigned copy_blocks(const CopyArgs& a, const RewriteArgs& w, int sms) {
   const int64_t units = (int64_t)a.n_pairs * a.n_layers * ((a.page_bytes + kUnit - 1) / kUnit);
   const int64_t blocks = std::max<int64_t>(units, w.lens_out ? w.max_seqs : 1);
-  return launch_early(k_kv_copy, dim3((unsigned)std::min<int64_t>(blocks, 8ll * sms)), kCopyThreads, 0, s, a, w);
+  return (unsigned)std::min<int64_t>(blocks, 8ll * sms);
+}
+cudaError_t launch_copy(const CopyArgs& a, const RewriteArgs& w, int sms, cudaStream_t s) {
+  return launch_early(k_kv_copy, dim3(copy_blocks(a, w, sms)), kCopyThreads, 0, s, a, w);
 }
 
 // Checks what every call with tables takes.
@@ -649,6 +727,11 @@ int np_kv_compact(const np_kv_desc* d, void* cache, const np_kv_tables* in, cons
   if (int rc = device(&sms)) return rc;
   const Pool p = pool_of(d, in);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (!same && d->n_pages <= kSmallPool) {
+    const CopyArgs a = copy_args(d, cache, cache, nullptr, nullptr, nullptr, std::max(1, d->n_pages / 2), in->status);
+    const RewriteArgs w{p.table, p.lens, nullptr, out->page_table, out->lens, p.shift, p.n_pages, p.max_seqs, p.max_pages};
+    return done(launch_early(k_kv_compact_small, dim3(copy_blocks(a, w, sms)), kCopyThreads, 0, s, p, out->refs, n_live, a, w));
+  }
   cudaError_t e = launch_early(k_kv_compact_plan, dim3(1), kPlanThreads, 0, s, p, out->refs, n_live);
   const RewriteArgs w{p.table, p.lens, p.pages(), out->page_table, out->lens, p.shift, p.n_pages, p.max_seqs, p.max_pages};
   if (e == cudaSuccess)

@@ -147,7 +147,7 @@ def test_fork_refusals():
 
 
 @pytest.mark.parametrize("in_place", [True, False])
-@pytest.mark.parametrize("P,layers,n_pages", [(16, 2, 40), (64, 5, 200), (16, 1, 9000)])
+@pytest.mark.parametrize("P,layers,n_pages", [(16, 2, 40), (64, 5, 200), (16, 3, 257), (16, 1, 2048), (16, 1, 2049), (16, 1, 9000)])
 def test_compact_moves_pages_down(P, layers, n_pages, in_place):
     c = Cache(layers=layers, hkv=2, hd=64, P=P, n_pages=n_pages, max_seqs=12)
     rng = np.random.default_rng(n_pages)
@@ -193,6 +193,21 @@ def test_compact_of_empty_full_and_compact_pools():
     c.pool.compact()
     c.check()
     assert n_live.item() == 4 and torch.equal(before.view(torch.int16), c.cache.view(torch.int16))
+
+
+@pytest.mark.parametrize("held", [[], [40, 16], [5]])
+def test_compact_into_other_tables_of_empty_full_and_compact_pools(held):
+    c = Cache(P=16, n_pages=4, max_seqs=4)
+    n_live = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    if held:
+        c.grow(list(range(len(held))), held)
+    before = c.cache.clone()
+    fresh = [torch.full_like(t, 55) for t in (c.table, c.lens, c.refs)]
+    nb.np_kv_compact(c.desc, c.cache, c.tables, nb.make_kv_tables(*fresh, None, None), n_live)
+    live, moves = c.pool.compact()
+    c.table, c.lens, c.refs = fresh
+    c.check()
+    assert n_live.item() == live and not moves and torch.equal(before.view(torch.int16), c.cache.view(torch.int16))
 
 
 def test_copy_pages_between_caches():

@@ -26,6 +26,9 @@
 //   (m, l, O) in the workspace and the last to arrive joins them in the order of the tokens, so that results do not depend on
 //   who was last.
 // * The first keys and values of a block's next piece are asked for before the warps' results of the last are joined.
+// * An infinity in V meets two terms of P, of which the second may be 0 or below it, and factors that underflow: the sums make a NaN of
+//   it.  So where a piece's result is no finite number though its sum is one, the block looks through the piece's V (mend) and stores
+//   what the tokens make of it; joins take infinities as they are.
 //
 // Measured (pages of 64 scattered over the pool, caches larger than the L2 in turn): sixteen sequences of 0 to 4095 tokens, 32 heads
 // of 128, 57.5 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 165 us, 97 %; one of 131071 tokens, 64 heads over 8, 92.6 us,
@@ -39,6 +42,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "np_attn.h"
 #include "np_device.cuh"
@@ -163,6 +167,80 @@ __device__ __forceinline__ int row_len(const DecodeArgs& a, int i, int* seq_out)
     return 0;
   }
   return len;
+}
+
+template <class T>
+__device__ __forceinline__ constexpr uint32_t infinity_bits() {
+  return std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+}
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+// By a whole block: results of tiles [ta, tb) of (row, pair) that are not finite, where V has anything of that kind among them.  Weights are
+// above 0, so an infinity stays one, and two of different signs or a NaN make a NaN; what the sums made of finite values stays.  V is looked
+// through once for all heads, eight values to a thread.  `odd`: bit k if the thread is to look at the four values of its turn k over heads and
+// head_dim; part_o: of the partial result, nullptr: out.  seen: HD ints of shared memory that are free.  One of 131071 tokens a NaN, 64
+// heads over 8: 201 us a call in place of 93. (One block that looks through all of V behind the join: 10 ms.)
+template <class T, int HD>
+__device__ __noinline__ void mend(const DecodeArgs& a, uint32_t odd, int row, int pair, int ta, int tb, int h0, int heads, float* part_o, int* seen) {
+  constexpr int kCols = HD / 8, kStep = kThreads / kCols, kAhead = 4;
+  constexpr uint32_t kInf = infinity_bits<T>();
+  const int tid = threadIdx.x;
+  for (int d = tid; d < HD; d += kThreads) seen[d] = 0;
+  __syncthreads();
+  int seq;
+  const int64_t len = min((int64_t)row_len(a, row, &seq), (int64_t)tb * kTile);
+  const int col = tid % kCols;
+  const int32_t* pages = a.table + (size_t)seq * a.max_pages;
+  const int64_t head_bytes = (int64_t)(HD * 2) << a.shift;
+  const char* v = a.cache + (a.n_kv_heads + pair / a.blocks_of_heads) * head_bytes + col * 16;
+  uint32_t bits = 0;  // value x of the column: 1 << x a NaN, 256 << x inf, 65536 << x -inf
+  for (int64_t j0 = (int64_t)ta * kTile + tid / kCols; j0 < len; j0 += kAhead * kStep) {
+    int pg[kAhead];
+    uint4 w[kAhead];
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) pg[y] = j0 + y * kStep < len ? pages[(j0 + y * kStep) >> a.shift] : -1;
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) {
+      w[y] = make_uint4(0, 0, 0, 0);
+      if ((unsigned)pg[y] < (unsigned)a.n_pages)
+        w[y] = npd::ldg_stream(v + (int64_t)pg[y] * 2 * a.n_kv_heads * head_bytes + ((j0 + y * kStep) & ((1 << a.shift) - 1)) * (HD * 2));
+    }
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const uint32_t b = word(w[y], x >> 1) >> (x & 1) * 16 & 0xffffu;
+        if ((b & kInf) == kInf) bits |= (b & 0x7fffu) != kInf ? 1u << x : b == kInf ? 256u << x : 65536u << x;
+      }
+  }
+  for (int x = 0; bits && x < 8; ++x)
+    if (const int what = bits >> x & 0x10101) atomicOr(&seen[col * 8 + x], what);
+  __syncthreads();
+  for (int x = tid; odd && x < heads * (HD / 4); x += kThreads, odd >>= 1) {
+    if (!(odd & 1u)) continue;
+    const int h = x / (HD / 4), d = x % (HD / 4) * 4;
+    uint16_t* out = a.out + row * a.o_token + (int64_t)(h0 + h) * a.o_head + d;
+    float* part = part_o + h * HD + d;
+    for (int i = 0; i < 4; ++i) {
+      const int what = seen[d + i];
+      if (!what) continue;
+      const uint32_t now = what == 0x100 ? kInf : what == 0x10000 ? kInf | 0x8000u : 0x7fffu;
+      if (part_o == nullptr) out[i] = (uint16_t)now;
+      else __stcg(&part[i], what == 0x100 ? INFINITY : what == 0x10000 ? -INFINITY : __uint_as_float(0x7fffffffu));
+    }
+  }
+  __syncthreads();
+}
+
+// What four values that were added up are, where the sum is not finite: the same of the values alone, whatever their factors.
+__device__ __forceinline__ void keep_infinite(float4& acc, const float4& v) {
+  auto one = [](float& s, float x) {
+    if (not_finite(x)) s = not_finite(s) ? s + x : x;
+  };
+  one(acc.x, v.x);
+  one(acc.y, v.y);
+  one(acc.z, v.z);
+  one(acc.w, v.w);
 }
 
 // Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
@@ -391,6 +469,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     acc.z += f * v.z;
     acc.w += f * v.w;
   };
+  auto odd_four = [](const float4& v) { return not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w); };
   // four values of a head's result; its log of the sum with the first
   auto result = [&](int i, int h, int d, const float4& acc, float use, float sum) {
     const bool none = sum == 0.f;
@@ -605,7 +684,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     if (any) keep_queries();
     const bool whole = e.ta == 0 && e.tb == e.tiles;
     const int slot = 2 * blockIdx.x + (e.ta == 0 ? 1 : 0);
-    for (int x = tid; x < e.heads * (HD / 4); x += kThreads) {
+    uint32_t odd = 0, turn = 1;  // bit k: the values of turn k below are not finite, and the sum does not say why
+    for (int x = tid; x < e.heads * (HD / 4); x += kThreads, turn <<= 1) {
       const int h = x / (HD / 4), d = x % (HD / 4) * 4;
       float top = -INFINITY;
 #pragma unroll
@@ -620,6 +700,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         sum += f * s_ml[w][h][1];
         add(acc, f, v);
       }
+      if (odd_four(acc) && !not_finite(sum) && !(whole && sum == 0.f)) odd |= turn;
       if (whole) {
         result(e.row, e.h0 + h, d, acc, use, sum);
       } else {
@@ -627,6 +708,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         if (d == 0) __stcg(reinterpret_cast<float2*>(&a.part_ml[(slot * HB + h) * 2]), make_float2(top, sum));
       }
     }
+    if (__syncthreads_or(odd))  // s_o and s_ml are free from here on, the next piece's queries are where all warps read them
+      mend<T, HD>(a, odd, e.row, e.pair, e.ta, e.tb, e.h0, e.heads, whole ? nullptr : a.part_o + (size_t)slot * HB * HD, reinterpret_cast<int*>(&s_o[0][0][0]));
     if (!whole) {
       // ---- the last block to arrive joins up to kJoin neighbouring pieces; the last of those that did joins what they got
       const int c0 = block_of(e.first_w + kStart), c1 = block_of(e.first_w + kStart + e.tiles - 1), pieces = c1 - c0 + 1;
@@ -677,6 +760,14 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
               add(acc, f, v[y]);
             }
           }
+          if (there && odd_four(acc)) {  // factors that are 0 make a NaN of an infinity
+            float4 kept = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int y = 0; y < n; ++y) keep_infinite(kept, __ldcg(reinterpret_cast<const float4*>(&a.part_o[(size_t)(slot_of(b + y * step) + h) * HD + d])));
+            if (not_finite(kept.x)) acc.x = kept.x;
+            if (not_finite(kept.y)) acc.y = kept.y;
+            if (not_finite(kept.z)) acc.z = kept.z;
+            if (not_finite(kept.w)) acc.w = kept.w;
+          }
           __syncwarp();  // b's place is read by the HD / 4 lanes of a head, all of this warp: they are done
           if (!there) continue;
           if (final) {
@@ -694,7 +785,6 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         if (groups > 1 && last_of(&a.pair_count[(size_t)e.row * pairs + e.pair], groups)) join(c0, groups, kJoin, true);
       }
     }
-    __syncthreads();  // s_o, s_ml and s_last are free for the next piece
   }
 }
 

@@ -141,6 +141,33 @@ __device__ __forceinline__ int block_inclusive_scan_1024(int v, int* wsum, int l
   return wsum[wid] + inc;
 }
 
+// The same for numbers of [0, kSumTop], whose sums stop at kSumTop (a sum that is below it is exact).
+constexpr int kSumTop = (1 << 30) - 1;
+__device__ __forceinline__ int sum_to_top(int a, int b) { return min(kSumTop, a + b); }
+__device__ __forceinline__ int block_inclusive_scan_to_top_1024(int v, int* wsum, int lane, int wid) {
+  int inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int t = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc = sum_to_top(inc, t);
+  }
+  if (lane == 31) wsum[wid] = inc;
+  __syncthreads();
+  if (wid == 0) {
+    int winc = wsum[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, winc, o);
+      if (lane >= o) winc = sum_to_top(winc, t);
+    }
+    const int before = __shfl_up_sync(0xffffffffu, winc, 1);
+    wsum[lane] = lane ? before : 0;
+    if (lane == 31) wsum[32] = winc;
+  }
+  __syncthreads();
+  return sum_to_top(wsum[wid], inc);
+}
+
 // The n lowest set bits of m (all of m if it has fewer).
 __device__ __forceinline__ uint32_t lowest_bits(uint32_t m, int n) {
   if (n <= 0) return 0u;

@@ -196,7 +196,9 @@ k_kv_take(Pool p, const int32_t* __restrict__ a, const int32_t* __restrict__ b, 
     if (!ok) need = 0;
   }
   __syncthreads();
-  const int end = npd::block_inclusive_scan_1024(need, red, lane, wid);
+  // sums past the pool are too many, however many: up to 1024 sequences may ask for 2^22 pages each
+  static_assert(NP_KV_MAX_PAGES < npd::kSumTop, "a sum that stops is more than a pool has");
+  const int end = npd::block_inclusive_scan_to_top_1024(need, red, lane, wid);
   const int total = red[32];
   __syncthreads();
   int32_t* pages = total <= kFewPages ? s_pages : p.pages();

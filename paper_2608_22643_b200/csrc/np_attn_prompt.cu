@@ -50,6 +50,10 @@ namespace {
 
 constexpr int kRows = 128;              // query rows of a tile, keys of a tile
 constexpr float kGrow = 8.f;            // log2 of the growth of a maximum that is let pass
+// The largest score (times log2(e), either sign) that an exponent may be formed from by one fused step, s * scale2 - m.  m is a rounded product;
+// what the rounding took off stays in the exponent, 1 at most up to here, and cancels between P and its sum.  Past it that passes the range
+// of P (2^16 in fp16) and in the end of fp32, so the products are rounded first, as m is.
+constexpr float kLarge = 16777216.f;
 constexpr int kPlans = 2;               // blocks of work that are laid out ahead
 constexpr uint32_t kWaitPolls = 1u << 26;  // a second or two: a tile without rows waits for a whole block of work of the other
 struct PromptArgs {
@@ -728,12 +732,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
         // On the assumption that the maximum has not grown much, the first half's exponentials need not wait for it: it is found
         // beside them, by units that they leave idle.  (The maximum first: 390 cycles of 2350 for a tile.)
-        float part = 0.f, now;
+        float part = 0.f, now, sc = a.scale2;
         bool fast = false;
         if (j > 0) {
           part = softmax_half<kBf16, 0>(s, a.scale2, m, ts);
           now = row_max(s) * a.scale2;
-          fast = __all_sync(0xffffffffu, !valid || (now <= m + kGrow && m > -INFINITY && now < INFINITY));
+          fast = __all_sync(0xffffffffu, !valid || (now <= m + kGrow && fabsf(m) <= kLarge && now < INFINITY));
         } else {
           now = row_max(s) * a.scale2;
         }
@@ -758,10 +762,15 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             }
           }
           use = m == -INFINITY ? 0.f : m;
-          part = softmax_half<kBf16, 0>(s, a.scale2, use, ts);
+          if (__any_sync(0xffffffffu, valid && fabsf(use) > kLarge)) {
+#pragma unroll
+            for (int c = 0; c < kRows; ++c) s[c] = __float_as_uint(__uint_as_float(s[c]) * sc);
+            sc = 1.f;
+          }
+          part = softmax_half<kBf16, 0>(s, sc, use, ts);
         }
         arrive(&p_half[i]);
-        l += part + softmax_half<kBf16, kRows / 2>(s, a.scale2, use, ts);
+        l += part + softmax_half<kBf16, kRows / 2>(s, sc, use, ts);
         arrive(&p_full[i]);
       }
       if (ok) ok = wait_all(&o_full[i], o_cnt++ & 1u);

@@ -251,6 +251,17 @@ constexpr int blocks_per_sm(int hd, int heads) { return hd == 64 ? (heads == 8 ?
 
 constexpr int kSlots = 2;  // sixteen heads: chunks of a warp on their way
 
+// What a warp's lanes tell each other of waits that were given up.
+struct WarpWaits {
+  volatile int* word;
+  int32_t* status;
+  __device__ __forceinline__ bool lost() { return *word != 0; }
+  __device__ __forceinline__ void lose() {
+    *word = 1;
+    atomicOr(status, NP_KV_S_TIMEOUT);
+  }
+};
+
 template <class T, int HD, bool kWide>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kWide ? 16 : 8))
 k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
@@ -271,9 +282,11 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   __shared__ float s_ml[kWarps][HB][2];
   __shared__ int64_t s_wsum[kWarps];
   __shared__ int s_last;
+  __shared__ volatile int s_lost[kWarps];  // a wait of the warp was given up
   if (kWide && (threadIdx.x & 31) == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
     for (int i = 0; i < kSlots; ++i) npp::mbar_init(&s_full[threadIdx.x >> 5][i], 1);
+    s_lost[threadIdx.x >> 5] = 0;
     npp::fence_barrier_init();
   }
   npp::pdl_wait_prior();
@@ -385,7 +398,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   int chunk_end, c, have, have_next, pg_next;  // chunks of 16 tokens
   int64_t at, at_next;
   int waiting[kSlots];                 // tokens of the chunks in this warp's ring
-  uint32_t asked = 0, used = 0;        // of the ring, so far
+  npp::WarpRing<kSlots> uses;
+  WarpWaits waits = {&s_lost[wid], a.status};
   const uint32_t ring = ((npp::smem_addr(s_dyn) + 1023) & ~1023u) + wid * kSlots * kSlot;
   // what a lane reads with load_tiles: rows (tokens) 0-7 and 8-15 of two neighbouring 16-byte columns, 128-byte swizzle
   const uint32_t lane_row = ((lane & 7) + (lane >> 4) * 8) * 128, lane_col = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
@@ -430,12 +444,11 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       atomicOr(a.status, NP_KV_S_PAGE);
       return 0;
     }
-    if (lane == 0) {
-      uint64_t* bar = &s_full[wid][asked % kSlots];
-      npp::mbar_expect_tx(bar, kSlot);
-      tma_load_chunk(ring + asked % kSlots * kSlot, &map, p.first_row + (int)(((int64_t)chunk * 16) & ((1 << a.shift) - 1)), pg, bar);
+    if (lane == 0 && uses.may_ask()) {
+      const uint32_t slot = uses.slot(uses.asked++);
+      npp::mbar_expect_tx(&s_full[wid][slot], kSlot);
+      tma_load_chunk(ring + slot * kSlot, &map, p.first_row + (int)(((int64_t)chunk * 16) & ((1 << a.shift) - 1)), pg, &s_full[wid][slot]);
     }
-    ++asked;
     return (int)min((int64_t)16, p.len - (int64_t)chunk * 16);
   };
   // asks for the queries and the first keys and values of a piece
@@ -588,11 +601,15 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         const int now = waiting[0], pg = pg_next;
         pg_next = page_of(c + (kSlots + 1) * kWarps);
         if (now > 0) {
-          const uint32_t k_at = ring + used % kSlots * kSlot, v_at = k_at + kHalf;
+          const uint32_t k_at = ring + uses.slot(uses.used) * kSlot, v_at = k_at + kHalf;
           uint32_t polls = 0;
-          while (!npp::mbar_try_wait(&s_full[wid][used % kSlots], (used / kSlots) & 1u) && polls < 4 * npp::kSpinLimit)
-            if (++polls == npp::kSpinLimit) atomicOr(a.status, NP_KV_S_TIMEOUT);
-          ++used;
+#pragma unroll 1
+          while (!npp::mbar_try_wait(&s_full[wid][uses.slot(uses.used)], uses.parity(uses.used)))
+            if (npp::warp_ring_wait_step<npp::kSpinLimit>(polls, waits)) {
+              uses.lost = true;
+              break;
+            }
+          ++uses.used;
           if (now < 16) {  // tokens that are not there: zero, whatever their places hold
             for (int e = lane; e < (16 - now) * (HD / 8); e += 32) {
               const int r = now + e / (HD / 8), d = e % (HD / 8);
@@ -785,6 +802,10 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         if (groups > 1 && last_of(&a.pair_count[(size_t)e.row * pairs + e.pair], groups)) join(c0, groups, kJoin, true);
       }
     }
+  }
+  if (kWide && lane == 0 && uses.lost) {  // a block leaves when its copies have landed
+    uint32_t patience = npp::kSpinLimit;
+    npp::drain_ring(s_full[wid], kSlots, uses.slot(uses.asked), uses.parity(uses.asked), patience);
   }
 }
 

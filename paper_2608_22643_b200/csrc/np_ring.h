@@ -1,5 +1,6 @@
 // A wait on the barriers of a ring of shared-memory slots that bulk copies fill: its rule alone, without the hardware.
-// np_pipe.cuh puts mbarriers under it, tests/test_ring_replay.py a model that replays it on the host.
+// np_pipe.cuh puts mbarriers under it, tests/test_ring_replay.py a model that replays it on the host.  At the end of the file the same for a
+// ring that one warp fills and reads (np_attn_decode.cu; tests/test_warp_ring_replay.py).
 //
 // A slot has two barriers: `full` (the lane that fills the ring arms it, the copies complete it) and `empty` (its readers).  A
 // barrier's parity tells the phase before the current one from the current one and nothing older, so a wait means what it says only
@@ -35,6 +36,30 @@ NP_RING_FN bool ring_wait_step(uint32_t& polls, Block& b) {
   }
   if (++polls == kLimit) b.lower();
   return false;
+}
+
+// A ring of kSlots slots of one warp, use u in slot u % kSlots.  One lane asks for copies, all lanes wait for them and read; there is no
+// barrier for free slots: a slot is asked for again by the lane that has waited for its last use, behind a barrier of the warp.  So the
+// lane asks for nothing more once a wait of its own was given up: the copies of that use may still be on their way.  The warp goes on with
+// what lies there (its results are reported as incomplete), no later wait is longer than a poll, and at its end the lane waits for the
+// copies that it has asked for.
+template <int kSlots>
+struct WarpRing {
+  uint32_t asked = 0, used = 0;  // uses so far; `asked` is the lane's that asks
+  bool lost = false;             // a wait of this lane was given up
+  static NP_RING_FN uint32_t slot(uint32_t use) { return use % kSlots; }
+  static NP_RING_FN uint32_t parity(uint32_t use) { return use / kSlots & 1u; }
+  NP_RING_FN bool may_ask() const { return !lost; }
+};
+
+// The step behind a poll that has found a use not complete.  True: the wait is given up.  Warp: lost() tells whether any lane's wait was
+// given up, lose() says so and reports it.
+template <uint32_t kLimit, class Warp>
+NP_RING_FN bool warp_ring_wait_step(uint32_t& polls, Warp& w) {
+  if (w.lost()) return true;
+  if (++polls < kLimit) return false;
+  w.lose();
+  return true;
 }
 
 }  // namespace npp

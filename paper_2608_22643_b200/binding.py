@@ -347,8 +347,12 @@ def _attn():
         load()
         try:
             from . import np_attn_bind
+            from .build import bind_target
         except ImportError as e:
             raise RuntimeError(f"np_attn_bind.so is not usable ({e}): build it with `python -m paper_2608_22643_b200.build`") from e
+        if np_attn_bind.built_for != bind_target():
+            raise RuntimeError(f"np_attn_bind.so was built for {np_attn_bind.built_for}, this is {bind_target()}: build it again with "
+                               "`python -m paper_2608_22643_b200.build`")
         np_attn_bind.setup(NpError)
         _calls = np_attn_bind
     return _calls

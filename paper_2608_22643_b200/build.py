@@ -6,6 +6,7 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -74,25 +75,41 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     return LIB_PATH
 
 
-def _build_binding(nvcc: str, force: bool) -> None:
-    """``np_attn_bind.so``: a CPython module over libnp.so and torch's tensors.  Built again when torch or the interpreter changes."""
+def bind_target() -> str:
+    """What a compiled binding is good for: this torch and this interpreter."""
     import torch
 
-    home = os.path.dirname(os.path.abspath(torch.__file__))
-    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
-    cmd = ["g++", "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-Wno-unknown-pragmas", "-I", INCLUDE, "-I", sysconfig.get_paths()["include"]]
-    for d in (os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")):
-        cmd += ["-isystem", d]
-    cmd += [BIND_SOURCE, "-o", BIND_PATH, "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", HERE, "-lnp",
-            "-Wl,-rpath,$ORIGIN"]
+    return f"torch {torch.__version__}, python {sys.version}"
+
+
+def _build_binding(nvcc: str, force: bool) -> None:
+    """``np_attn_bind.so``: a CPython module over libnp.so and torch's tensors.  Built again when torch or the interpreter changes.  Where it
+    cannot be built (no torch, no headers of torch's or the interpreter's, no g++) there is none afterwards, and the calls that need it
+    say so; the library does not need it."""
     made_by = os.path.join(OBJ_DIR, "np_attn_bind.made_by")
-    how = f"torch {torch.__version__}, python {sys.version}"
-    same = os.path.exists(made_by) and open(made_by).read() == how
-    if not force and same and not _stale(BIND_PATH, [BIND_SOURCE, os.path.join(INCLUDE, "np.h"), os.path.abspath(__file__)]):
+    try:
+        import torch
+
+        how = bind_target()
+        same = os.path.exists(made_by) and open(made_by).read() == how
+        if not force and same and not _stale(BIND_PATH, [BIND_SOURCE, os.path.join(INCLUDE, "np.h"), os.path.abspath(__file__)]):
+            return
+        home = os.path.dirname(os.path.abspath(torch.__file__))
+        cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
+        cmd = ["g++", "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-Wno-unknown-pragmas", "-I", INCLUDE, "-I", sysconfig.get_paths()["include"]]
+        for d in (os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")):
+            cmd += ["-isystem", d]
+        cmd += [f'-DNP_BUILT_FOR="{how}"', BIND_SOURCE, "-o", BIND_PATH, "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+                "-L", HERE, "-lnp", "-Wl,-rpath,$ORIGIN"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        why = "" if r.returncode == 0 else "g++ failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr
+    except (ImportError, OSError) as e:
+        why = str(e)
+    if why:
+        if os.path.exists(BIND_PATH):
+            os.remove(BIND_PATH)
+        warnings.warn(f"np_attn_bind.so could not be built; the cache and attention calls of the Python binding need it: {why}")
         return
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("g++ failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
     with open(made_by, "w") as f:
         f.write(how)
 

@@ -355,5 +355,7 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "np_attn_bind", nullptr, -1, g_me
 PyMODINIT_FUNC PyInit_np_attn_bind(void) {
   g_room = PyUnicode_InternFromString("room");
   g_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-  return g_room && g_cuda_stream ? PyModule_Create(&g_module) : nullptr;
+  PyObject* m = g_room && g_cuda_stream ? PyModule_Create(&g_module) : nullptr;
+  if (m && PyModule_AddStringConstant(m, "built_for", NP_BUILT_FOR) != 0) Py_CLEAR(m);  // binding.py compares
+  return m;
 }

@@ -55,7 +55,10 @@ constexpr float kGrow = 8.f;            // log2 of the growth of a maximum that 
 // of P (2^16 in fp16) and in the end of fp32, so the products are rounded first, as m is.
 constexpr float kLarge = 16777216.f;
 constexpr int kPlans = 2;               // blocks of work that are laid out ahead
-constexpr uint32_t kWaitPolls = 1u << 26;  // a second or two: a tile without rows waits for a whole block of work of the other
+// Polls that a wait may take, a second or two: a tile without rows waits for a whole block of work of the other.  Rows that are computed again
+// take longer than that from a million tokens on, and the block's other roles wait for them; so a warp that does it raises the block's
+// limit by 2^22 polls (100 ms) for every kBeat tokens (12 ms), to 2^30 (half a minute) at most.
+constexpr int kWaitPolls = 1 << 26, kMostPolls = 1 << 30, kBeatPolls = 1 << 22, kBeat = 1 << 16;
 struct PromptArgs {
   const uint16_t* q;
   const uint16_t* k;
@@ -212,10 +215,16 @@ __device__ __forceinline__ float widen(uint16_t x) {
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
+// A step of rows that are computed again: what waits for them may take longer.  A limit of 0 stays.
+__device__ __forceinline__ void raise_limit(int* limit) {
+  const int was = *static_cast<volatile int*>(limit);
+  if (was > 0 && was < kMostPolls) atomicCAS(limit, was, was + kBeatPolls);
+}
+
 // Rows by plain loads, over the tokens that they see and no others; results replace what is not finite, where they are finite themselves.
 // Four rows and eight tokens at a time: a lane has HD / 32 values of head_dim, then one of the 32 scores.
 template <bool kBf16, int HD>
-__device__ __noinline__ void rows_again(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, int lane) {
+__device__ __noinline__ void rows_again(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, int lane, int* limit) {
   constexpr int N = HD / 32, R = 4, T = 8;
   auto load = [](const uint16_t* p, float (&x)[N]) {
     uint32_t w[N / 2];
@@ -249,6 +258,7 @@ __device__ __noinline__ void rows_again(const PromptArgs& a, uint32_t rows, int 
     const int mine = lane < 8 ? tok[0] : lane < 16 ? tok[1] : lane < 24 ? tok[2] : tok[3];
     float top = -INFINITY, sum = 0.f;  // of row lane / 8; the sum of tokens lane % 8, + 8, ...
     for (int base = 0; base <= last; base += T) {
+      if ((base & (kBeat - 1)) == 0 && lane == 0) raise_limit(limit);
       float s[R * T], v[T][N];
 #pragma unroll
       for (int x = 0; x < T; ++x) {
@@ -312,7 +322,8 @@ __device__ __noinline__ void rows_again(const PromptArgs& a, uint32_t rows, int 
 // the last of 8192 tokens, whose tile of 128 keys has rows that do not see it, makes 11 ms of a call of 0.9 (64 heads over 8; 50 ms a row at a
 // time); NaN in all tokens, which every row sees, 8.5.
 template <bool kBf16, int HD>
-__device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, float row_l, int lane) {
+__device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int start, int row_tok, int row_head, int kvh, float row_l, int lane,
+                                       int* limit) {
   constexpr int N = HD / 32;  // values of a lane: lane, lane + 32, ...
   int odd[N];                 // of the tokens so far: 1 a NaN, 2 inf, 4 -inf
 #pragma unroll
@@ -327,15 +338,17 @@ __device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int s
     if (not_finite(l)) continue;  // a score is no number: all of the row is none
     uint16_t* out = a.out + (int64_t)(start + tok) * a.o_token + (int64_t)head * a.o_head + lane;
     bool left = false;
-    if (l != 0.f) {
+    while (l != 0.f && upto <= tok) {
+      const int end = min(tok, upto + kBeat - 1);
 #pragma unroll 4
-      for (int j = upto; j <= tok; ++j)
+      for (int j = upto; j <= end; ++j)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const float x = widen<kBf16>(v0[j * a.v_token + i * 32]);
           if (not_finite(x)) odd[i] |= x == INFINITY ? 2 : x == -INFINITY ? 4 : 1;
         }
-      upto = max(upto, tok + 1);
+      upto = end + 1;
+      if (lane == 0) raise_limit(limit);
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -348,7 +361,7 @@ __device__ __noinline__ void mend_rows(const PromptArgs& a, uint32_t rows, int s
     if (__any_sync(0xffffffffu, left)) again |= 1u << src;
   }
   __syncwarp();
-  if (again) rows_again<kBf16, HD>(a, again, start, row_tok, row_head, kvh, lane);
+  if (again) rows_again<kBf16, HD>(a, again, start, row_tok, row_head, kvh, lane, limit);
 }
 
 template <int HD, int kTiles>
@@ -435,7 +448,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   __shared__ __align__(8) uint64_t full[S::kStages], empty[S::kStages], q_full, q_empty, s_full[kTiles], p_half[kTiles], p_full[kTiles], o_full[kTiles], o_empty[kTiles],
       plan_full[kPlans], plan_empty[kPlans];
   __shared__ uint32_t s_tmem;
-  __shared__ volatile int s_ok[2];
+  __shared__ int s_limit;  // polls that a wait may take; 0: one has run out
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -463,8 +476,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       npp::mbar_init(&plan_empty[i], S::kPlanReaders);
     }
     npp::fence_barrier_init();
-    s_ok[0] = 1;
-    s_ok[1] = 0;
+    s_limit = kWaitPolls;
   }
   // the plan warp counts the blocks of each prompt while the others set up
   if (wid == S::kPlanWarp) {
@@ -490,12 +502,13 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   const uint32_t tmem = s_tmem;
   // true: the phase is complete; false: this or another wait of the block has run out
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    uint32_t polls = 0;
+    int polls = 0;
 #pragma unroll 1
     while (!npp::mbar_try_wait(bar, parity)) {
-      if (!s_ok[0]) return false;
-      if (++polls == kWaitPolls) {
-        s_ok[0] = 0;
+      const int limit = *static_cast<volatile int*>(&s_limit);
+      if (limit == 0) return false;
+      if (++polls >= limit) {
+        *static_cast<volatile int*>(&s_limit) = 0;
         atomicOr(a.status, NP_KV_S_TIMEOUT);
       }
     }
@@ -597,7 +610,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           }
         }
       }
-      if (!s_ok[0]) {  // after a time-out nobody else waits for the copies
+      if (*static_cast<volatile int*>(&s_limit) == 0) {  // after a time-out nobody else waits for the copies
         uint32_t patience = npp::kSpinLimit;
         npp::drain_ring(full, S::kStages, stage, use & 1u, patience);
         npp::wait_landed(&q_full, n & 1u, patience);
@@ -811,7 +824,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       if (valid && a.lse)
         a.lse[(size_t)(w.start + tok) * a.n_heads + head] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * kLn2 + logf(l);
       const uint32_t odd = __ballot_sync(0xffffffffu, valid && big >= 0x7f800000u);
-      if (odd) mend_rows<kBf16, HD>(a, odd, w.start, tok, head, w.kvh, l, lane);
+      if (odd) mend_rows<kBf16, HD>(a, odd, w.start, tok, head, w.kvh, l, lane, &s_limit);
     }
   }
   fence_before();

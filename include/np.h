@@ -550,8 +550,9 @@ const char* np_trunk_last_error(void);
  *   page_table[s][i]  page with tokens [i * page_tokens, (i + 1) * page_tokens) of sequence s; -1 past its pages
  *   lens[s]           tokens of sequence s
  *   refs[p]           sequences that hold page p; 0 = free
- * Sequences made by np_kv_fork share their parents' full pages; a partly filled page belongs to one sequence alone,
- * so np_kv_append of tokens that np_kv_reserve made room for never writes a page that another sequence reads. */
+ * Sequences made by np_kv_fork share their parents' full pages; a partly filled page belongs to one sequence alone.
+ * So np_kv_append of tokens that np_kv_reserve made room for never writes a page that another sequence reads, as long as they are
+ * appended, in every layer, before their sequence is forked: which pages are full goes by lengths, and reserving grows those. */
 #define NP_T_BF16 0
 #define NP_T_FP16 1
 #define NP_KV_MAX_SEQS   1024
@@ -628,8 +629,9 @@ int np_kv_append(const np_kv_desc* desc, void* cache, int32_t layer, const np_kv
 
 /* Sequence dst[i] (empty, listed once) begins as a copy of sequence src[i] (dev [n] each): it shares the full pages, and a
  * partly filled last page is copied, in every layer, to a page of its own (list order, lowest free number first).  A
- * source may be listed often.  All sources are taken as they were before the call: tokens that were reserved and are
- * appended to a source later are not in the copy's last page. */
+ * source may be listed often.  All sources are taken as they were before the call.  Append what was reserved, in every layer, before
+ * that: of tokens that are appended to a source later, those in its full pages are the copy's too (the pages are shared), those in the
+ * last, partly filled one are not. */
 int np_kv_fork(const np_kv_desc* desc, void* cache, const np_kv_tables* tables, const int32_t* src, const int32_t* dst,
                int32_t n, void* stream);
 

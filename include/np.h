@@ -660,7 +660,7 @@ int np_kv_copy_pages(const np_kv_desc* desc, void* dst_cache, const void* src_ca
  * length 0, and a row whose seqs[i] is negative (padding), give zeros and lse -inf, and so does a row whose scores are all
  * -inf.  fp32 scores, softmax and sums.
  *   q, out     n rows of n_heads heads; out may not overlap q, its strides are above 0 along more than one row or head
- *   scale      positive and finite
+ *   scale      positive; times log2(e) finite
  *   lse        dev fp32 [n][n_heads] or NULL: log sum_j exp(scale * q . k_j)
  *   seqs       dev [n] or NULL: 0..n-1; the same sequence may be listed often
  *   workspace  dev, 16-byte aligned, workspace_bytes long: at least np_attn_workspace_bytes; zeroed by the caller before its
@@ -677,7 +677,7 @@ int np_attn_decode(const np_kv_desc* desc, const void* cache, int32_t layer, con
  *   q, out  n_tokens rows of n_heads heads, k, v  n_tokens rows of n_kv_heads heads; strides above 0 along more than one
  *           token or head; out may not overlap the others
  *   cu      dev int32 [n + 1], ascending, 0 <= cu <= n_tokens; a prompt may be empty
- *   scale   positive and finite
+ *   scale   positive; times log2(e) finite
  *   lse     dev fp32 [n_tokens][n_heads] or NULL
  *   status  dev int32 [1], zeroed by the caller before its first use
  * head_dim 64 or 128, n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= NP_ATTN_MAX_GROUP, 1 <= n <= NP_KV_MAX_SEQS.

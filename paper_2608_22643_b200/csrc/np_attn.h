@@ -5,11 +5,24 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <cfloat>
+#include <cmath>
+
 #include "np.h"
 
 namespace npa {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// scale * log2(e): scores are kept in base two.  Below the normal numbers, which the kernels flush to 0 (and 0 * -inf is no number), the
+// least of them: either way products of finite scores this small are 0 to an exponential.  False: no scale.
+inline bool scale_base2(float scale, float* out) {
+  *out = scale * kLog2e;
+  if (!(scale > 0.f) || !std::isfinite(*out)) return false;
+  if (*out < FLT_MIN) *out = FLT_MIN;
+  return true;
+}
+constexpr const char* kScaleError = "scale must be positive, and times log2(e) finite";
 
 // Keeps the text for np_attn_last_error and returns the code.
 int fail(int code, const char* msg);

@@ -884,7 +884,8 @@ int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const 
   if ((uintptr_t)cache % 16 || (uintptr_t)workspace % 16) return fail(NP_E_INVAL, "cache and workspace must be 16-byte aligned");
   if (workspace_bytes < space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n)) return fail(NP_E_INVAL, "workspace is smaller than np_attn_workspace_bytes says");
   if (layer < 0 || layer >= d->n_layers) return fail(NP_E_INVAL, "layer outside the cache");
-  if (!std::isfinite(scale) || scale <= 0.f) return fail(NP_E_INVAL, "scale must be positive and finite");
+  float scale2;
+  if (!scale_base2(scale, &scale2)) return fail(NP_E_INVAL, kScaleError);
   if (const char* m = rows_error(q)) return fail(NP_E_INVAL, m);
   if (const char* m = rows_error(out)) return fail(NP_E_INVAL, m);
   if ((n > 1 && out->token_stride == 0) || (n_heads > 1 && out->head_stride == 0)) return fail(NP_E_INVAL, "rows of the result need strides above 0");
@@ -910,7 +911,7 @@ int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const 
   a.group = n_heads / d->n_kv_heads;
   const int hb = heads_per_block(a.group);
   a.blocks_of_heads = (a.group + hb - 1) / hb;
-  a.scale2 = scale * kLog2e;
+  a.scale2 = scale2;
   a.shift = log2_of(d->page_tokens);
   a.n_pages = d->n_pages;
   a.max_seqs = d->max_seqs;

@@ -883,7 +883,8 @@ extern "C" int np_attn_prompt(const np_attn_shape* d, const np_rows* q, const np
   if (group > NP_ATTN_MAX_GROUP) return fail(NP_E_INVAL, "more than NP_ATTN_MAX_GROUP query heads to a key-value head");
   if (n < 1 || n > NP_KV_MAX_SEQS) return fail(NP_E_INVAL, "n outside [1, NP_KV_MAX_SEQS]");
   if (n_tokens < 0) return fail(NP_E_INVAL, "n_tokens must not be negative");
-  if (!std::isfinite(scale) || scale <= 0.f) return fail(NP_E_INVAL, "scale must be positive and finite");
+  float scale2;
+  if (!scale_base2(scale, &scale2)) return fail(NP_E_INVAL, kScaleError);
   if (n_tokens == 0) return NP_OK;
   if (!cu || !status) return fail(NP_E_INVAL, "NULL argument");
   for (const np_rows* r : {q, k, v, out})
@@ -915,7 +916,7 @@ extern "C" int np_attn_prompt(const np_attn_shape* d, const np_rows* q, const np
   a.n_kv_heads = d->n_kv_heads;
   a.group = group;
   a.tile_tokens = kRows / group;
-  a.scale2 = scale * kLog2e;
+  a.scale2 = scale2;
   a.out32 = (uintptr_t)out->data % 32 == 0 && out->token_stride % 16 == 0 && out->head_stride % 16 == 0;
   if (((int64_t)n_tokens / a.tile_tokens + n) * d->n_kv_heads > 0x7fffffffLL) return fail(NP_E_INVAL, "too many tokens for one call");
   int sms;

@@ -232,15 +232,26 @@ __device__ __noinline__ void mend(const DecodeArgs& a, uint32_t odd, int row, in
   __syncthreads();
 }
 
-// What four values that were added up are, where the sum is not finite: the same of the values alone, whatever their factors.
-__device__ __forceinline__ void keep_infinite(float4& acc, const float4& v) {
-  auto one = [](float& s, float x) {
-    if (not_finite(x)) s = not_finite(s) ? s + x : x;
+// Four values of joined partial results that are not finite: factors that are 0 make a NaN of an infinity, so they are what the partial results
+// that are not finite add up to by themselves.  part: the four values of the first, `next` to those of the next, n of them; the first
+// `extra` further where it is in its block's second place.
+__device__ __noinline__ float4 keep_infinite(float4 acc, const float* part, int64_t extra, int64_t next, int n) {
+  float4 kept = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [](float& sum, float x) {
+    if (not_finite(x)) sum += x;
   };
-  one(acc.x, v.x);
-  one(acc.y, v.y);
-  one(acc.z, v.z);
-  one(acc.w, v.w);
+  for (int y = 0; y < n; ++y) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(part + y * next + (y ? 0 : extra)));
+    add(kept.x, v.x);
+    add(kept.y, v.y);
+    add(kept.z, v.z);
+    add(kept.w, v.w);
+  }
+  if (not_finite(kept.x)) acc.x = kept.x;
+  if (not_finite(kept.y)) acc.y = kept.y;
+  if (not_finite(kept.z)) acc.z = kept.z;
+  if (not_finite(kept.w)) acc.w = kept.w;
+  return acc;
 }
 
 // Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
@@ -777,14 +788,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
               add(acc, f, v[y]);
             }
           }
-          if (there && odd_four(acc)) {  // factors that are 0 make a NaN of an infinity
-            float4 kept = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int y = 0; y < n; ++y) keep_infinite(kept, __ldcg(reinterpret_cast<const float4*>(&a.part_o[(size_t)(slot_of(b + y * step) + h) * HD + d])));
-            if (not_finite(kept.x)) acc.x = kept.x;
-            if (not_finite(kept.y)) acc.y = kept.y;
-            if (not_finite(kept.z)) acc.z = kept.z;
-            if (not_finite(kept.w)) acc.w = kept.w;
-          }
+          if (there && odd_four(acc))
+            acc = keep_infinite(acc, a.part_o + (size_t)(2 * b * HB + h) * HD + d, b == c0 ? HB * HD : 0, (int64_t)2 * step * HB * HD, n);
           __syncwarp();  // b's place is read by the HD / 4 lanes of a head, all of this warp: they are done
           if (!there) continue;
           if (final) {

@@ -658,7 +658,9 @@ int np_kv_copy_pages(const np_kv_desc* desc, void* dst_cache, const void* src_ca
  *   out[i][h] = sum_j softmax_j(scale * q[i][h] . k_j) v_j   over the lens[seqs[i]] tokens of sequence seqs[i]
  * (the new token among them: append it first).  Keys and values past a sequence's length have no effect.  A sequence of
  * length 0, and a row whose seqs[i] is negative (padding), give zeros and lse -inf, and so does a row whose scores are all
- * -inf.  fp32 scores, softmax and sums.
+ * -inf.  Else an infinity or a NaN among the values shows in the rows that see it, however small its weight.  fp32 scores,
+ * softmax and sums; sums are taken before they are divided, so bf16 values whose sum over the tokens passes fp32's range give a
+ * result that is not finite.
  *   q, out     n rows of n_heads heads; out may not overlap q, its strides are above 0 along more than one row or head
  *   scale      positive; times log2(e) finite
  *   lse        dev fp32 [n][n_heads] or NULL: log sum_j exp(scale * q . k_j)
@@ -681,8 +683,8 @@ int np_attn_decode(const np_kv_desc* desc, const void* cache, int32_t layer, con
  *   lse     dev fp32 [n_tokens][n_heads] or NULL
  *   status  dev int32 [1], zeroed by the caller before its first use
  * head_dim 64 or 128, n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= NP_ATTN_MAX_GROUP, 1 <= n <= NP_KV_MAX_SEQS.
- * Scores, softmax and sums in fp32; the probabilities are rounded to the rows' type for the second product.  Later tokens
- * and other prompts have no effect on a row, infinities and NaN among them. */
+ * Scores, softmax and sums in fp32, values that are not finite as for np_attn_decode; the probabilities are rounded to the rows'
+ * type for the second product.  Later tokens and other prompts have no effect on a row, infinities and NaN among them. */
 typedef struct np_attn_shape {
   int32_t dtype;        /* NP_T_* */
   int32_t n_heads;

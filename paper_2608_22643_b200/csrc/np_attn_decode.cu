@@ -31,10 +31,10 @@
 //   what the tokens make of it; joins take infinities as they are.
 //
 // Measured (pages of 64 scattered over the pool, caches larger than the L2 in turn): sixteen sequences of 0 to 4095 tokens, 32 heads
-// of 128, 57.5 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 165 us, 97 %; one of 131071 tokens, 64 heads over 8, 92.6 us,
-// 89 %; one of 100 tokens 4.6 us.  What is not the stream is the launch, three loads that depend on one another (length, page
+// of 128, 57.3 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 159 us, 100 %; one of 131071 tokens, 64 heads over 8, 91.9 us,
+// 89 %; one of 100 tokens 4.7 us.  What is not the stream is the launch, three loads that depend on one another (length, page
 // number, keys) and the joins.  Groups of more than eight heads are bound by the steps
-// between a warp's loads: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, 53.0 us, 76 % (69 % with keys and values
+// between a warp's loads: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, 53.8 us, 74 % (69 % with keys and values
 // in registers, 55 % with 16-byte asynchronous copies in place of TMA, 70 % with the chunks beyond asked into the L2 ahead, 74 % with
 // keys and values as two copies).
 #include <cuda_bf16.h>
@@ -815,7 +815,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 }
 
 // Heads of a block.  Sixteen read keys and values once for up to sixteen heads, eight have more warps: 64 sequences of 2000 tokens, 64
-// heads over 4, 53 us with sixteen and 81 with eight, which read everything twice.
+// heads over 4, 54 us with sixteen and 81 with eight, which read everything twice.
 int heads_per_block(int group) { return group <= 8 ? 8 : 16; }
 
 // A layer of the cache as (64 values, rows of a page's heads, halves of head_dim, keys and values, pages); a box is a chunk.

@@ -6,8 +6,9 @@
 // S, P and O in tensor memory; the softmax between them runs on the plain cores.  Per 128 x 128 scores at head_dim 128 the
 // products take 1024 cycles of the tensor cores, their operands as many of shared memory's bandwidth, and the exponentials 1024
 // cycles of the special function units, so all three have to overlap completely.  They do to 60 % (3260 cycles for two such tiles,
-// both pipes busy 60 % of the time); what is left is hand-overs between the roles.  8192 tokens, 64 heads over 8: 865 us (1270
-// TFLOP/s) as long as the clock holds, 955 and 1150 in the long run, at the power limit.
+// both pipes busy 60 % of the time); what is left is hand-overs between the roles.  8192 tokens, 64 heads over 8: 900 us (1220
+// TFLOP/s) as long as the clock holds, 960 to 1015 (1080 to 1150) in the long run, at the power limit.  With heads of 64 the exponentials
+// stay what they are and the products halve: 8192 tokens, 64 heads, 764 us (720 TFLOP/s), exponential units busy 66 %.
 //
 // * A block holds two tiles of 128 query rows of the same key-value head (or an SM two blocks of one tile, for short prompts).
 //   While the plain cores do one tile's softmax, the tensor cores do the other's products.  Roles: four warps to a tile (softmax and
@@ -29,7 +30,7 @@
 //   simpler, and cost 2 to 10 %: its code, mostly.)
 // * Short prompts wait for instructions: what is off the usual path (rescaling, the result) is kept in loops.  Unrolled, twelve
 //   prompts of 0 to 1500 tokens, 32 heads, took 90 us instead of 80.  Measured and dropped: exponentials on the FMA units by a
-//   polynomial (they are no less busy), two lanes to a row (the exchange costs what the halves save), scores read from tensor
+//   polynomial (they are no less busy; heads of 128), two lanes to a row (the exchange costs what the halves save), scores read from tensor
 //   memory 32 at a time, a warp of products for each tile (the tiles fall into step), the next block's first scores before the
 //   other tile's last product.
 //

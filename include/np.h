@@ -555,12 +555,13 @@ const char* np_trunk_last_error(void);
  * appended, in every layer, before their sequence is forked: which pages are full goes by lengths, and reserving grows those. */
 #define NP_T_BF16 0
 #define NP_T_FP16 1
+#define NP_KV_E4M3 16        /* added to a description's dtype: the cache holds 8 bits for each value */
 #define NP_KV_MAX_SEQS   1024
 #define NP_KV_MAX_PAGES  (1 << 22)
 #define NP_ATTN_MAX_GROUP 128
 
 typedef struct np_kv_desc {
-  int32_t dtype;         /* NP_T_*: of the cache, and of the rows that go in and out */
+  int32_t dtype;         /* NP_T_*: of the cache, and of the rows that go in and out; with NP_KV_E4M3 added, of the rows alone */
   int32_t n_layers;      /* >= 1 */
   int32_t n_kv_heads;    /* 1..1024 */
   int32_t head_dim;      /* 64 or 128 */
@@ -570,6 +571,16 @@ typedef struct np_kv_desc {
   int32_t max_pages;     /* entries of a row, 1..n_pages; max_pages * page_tokens < 2^31 */
   int32_t reserved[4];   /* 0 */
 } np_kv_desc;
+
+/* A cache with NP_KV_E4M3 in its description's dtype holds each row of head_dim values (of one token, key-value head, and keys or values) as
+ * head_dim numbers of 8 bits (e4m3: 4 bits of exponent, 3 of fraction, no infinities) and a power of two that all of them are times.
+ * A page is then 2 * n_kv_heads * page_tokens * (head_dim + 1) bytes, and the cache dev [n_layers][n_pages][page's bytes], 16-byte aligned:
+ *   e4m3   [2][n_kv_heads][page_tokens][head_dim]      values
+ *   uint8  [2][n_kv_heads][page_tokens]                127 + the exponent of their power of two
+ * A row is written with the least exponent e of -60 .. 120 for which its largest finite magnitude is at most 448 * 2^e; each value is
+ * rounded to nearest, ties to even, so it is off by at most 2^-4 of itself or 2^(e - 10).  Infinities and NaN become NaN.  np_kv_append,
+ * np_kv_append_rotated, np_kv_read and the attention calls know the form; page tables and the calls that move whole pages are the same
+ * for both. */
 
 /* Device arrays of a cache.  np_kv_reset writes the empty state into all of them. */
 typedef struct np_kv_tables {
@@ -603,6 +614,15 @@ typedef struct np_rows {
   int64_t head_stride;
 } np_rows;
 
+/* Heads of the calls that need no cache. */
+typedef struct np_attn_shape {
+  int32_t dtype;        /* NP_T_* */
+  int32_t n_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t reserved[4];  /* 0 */
+} np_attn_shape;
+
 /* Buffer sizes for a description.  Pure host arithmetic.  NP_E_INVAL on a bad description. */
 int np_kv_sizes(const np_kv_desc* desc, np_kv_sizes_out* out);
 
@@ -626,6 +646,46 @@ int np_kv_reserve(const np_kv_desc* desc, const np_kv_tables* tables, const int3
 int np_kv_append(const np_kv_desc* desc, void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* k,
                  const np_rows* v, int32_t n_tokens, const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n,
                  void* stream);
+
+/* Norm and rotation of queries and keys, for each row x of head_dim values (one token and head) by itself:
+ *   y = x / sqrt(mean(x^2) + eps) * gain          (y = x without a gain)
+ * and of the first rot_dim values the pairs (a, b) of y, the i-th by the angle t = position * freq[i]:
+ *   (a cos t - b sin t, b cos t + a sin t)
+ * All in fp32, the angles in fp64, rounded once to the rows' type.  Values from rot_dim on are normed alone. */
+#define NP_ROT_HALVES     0   /* pair i: values i and i + rot_dim / 2 */
+#define NP_ROT_NEIGHBOURS 1   /* pair i: values 2i and 2i + 1 */
+typedef struct np_rotation {
+  const double* freq;    /* dev [rot_dim / 2], radians per position; NULL where rot_dim is 0 */
+  const float* q_gain;   /* dev [head_dim]; NULL: queries are not normed */
+  const float* k_gain;   /* the same for keys */
+  int32_t rot_dim;       /* a multiple of 16, 0..head_dim */
+  int32_t pairs;         /* NP_ROT_* */
+  float eps;             /* positive (not below the normal numbers) and finite */
+  int32_t reserved[3];   /* 0 */
+} np_rotation;
+
+/* Queries and keys of new tokens, normed and rotated: row cu[i] + j is at position start[i] + j, j < cu[i + 1] - cu[i], as for
+ * np_kv_append.  Rows from cu[n] on (and before cu[0]), and those of an i with start[i] < 0, are left as they were.
+ *   q, q_out   n_tokens rows of n_heads heads;  k, k_out  n_tokens rows of n_kv_heads heads.  A result may be its input itself (the same
+ *              data and strides) and may not overlap the inputs or the other result in another way; its strides are above 0 along
+ *              more than one row or head
+ *   cu    dev [n + 1] ascending (NULL: one token each, n_tokens == n),  start  dev [n] */
+int np_attn_rotate(const np_attn_shape* shape, const np_rotation* rotation, const np_rows* q, const np_rows* k, const np_rows* q_out,
+                   const np_rows* k_out, int32_t n_tokens, const int32_t* cu, const int32_t* start, int32_t n, void* stream);
+
+/* np_attn_rotate whose keys go straight into their pages, and np_kv_append of the values, in one pass: the cache then holds what the two
+ * calls would have written, bit for bit.  Queries are rotated wherever their position is known, whether or not their keys have a place. */
+int np_kv_append_rotated(const np_kv_desc* desc, void* cache, int32_t layer, const np_kv_tables* tables, const np_rotation* rotation,
+                         const np_rows* q, int32_t n_heads, const np_rows* k, const np_rows* v, const np_rows* q_out, int32_t n_tokens,
+                         const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n, void* stream);
+
+/* The other way: keys and values of tokens that are in their pages, as rows.  Row cu[i] + j is position start[i] + j of sequence seqs[i];
+ * rows whose position is at or past the sequence's length, or in a page that is not there, and those that np_kv_append would pass over, are
+ * left as they were.  Values of an e4m3 cache are rounded to the rows' type; finite ones stay finite (what is past its largest becomes
+ * the largest).
+ *   k, v   n_tokens rows of n_kv_heads heads, written; strides above 0 along more than one row or head */
+int np_kv_read(const np_kv_desc* desc, const void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* k, const np_rows* v,
+               int32_t n_tokens, const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n, void* stream);
 
 /* Sequence dst[i] (empty, listed once) begins as a copy of sequence src[i] (dev [n] each): it shares the full pages, and a
  * partly filled last page is copied, in every layer, to a page of its own (list order, lowest free number first).  A
@@ -674,6 +734,28 @@ int np_attn_decode(const np_kv_desc* desc, const void* cache, int32_t layer, con
                    int32_t n_heads, const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse,
                    void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* For n_groups groups of rows (group g: rows cu[g] .. cu[g + 1] - 1 of a call with the sequences `seqs`), the tokens that all sequences of
+ * the group begin with in the same pages, full ones: what np_kv_fork has let them share and they still have in common.  0 for a group
+ * with fewer than two rows that have a sequence; rows with a negative number have none.  Holds until a sequence of them is freed or forked
+ * into, and for all layers.
+ *   seqs  dev [n] or NULL: 0..n-1,  cu  dev [n_groups + 1] ascending, 0 <= cu <= n,  shared  dev [n_groups] */
+int np_kv_shared(const np_kv_desc* desc, const np_kv_tables* tables, const int32_t* seqs, int32_t n, const int32_t* cu, int32_t n_groups,
+                 int32_t* shared, void* stream);
+
+/* np_attn_decode of rows whose groups share their first tokens: those are read and their scores taken once for all rows of a group, as one
+ * matrix product, and joined with what each row's own tokens give.  The result is np_attn_decode's but for rounding (the shared tokens'
+ * probabilities are rounded to the rows' type, as np_attn_prompt's are), and the same from run to run.
+ *   cu         dev [n_groups + 1] ascending, 0 <= cu <= n: the groups.  Rows outside of them share nothing
+ *   shared     dev [n_groups]: tokens, from np_kv_shared, or any multiple of page_tokens up to that; 0: nothing.  The pages of the group's first row
+ *              with a sequence are read for all of its rows.  Where a group's rows do not all have that many tokens, or they do not fill
+ *              pages, it shares nothing (NP_KV_S_LENGTH)
+ *   workspace  as np_attn_decode's, np_attn_shared_workspace_bytes long at least; the two calls may share one
+ * n_heads / n_kv_heads <= NP_ATTN_MAX_GROUP.  Over an e4m3 cache every row is computed by itself, as np_attn_decode does. */
+int np_attn_shared_workspace_bytes(const np_kv_desc* desc, int32_t n_heads, int32_t n, uint64_t* out);
+int np_attn_decode_shared(const np_kv_desc* desc, const void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* q,
+                          int32_t n_heads, const int32_t* seqs, int32_t n, const int32_t* cu, const int32_t* shared, int32_t n_groups,
+                          float scale, const np_rows* out, float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* Causal attention over n packed prompts: rows cu[s] .. cu[s + 1] - 1 are the tokens of prompt s in order, and each sees the
  * rows of its own prompt up to itself.  Rows of out and lse from cu[n] on (and before cu[0]) are left as they were.
  *   q, out  n_tokens rows of n_heads heads, k, v  n_tokens rows of n_kv_heads heads; strides above 0 along more than one
@@ -685,13 +767,6 @@ int np_attn_decode(const np_kv_desc* desc, const void* cache, int32_t layer, con
  * head_dim 64 or 128, n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= NP_ATTN_MAX_GROUP, 1 <= n <= NP_KV_MAX_SEQS.
  * Scores, softmax and sums in fp32, values that are not finite as for np_attn_decode; the probabilities are rounded to the rows'
  * type for the second product.  Later tokens and other prompts have no effect on a row, infinities and NaN among them. */
-typedef struct np_attn_shape {
-  int32_t dtype;        /* NP_T_* */
-  int32_t n_heads;
-  int32_t n_kv_heads;
-  int32_t head_dim;
-  int32_t reserved[4];  /* 0 */
-} np_attn_shape;
 int np_attn_prompt(const np_attn_shape* shape, const np_rows* q, const np_rows* k, const np_rows* v, const int32_t* cu, int32_t n,
                    int32_t n_tokens, float scale, const np_rows* out, float* lse, int32_t* status, void* stream);
 

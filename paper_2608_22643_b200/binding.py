@@ -43,6 +43,7 @@ EXPORTED = [
     "np_launch_count", "np_chain_launches", "np_speculate", "np_install_speculative", "np_get_speculative", "np_mlp_kernel_name", "np_selftest_bounded_wait", "np_predict_logits_noalloc", "np_noalloc_check", "np_noalloc_last_error",
     "np_trunk_workspace_floats", "np_trunk_forward", "np_trunk_last_error",
     "np_kv_sizes", "np_kv_reset", "np_kv_reserve", "np_kv_append", "np_kv_fork", "np_kv_free", "np_kv_compact", "np_kv_copy_pages",
+    "np_kv_append_rotated", "np_kv_read", "np_kv_shared", "np_attn_rotate", "np_attn_decode_shared", "np_attn_shared_workspace_bytes",
     "np_attn_workspace_bytes", "np_attn_decode", "np_attn_prompt", "np_attn_check", "np_attn_last_error",
 ]
 
@@ -88,7 +89,8 @@ class np_delta_view(C.Structure):
         "delta_ids", "delta_slots", "evict_ids", "overflow_ids", "active_ids", "active_slots", "counters")]
 
 
-NP_T_BF16, NP_T_FP16 = 0, 1
+NP_T_BF16, NP_T_FP16, NP_KV_E4M3 = 0, 1, 16
+NP_ROT_HALVES, NP_ROT_NEIGHBOURS = 0, 1
 NP_KV_S_PAGE, NP_KV_S_SEQ, NP_KV_S_LENGTH, NP_KV_S_TIMEOUT, NP_KV_S_FULL = 1, 2, 4, 8, 32
 
 
@@ -113,6 +115,12 @@ class np_rows(C.Structure):
 
 class np_attn_shape(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_heads", "n_kv_heads", "head_dim")] + [("reserved", C.c_int32 * 4)]
+
+
+class np_rotation(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("rot_dim", C.c_int32), ("pairs", C.c_int32),
+                ("eps", C.c_float), ("reserved", C.c_int32 * 3)]
+    room = None   # make_rotation: device, and values of a gain (-1: no gains)
 
 
 class NpError(RuntimeError):
@@ -192,6 +200,12 @@ def load() -> C.CDLL:
         "np_attn_decode": [kvd, vp, i32, kvt, rows, i32, vp, i32, C.c_float, rows, vp, vp, C.c_uint64, vp],
         "np_attn_prompt": [vp, rows, rows, rows, vp, i32, i32, C.c_float, rows, vp, vp, vp],
         "np_attn_check": [vp, vp],
+        "np_attn_rotate": [vp, vp, rows, rows, rows, rows, i32, vp, vp, i32, vp],
+        "np_kv_append_rotated": [kvd, vp, i32, kvt, vp, rows, i32, rows, rows, rows, i32, vp, vp, vp, i32, vp],
+        "np_kv_read": [kvd, vp, i32, kvt, rows, rows, i32, vp, vp, vp, i32, vp],
+        "np_kv_shared": [kvd, kvt, vp, i32, vp, i32, vp, vp],
+        "np_attn_shared_workspace_bytes": [kvd, i32, i32, C.POINTER(C.c_uint64)],
+        "np_attn_decode_shared": [kvd, vp, i32, kvt, rows, i32, vp, i32, vp, vp, i32, C.c_float, rows, vp, vp, C.c_uint64, vp],
     })
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -365,12 +379,13 @@ def _attn_check(rc: int) -> int:
 
 
 def make_kv_desc(dtype, n_layers: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int, max_seqs: int,
-                 max_pages: Optional[int] = None) -> np_kv_desc:
-    """``dtype``: torch.bfloat16 or torch.float16 (or an NP_T_* code)."""
+                 max_pages: Optional[int] = None, e4m3: bool = False) -> np_kv_desc:
+    """``dtype``: torch.bfloat16 or torch.float16 (or an NP_T_* code).  ``e4m3``: the cache holds 8 bits for each value; it is a uint8 tensor
+    [layers][pages][np_kv_sizes(desc).page_bytes] then."""
     code = _ATTN_DTYPE.get(dtype, dtype)
     if not isinstance(code, int):
         raise NpError(NP_E_INVAL, f"no cache of {dtype}: bfloat16 or float16")
-    return np_kv_desc(code, n_layers, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
+    return np_kv_desc(code | NP_KV_E4M3 if e4m3 else code, n_layers, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
                       n_pages if max_pages is None else max_pages)
 
 
@@ -384,6 +399,25 @@ def make_kv_tables(page_table, lens, refs, scratch, status) -> np_kv_tables:
     tables = np_kv_tables(*[None if t is None else t.data_ptr() for t in tensors])
     tables.room = (page_table.get_device(), page_table.numel(), lens.numel(), refs.numel(), -1 if scratch is None else scratch.numel())
     return tables
+
+
+def make_rotation(freq, q_gain=None, k_gain=None, neighbours: bool = False, eps: float = 1e-6) -> np_rotation:
+    """Norm and rotation by position.  ``freq``: float64 [rot_dim / 2], radians per position (None: no rotation); ``q_gain``, ``k_gain``: float32
+    [head_dim] (None: not normed); contiguous tensors of one CUDA device, which the caller keeps alive.  ``neighbours``: pairs are values 2i and
+    2i + 1, else i and i + rot_dim / 2."""
+    tensors = [t for t in (freq, q_gain, k_gain) if t is not None]
+    for t in tensors:
+        want = torch.float64 if t is freq else torch.float32
+        if t.device != tensors[0].device or not t.is_cuda or t.dtype is not want or not t.is_contiguous() or t.dim() != 1:
+            raise NpError(NP_E_INVAL, f"expected contiguous {want} vectors of one CUDA device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if q_gain is not None and k_gain is not None and q_gain.numel() != k_gain.numel():
+        raise NpError(NP_E_INVAL, f"gains of {q_gain.numel()} and {k_gain.numel()} values")
+    r = np_rotation(*[None if t is None or t.numel() == 0 else t.data_ptr() for t in (freq, q_gain, k_gain)], 0 if freq is None else 2 * freq.numel(),
+                    NP_ROT_NEIGHBOURS if neighbours else NP_ROT_HALVES, eps)
+    gain = q_gain if q_gain is not None else k_gain
+    if tensors:
+        r.room = (tensors[0].get_device(), -1 if gain is None else gain.numel())
+    return r
 
 
 def np_kv_sizes(desc: np_kv_desc) -> np_kv_sizes_out:
@@ -404,6 +438,21 @@ def np_kv_reserve(desc, tables, seqs, n_new, start_out=None, stream=None) -> int
 def np_kv_append(desc, cache, layer: int, tables, k, v, seqs, cu, start, stream=None) -> int:
     """``cu`` None: one token for each sequence."""
     return _attn().kv_append(desc, cache, layer, tables, k, v, seqs, cu, start, stream)
+
+
+def np_kv_append_rotated(desc, cache, layer: int, tables, rotation, q, k, v, q_out, seqs, cu, start, stream=None) -> int:
+    """np_attn_rotate whose keys go into the cache, and np_kv_append of the values, in one pass."""
+    return _attn().kv_append_rotated(desc, cache, layer, tables, rotation, q, k, v, q_out, seqs, cu, start, stream)
+
+
+def np_kv_read(desc, cache, layer: int, tables, k, v, seqs, cu, start, stream=None) -> int:
+    """``k``, ``v``: rows that are written; ``cu`` None: one token for each sequence."""
+    return _attn().kv_read(desc, cache, layer, tables, k, v, seqs, cu, start, stream)
+
+
+def np_kv_shared(desc, tables, seqs, cu, shared, n: Optional[int] = None, stream=None) -> int:
+    """``cu`` int32, one more than groups; ``shared`` int32, one for each group; ``seqs`` None: rows are sequences 0..n-1 (``n`` None: all)."""
+    return _attn().kv_shared(desc, tables, seqs, cu, shared, n, stream)
 
 
 def np_kv_fork(desc, cache, tables, src, dst, stream=None) -> int:
@@ -432,6 +481,23 @@ def np_attn_workspace_bytes(desc, n_heads: int, n: int) -> int:
 def np_attn_decode(desc, cache, layer: int, tables, q, out, workspace, seqs=None, scale: Optional[float] = None, lse=None, stream=None) -> int:
     """``scale`` None: 1 / sqrt(head_dim).  ``workspace``: a uint8 tensor, zeroed before its first use."""
     return _attn().attn_decode(desc, cache, layer, tables, q, out, workspace, seqs, scale, lse, stream)
+
+
+def np_attn_rotate(rotation, q, k, q_out, k_out, cu, start, stream=None) -> int:
+    """``q_out`` may be ``q`` and ``k_out`` may be ``k``; ``cu`` None: one token for each of ``start``."""
+    return _attn().attn_rotate(rotation, q, k, q_out, k_out, cu, start, stream)
+
+
+def np_attn_shared_workspace_bytes(desc, n_heads: int, n: int) -> int:
+    out = C.c_uint64()
+    _attn_check(load().np_attn_shared_workspace_bytes(C.byref(desc), n_heads, n, C.byref(out)))
+    return out.value
+
+
+def np_attn_decode_shared(desc, cache, layer: int, tables, q, out, workspace, cu, shared, seqs=None, scale: Optional[float] = None, lse=None,
+                          stream=None) -> int:
+    """np_attn_decode of rows whose groups (``cu``) share their first ``shared`` tokens."""
+    return _attn().attn_decode_shared(desc, cache, layer, tables, q, out, workspace, cu, shared, seqs, scale, lse, stream)
 
 
 def np_attn_prompt(q, k, v, cu, out, status, scale: Optional[float] = None, lse=None, stream=None) -> int:

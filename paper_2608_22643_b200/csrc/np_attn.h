@@ -1,4 +1,4 @@
-// Shared by the translation units of the paged cache and its attention (np_kv.cu, np_attn_decode.cu, np_attn_prompt.cu).
+// Shared by the translation units of the paged cache and its attention (np_kv.cu, np_kv_rows.cu, np_attn_decode.cu, np_attn_prompt.cu).
 #pragma once
 
 #include <cuda.h>
@@ -30,6 +30,12 @@ int fail_cuda(cudaError_t e);
 
 // Text of what is wrong with a description; NULL: nothing.
 const char* desc_error(const np_kv_desc* d);
+inline bool held_in_8(const np_kv_desc* d) { return (d->dtype & NP_KV_E4M3) != 0; }
+inline int row_type(const np_kv_desc* d) { return d->dtype & ~NP_KV_E4M3; }
+// Bytes of one page of one layer.
+inline int64_t page_bytes(const np_kv_desc* d) {
+  return (int64_t)2 * d->n_kv_heads * d->page_tokens * (held_in_8(d) ? d->head_dim + 1 : d->head_dim * 2);
+}
 const char* rows_error(const np_rows* r);
 bool tables_ok(const np_kv_tables* t);  // no pointer NULL
 
@@ -55,6 +61,19 @@ inline EncodeFn encode_fn() {
 
 // SM count of the current device; false: no device.
 bool device_sms(int* sms);
+
+// np_kv_append into a cache of 8 bits, behind the checks (np_kv_rows.cu).
+int append_held(const np_kv_desc* d, void* cache, int32_t layer, const np_kv_tables* t, const np_rows* k, const np_rows* v, int32_t n_tokens,
+                const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n, void* stream);
+
+// np_attn_decode behind its checks, and these (np_attn_decode.cu); shared: rows begin behind what their groups share.
+struct SharedArgs;
+int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads, const int32_t* seqs,
+           int32_t n, float scale2, const np_rows* out, float* lse, void* workspace, const SharedArgs* shared, int sms, cudaStream_t s);
+uint64_t decode_space_bytes(int n_kv_heads, int group, int n);
+const char* decode_heads_error(const np_kv_desc* d, int n_heads, int n);
+const char* decode_error(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads, int32_t n,
+                         float scale, const np_rows* out, const void* workspace, float* scale2);
 
 // A launch whose blocks may be scheduled while the kernel before it in the stream ends; the kernel begins with
 // npp::pdl_wait_prior().

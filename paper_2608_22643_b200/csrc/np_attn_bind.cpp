@@ -118,13 +118,24 @@ np_rows rows(PyObject* o, at::ScalarType type, int device, int64_t tokens, int64
 }
 
 at::ScalarType type_of(const np_kv_desc& d) {
-  if (d.dtype != NP_T_BF16 && d.dtype != NP_T_FP16) refuse("desc: dtype must be NP_T_BF16 or NP_T_FP16");
-  return d.dtype == NP_T_BF16 ? at::kBFloat16 : at::kHalf;
+  const int type = d.dtype & ~NP_KV_E4M3;
+  if (type != NP_T_BF16 && type != NP_T_FP16) refuse("desc: dtype must be NP_T_BF16 or NP_T_FP16, or one of them and NP_KV_E4M3");
+  return type == NP_T_BF16 ? at::kBFloat16 : at::kHalf;
 }
 
 void* cache_of(PyObject* o, const np_kv_desc& d, int device, const char* name) {
   const at::Tensor& t = tensor(o, name);
   const at::ScalarType type = type_of(d);
+  if (d.dtype & NP_KV_E4M3) {
+    const int64_t page = (int64_t)2 * d.n_kv_heads * d.page_tokens * (d.head_dim + 1);
+    if (t.get_device() != device || t.scalar_type() != at::kByte || !t.is_contiguous() || t.dim() != 3 || t.size(0) != d.n_layers || t.size(1) != d.n_pages ||
+        t.size(2) != page) {
+      std::ostringstream s;
+      s << name << ": expected a contiguous cache [" << d.n_layers << "][" << d.n_pages << "][" << page << "] of bytes on the current CUDA device, got " << describe(t);
+      refuse(s.str());
+    }
+    return t.data_ptr();
+  }
   if (t.get_device() != device || t.scalar_type() != type || !t.is_contiguous() || t.dim() != 6 || t.size(0) != d.n_layers || t.size(1) != d.n_pages ||
       t.size(2) != 2 || t.size(3) != d.n_kv_heads || t.size(4) != d.page_tokens || t.size(5) != d.head_dim) {
     std::ostringstream s;
@@ -330,6 +341,126 @@ PyObject* attn_prompt(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// A rotation whose tensors (if make_rotation made it: (device, head_dim of its gains or -1)) serve the call.
+np_rotation rotation_of(PyObject* o, int64_t head_dim, int device) {
+  const np_rotation r = structure<np_rotation>(o, "rotation");
+  PyObject* room = PyObject_GetAttr(o, g_room);
+  if (!room) throw Raised{};
+  long long has[2] = {0};
+  const bool known = PyTuple_Check(room) && PyTuple_GET_SIZE(room) == 2;
+  if (known)
+    for (int i = 0; i < 2; ++i) has[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(room, i));
+  Py_DECREF(room);
+  if (PyErr_Occurred()) throw Raised{};
+  if (known && (has[0] != device || (has[1] >= 0 && has[1] != head_dim))) {
+    std::ostringstream s;
+    s << "rotation: tensors on device " << has[0] << " with gains of " << has[1] << " values do not serve heads of " << head_dim << " on device " << device;
+    refuse(s.str());
+  }
+  return r;
+}
+
+// The sequences' starts, and the rows that they say where to put.
+struct Tokens {
+  int n;
+  const int32_t *seqs, *cu, *start;
+  Tokens(PyObject* seqs_, PyObject* cu_, PyObject* start_, int dev)
+      : n(as_int(tensor(start_, "start").numel(), "start")),
+        seqs(ints(seqs_, dev, n, "seqs")),
+        cu(ints(cu_, dev, (int64_t)n + 1, "cu")),
+        start(ints(start_, dev, n, "start")) {}
+};
+
+PyObject* attn_rotate(PyObject*, Args a, Py_ssize_t n) {
+  return answer(n, 8, [&] {
+    const int dev = current_device();
+    const at::Tensor &qt = tensor(a[1], "q"), &kt = tensor(a[2], "k");
+    if (qt.dim() != 3 || kt.dim() != 3) refuse("q and k: expected rows [tokens][heads][head_dim], got " + describe(qt) + " and " + describe(kt));
+    const at::ScalarType type = qt.scalar_type();
+    if (type != at::kBFloat16 && type != at::kHalf) refuse("q: expected bfloat16 or float16, got " + describe(qt));
+    const int tokens = as_int(qt.size(0), "q"), heads = as_int(qt.size(1), "q"), kv = as_int(kt.size(1), "k"), hd = as_int(qt.size(2), "q");
+    const np_rotation r = rotation_of(a[0], hd, dev);
+    const np_rows q = rows(a[1], type, dev, tokens, heads, hd, "q"), k = rows(a[2], type, dev, tokens, kv, hd, "k"),
+                  qo = rows(a[3], type, dev, tokens, heads, hd, "q_out"), ko = rows(a[4], type, dev, tokens, kv, hd, "k_out");
+    const Tokens w(Py_None, a[5], a[6], dev);
+    void* s = stream_of(a[7]);
+    const np_attn_shape shape = {type == at::kBFloat16 ? NP_T_BF16 : NP_T_FP16, heads, kv, hd, {0, 0, 0, 0}};
+    return outside([&] { return np_attn_rotate(&shape, &r, &q, &k, &qo, &ko, tokens, w.cu, w.start, w.n, s); });
+  });
+}
+
+PyObject* kv_append_rotated(PyObject*, Args a, Py_ssize_t n) {
+  return answer(n, 13, [&] {
+    const int dev = current_device();
+    const np_kv_desc d = structure<np_kv_desc>(a[0], "desc");
+    void* cache = cache_of(a[1], d, dev, "cache");
+    const int layer = int_of(a[2], "layer");
+    const np_kv_tables t = tables_of(a[3], d, dev, "tables");
+    const np_rotation r = rotation_of(a[4], d.head_dim, dev);
+    const at::Tensor& qt = tensor(a[5], "q");
+    if (qt.dim() != 3) refuse("q: expected rows [tokens][heads][head_dim], got " + describe(qt));
+    const int tokens = as_int(qt.size(0), "q"), heads = as_int(qt.size(1), "q");
+    const at::ScalarType type = type_of(d);
+    const np_rows q = rows(a[5], type, dev, tokens, heads, d.head_dim, "q"), k = rows(a[6], type, dev, tokens, d.n_kv_heads, d.head_dim, "k"),
+                  v = rows(a[7], type, dev, tokens, d.n_kv_heads, d.head_dim, "v"), qo = rows(a[8], type, dev, tokens, heads, d.head_dim, "q_out");
+    const Tokens w(a[9], a[10], a[11], dev);
+    void* s = stream_of(a[12]);
+    return outside([&] { return np_kv_append_rotated(&d, cache, layer, &t, &r, &q, heads, &k, &v, &qo, tokens, w.seqs, w.cu, w.start, w.n, s); });
+  });
+}
+
+PyObject* kv_read(PyObject*, Args a, Py_ssize_t n) {
+  return answer(n, 10, [&] {
+    const int dev = current_device();
+    const np_kv_desc d = structure<np_kv_desc>(a[0], "desc");
+    const void* cache = cache_of(a[1], d, dev, "cache");
+    const int layer = int_of(a[2], "layer");
+    const np_kv_tables t = tables_of(a[3], d, dev, "tables");
+    const at::Tensor& kt = tensor(a[4], "k");
+    const int tokens = kt.dim() > 0 ? as_int(kt.size(0), "k") : 0;
+    const np_rows k = rows(a[4], type_of(d), dev, tokens, d.n_kv_heads, d.head_dim, "k"), v = rows(a[5], type_of(d), dev, tokens, d.n_kv_heads, d.head_dim, "v");
+    const Tokens w(a[6], a[7], a[8], dev);
+    void* s = stream_of(a[9]);
+    return outside([&] { return np_kv_read(&d, cache, layer, &t, &k, &v, tokens, w.seqs, w.cu, w.start, w.n, s); });
+  });
+}
+
+PyObject* kv_shared(PyObject*, Args a, Py_ssize_t n) {
+  return answer(n, 7, [&] {
+    const int dev = current_device();
+    const np_kv_desc d = structure<np_kv_desc>(a[0], "desc");
+    const np_kv_tables t = tables_of(a[1], d, dev, "tables");
+    const int groups = as_int(tensor(a[4], "shared").numel(), "shared");
+    const int m = a[5] != Py_None ? int_of(a[5], "n") : a[2] != Py_None ? as_int(tensor(a[2], "seqs").numel(), "seqs") : d.max_seqs;
+    const int32_t *seqs = ints(a[2], dev, m, "seqs"), *cu = ints(a[3], dev, (int64_t)groups + 1, "cu");
+    int32_t* shared = ints(a[4], dev, groups, "shared");
+    void* s = stream_of(a[6]);
+    return outside([&] { return np_kv_shared(&d, &t, seqs, m, cu, groups, shared, s); });
+  });
+}
+
+PyObject* attn_decode_shared(PyObject*, Args a, Py_ssize_t n) {
+  return answer(n, 13, [&] {
+    const int dev = current_device();
+    const np_kv_desc d = structure<np_kv_desc>(a[0], "desc");
+    const void* cache = cache_of(a[1], d, dev, "cache");
+    const int layer = int_of(a[2], "layer");
+    const np_kv_tables t = tables_of(a[3], d, dev, "tables");
+    const at::Tensor &qt = tensor(a[4], "q"), &wt = tensor(a[6], "workspace");
+    if (qt.dim() != 3) refuse("q: expected rows [sequences][heads][head_dim], got " + describe(qt));
+    const int m = as_int(qt.size(0), "q"), heads = as_int(qt.size(1), "q");
+    const np_rows q = rows(a[4], type_of(d), dev, m, heads, d.head_dim, "q"), out = rows(a[5], type_of(d), dev, m, heads, d.head_dim, "out");
+    void* space = array<void>(a[6], at::kByte, dev, 0, "workspace");
+    const uint64_t bytes = wt.numel();
+    const int groups = as_int(tensor(a[8], "shared").numel(), "shared");
+    const int32_t *cu = ints(a[7], dev, (int64_t)groups + 1, "cu"), *shared = ints(a[8], dev, groups, "shared"), *seqs = ints(a[9], dev, m, "seqs");
+    const float scale = (float)scale_of(a[10], d.head_dim);
+    float* lse = array<float>(a[11], at::kFloat, dev, (int64_t)m * heads, "lse");
+    void* s = stream_of(a[12]);
+    return outside([&] { return np_attn_decode_shared(&d, cache, layer, &t, &q, heads, seqs, m, cu, shared, groups, scale, &out, lse, space, bytes, s); });
+  });
+}
+
 PyObject* attn_check(PyObject*, Args a, Py_ssize_t n) {
   return answer(n, 2, [&] {
     const int32_t* status = ints(a[0], current_device(), 1, "status");
@@ -346,6 +477,7 @@ PyObject* setup(PyObject*, PyObject* type) {
 #define NP_CALL(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {NP_CALL(kv_reset),   NP_CALL(kv_reserve),    NP_CALL(kv_append),   NP_CALL(kv_fork),     NP_CALL(kv_free),
                            NP_CALL(kv_compact), NP_CALL(kv_copy_pages), NP_CALL(attn_decode), NP_CALL(attn_prompt), NP_CALL(attn_check),
+                           NP_CALL(attn_rotate), NP_CALL(kv_append_rotated), NP_CALL(kv_read), NP_CALL(kv_shared), NP_CALL(attn_decode_shared),
                            {"setup", setup, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "np_attn_bind", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

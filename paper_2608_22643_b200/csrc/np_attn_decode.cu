@@ -45,6 +45,7 @@
 #include <type_traits>
 
 #include "np_attn.h"
+#include "np_attn_groups.cuh"
 #include "np_device.cuh"
 #include "np_internal.h"
 #include "np_pipe.cuh"
@@ -81,7 +82,12 @@ struct DecodeArgs {
   float scale2;              // scale * log2(e)
   int n, n_heads, n_kv_heads, group, blocks_of_heads;  // heads of a group: blocks_of_heads pieces of HB
   int shift, n_pages, max_seqs, max_pages;
+  int64_t page_bytes;
+  SharedArgs shared;  // kTail: tokens that other rows share, and their partial results
 };
+
+// How keys and values get to the products: in the rows' type, up to eight or sixteen heads of a group at once; in 8 bits, the same.
+enum Form { kEight, kSixteen, kHeldEight, kHeldSixteen };
 
 template <class T>
 struct Half2;
@@ -139,6 +145,16 @@ __device__ __forceinline__ void load_tiles_transposed(uint32_t addr, uint32_t (&
                : "r"(addr)
                : "memory");
 }
+// Four e4m3 values as fp16, which holds all of them: bytes 0 and 1, bytes 2 and 3.
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+// Two of the queries' values in fp32.
+template <class T>
+__device__ __forceinline__ float2 widen2(uint32_t w) {
+  if constexpr (std::is_same<T, __half>::value) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  else return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
 // keys and values of sixteen tokens: (64 values, rows of a page's heads, halves of head_dim, keys and values, pages)
 __device__ __forceinline__ void tma_load_chunk(uint32_t dst, const CUtensorMap* map, int row, int page, uint64_t* bar) {
   asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %2, %4}], [%5];" ::"r"(dst),
@@ -146,6 +162,18 @@ __device__ __forceinline__ void tma_load_chunk(uint32_t dst, const CUtensorMap* 
                : "memory");
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// 16 or 8 bytes that are used once
+__device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[4]) {
+  const uint4 v = npd::ldg_stream(p);
+  w[0] = v.x;
+  w[1] = v.y;
+  w[2] = v.z;
+  w[3] = v.w;
+}
+__device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[2]) {
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+}
 
 // a / b, by 32 bits where they do
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
@@ -181,16 +209,16 @@ __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x)
 // head_dim; part_o: of the partial result, nullptr: out.  seen: HD ints of shared memory that are free.  One of 131071 tokens a NaN, 64
 // heads over 8: 201 us a call in place of 93. (One block that looks through all of V behind the join: 10 ms.)
 template <class T, int HD>
-__device__ __noinline__ void mend(const DecodeArgs& a, uint32_t odd, int row, int pair, int ta, int tb, int h0, int heads, float* part_o, int* seen) {
+__device__ __noinline__ void mend(const DecodeArgs& a, uint32_t odd, int row, int first, int pair, int ta, int tb, int h0, int heads, float* part_o, int* seen) {
   constexpr int kCols = HD / 8, kStep = kThreads / kCols, kAhead = 4;
   constexpr uint32_t kInf = infinity_bits<T>();
   const int tid = threadIdx.x;
   for (int d = tid; d < HD; d += kThreads) seen[d] = 0;
   __syncthreads();
   int seq;
-  const int64_t len = min((int64_t)row_len(a, row, &seq), (int64_t)tb * kTile);
+  const int64_t len = min((int64_t)row_len(a, row, &seq) - first, (int64_t)tb * kTile);
   const int col = tid % kCols;
-  const int32_t* pages = a.table + (size_t)seq * a.max_pages;
+  const int32_t* pages = a.table + (size_t)seq * a.max_pages + (first >> a.shift);
   const int64_t head_bytes = (int64_t)(HD * 2) << a.shift;
   const char* v = a.cache + (a.n_kv_heads + pair / a.blocks_of_heads) * head_bytes + col * 16;
   uint32_t bits = 0;  // value x of the column: 1 << x a NaN, 256 << x inf, 65536 << x -inf
@@ -254,11 +282,75 @@ __device__ __noinline__ float4 keep_infinite(float4 acc, const float* part, int6
   return acc;
 }
 
+// The partial results of the `tokens` that row i and its group share join those of its own: four values of head h, its maximum and its sum.
+template <int HD>
+__device__ __forceinline__ void join_shared(const DecodeArgs& a, int tokens, int group, int i, int h, int d, float4& acc, float& top, float& sum) {
+  npp::pdl_wait_prior();
+  const SharedArgs& s = a.shared;
+  const GroupPlan plan = s.plan[group];
+  const LinePlan line = *s.line;
+  const int kvh = h / a.group, member = i - plan.row0, block = member / s.members, in_block = member - block * s.members, tile = in_block / s.tile_members;
+  const int row = tile * kSharedTile + (in_block - tile * s.tile_members) * a.group + h - kvh * a.group;
+  const int64_t tiles = (tokens + kSharedTile - 1) / kSharedTile, w = plan.first_w + ((int64_t)kvh * plan.row_blocks + block) * tiles;
+  auto block_of = [&](int64_t x) { return (int)(x < line.more * (line.each + 1) ? divide(x, line.each + 1) : line.more + divide(x - line.more * (line.each + 1), line.each)); };
+  const int c0 = block_of(w), c1 = block_of(w + tiles - 1);
+  constexpr int kAhead = 4;
+  const float own[4] = {acc.x, acc.y, acc.z, acc.w};
+  for (int b0 = c0; b0 <= c1; b0 += kAhead) {
+    float2 ml[kAhead];
+    float4 v[kAhead];
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) {
+      ml[y] = make_float2(-INFINITY, 0.f);
+      v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (b0 + y > c1) continue;
+      const int64_t slot = c0 == c1 ? (int64_t)i * a.n_heads + h : (int64_t)(2 * (b0 + y) + (b0 + y == c0)) * s.part_rows + row;
+      ml[y] = __ldcg(reinterpret_cast<const float2*>((c0 == c1 ? s.row_ml : s.part_ml) + slot * 2));
+      v[y] = __ldcg(reinterpret_cast<const float4*>((c0 == c1 ? s.row_o : s.part_o) + slot * HD + d));
+    }
+    float now = top;
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) now = fmaxf(now, ml[y].x);
+    const float use = now == -INFINITY ? 0.f : now, f0 = exp2_fast(top - use);
+    top = now;
+    sum *= f0;
+    acc = make_float4(acc.x * f0, acc.y * f0, acc.z * f0, acc.w * f0);
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) {
+      const float f = exp2_fast(ml[y].x - use);
+      sum += f * ml[y].y;
+      acc.x += f * v[y].x;
+      acc.y += f * v[y].y;
+      acc.z += f * v[y].z;
+      acc.w += f * v[y].w;
+    }
+  }
+  if (not_finite(sum) || !(not_finite(acc.x) || not_finite(acc.y) || not_finite(acc.z) || not_finite(acc.w))) return;
+  // factors that are 0 make a NaN of an infinity: what is not finite is what the parts that are not add up to
+  float* const to[4] = {&acc.x, &acc.y, &acc.z, &acc.w};
+  for (int x = 0; x < 4; ++x) {
+    float kept = not_finite(own[x]) ? own[x] : 0.f;
+    for (int b = c0; b <= c1; ++b) {
+      const int64_t slot = c0 == c1 ? (int64_t)i * a.n_heads + h : (int64_t)(2 * b + (b == c0)) * s.part_rows + row;
+      const float v = __ldcg((c0 == c1 ? s.row_o : s.part_o) + slot * HD + d + x);
+      if (not_finite(v)) kept += v;
+    }
+    if (not_finite(kept)) *to[x] = kept;
+  }
+}
+
 // Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
 // accumulators.  us with one more and with this many (sixteen heads: with keys and values in registers): 128 values, eight heads, four blocks 113 (the long sequence) and 186 (64 of 1000),
 // three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16 sequences of 2000, five
 // 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
-constexpr int blocks_per_sm(int hd, int heads) { return hd == 64 ? (heads == 8 ? 4 : 3) : (heads == 8 ? 3 : 2); }
+constexpr int blocks_per_sm(int hd, int form) {
+  return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 2 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
+}
+
+// In 8 bits sums are of 2^(s - m + kHeldShift): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.
+constexpr float kHeldShift = 30.f, kHeldUp = 0x1p30f;
+
+constexpr uint32_t kTailBytes = NP_KV_MAX_SEQS * 6;  // of what kTail keeps of the groups
 
 constexpr int kSlots = 2;  // sixteen heads: chunks of a warp on their way
 
@@ -273,11 +365,15 @@ struct WarpWaits {
   }
 };
 
-template <class T, int HD, bool kWide>
-__global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kWide ? 16 : 8))
+// kTail: rows begin behind the tokens that their group shares, whose partial results are joined to theirs.
+template <class T, int HD, int kForm, bool kTail>
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kForm))
 k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
-  constexpr int HB = kWide ? 16 : 8;  // heads of a block, at most
-  constexpr int KV = HD / 32;        // 16-byte pieces of a key row per lane
+  constexpr bool kWide = kForm == kSixteen, kHeld = kForm == kHeldEight || kForm == kHeldSixteen;
+  constexpr int HB = kForm == kSixteen || kForm == kHeldSixteen ? 16 : 8;  // heads of a block, at most
+  constexpr int NT = HB / 8, NH = kHeld ? 2 * NT : 2;  // in 8 bits: eights of heads; heads of a lane's scores
+  constexpr int KV = kHeld ? HD / 64 : HD / 32;        // 16-byte pieces of a key row per lane
+  constexpr int VW = HD / 32;                          // in 8 bits: words of a value row per lane
   constexpr int VC = HD / 64;        // 16-byte pieces of a value row per lane
   constexpr int QV = HB * HD / 8 / kThreads > 0 ? HB * HD / 8 / kThreads : 1;  // 16-byte pieces of the queries per thread
   // Sixteen heads: sixteen-value steps along head_dim; bytes of a chunk's keys, and of its keys and values
@@ -294,22 +390,46 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   __shared__ int64_t s_wsum[kWarps];
   __shared__ int s_last;
   __shared__ volatile int s_lost[kWarps];  // a wait of the warp was given up
+  int* const s_first = reinterpret_cast<int*>(s_dyn);                                    // kTail: tokens that the row's group shares
+  uint16_t* const s_group = reinterpret_cast<uint16_t*>(s_dyn + NP_KV_MAX_SEQS * 4);     // and the group
   if (kWide && (threadIdx.x & 31) == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
     for (int i = 0; i < kSlots; ++i) npp::mbar_init(&s_full[threadIdx.x >> 5][i], 1);
     s_lost[threadIdx.x >> 5] = 0;
     npp::fence_barrier_init();
   }
-  npp::pdl_wait_prior();
+  // The kernel of the shared tokens lets this one begin when all that came before it is done; its own results are waited for where they are
+  // needed, and by every block before it leaves.
+  if (!kTail) npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
   const int pairs = a.n_kv_heads * a.blocks_of_heads;   // (key-value head, block of its query heads)
+
+  if constexpr (kTail) {
+    for (int i = tid; i < a.n; i += kThreads) s_first[i] = 0;
+    __syncthreads();
+    for (int x = wid; x < a.shared.n_groups; x += kWarps) {
+      int lo, hi, seq;
+      group_rows(a.shared, a.n, x, &lo, &hi);
+      const int tokens = group_tokens(a.shared, x, lo, hi, a.seqs, a.lens, a.max_seqs, a.max_pages, a.shift, a.status, &seq);
+      for (int i = lo + lane; i < hi; i += 32) {
+        s_first[i] = tokens;
+        s_group[i] = (uint16_t)x;
+      }
+    }
+    __syncthreads();
+  }
+  // tokens of row i of the call that are its own
+  auto own_len = [&](int i, int* seq) {
+    const int len = row_len(a, i, seq);
+    return kTail && len > 0 ? len - s_first[i] : len;
+  };
 
   // ---- units (tiles, and a group's start) of every row, summed up; rows without tokens are answered here
   int64_t run = 0;
   if (a.n <= 32) {  // every warp by itself: all write the same
     int len = 0, seq = -1;
-    if (lane < a.n) len = row_len(a, lane, &seq);
+    if (lane < a.n) len = own_len(lane, &seq);
     int64_t inc = len > 0 ? ((int64_t)len + kTile - 1) / kTile + kStart : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -323,7 +443,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     for (int base = 0; base < a.n; base += kThreads) {
       const int i = base + tid;
       int len = 0, seq = -1;
-      if (i < a.n) len = row_len(a, i, &seq);
+      if (i < a.n) len = own_len(i, &seq);
       int64_t inc = len > 0 ? ((int64_t)len + kTile - 1) / kTile + kStart : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -339,8 +459,28 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       __syncthreads();
     }
   }
+  // four values of a head's result; its log of the sum with the first
+  auto result = [&](int i, int h, int d, float4 acc, float top, float sum) {
+    if constexpr (kTail) {
+      if (s_first[i] > 0) join_shared<HD>(a, s_first[i], s_group[i], i, h, d, acc, top, sum);
+    }
+    const float use = top == -INFINITY ? 0.f : top;
+    const bool none = sum == 0.f;
+    const float inv = none ? 0.f : 1.f / sum;
+    uint2 r;
+    if constexpr (kHeld) acc = make_float4(acc.x * kHeldUp, acc.y * kHeldUp, acc.z * kHeldUp, acc.w * kHeldUp);
+    r.x = (uint32_t)Half2<T>::round(none ? 0.f : acc.x * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.y * inv) << 16;
+    r.y = (uint32_t)Half2<T>::round(none ? 0.f : acc.z * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.w * inv) << 16;
+    *reinterpret_cast<uint2*>(a.out + i * a.o_token + (int64_t)h * a.o_head + d) = r;
+    if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = none ? -INFINITY : (kHeld ? use - kHeldShift : use) * kLn2 + logf(sum);
+  };
   for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
     if (s_end[i] != (i ? s_end[i - 1] : 0)) continue;
+    int seq;
+    if (kTail && s_first[i] > 0 && row_len(a, i, &seq) > 0) {  // all of its tokens are shared
+      for (int x = tid; x < a.n_heads * (HD / 4); x += kThreads) result(i, x / (HD / 4), x % (HD / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
+      continue;
+    }
     for (int e = tid; e < a.n_heads * (HD / 8); e += kThreads) {
       const int h = e / (HD / 8), d = e % (HD / 8) * 8;
       *reinterpret_cast<uint4*>(a.out + i * a.o_token + h * a.o_head + d) = make_uint4(0, 0, 0, 0);
@@ -350,7 +490,10 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   // the line's W units over G blocks: the first `more` blocks take each + 1 of them, the others each
   const int64_t W = run * pairs;
   const int G = (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
-  if ((int)blockIdx.x >= G) return;
+  if ((int)blockIdx.x >= G) {
+    if (kTail) npp::pdl_wait_prior();
+    return;
+  }
   const int64_t each = divide(W, G), more = W - each * G;
   auto block_of = [&](int64_t w) { return (int)(w < more * (each + 1) ? divide(w, each + 1) : more + divide(w - more * (each + 1), each)); };
   int64_t w0 = blockIdx.x * each + min((int64_t)blockIdx.x, more);
@@ -366,7 +509,9 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     row = lo;
   }
 
-  const int64_t head_bytes = (int64_t)(HD * 2) << a.shift, page_bytes = 2 * a.n_kv_heads * head_bytes;
+  constexpr int kRowBytes = kHeld ? HD : HD * 2;
+  const int64_t head_bytes = (int64_t)kRowBytes << a.shift, page_bytes = a.page_bytes;
+  const int64_t exponents = 2 * a.n_kv_heads * head_bytes;  // in 8 bits: of a page, from its start
   struct Piece {  // tiles [ta, tb) of one (row, pair)
     int row, pair, h0, heads, len, tiles, ta, tb;
     int64_t first_w;  // of its pair, on the line
@@ -374,6 +519,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     int first_row;    // of its key-value head in a page
     const char* kbase;
     const char* vbase;
+    const char* ebase;
   };
   // the next piece with tokens from w0 on; false: none is left
   auto next_piece = [&](Piece& p) {
@@ -391,31 +537,34 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       p.pair = pair;
       p.tiles = (int)(units - kStart);
       int seq;
-      p.len = row_len(a, row, &seq);
+      p.len = own_len(row, &seq);
       const int kvh = pair / a.blocks_of_heads, hb = pair - kvh * a.blocks_of_heads;
       p.h0 = kvh * a.group + hb * HB;
       p.heads = min(HB, a.group - hb * HB);
-      p.pages = a.table + (size_t)seq * a.max_pages;
+      p.pages = a.table + (size_t)seq * a.max_pages + (kTail ? s_first[row] >> a.shift : 0);
       p.first_row = kvh << a.shift;
       p.kbase = a.cache + kvh * head_bytes;
       p.vbase = p.kbase + a.n_kv_heads * head_bytes;
+      p.ebase = a.cache + exponents + ((int64_t)kvh << a.shift);
       return true;
     }
     return false;
   };
 
-  uint4 qf[QV], kf[2][KV], vf[4][VC];
+  uint4 qf[QV], kf[2][KV], vf[kHeld ? 1 : 4][VC];
+  uint32_t vw[kHeld ? 4 : 1][VW], ex[kHeld ? 4 : 1];  // in 8 bits: values; exponents of keys and values of tokens g and g + 8
   Piece p = {};
   int chunk_end, c, have, have_next, pg_next;  // chunks of 16 tokens
   int64_t at, at_next;
   int waiting[kSlots];                 // tokens of the chunks in this warp's ring
   npp::WarpRing<kSlots> uses;
   WarpWaits waits = {&s_lost[wid], a.status};
-  const uint32_t ring = ((npp::smem_addr(s_dyn) + 1023) & ~1023u) + wid * kSlots * kSlot;
+  const uint32_t ring = ((npp::smem_addr(s_dyn) + (kTail ? kTailBytes : 0) + 1023) & ~1023u) + wid * kSlots * kSlot;
   // what a lane reads with load_tiles: rows (tokens) 0-7 and 8-15 of two neighbouring 16-byte columns, 128-byte swizzle
   const uint32_t lane_row = ((lane & 7) + (lane >> 4) * 8) * 128, lane_col = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
   auto tiles_at = [&](uint32_t base, int step) { return base + lane_row + (step >> 2) * 2048 + (((step & 3) << 5) ^ lane_col); };
   // where the chunk's page starts, and how many of its tokens there are (0: nothing to read)
+  uint32_t ex_next[4] = {0, 0, 0, 0};
   auto chunk_of = [&](int chunk, int pg, int& n, int64_t& off) {
     n = 0;
     off = 0;
@@ -425,26 +574,49 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       return;
     }
     n = (int)min((int64_t)16, p.len - (int64_t)chunk * 16);
-    off = pg * page_bytes + (int64_t)((chunk * 16) & ((1 << a.shift) - 1)) * (HD * 2);
+    const int place = (chunk * 16) & ((1 << a.shift) - 1);
+    off = pg * page_bytes + (int64_t)place * kRowBytes;
+    if constexpr (kHeld) {
+      const uint8_t* e = reinterpret_cast<const uint8_t*>(p.ebase) + pg * page_bytes + place + g;
+      const int64_t values = (int64_t)a.n_kv_heads << a.shift;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const bool there = g + 8 * r < n;
+        ex_next[r] = there ? __ldg(e + 8 * r) : 0u;
+        ex_next[2 + r] = there ? __ldg(e + 8 * r + values) : 0u;
+      }
+    }
   };
   auto page_of = [&](int chunk) { return chunk < chunk_end ? p.pages[(int)(((int64_t)chunk * 16) >> a.shift)] : 0; };
+  auto keep_exponents = [&] {
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ex[i] = ex_next[i];
+    }
+  };
   auto load_k = [&](int n, int64_t off) {
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int j = 0; j < KV; ++j) {
         kf[r][j] = make_uint4(0, 0, 0, 0);
-        if (g + 8 * r < n) kf[r][j] = npd::ldg_stream(p.kbase + off + (g + 8 * r) * (HD * 2) + (t + 4 * j) * 16);
+        if (g + 8 * r < n) kf[r][j] = npd::ldg_stream(p.kbase + off + (g + 8 * r) * kRowBytes + (t + 4 * j) * 16);
       }
   };
   auto load_v = [&](int n, int64_t off) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
+      if constexpr (kHeld) {
 #pragma unroll
-      for (int x = 0; x < VC; ++x) {
-        vf[r][x] = make_uint4(0, 0, 0, 0);
-        if (tok < n) vf[r][x] = npd::ldg_stream(p.vbase + off + tok * (HD * 2) + (g + 8 * x) * 16);
+        for (int x = 0; x < VW; ++x) vw[r][x] = 0;
+        if (tok < n) load_words(p.vbase + off + tok * HD + g * (HD / 8), vw[r]);
+      } else {
+#pragma unroll
+        for (int x = 0; x < VC; ++x) {
+          vf[r][x] = make_uint4(0, 0, 0, 0);
+          if (tok < n) vf[r][x] = npd::ldg_stream(p.vbase + off + tok * (HD * 2) + (g + 8 * x) * 16);
+        }
       }
     }
   };
@@ -482,6 +654,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       pg_next = pg[kSlots];
     } else {
       chunk_of(c, pg[0], have, at);
+      keep_exponents();
       load_k(have, at);
       load_v(have, at);
       pg_next = pg[1];
@@ -494,16 +667,6 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     acc.w += f * v.w;
   };
   auto odd_four = [](const float4& v) { return not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w); };
-  // four values of a head's result; its log of the sum with the first
-  auto result = [&](int i, int h, int d, const float4& acc, float use, float sum) {
-    const bool none = sum == 0.f;
-    const float inv = none ? 0.f : 1.f / sum;
-    uint2 r;
-    r.x = (uint32_t)Half2<T>::round(none ? 0.f : acc.x * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.y * inv) << 16;
-    r.y = (uint32_t)Half2<T>::round(none ? 0.f : acc.z * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.w * inv) << 16;
-    *reinterpret_cast<uint2*>(a.out + i * a.o_token + (int64_t)h * a.o_head + d) = r;
-    if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = none ? -INFINITY : use * kLn2 + logf(sum);
-  };
   // the queries that begin() asked for go where all warps read them; a barrier follows
   auto keep_queries = [&] {
 #pragma unroll
@@ -519,7 +682,12 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   }
   __syncthreads();
   while (any) {
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[kWide ? 2 * KS : VC * 4][4];
+    float m[NH], l[NH], o[kWide ? 2 * KS : kHeld ? NT * (HD / 16) : VC * 4][4];
+#pragma unroll
+    for (int i = 0; i < NH; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+    }
 #pragma unroll
     for (auto& x : o) x[0] = x[1] = x[2] = x[3] = 0.f;
     uint32_t qr[kWide ? KS : 1][4];  // sixteen heads: the queries of heads g and g + 8, values 16 j + 2t, + 1 and those eight further
@@ -529,27 +697,140 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
         for (int i = 0; i < 4; ++i) qr[j][i] = *reinterpret_cast<const uint32_t*>(s_q + (g + (i & 1) * 8) * QR + j * 32 + t * 4 + (i >> 1) * 16);
     }
+    // In 8 bits: the queries in fp16, times a power of two that brings the largest finite one of a head to 2^14, and what scores of heads
+    // 2t and 2t + 1 (and those eight further) are to be multiplied with.
+    uint32_t qh[kHeld ? NT : 1][kHeld ? HD / 8 : 1];
+    float up[NH];
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        const unsigned char* row = s_q + (g + 8 * x) * QR;
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < HD / 8; ++j) {
+          qh[x][j] = *reinterpret_cast<const uint32_t*>(row + (t + 4 * (j >> 3)) * 32 + (j & 7) * 4);
+          const float2 f = widen2<T>(qh[x][j]);
+          const uint32_t b0 = __float_as_uint(f.x) & 0x7fffffffu, b1 = __float_as_uint(f.y) & 0x7fffffffu;
+          top = max(top, max(b0 < 0x7f800000u ? b0 : 0u, b1 < 0x7f800000u ? b1 : 0u));
+        }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = max((int)(top >> 23), 29) - 14;  // biased exponent of the power of two to divide by: 15 to 240
+        const float by = __uint_as_float((uint32_t)(254 - e) << 23), back = __uint_as_float((uint32_t)e << 23);
+#pragma unroll
+        for (int j = 0; j < HD / 8; ++j) {
+          const float2 f = widen2<T>(qh[x][j]);
+          const __half2 h = __floats2half2_rn(f.x * by, f.y * by);
+          qh[x][j] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        const float mine = fminf(fmaxf(a.scale2 * back, FLT_MIN), FLT_MAX);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) up[2 * x + i] = __shfl_sync(0xffffffffu, mine, (2 * t + i) * 4);
+      }
+    }
     // the maxima of the two heads grow to `top`, what has been added up is rescaled (by(i, factor) for the accumulators of head i), `use` is
     // what to take off
-    auto raise = [&](const float (&top)[2], float (&use)[2], auto by) {
-      float now[2];
+    auto raise = [&](const auto& top, auto& use, auto by) {
+      float now[NH];
       bool grew = false;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < NH; ++i) {
         now[i] = fmaxf(m[i], top[i]);
         use[i] = now[i] == -INFINITY ? 0.f : now[i];  // -inf so far: nothing has been added up yet
         grew |= now[i] > m[i];
       }
       if (!__any_sync(0xffffffffu, grew)) return;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < NH; ++i) {
         const float f = exp2_fast(m[i] - use[i]);
         m[i] = now[i];
         l[i] *= f;
         by(i, f);
       }
     };
-    if constexpr (!kWide) {
+    if constexpr (kHeld) {
+      for (; c < chunk_end; c += kWarps) {
+        chunk_of(c + kWarps, pg_next, have_next, at_next);
+        pg_next = page_of(c + 2 * kWarps);
+        // ---- S^T = K Q^T, without their powers of two
+        float s[NT][4];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < KV; ++j)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t a0, a1, a2, a3;
+            widen4(word(kf[0][j], w), a0, a2);
+            widen4(word(kf[1][j], w), a1, a3);
+#pragma unroll
+            for (int x = 0; x < NT; ++x) Half2<__half>::mma(s[x], a0, a1, a2, a3, qh[x][8 * j + 2 * w], qh[x][8 * j + 2 * w + 1]);
+          }
+        load_k(have_next, at_next);
+        // ---- softmax: s[x][0], s[x][1] are token g, s[x][2], s[x][3] token g + 8; heads 8x + 2t and 8x + 2t + 1.  A token's values are times
+        // 2^lv: their weight is 2^(s + lv - m), m the largest s + lv, and the sum is of 2^(s - m).
+        float lv[2], top[NH], use[NH];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float power = __uint_as_float(ex[r] << 23);
+          const bool there = g + 8 * r < have;
+          lv[r] = (float)(int)ex[2 + r] - 127.f;
+#pragma unroll
+          for (int x = 0; x < NT; ++x)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[x][2 * r + i] = there ? s[x][2 * r + i] * up[2 * x + i] * power : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < NH; ++i) {
+          top[i] = fmaxf(s[i >> 1][i & 1] + lv[0], s[i >> 1][(i & 1) + 2] + lv[1]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+        }
+        raise(top, use, [&](int i, float f) {
+#pragma unroll
+          for (int v = 0; v < HD / 16; ++v) {
+            o[(i >> 1) * (HD / 16) + v][i & 1] *= f;
+            o[(i >> 1) * (HD / 16) + v][(i & 1) + 2] *= f;
+          }
+        });
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float e = s[x][2 * r + i] - use[2 * x + i];
+              l[2 * x + i] += exp2_fast(e + kHeldShift);
+              w[i] = exp2_fast(e + lv[r]);
+            }
+            uint32_t hi, lo;
+            Half2<__half>::split(w[0], w[1], hi, lo);
+            ph[x][r] = transpose8x8(hi);
+            pl[x][r] = transpose8x8(lo);
+          }
+        // ---- O^T += V^T W^T
+#pragma unroll
+        for (int w = 0; w < VW; ++w)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t order = half ? 0x7362 : 0x5140;
+            uint32_t a0, a1, a2, a3;
+            widen4(__byte_perm(vw[0][w], vw[1][w], order), a0, a1);
+            widen4(__byte_perm(vw[2][w], vw[3][w], order), a2, a3);
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+              Half2<__half>::mma(o[x * (HD / 16) + 2 * w + half], a0, a1, a2, a3, ph[x][0], ph[x][1]);
+              Half2<__half>::mma(o[x * (HD / 16) + 2 * w + half], a0, a1, a2, a3, pl[x][0], pl[x][1]);
+            }
+          }
+        load_v(have_next, at_next);
+        keep_exponents();
+        have = have_next;
+        at = at_next;
+      }
+    } else if constexpr (!kWide) {
       for (; c < chunk_end; c += kWarps) {
         chunk_of(c + kWarps, pg_next, have_next, at_next);
         pg_next = page_of(c + 2 * kWarps);
@@ -689,8 +970,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     any = next_piece(p);
     if (any) begin();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int h = kWide ? g + 8 * i : 2 * t + i;
+    for (int i = 0; i < NH; ++i) {
+      const int h = kWide ? g + 8 * i : kHeld ? (i >> 1) * 8 + 2 * t + (i & 1) : 2 * t + i;
 #pragma unroll
       for (int x = kWide ? 1 : 4; x < (kWide ? 4 : 32); x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
       if (h < e.heads) {
@@ -698,7 +979,12 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
           s_ml[wid][h][0] = m[i];
           s_ml[wid][h][1] = l[i];
         }
-        if constexpr (!kWide) {
+        if constexpr (kHeld) {
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k)
+            *reinterpret_cast<float2*>(&s_o[wid][h][g * (HD / 8) + 2 * k]) =
+                make_float2(o[(i >> 1) * (HD / 16) + k][i & 1], o[(i >> 1) * (HD / 16) + k][(i & 1) + 2]);
+        } else if constexpr (!kWide) {
 #pragma unroll
           for (int k = 0; k < VC * 4; ++k)
             *reinterpret_cast<float2*>(&s_o[wid][h][(g + 8 * (k >> 2)) * 8 + 2 * (k & 3)]) = make_float2(o[k][i], o[k][i + 2]);
@@ -730,14 +1016,15 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       }
       if (odd_four(acc) && !not_finite(sum) && !(whole && sum == 0.f)) odd |= turn;
       if (whole) {
-        result(e.row, e.h0 + h, d, acc, use, sum);
+        result(e.row, e.h0 + h, d, acc, top, sum);
       } else {
         __stcg(reinterpret_cast<float4*>(&a.part_o[((size_t)slot * HB + h) * HD + d]), acc);
         if (d == 0) __stcg(reinterpret_cast<float2*>(&a.part_ml[(slot * HB + h) * 2]), make_float2(top, sum));
       }
     }
-    if (__syncthreads_or(odd))  // s_o and s_ml are free from here on, the next piece's queries are where all warps read them
-      mend<T, HD>(a, odd, e.row, e.pair, e.ta, e.tb, e.h0, e.heads, whole ? nullptr : a.part_o + (size_t)slot * HB * HD, reinterpret_cast<int*>(&s_o[0][0][0]));
+    if (kHeld) __syncthreads();  // e4m3 has no infinities, and a NaN stays one by itself
+    else if (__syncthreads_or(odd))  // s_o and s_ml are free from here on, the next piece's queries are where all warps read them
+      mend<T, HD>(a, odd, e.row, kTail ? s_first[e.row] : 0, e.pair, e.ta, e.tb, e.h0, e.heads, whole ? nullptr : a.part_o + (size_t)slot * HB * HD, reinterpret_cast<int*>(&s_o[0][0][0]));
     if (!whole) {
       // ---- the last block to arrive joins up to kJoin neighbouring pieces; the last of those that did joins what they got
       const int c0 = block_of(e.first_w + kStart), c1 = block_of(e.first_w + kStart + e.tiles - 1), pieces = c1 - c0 + 1;
@@ -793,7 +1080,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
           __syncwarp();  // b's place is read by the HD / 4 lanes of a head, all of this warp: they are done
           if (!there) continue;
           if (final) {
-            result(e.row, e.h0 + h, d, acc, top == -INFINITY ? 0.f : top, sum);
+            result(e.row, e.h0 + h, d, acc, top, sum);
           } else {
             const int sl = slot_of(b) + h;
             __stcg(reinterpret_cast<float4*>(&a.part_o[(size_t)sl * HD + d]), acc);
@@ -812,6 +1099,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     uint32_t patience = npp::kSpinLimit;
     npp::drain_ring(s_full[wid], kSlots, uses.slot(uses.asked), uses.parity(uses.asked), patience);
   }
+  if (kTail) npp::pdl_wait_prior();
 }
 
 // Heads of a block.  Sixteen read keys and values once for up to sixteen heads, eight have more warps: 64 sequences of 2000 tokens, 64
@@ -830,22 +1118,23 @@ bool make_map(CUtensorMap* map, const DecodeArgs& a, int hd) {
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class T, int HD, bool kWide>
+template <class T, int HD, int kForm, bool kTail>
 cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int sms, cudaStream_t s) {
-  size_t ring = 0;
-  if (kWide) {
+  size_t room = kTail ? kTailBytes : 0;
+  if (kForm == kSixteen) {
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kWide>), &done);
+    const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kForm, kTail>), &done);
     if (e != cudaSuccess) return e;
-    ring = (size_t)kWarps * kSlots * 16 * HD * 4 + 1024;
+    room += (size_t)kWarps * kSlots * 16 * HD * 4 + 1024;
   }
-  const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(HD, kWide ? 16 : 8) * sms));
-  return launch_early(k_attn_decode<T, HD, kWide>, grid, kThreads, ring, s, map, a);
+  const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(HD, kForm) * sms));
+  return launch_early(k_attn_decode<T, HD, kForm, kTail>, grid, kThreads, room, s, map, a);
 }
-template <class T>
-cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hd, int hb, int sms, cudaStream_t s) {
-  if (hd == 128) return hb == 8 ? launch<T, 128, false>(map, a, sms, s) : launch<T, 128, true>(map, a, sms, s);
-  return hb == 8 ? launch<T, 64, false>(map, a, sms, s) : launch<T, 64, true>(map, a, sms, s);
+template <class T, int HD>
+cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hb, bool held, bool tail, int sms, cudaStream_t s) {
+  if (held) return hb == 8 ? launch<T, HD, kHeldEight, false>(map, a, sms, s) : launch<T, HD, kHeldSixteen, false>(map, a, sms, s);
+  if (tail) return hb == 8 ? launch<T, HD, kEight, true>(map, a, sms, s) : launch<T, HD, kSixteen, true>(map, a, sms, s);
+  return hb == 8 ? launch<T, HD, kEight, false>(map, a, sms, s) : launch<T, HD, kSixteen, false>(map, a, sms, s);
 }
 
 // [(m, l) of the partial results][their O][counts]: the counts start at the same place for every description and n, and the
@@ -864,41 +1153,14 @@ const char* heads_error(const np_kv_desc* d, int n_heads, int n) {
 }
 
 }  // namespace
-}  // namespace npa
 
-using namespace npa;
+uint64_t decode_space_bytes(int n_kv_heads, int group, int n) { return space_bytes(n_kv_heads, group, n); }
 
-extern "C" {
-
-int np_attn_workspace_bytes(const np_kv_desc* d, int32_t n_heads, int32_t n, uint64_t* out) {
-  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
-  if (const char* m = heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
-  if (!out) return fail(NP_E_INVAL, "NULL argument");
-  *out = space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n);
-  return NP_OK;
-}
-
-int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads,
-                   const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse, void* workspace,
-                   uint64_t workspace_bytes, void* stream) {
-  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
-  if (const char* m = heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
-  if (!seqs && n > d->max_seqs) return fail(NP_E_INVAL, "n is above max_seqs");
-  if (n == 0) return NP_OK;
-  if (!cache || !workspace || !t || !t->page_table || !t->lens || !t->status) return fail(NP_E_INVAL, "NULL argument");
-  if ((uintptr_t)cache % 16 || (uintptr_t)workspace % 16) return fail(NP_E_INVAL, "cache and workspace must be 16-byte aligned");
-  if (workspace_bytes < space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n)) return fail(NP_E_INVAL, "workspace is smaller than np_attn_workspace_bytes says");
-  if (layer < 0 || layer >= d->n_layers) return fail(NP_E_INVAL, "layer outside the cache");
-  float scale2;
-  if (!scale_base2(scale, &scale2)) return fail(NP_E_INVAL, kScaleError);
-  if (const char* m = rows_error(q)) return fail(NP_E_INVAL, m);
-  if (const char* m = rows_error(out)) return fail(NP_E_INVAL, m);
-  if ((n > 1 && out->token_stride == 0) || (n_heads > 1 && out->head_stride == 0)) return fail(NP_E_INVAL, "rows of the result need strides above 0");
-  int sms;
-  if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
-  const int64_t page = (int64_t)2 * d->n_kv_heads * d->page_tokens * d->head_dim * 2;
+int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads, const int32_t* seqs, int32_t n,
+           float scale2, const np_rows* out, float* lse, void* workspace, const SharedArgs* shared, int sms, cudaStream_t s) {
   DecodeArgs a = {};
-  a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * page;
+  a.page_bytes = page_bytes(d);
+  a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * a.page_bytes;
   a.table = t->page_table;
   a.lens = t->lens;
   a.seqs = seqs;
@@ -921,16 +1183,62 @@ int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const 
   a.n_pages = d->n_pages;
   a.max_seqs = d->max_seqs;
   a.max_pages = d->max_pages;
+  if (shared) a.shared = *shared;
   char* ws = static_cast<char*>(workspace);
   a.part_ml = reinterpret_cast<float*>(ws);
   a.part_o = reinterpret_cast<float*>(ws + kSpaceO);
   a.count = reinterpret_cast<unsigned int*>(ws + kSpaceCounts);
   a.pair_count = reinterpret_cast<unsigned int*>(ws + kSpacePairs);
+  const bool held = held_in_8(d), tail = shared != nullptr;
   CUtensorMap map = {};
-  if (hb == 16 && !make_map(&map, a, d->head_dim)) return fail(NP_E_INVAL, "a cache that a tensor map does not describe");
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = d->dtype == NP_T_BF16 ? launch<__nv_bfloat16>(map, a, d->head_dim, hb, sms, s) : launch<__half>(map, a, d->head_dim, hb, sms, s);
+  if (hb == 16 && !held && !make_map(&map, a, d->head_dim)) return fail(NP_E_INVAL, "a cache that a tensor map does not describe");
+  cudaError_t e;
+  if (row_type(d) == NP_T_BF16) e = d->head_dim == 128 ? launch<__nv_bfloat16, 128>(map, a, hb, held, tail, sms, s) : launch<__nv_bfloat16, 64>(map, a, hb, held, tail, sms, s);
+  else e = d->head_dim == 128 ? launch<__half, 128>(map, a, hb, held, tail, sms, s) : launch<__half, 64>(map, a, hb, held, tail, sms, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);
+}
+
+const char* decode_error(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads, int32_t n,
+                         float scale, const np_rows* out, const void* workspace, float* scale2) {
+  if (!cache || !workspace || !t || !t->page_table || !t->lens || !t->status) return "NULL argument";
+  if ((uintptr_t)cache % 16 || (uintptr_t)workspace % 16) return "cache and workspace must be 16-byte aligned";
+  if (layer < 0 || layer >= d->n_layers) return "layer outside the cache";
+  if (!scale_base2(scale, scale2)) return kScaleError;
+  if (const char* m = rows_error(q)) return m;
+  if (const char* m = rows_error(out)) return m;
+  if ((n > 1 && out->token_stride == 0) || (n_heads > 1 && out->head_stride == 0)) return "rows of the result need strides above 0";
+  return nullptr;
+}
+
+const char* decode_heads_error(const np_kv_desc* d, int n_heads, int n) { return heads_error(d, n_heads, n); }
+
+}  // namespace npa
+
+using namespace npa;
+
+extern "C" {
+
+int np_attn_workspace_bytes(const np_kv_desc* d, int32_t n_heads, int32_t n, uint64_t* out) {
+  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
+  if (const char* m = heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
+  if (!out) return fail(NP_E_INVAL, "NULL argument");
+  *out = space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n);
+  return NP_OK;
+}
+
+int np_attn_decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads,
+                   const int32_t* seqs, int32_t n, float scale, const np_rows* out, float* lse, void* workspace,
+                   uint64_t workspace_bytes, void* stream) {
+  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
+  if (const char* m = heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
+  if (!seqs && n > d->max_seqs) return fail(NP_E_INVAL, "n is above max_seqs");
+  if (n == 0) return NP_OK;
+  float scale2;
+  if (const char* m = decode_error(d, cache, layer, t, q, n_heads, n, scale, out, workspace, &scale2)) return fail(NP_E_INVAL, m);
+  if (workspace_bytes < space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n)) return fail(NP_E_INVAL, "workspace is smaller than np_attn_workspace_bytes says");
+  int sms;
+  if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
+  return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, nullptr, sms, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -32,7 +32,7 @@ int fail_cuda(cudaError_t e) { return fail(NP_E_CUDA, cudaGetErrorString(e)); }
 
 const char* desc_error(const np_kv_desc* d) {
   if (!d) return "NULL description";
-  if (d->dtype != NP_T_BF16 && d->dtype != NP_T_FP16) return "dtype must be NP_T_BF16 or NP_T_FP16";
+  if (row_type(d) != NP_T_BF16 && row_type(d) != NP_T_FP16) return "dtype must be NP_T_BF16 or NP_T_FP16, or one of them and NP_KV_E4M3";
   if (d->n_layers < 1 || d->n_kv_heads < 1 || d->n_kv_heads > 1024) return "n_layers must be positive, n_kv_heads in [1, 1024]";
   if (d->head_dim != 64 && d->head_dim != 128) return "head_dim must be 64 or 128";
   const int p = d->page_tokens;
@@ -481,6 +481,64 @@ k_kv_compact_small(Pool p, int32_t* refs_out, int32_t* __restrict__ n_live, Copy
   copy_and_rewrite(a, w);
 }
 
+// The tokens in full pages that all rows of a group begin with: a block per group.  Pages are compared a block's threads at a time with those of
+// the group's first sequence, up to the first that differ.
+constexpr int kSharedThreads = 512;
+
+__global__ void __launch_bounds__(kSharedThreads)
+k_kv_shared(Pool p, const int32_t* __restrict__ seqs, int n, const int32_t* __restrict__ cu, int32_t* __restrict__ shared) {
+  __shared__ int s_seq[NP_KV_MAX_SEQS];
+  __shared__ int s_full, s_members, s_first;
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+  const int tid = threadIdx.x;
+  const int lo = min(max(cu[blockIdx.x], 0), n), hi = max(lo, min(cu[blockIdx.x + 1], n));
+  if (tid == 0) {
+    s_full = p.max_pages;
+    s_members = 0;
+    s_first = NP_KV_MAX_SEQS;
+  }
+  __syncthreads();
+  for (int i = lo + tid; i < hi; i += kSharedThreads) {
+    int seq = seqs ? seqs[i] : i, full = 0;
+    if (seq >= p.max_seqs) {
+      seq = -1;
+      atomicOr(p.status, NP_KV_S_SEQ);
+    }
+    if (seq >= 0) {
+      const int len = p.lens[seq];
+      if (pages_of(p, len) < 0) atomicOr(p.status, NP_KV_S_LENGTH);
+      else full = len >> p.shift;
+      atomicMin(&s_full, full);
+      atomicAdd(&s_members, 1);
+      atomicMin(&s_first, i - lo);
+    }
+    s_seq[i - lo] = seq;
+  }
+  __syncthreads();
+  const int members = hi - lo, first = s_first, full = s_members > 1 ? s_full : 0;
+  int common = full;
+  for (int j0 = 0; j0 < full; j0 += kSharedThreads) {
+    const int j = j0 + tid;
+    bool differs = false;
+    if (j < full) {
+      const int page = p.table[(size_t)s_seq[first] * p.max_pages + j];
+      differs = (unsigned)page >= (unsigned)p.n_pages;
+#pragma unroll 8
+      for (int i = first + 1; i < members; ++i) {
+        const int seq = s_seq[i];
+        differs |= seq >= 0 && p.table[(size_t)seq * p.max_pages + j] != page;
+      }
+    }
+    if (differs) atomicMin(&s_full, j);
+    if (__syncthreads_or(differs)) {
+      common = s_full;
+      break;
+    }
+  }
+  if (tid == 0) shared[blockIdx.x] = common << p.shift;
+}
+
 struct AppendArgs {
   char* cache;               // of the layer
   const char* k;
@@ -578,8 +636,6 @@ k_kv_reset(Pool p, int64_t scratch) {
   if (i == 0) *p.status = 0;
 }
 
-int64_t page_bytes(const np_kv_desc* d) { return (int64_t)2 * d->n_kv_heads * d->page_tokens * d->head_dim * 2; }
-
 CopyArgs copy_args(const np_kv_desc* d, void* dst, const void* src, const int32_t* from, const int32_t* to, const int32_t* count, int n,
                    int32_t* status) {
   const int64_t pb = page_bytes(d);
@@ -673,6 +729,7 @@ int np_kv_append(const np_kv_desc* d, void* cache, int32_t layer, const np_kv_ta
   if (layer < 0 || layer >= d->n_layers) return fail(NP_E_INVAL, "layer outside the cache");
   if (const char* m = rows_error(k)) return fail(NP_E_INVAL, m);
   if (const char* m = rows_error(v)) return fail(NP_E_INVAL, m);
+  if (held_in_8(d)) return append_held(d, cache, layer, t, k, v, n_tokens, seqs, cu, start, n, stream);
   AppendArgs a = {};
   a.cache = static_cast<char*>(cache) + (int64_t)layer * d->n_pages * page_bytes(d);
   a.k = static_cast<const char*>(k->data);
@@ -708,6 +765,19 @@ int np_kv_fork(const np_kv_desc* d, void* cache, const np_kv_tables* t, const in
   cudaError_t e = launch_early(k_kv_take<true>, dim3(1), kPlanThreads, 0, s, p, src, dst, (int)n, (int32_t*)nullptr);
   if (e == cudaSuccess) e = launch_copy(copy_args(d, cache, cache, p.pair_src(), p.pair_dst(), nullptr, n, nullptr), RewriteArgs{}, sms, s);
   return done(e);
+}
+
+int np_kv_shared(const np_kv_desc* d, const np_kv_tables* t, const int32_t* seqs, int32_t n, const int32_t* cu, int32_t n_groups, int32_t* shared,
+                 void* stream) {
+  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
+  if (!t || !t->page_table || !t->lens || !t->status) return fail(NP_E_INVAL, "a table pointer is NULL");
+  if (n < 0 || n > NP_KV_MAX_SEQS || (!seqs && n > d->max_seqs)) return fail(NP_E_INVAL, "n outside [0, NP_KV_MAX_SEQS], or above max_seqs");
+  if (n_groups < 0 || n_groups > NP_KV_MAX_SEQS) return fail(NP_E_INVAL, "n_groups outside [0, NP_KV_MAX_SEQS]");
+  if (n_groups == 0) return NP_OK;
+  if (!cu || !shared) return fail(NP_E_INVAL, "NULL argument");
+  int sms;
+  if (int rc = device(&sms)) return rc;
+  return done(launch_early(k_kv_shared, dim3(n_groups), kSharedThreads, 0, static_cast<cudaStream_t>(stream), pool_of(d, t), seqs, (int)n, cu, shared));
 }
 
 int np_kv_free(const np_kv_desc* d, const np_kv_tables* t, const int32_t* seqs, int32_t n, void* stream) {

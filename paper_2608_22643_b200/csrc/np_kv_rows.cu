@@ -1,0 +1,561 @@
+// Rows of heads on their way: norm and rotation of queries and keys (np_attn_rotate), the same into the cache's pages
+// (np_kv_append_rotated), into and out of a cache of 8 bits (np_kv_append, np_kv_read).
+//
+//   y = x / sqrt(mean(x^2) + eps) * gain,   (a, b) -> (a cos t - b sin t, b cos t + a sin t),   t = position * freq[i]
+//   e = the least of -60 .. 120 with max|x| <= 448 * 2^e,   x -> e4m3(x * 2^-e)
+//
+// Every value is read and written once, so the bytes bound all of this.  A row of head_dim values belongs to 16 (or 8) lanes, 16 bytes each;
+// a lane has four such pieces on their way before it works on the first.  The lane with the other half of a pair is a shuffle away.
+//
+// Cosines and sines belong to a token, not to a head: a block works them out once for its few tokens, while its loads are on their way.
+// The angle is a product in fp64 that is brought to a fraction of a turn there (a position of 2^31 leaves 2^-24 of a turn), so fp32 does for the
+// rest.
+//
+// Powers of two as scales make the 8 bits a matter of integers and one rounding: x * 2^-e is exact, so nothing of what is held depends on
+// how it was computed.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "np_attn.h"
+#include "np_device.cuh"
+#include "np_internal.h"
+#include "np_pipe.cuh"
+
+namespace npa {
+namespace {
+
+constexpr int kThreads = 256, kVecs = 4;
+template <int HD>
+struct Rows {
+  static constexpr int kLanes = HD / 8;                      // of a row
+  static constexpr int kTurn = kThreads / kLanes;            // rows of a block at a time
+  static constexpr int kBlock = kTurn * kVecs;
+  static constexpr int kTokens = kBlock / 2 + 2;             // of a block at most: a token has two rows or more
+};
+
+struct RowsArgs {
+  const uint16_t* q;
+  uint16_t* k;
+  uint16_t* v;
+  uint16_t* q_out;
+  uint16_t* k_out;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, qo_token, qo_head, ko_token, ko_head;  // elements
+  const int32_t* seqs;
+  const int32_t* cu;
+  const int32_t* start;
+  int n, n_tokens, nq, nkv, rows;  // rows of a token: queries, keys, then values if there is a cache
+  // the cache
+  char* cache;  // of the layer; nullptr: none
+  const int32_t* table;
+  const int32_t* lens;
+  int32_t* status;
+  int64_t page_bytes;
+  int shift, n_pages, max_seqs, max_pages;
+  // the rotation
+  const double* freq;
+  const float* q_gain;
+  const float* k_gain;
+  float eps;
+  int half, neighbours;  // 16-byte pieces of half the values that turn
+};
+
+template <class T>
+__device__ __forceinline__ float2 widen(uint32_t w);
+template <>
+__device__ __forceinline__ float2 widen<__nv_bfloat16>(uint32_t w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ float2 widen<__half>(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <class T>
+__device__ __forceinline__ uint32_t pack(float x, float y);
+template <>
+__device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float x, float y) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pack<__half>(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <class T>
+__device__ __forceinline__ void widen8(const uint4& v, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = widen<T>(w[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+template <class T>
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+  return make_uint4(pack<T>(x[0], x[1]), pack<T>(x[2], x[3]), pack<T>(x[4], x[5]), pack<T>(x[6], x[7]));
+}
+template <class T>
+__device__ __forceinline__ float largest() {
+  return std::is_same<T, __half>::value ? 65504.f : __uint_as_float(0x7f7f0000u);
+}
+
+// Where the tokens [t0, t1] of a block are: their position (-1: the row is passed over), their page (-1: no place in the cache) and their
+// place in it.
+struct Place {
+  int64_t pos;
+  int page, at;
+};
+__device__ __forceinline__ Place place_of(const RowsArgs& a, int t) {
+  Place p = {-1, -1, 0};
+  int i = -1, off = 0;
+  if (!a.cu) {
+    i = t < a.n ? t : -1;
+  } else if (t >= a.cu[0] && t < a.cu[a.n]) {
+    int lo = 0, hi = a.n - 1;  // the last i with cu[i] <= t
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.cu[mid] <= t) lo = mid;
+      else hi = mid - 1;
+    }
+    i = lo;
+    off = t - a.cu[lo];
+  }
+  if (i < 0 || off < 0) return p;
+  const int st = a.start[i], seq = !a.cache ? 0 : a.seqs ? a.seqs[i] : i;
+  if (st < 0) return p;
+  p.pos = (int64_t)st + off;
+  if (!a.cache) return p;
+  if (seq < 0 || seq >= a.max_seqs) {
+    atomicOr(a.status, NP_KV_S_SEQ);
+  } else if (p.pos < a.lens[seq]) {
+    const int64_t j = p.pos >> a.shift;
+    const int pg = j < a.max_pages ? a.table[(size_t)seq * a.max_pages + j] : -1;
+    if ((unsigned)pg < (unsigned)a.n_pages) {
+      p.page = pg;
+      p.at = (int)(p.pos & ((1 << a.shift) - 1));
+    } else {
+      atomicOr(a.status, NP_KV_S_PAGE);
+    }
+  }
+  return p;
+}
+
+// The biased exponent of a row's power of two, from the bits of its largest finite magnitude: 448 = 1.75 * 2^8.
+__device__ __forceinline__ int exponent_of(uint32_t top) {
+  return min(max((int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), 67), 247);
+}
+// Eight values times a power of two as e4m3; infinities become NaN.
+__device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float power) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float y[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float z = x[2 * i + j];
+      y[j] = (__float_as_uint(z) & 0x7fffffffu) == 0x7f800000u ? __uint_as_float(0x7fffffffu) : z * power;
+    }
+    w[i] = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
+  }
+  return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+}
+
+// kRotate: norm and rotation.  kHeld: keys and values go into pages of 8 bits.
+template <class T, int HD, bool kRotate, bool kHeld>
+__global__ void __launch_bounds__(kThreads)
+k_rows_in(const __grid_constant__ RowsArgs a) {
+  using R = Rows<HD>;
+  constexpr int L = R::kLanes;
+  __shared__ Place s_place[R::kTokens];
+  __shared__ __align__(16) float s_cos[kRotate ? R::kTokens : 1][HD / 2], s_sin[kRotate ? R::kTokens : 1][HD / 2];
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+  const int tid = threadIdx.x, piece = tid % L;
+  const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock, last = min(total, first + R::kBlock) - 1;
+  const int t0 = (int)(first / a.rows), tokens = (int)(last / a.rows) - t0 + 1;
+  uint4 raw[kVecs];
+  int tok[kVecs], of[kVecs];
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const uint32_t row = first + j * R::kTurn + tid / L;
+    raw[j] = make_uint4(0, 0, 0, 0);
+    tok[j] = -1;
+    of[j] = 0;
+    if (row > last) continue;
+    const int t = (int)(row / a.rows), r = (int)(row - (uint32_t)t * a.rows);
+    tok[j] = t;
+    of[j] = r;
+    const uint16_t* src = r < a.nq            ? a.q + t * a.q_token + r * a.q_head
+                          : r < a.nq + a.nkv ? a.k + t * a.k_token + (r - a.nq) * a.k_head
+                                             : a.v + t * a.v_token + (r - a.nq - a.nkv) * a.v_head;
+    raw[j] = *reinterpret_cast<const uint4*>(src + piece * 8);
+  }
+  for (int t = tid; t < tokens; t += kThreads) s_place[t] = place_of(a, t0 + t);
+  __syncthreads();
+  if (kRotate && a.half) {
+    const int pairs = a.half * 8;
+    for (int x = tid; x < tokens * pairs; x += kThreads) {
+      const int t = x / pairs, i = x - t * pairs;
+      double turns = (double)s_place[t].pos * (a.freq[i] * 0.15915494309189533577);  // 1 / (2 pi)
+      turns -= rint(turns);
+      float s, c;
+      sincospif(2.f * (float)turns, &s, &c);
+      s_cos[t][i] = c;
+      s_sin[t][i] = s;
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const int r = of[j];
+    const bool query = r < a.nq, key = !query && r < a.nq + a.nkv;
+    const Place p = tok[j] < 0 ? Place{-1, -1, 0} : s_place[tok[j] - t0];
+    if (kRotate) {
+      float x[8];
+      widen8<T>(raw[j], x);
+      if (a.q_gain || a.k_gain) {
+        auto sum_of_squares = [&] {
+          float ss = x[0] * x[0];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+#pragma unroll
+          for (int o = 1; o < L; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          return ss;
+        };
+        float ss = sum_of_squares(), eps = a.eps;
+        const float* gain = query ? a.q_gain : key ? a.k_gain : nullptr;
+        if (__any_sync(0xffffffffu, gain && ss == INFINITY)) {  // squares past fp32's range: of values 2^-80 as large
+          const bool mine = gain && ss == INFINITY;
+          if (mine) {
+            eps = 0.f;  // nothing beside such squares
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= 0x1p-80f;
+          }
+          const float again = sum_of_squares();
+          if (mine) ss = again;
+        }
+        if (gain) {
+          const float f = rsqrtf(ss * (1.f / HD) + eps);
+          const float4 g0 = *reinterpret_cast<const float4*>(gain + piece * 8), g1 = *reinterpret_cast<const float4*>(gain + piece * 8 + 4);
+          const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = x[i] * f * g[i];
+        }
+      }
+      const int t = max(tok[j] - t0, 0);
+      const bool turns = (query || key) && piece < 2 * a.half;
+      if (a.neighbours) {
+        if (turns) {
+          const float4 c = *reinterpret_cast<const float4*>(&s_cos[t][piece * 4]), s = *reinterpret_cast<const float4*>(&s_sin[t][piece * 4]);
+          const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float u = x[2 * i], w = x[2 * i + 1];
+            x[2 * i] = u * cc[i] - w * ss[i];
+            x[2 * i + 1] = w * cc[i] + u * ss[i];
+          }
+        }
+      } else if (a.half) {
+        const bool low = piece < a.half;
+        const int other = piece >= 2 * a.half ? 0 : low ? a.half : -a.half, lane = tid & 31, i0 = turns ? (low ? piece : piece - a.half) * 8 : 0;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], lane + other);
+        if (turns) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 4) {
+            const float4 c = *reinterpret_cast<const float4*>(&s_cos[t][i0 + i]), s = *reinterpret_cast<const float4*>(&s_sin[t][i0 + i]);
+            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int z = 0; z < 4; ++z) x[i + z] = fmaf(x[i + z], cc[z], low ? -y[i + z] * ss[z] : y[i + z] * ss[z]);
+          }
+        }
+      }
+      raw[j] = pack8<T>(x);
+    }
+    if (kRotate && (query || (key && !a.cache))) {
+      if (p.pos >= 0) {
+        uint16_t* to = query ? a.q_out + tok[j] * a.qo_token + r * a.qo_head : a.k_out + tok[j] * a.ko_token + (r - a.nq) * a.ko_head;
+        *reinterpret_cast<uint4*>(to + piece * 8) = raw[j];
+      }
+    }
+    const int row = ((r - a.nq) << a.shift) + p.at;  // of the page, where this is a key or a value with a place
+    if (kHeld) {
+      float x[8];
+      widen8<T>(raw[j], x);
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
+        top = max(top, b < 0x7f800000u ? b : 0u);
+      }
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (!query && p.page >= 0) {
+        const int e = exponent_of(top);
+        char* page = a.cache + p.page * a.page_bytes;
+        *reinterpret_cast<uint2*>(page + (int64_t)row * HD + piece * 8) = to_e4m3(x, __uint_as_float((uint32_t)(254 - e) << 23));
+        if (piece == 0) page[((int64_t)2 * a.nkv << a.shift) * HD + row] = (char)e;
+      }
+    } else if (!query && a.cache && p.page >= 0) {
+      *reinterpret_cast<uint4*>(a.cache + p.page * a.page_bytes + (int64_t)row * (HD * 2) + piece * 16) = raw[j];
+    }
+  }
+}
+
+template <class T, int HD, bool kHeld>
+__global__ void __launch_bounds__(kThreads)
+k_rows_out(const __grid_constant__ RowsArgs a) {
+  using R = Rows<HD>;
+  constexpr int L = R::kLanes;
+  __shared__ Place s_place[R::kTokens];
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+  const int tid = threadIdx.x, piece = tid % L;
+  const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock, last = min(total, first + R::kBlock) - 1;
+  const int t0 = (int)(first / a.rows), tokens = (int)(last / a.rows) - t0 + 1;
+  for (int t = tid; t < tokens; t += kThreads) s_place[t] = place_of(a, t0 + t);
+  __syncthreads();
+  uint4 raw[kVecs];
+  float power[kVecs];
+  uint16_t* to[kVecs];
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const uint32_t row = first + j * R::kTurn + tid / L;
+    to[j] = nullptr;
+    if (row > last) continue;
+    const int t = (int)(row / a.rows), r = (int)(row - (uint32_t)t * a.rows);
+    const Place p = s_place[t - t0];
+    if (p.page < 0) continue;
+    to[j] = (r < a.nkv ? a.k + t * a.k_token + r * a.k_head : a.v + t * a.v_token + (r - a.nkv) * a.v_head) + piece * 8;
+    const char* page = a.cache + p.page * a.page_bytes;
+    const int at = (r << a.shift) + p.at;
+    if (kHeld) {
+      const uint2 w = *reinterpret_cast<const uint2*>(page + (int64_t)at * HD + piece * 8);
+      raw[j] = make_uint4(w.x, w.y, 0, 0);
+      power[j] = __uint_as_float((uint32_t)(uint8_t)page[((int64_t)2 * a.nkv << a.shift) * HD + at] << 23);
+    } else {
+      raw[j] = *reinterpret_cast<const uint4*>(page + (int64_t)at * (HD * 2) + piece * 16);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    if (!to[j]) continue;
+    if (kHeld) {
+      float x[8];
+      const uint32_t w[4] = {raw[j].x & 0xffffu, raw[j].x >> 16, raw[j].y & 0xffffu, raw[j].y >> 16};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w[i], __NV_E4M3);
+        const float2 f = __half22float2(__half2(h));
+        x[2 * i] = f.x * power[j];
+        x[2 * i + 1] = f.y * power[j];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = x[i] > largest<T>() ? largest<T>() : x[i] < -largest<T>() ? -largest<T>() : x[i];  // NaN stays
+      raw[j] = pack8<T>(x);
+    }
+    *reinterpret_cast<uint4*>(to[j]) = raw[j];
+  }
+}
+
+template <class T>
+cudaError_t launch_in(const RowsArgs& a, int hd, bool rotate, bool held, cudaStream_t s) {
+  const int block = hd == 128 ? Rows<128>::kBlock : Rows<64>::kBlock;
+  const dim3 grid((unsigned)(((int64_t)a.n_tokens * a.rows + block - 1) / block));
+  auto go = [&](auto kernel) { return launch_early(kernel, grid, kThreads, 0, s, a); };
+  if (hd == 128) return !rotate ? go(k_rows_in<T, 128, false, true>) : held ? go(k_rows_in<T, 128, true, true>) : go(k_rows_in<T, 128, true, false>);
+  return !rotate ? go(k_rows_in<T, 64, false, true>) : held ? go(k_rows_in<T, 64, true, true>) : go(k_rows_in<T, 64, true, false>);
+}
+template <class T>
+cudaError_t launch_out(const RowsArgs& a, int hd, bool held, cudaStream_t s) {
+  const int block = hd == 128 ? Rows<128>::kBlock : Rows<64>::kBlock;
+  const dim3 grid((unsigned)(((int64_t)a.n_tokens * a.rows + block - 1) / block));
+  auto go = [&](auto kernel) { return launch_early(kernel, grid, kThreads, 0, s, a); };
+  if (hd == 128) return held ? go(k_rows_out<T, 128, true>) : go(k_rows_out<T, 128, false>);
+  return held ? go(k_rows_out<T, 64, true>) : go(k_rows_out<T, 64, false>);
+}
+
+// What is wrong with rows that are written.
+const char* out_error(const np_rows* r, int n_tokens, int heads) {
+  if (const char* m = rows_error(r)) return m;
+  if ((n_tokens > 1 && r->token_stride == 0) || (heads > 1 && r->head_stride == 0)) return "rows of a result need strides above 0";
+  return nullptr;
+}
+
+const char* rotation_error(const np_rotation* r, int head_dim) {
+  if (!r) return "NULL rotation";
+  if (r->rot_dim < 0 || r->rot_dim > head_dim || r->rot_dim % 16) return "rot_dim must be a multiple of 16 in [0, head_dim]";
+  if (r->pairs != NP_ROT_HALVES && r->pairs != NP_ROT_NEIGHBOURS) return "pairs must be NP_ROT_HALVES or NP_ROT_NEIGHBOURS";
+  if (r->rot_dim && (!r->freq || (uintptr_t)r->freq % 8)) return "freq must be there, and 8-byte aligned";
+  if ((uintptr_t)r->q_gain % 16 || (uintptr_t)r->k_gain % 16) return "gains must be 16-byte aligned";
+  if (!(r->eps >= FLT_MIN) || !std::isfinite(r->eps)) return "eps must be positive, not below the normal numbers, and finite";
+  for (int x : r->reserved)
+    if (x) return "reserved must be 0";
+  return nullptr;
+}
+
+// Counts and places of tokens, the same for all calls.
+const char* tokens_error(int32_t n_tokens, const int32_t* cu, int32_t n) {
+  if (n < 0 || n_tokens < 0) return "n and n_tokens must not be negative";
+  if (!cu && n_tokens != n) return "without cu there is one token for each sequence";
+  return nullptr;
+}
+
+void put_rotation(RowsArgs& a, const np_rotation* r) {
+  a.freq = r->freq;
+  a.q_gain = r->q_gain;
+  a.k_gain = r->k_gain;
+  a.eps = r->eps;
+  a.half = r->rot_dim / 16;
+  a.neighbours = r->pairs == NP_ROT_NEIGHBOURS;
+}
+void put_tokens(RowsArgs& a, int n_tokens, const int32_t* seqs, const int32_t* cu, const int32_t* start, int n) {
+  a.seqs = seqs;
+  a.cu = cu;
+  a.start = start;
+  a.n = n;
+  a.n_tokens = n_tokens;
+}
+void put_rows(const np_rows* r, uint16_t** data, int64_t* token, int64_t* head) {
+  *data = static_cast<uint16_t*>(r->data);
+  *token = r->token_stride;
+  *head = r->head_stride;
+}
+void put_cache(RowsArgs& a, const np_kv_desc* d, const void* cache, int layer, const np_kv_tables* t) {
+  a.page_bytes = page_bytes(d);
+  a.cache = static_cast<char*>(const_cast<void*>(cache)) + (int64_t)layer * d->n_pages * a.page_bytes;
+  a.table = t->page_table;
+  a.lens = t->lens;
+  a.status = t->status;
+  a.shift = log2_of(d->page_tokens);
+  a.n_pages = d->n_pages;
+  a.max_seqs = d->max_seqs;
+  a.max_pages = d->max_pages;
+  a.nkv = d->n_kv_heads;
+}
+constexpr const char* kTooMany = "too many rows for one call";
+bool too_many(const RowsArgs& a) { return (int64_t)a.n_tokens * a.rows > 0x7fffffffLL - 2 * Rows<64>::kBlock; }
+
+// What every call over a cache checks; 1: there is nothing to do.
+int enter(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* k, const np_rows* v, int32_t n_tokens,
+          const int32_t* cu, const int32_t* start, int32_t n) {
+  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
+  if (!t || !t->page_table || !t->lens || !t->status) return fail(NP_E_INVAL, "a table pointer is NULL");
+  if (const char* m = tokens_error(n_tokens, cu, n)) return fail(NP_E_INVAL, m);
+  if (n > d->max_seqs) return fail(NP_E_INVAL, "n outside [0, max_seqs]");
+  if (n == 0 || n_tokens == 0) return 1;
+  if (!cache || !start) return fail(NP_E_INVAL, "NULL argument");
+  if ((uintptr_t)cache % 16) return fail(NP_E_INVAL, "cache must be 16-byte aligned");
+  if (layer < 0 || layer >= d->n_layers) return fail(NP_E_INVAL, "layer outside the cache");
+  if (const char* m = rows_error(k)) return fail(NP_E_INVAL, m);
+  if (const char* m = rows_error(v)) return fail(NP_E_INVAL, m);
+  return NP_OK;
+}
+
+int run(const RowsArgs& a, int type, int hd, bool out, bool rotate, bool held, void* stream) {
+  if (too_many(a)) return fail(NP_E_INVAL, kTooMany);
+  int sms;
+  if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (out) e = type == NP_T_BF16 ? launch_out<__nv_bfloat16>(a, hd, held, s) : launch_out<__half>(a, hd, held, s);
+  else e = type == NP_T_BF16 ? launch_in<__nv_bfloat16>(a, hd, rotate, held, s) : launch_in<__half>(a, hd, rotate, held, s);
+  return e == cudaSuccess ? NP_OK : fail_cuda(e);
+}
+
+}  // namespace
+
+int append_held(const np_kv_desc* d, void* cache, int32_t layer, const np_kv_tables* t, const np_rows* k, const np_rows* v, int32_t n_tokens,
+                const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n, void* stream) {
+  RowsArgs a = {};
+  put_tokens(a, n_tokens, seqs, cu, start, n);
+  put_cache(a, d, cache, layer, t);
+  put_rows(k, &a.k, &a.k_token, &a.k_head);
+  put_rows(v, &a.v, &a.v_token, &a.v_head);
+  a.rows = 2 * a.nkv;
+  return run(a, row_type(d), d->head_dim, false, false, true, stream);
+}
+
+}  // namespace npa
+
+using namespace npa;
+
+extern "C" {
+
+int np_attn_rotate(const np_attn_shape* d, const np_rotation* r, const np_rows* q, const np_rows* k, const np_rows* q_out, const np_rows* k_out,
+                   int32_t n_tokens, const int32_t* cu, const int32_t* start, int32_t n, void* stream) {
+  if (!d) return fail(NP_E_INVAL, "NULL argument");
+  if (d->dtype != NP_T_BF16 && d->dtype != NP_T_FP16) return fail(NP_E_INVAL, "dtype must be NP_T_BF16 or NP_T_FP16");
+  if (d->head_dim != 64 && d->head_dim != 128) return fail(NP_E_INVAL, "head_dim must be 64 or 128");
+  if (d->n_kv_heads < 1 || d->n_kv_heads > 1024 || d->n_heads < 1 || d->n_heads > (1 << 17))
+    return fail(NP_E_INVAL, "n_kv_heads must be in [1, 1024], n_heads in [1, 131072]");
+  for (int x : d->reserved)
+    if (x) return fail(NP_E_INVAL, "reserved must be 0");
+  if (const char* m = rotation_error(r, d->head_dim)) return fail(NP_E_INVAL, m);
+  if (const char* m = tokens_error(n_tokens, cu, n)) return fail(NP_E_INVAL, m);
+  if (n == 0 || n_tokens == 0) return NP_OK;
+  if (!start) return fail(NP_E_INVAL, "NULL argument");
+  if (const char* m = rows_error(q)) return fail(NP_E_INVAL, m);
+  if (const char* m = rows_error(k)) return fail(NP_E_INVAL, m);
+  if (const char* m = out_error(q_out, n_tokens, d->n_heads)) return fail(NP_E_INVAL, m);
+  if (const char* m = out_error(k_out, n_tokens, d->n_kv_heads)) return fail(NP_E_INVAL, m);
+  RowsArgs a = {};
+  put_tokens(a, n_tokens, nullptr, cu, start, n);
+  put_rotation(a, r);
+  uint16_t* qd;
+  put_rows(q, &qd, &a.q_token, &a.q_head);
+  a.q = qd;
+  put_rows(k, &a.k, &a.k_token, &a.k_head);
+  put_rows(q_out, &a.q_out, &a.qo_token, &a.qo_head);
+  put_rows(k_out, &a.k_out, &a.ko_token, &a.ko_head);
+  a.nq = d->n_heads;
+  a.nkv = d->n_kv_heads;
+  a.rows = a.nq + a.nkv;
+  return run(a, d->dtype, d->head_dim, false, true, false, stream);
+}
+
+int np_kv_append_rotated(const np_kv_desc* d, void* cache, int32_t layer, const np_kv_tables* t, const np_rotation* r, const np_rows* q,
+                         int32_t n_heads, const np_rows* k, const np_rows* v, const np_rows* q_out, int32_t n_tokens, const int32_t* seqs,
+                         const int32_t* cu, const int32_t* start, int32_t n, void* stream) {
+  if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
+  if (const char* m = rotation_error(r, d->head_dim)) return fail(NP_E_INVAL, m);
+  if (n_heads < 1 || n_heads > (1 << 17)) return fail(NP_E_INVAL, "n_heads outside [1, 131072]");
+  if (int rc = enter(d, cache, layer, t, k, v, n_tokens, cu, start, n)) return rc == 1 ? NP_OK : rc;
+  if (const char* m = rows_error(q)) return fail(NP_E_INVAL, m);
+  if (const char* m = out_error(q_out, n_tokens, n_heads)) return fail(NP_E_INVAL, m);
+  RowsArgs a = {};
+  put_tokens(a, n_tokens, seqs, cu, start, n);
+  put_rotation(a, r);
+  put_cache(a, d, cache, layer, t);
+  uint16_t* qd;
+  put_rows(q, &qd, &a.q_token, &a.q_head);
+  a.q = qd;
+  put_rows(k, &a.k, &a.k_token, &a.k_head);
+  put_rows(v, &a.v, &a.v_token, &a.v_head);
+  put_rows(q_out, &a.q_out, &a.qo_token, &a.qo_head);
+  a.nq = n_heads;
+  a.rows = a.nq + 2 * a.nkv;
+  return run(a, row_type(d), d->head_dim, false, true, held_in_8(d), stream);
+}
+
+int np_kv_read(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* k, const np_rows* v, int32_t n_tokens,
+               const int32_t* seqs, const int32_t* cu, const int32_t* start, int32_t n, void* stream) {
+  if (int rc = enter(d, cache, layer, t, k, v, n_tokens, cu, start, n)) return rc == 1 ? NP_OK : rc;
+  if (const char* m = out_error(k, n_tokens, d->n_kv_heads)) return fail(NP_E_INVAL, m);
+  if (const char* m = out_error(v, n_tokens, d->n_kv_heads)) return fail(NP_E_INVAL, m);
+  RowsArgs a = {};
+  put_tokens(a, n_tokens, seqs, cu, start, n);
+  put_cache(a, d, cache, layer, t);
+  put_rows(k, &a.k, &a.k_token, &a.k_head);
+  put_rows(v, &a.v, &a.v_token, &a.v_head);
+  a.rows = 2 * a.nkv;
+  return run(a, row_type(d), d->head_dim, true, false, held_in_8(d), stream);
+}
+
+}  // extern "C"

@@ -403,7 +403,7 @@ def make_kv_tables(page_table, lens, refs, scratch, status) -> np_kv_tables:
 
 def make_rotation(freq, q_gain=None, k_gain=None, neighbours: bool = False, eps: float = 1e-6) -> np_rotation:
     """Norm and rotation by position.  ``freq``: float64 [rot_dim / 2], radians per position (None: no rotation); ``q_gain``, ``k_gain``: float32
-    [head_dim] (None: not normed); contiguous tensors of one CUDA device, which the caller keeps alive.  ``neighbours``: pairs are values 2i and
+    [head_dim] (None: not normed); contiguous tensors of one CUDA device, which the result keeps alive.  ``neighbours``: pairs are values 2i and
     2i + 1, else i and i + rot_dim / 2."""
     tensors = [t for t in (freq, q_gain, k_gain) if t is not None]
     for t in tensors:
@@ -415,6 +415,7 @@ def make_rotation(freq, q_gain=None, k_gain=None, neighbours: bool = False, eps:
     r = np_rotation(*[None if t is None or t.numel() == 0 else t.data_ptr() for t in (freq, q_gain, k_gain)], 0 if freq is None else 2 * freq.numel(),
                     NP_ROT_NEIGHBOURS if neighbours else NP_ROT_HALVES, eps)
     gain = q_gain if q_gain is not None else k_gain
+    r.kept = tensors
     if tensors:
         r.room = (tensors[0].get_device(), -1 if gain is None else gain.numel())
     return r

@@ -669,7 +669,7 @@ typedef struct np_rotation {
  *   q, q_out   n_tokens rows of n_heads heads;  k, k_out  n_tokens rows of n_kv_heads heads.  A result may be its input itself (the same
  *              data and strides) and may not overlap the inputs or the other result in another way; its strides are above 0 along
  *              more than one row or head
- *   cu    dev [n + 1] ascending (NULL: one token each, n_tokens == n),  start  dev [n] */
+ *   cu    dev [n + 1] ascending, n <= NP_KV_MAX_SEQS (NULL: one token each, n_tokens == n, any number),  start  dev [n] */
 int np_attn_rotate(const np_attn_shape* shape, const np_rotation* rotation, const np_rows* q, const np_rows* k, const np_rows* q_out,
                    const np_rows* k_out, int32_t n_tokens, const int32_t* cu, const int32_t* start, int32_t n, void* stream);
 

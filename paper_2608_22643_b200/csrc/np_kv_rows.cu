@@ -4,8 +4,9 @@
 //   y = x / sqrt(mean(x^2) + eps) * gain,   (a, b) -> (a cos t - b sin t, b cos t + a sin t),   t = position * freq[i]
 //   e = the least of -60 .. 120 with max|x| <= 448 * 2^e,   x -> e4m3(x * 2^-e)
 //
-// Every value is read and written once, so the bytes bound all of this.  A row of head_dim values belongs to 16 (or 8) lanes, 16 bytes each;
-// a lane has four such pieces on their way before it works on the first.  The lane with the other half of a pair is a shuffle away.
+// Every value is read and written once, so the bytes bound all of this, if the instructions are few enough.  A row of head_dim values belongs
+// to head_dim / 16 lanes; a lane has two rows on their way before it works on the first.  Its values are eight and the eight that they are
+// pairs with, so nothing but the sum of squares and the largest magnitude goes from lane to lane.
 //
 // Cosines and sines belong to a token, not to a head: a block works them out once for its few tokens, while its loads are on their way.
 // The angle is a product in fp64 that is brought to a fraction of a turn there (a position of 2^31 leaves 2^-24 of a turn), so fp32 does for the
@@ -28,11 +29,12 @@
 namespace npa {
 namespace {
 
-constexpr int kThreads = 256, kVecs = 4;
-template <int HD>
+constexpr int kThreads = 128, kValues = 32;  // of a lane on their way
+template <int HD, int kEach>
 struct Rows {
-  static constexpr int kLanes = HD / 8;                      // of a row
+  static constexpr int kLanes = HD / kEach;                  // of a row: a lane has that many of its values
   static constexpr int kTurn = kThreads / kLanes;            // rows of a block at a time
+  static constexpr int kVecs = kValues / kEach;
   static constexpr int kBlock = kTurn * kVecs;
   static constexpr int kTokens = kBlock / 2 + 2;             // of a block at most: a token has two rows or more
 };
@@ -85,62 +87,77 @@ __device__ __forceinline__ uint32_t pack<__half>(float x, float y) {
   const __half2 h = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+// No further from 0 than the type's largest number; NaN stays.
 template <class T>
-__device__ __forceinline__ void widen8(const uint4& v, float (&x)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = widen<T>(w[i]);
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
-}
-template <class T>
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  return make_uint4(pack<T>(x[0], x[1]), pack<T>(x[2], x[3]), pack<T>(x[4], x[5]), pack<T>(x[6], x[7]));
-}
-template <class T>
-__device__ __forceinline__ float largest() {
-  return std::is_same<T, __half>::value ? 65504.f : __uint_as_float(0x7f7f0000u);
+__device__ __forceinline__ float to_finite(float x) {
+  const float most = std::is_same<T, __half>::value ? 65504.f : __uint_as_float(0x7f7f0000u);
+  return x > most ? most : x < -most ? -most : x;
 }
 
-// Where the tokens [t0, t1] of a block are: their position (-1: the row is passed over), their page (-1: no place in the cache) and their
-// place in it.
+template <class T>
+__device__ __forceinline__ void widen4(const uint2& v, float* x) {
+  const float2 a = widen<T>(v.x), b = widen<T>(v.y);
+  x[0] = a.x;
+  x[1] = a.y;
+  x[2] = b.x;
+  x[3] = b.y;
+}
+__device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
+  const float u = a, w = b;
+  a = u * c - w * s;
+  b = w * c + u * s;
+}
+
+// Where a token is: its position (-1: the row is passed over), its page (-1: no place in the cache) and its place in that.
 struct Place {
   int64_t pos;
   int page, at;
 };
-__device__ __forceinline__ Place place_of(const RowsArgs& a, int t) {
-  Place p = {-1, -1, 0};
-  int i = -1, off = 0;
-  if (!a.cu) {
-    i = t < a.n ? t : -1;
-  } else if (t >= a.cu[0] && t < a.cu[a.n]) {
-    int lo = 0, hi = a.n - 1;  // the last i with cu[i] <= t
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.cu[mid] <= t) lo = mid;
-      else hi = mid - 1;
-    }
-    i = lo;
-    off = t - a.cu[lo];
+// cu of the call goes to shared memory, where a block's threads find their tokens' sequences without a trip to memory for each step.
+__device__ __forceinline__ void keep_starts(const RowsArgs& a, int* cu) {
+  if (a.cu)
+    for (int i = threadIdx.x; i <= a.n; i += kThreads) cu[i] = a.cu[i];
+}
+// The sequence of token t, as a place in the call's lists; -1: none.  *off: the token's number in it.
+__device__ __forceinline__ int sequence_of(const RowsArgs& a, const int* cu, int t, int* off) {
+  *off = 0;
+  if (!a.cu) return t < a.n ? t : -1;
+  if (t < cu[0] || t >= cu[a.n]) return -1;
+  int lo = 0, hi = a.n - 1;  // the last i with cu[i] <= t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (cu[mid] <= t) lo = mid;
+    else hi = mid - 1;
   }
-  if (i < 0 || off < 0) return p;
+  *off = t - cu[lo];
+  return *off < 0 ? -1 : lo;
+}
+__device__ __forceinline__ int64_t position_of(const RowsArgs& a, const int* cu, int t) {
+  int off;
+  const int i = sequence_of(a, cu, t, &off), st = i < 0 ? -1 : a.start[i];
+  return st < 0 ? -1 : (int64_t)st + off;
+}
+__device__ __forceinline__ Place place_of(const RowsArgs& a, const int* cu, int t) {
+  Place p = {-1, -1, 0};
+  int off;
+  const int i = sequence_of(a, cu, t, &off);
+  if (i < 0) return p;
   const int st = a.start[i], seq = !a.cache ? 0 : a.seqs ? a.seqs[i] : i;
   if (st < 0) return p;
   p.pos = (int64_t)st + off;
   if (!a.cache) return p;
   if (seq < 0 || seq >= a.max_seqs) {
     atomicOr(a.status, NP_KV_S_SEQ);
-  } else if (p.pos < a.lens[seq]) {
-    const int64_t j = p.pos >> a.shift;
-    const int pg = j < a.max_pages ? a.table[(size_t)seq * a.max_pages + j] : -1;
-    if ((unsigned)pg < (unsigned)a.n_pages) {
-      p.page = pg;
-      p.at = (int)(p.pos & ((1 << a.shift) - 1));
-    } else {
-      atomicOr(a.status, NP_KV_S_PAGE);
-    }
+    return p;
+  }
+  const int64_t j = p.pos >> a.shift;
+  const int len = a.lens[seq], pg = j < a.max_pages ? a.table[(size_t)seq * a.max_pages + j] : -1;  // on their way together
+  if (p.pos >= len) return p;
+  if ((unsigned)pg < (unsigned)a.n_pages) {
+    p.page = pg;
+    p.at = (int)(p.pos & ((1 << a.shift) - 1));
+  } else {
+    atomicOr(a.status, NP_KV_S_PAGE);
   }
   return p;
 }
@@ -165,145 +182,176 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float power) {
   return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 
+enum Kind { kQuery, kKey, kValue };
+
 // kRotate: norm and rotation.  kHeld: keys and values go into pages of 8 bits.
 template <class T, int HD, bool kRotate, bool kHeld>
 __global__ void __launch_bounds__(kThreads)
 k_rows_in(const __grid_constant__ RowsArgs a) {
-  using R = Rows<HD>;
-  constexpr int L = R::kLanes;
-  __shared__ Place s_place[R::kTokens];
+  using R = Rows<HD, 8>;
+  constexpr int L = R::kLanes, kVecs = R::kVecs;
+  extern __shared__ int s_cu[];
+  __shared__ const uint16_t* s_src[R::kBlock];
+  __shared__ char* s_dst[R::kBlock];              // nullptr: the row is not written
+  __shared__ char* s_exponent[kHeld ? R::kBlock : 1];
+  __shared__ int s_row[R::kBlock];                // token of the block << 3 | whether it is normed << 2 | kind
+  __shared__ __align__(16) float s_gain[kRotate ? 2 : 1][HD];
+  __shared__ double s_freq[kRotate ? HD / 2 : 1];  // turns per position
   __shared__ __align__(16) float s_cos[kRotate ? R::kTokens : 1][HD / 2], s_sin[kRotate ? R::kTokens : 1][HD / 2];
+  const int tid = threadIdx.x, piece = tid % L, slot = tid / L;
+  const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock;
+  const int rows = (int)(min(total, first + R::kBlock) - first);
+  const int t0 = (int)(first / a.rows), tokens = (int)((first + rows - 1) / a.rows) - t0 + 1;
+  // ---- where rows come from
+  int t = 0, r = 0;
+  if (tid < rows) {
+    t = (int)((first + tid) / a.rows);
+    r = (int)(first + tid - (uint32_t)t * a.rows);
+    const int kind = r < a.nq ? kQuery : r < a.nq + a.nkv ? kKey : kValue;
+    s_src[tid] = kind == kQuery ? a.q + t * a.q_token + r * a.q_head
+                 : kind == kKey ? a.k + t * a.k_token + (r - a.nq) * a.k_head
+                                : a.v + t * a.v_token + (r - a.nq - a.nkv) * a.v_head;
+    const bool normed = kind == kQuery ? a.q_gain != nullptr : kind == kKey && a.k_gain != nullptr;
+    s_row[tid] = (t - t0) << 3 | (normed ? 4 : 0) | kind;
+  }
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
-  const int tid = threadIdx.x, piece = tid % L;
-  const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock, last = min(total, first + R::kBlock) - 1;
-  const int t0 = (int)(first / a.rows), tokens = (int)(last / a.rows) - t0 + 1;
-  uint4 raw[kVecs];
-  int tok[kVecs], of[kVecs];
+  keep_starts(a, s_cu);
+  if (kRotate && tid < a.half * 8) s_freq[tid] = a.freq[tid] * 0.15915494309189533577;  // 1 / (2 pi)
+  if (kRotate && tid < HD / 2) {  // two gains of each kind
+    const float2 one = make_float2(1.f, 1.f);
+    *reinterpret_cast<float2*>(&s_gain[0][2 * tid]) = a.q_gain ? *reinterpret_cast<const float2*>(a.q_gain + 2 * tid) : one;
+    *reinterpret_cast<float2*>(&s_gain[1][2 * tid]) = a.k_gain ? *reinterpret_cast<const float2*>(a.k_gain + 2 * tid) : one;
+  }
+  __syncthreads();
+  // A lane's eight values: four from o0 and four from o1 on.  Of halves that turn, so that pairs meet in a lane.
+  const bool turns = kRotate && piece < 2 * a.half, halves = turns && !a.neighbours;
+  const int o0 = halves ? 4 * piece : 8 * piece, o1 = halves ? 8 * a.half + 4 * piece : 8 * piece + 4;
+  uint2 raw[kVecs][2];
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
-    const uint32_t row = first + j * R::kTurn + tid / L;
-    raw[j] = make_uint4(0, 0, 0, 0);
-    tok[j] = -1;
-    of[j] = 0;
-    if (row > last) continue;
-    const int t = (int)(row / a.rows), r = (int)(row - (uint32_t)t * a.rows);
-    tok[j] = t;
-    of[j] = r;
-    const uint16_t* src = r < a.nq            ? a.q + t * a.q_token + r * a.q_head
-                          : r < a.nq + a.nkv ? a.k + t * a.k_token + (r - a.nq) * a.k_head
-                                             : a.v + t * a.v_token + (r - a.nq - a.nkv) * a.v_head;
-    raw[j] = *reinterpret_cast<const uint4*>(src + piece * 8);
+    raw[j][0] = raw[j][1] = make_uint2(0, 0);
+    const int i = j * R::kTurn + slot;
+    if (i >= rows) continue;
+    const uint16_t* src = s_src[i];
+    if (kRotate) {
+      raw[j][0] = *reinterpret_cast<const uint2*>(src + o0);
+      raw[j][1] = *reinterpret_cast<const uint2*>(src + o1);
+    } else {
+      const uint4 v = *reinterpret_cast<const uint4*>(src + o0);
+      raw[j][0] = make_uint2(v.x, v.y);
+      raw[j][1] = make_uint2(v.z, v.w);
+    }
   }
-  for (int t = tid; t < tokens; t += kThreads) s_place[t] = place_of(a, t0 + t);
-  __syncthreads();
+  // ---- where they go, and the angles of their tokens
+  if (tid < rows) {
+    const Place p = place_of(a, s_cu, t);
+    char* dst = nullptr;
+    if (kRotate && r < a.nq) {
+      if (p.pos >= 0) dst = reinterpret_cast<char*>(a.q_out + t * a.qo_token + r * a.qo_head);
+    } else if (kRotate && !a.cache) {
+      if (p.pos >= 0) dst = reinterpret_cast<char*>(a.k_out + t * a.ko_token + (r - a.nq) * a.ko_head);
+    } else if (p.page >= 0) {
+      const int64_t row = ((int64_t)(r - a.nq) << a.shift) + p.at;  // of the page
+      char* page = a.cache + p.page * a.page_bytes;
+      dst = page + row * (kHeld ? HD : HD * 2);
+      if (kHeld) s_exponent[tid] = page + ((int64_t)2 * a.nkv << a.shift) * HD + row;
+    }
+    s_dst[tid] = dst;
+  }
   if (kRotate && a.half) {
     const int pairs = a.half * 8;
     for (int x = tid; x < tokens * pairs; x += kThreads) {
-      const int t = x / pairs, i = x - t * pairs;
-      double turns = (double)s_place[t].pos * (a.freq[i] * 0.15915494309189533577);  // 1 / (2 pi)
-      turns -= rint(turns);
-      float s, c;
-      sincospif(2.f * (float)turns, &s, &c);
-      s_cos[t][i] = c;
-      s_sin[t][i] = s;
+      const int u = x / pairs, i = x - u * pairs;
+      double turn = (double)position_of(a, s_cu, t0 + u) * s_freq[i];
+      turn -= rint(turn);
+      float sin, cos;
+      sincospif(2.f * (float)turn, &sin, &cos);
+      s_cos[u][i] = cos;
+      s_sin[u][i] = sin;
     }
-    __syncthreads();
   }
+  __syncthreads();
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
-    const int r = of[j];
-    const bool query = r < a.nq, key = !query && r < a.nq + a.nkv;
-    const Place p = tok[j] < 0 ? Place{-1, -1, 0} : s_place[tok[j] - t0];
-    if (kRotate) {
-      float x[8];
-      widen8<T>(raw[j], x);
+    const int i = j * R::kTurn + slot;
+    const bool there = i < rows;
+    const int row = there ? s_row[i] : kValue, kind = row & 3;
+    char* dst = there ? s_dst[i] : nullptr;
+    float x[8];
+    if (kRotate && __any_sync(0xffffffffu, kind != kValue)) {
+      widen4<T>(raw[j][0], x);
+      widen4<T>(raw[j][1], x + 4);
       if (a.q_gain || a.k_gain) {
         auto sum_of_squares = [&] {
           float ss = x[0] * x[0];
 #pragma unroll
-          for (int i = 1; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+          for (int z = 1; z < 8; ++z) ss = fmaf(x[z], x[z], ss);
 #pragma unroll
           for (int o = 1; o < L; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
           return ss;
         };
         float ss = sum_of_squares(), eps = a.eps;
-        const float* gain = query ? a.q_gain : key ? a.k_gain : nullptr;
-        if (__any_sync(0xffffffffu, gain && ss == INFINITY)) {  // squares past fp32's range: of values 2^-80 as large
-          const bool mine = gain && ss == INFINITY;
-          if (mine) {
+        const bool normed = row & 4, past = normed && ss == INFINITY;
+        if (__any_sync(0xffffffffu, past)) {  // squares past fp32's range: of values 2^-80 as large
+          if (past) {
             eps = 0.f;  // nothing beside such squares
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= 0x1p-80f;
+            for (int z = 0; z < 8; ++z) x[z] *= 0x1p-80f;
           }
           const float again = sum_of_squares();
-          if (mine) ss = again;
+          if (past) ss = again;
         }
-        if (gain) {
+        if (normed) {
           const float f = rsqrtf(ss * (1.f / HD) + eps);
-          const float4 g0 = *reinterpret_cast<const float4*>(gain + piece * 8), g1 = *reinterpret_cast<const float4*>(gain + piece * 8 + 4);
+          const float4 g0 = *reinterpret_cast<const float4*>(&s_gain[kind][o0]), g1 = *reinterpret_cast<const float4*>(&s_gain[kind][o1]);
           const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = x[i] * f * g[i];
+          for (int z = 0; z < 8; ++z) x[z] = x[z] * f * g[z];
         }
       }
-      const int t = max(tok[j] - t0, 0);
-      const bool turns = (query || key) && piece < 2 * a.half;
-      if (a.neighbours) {
-        if (turns) {
-          const float4 c = *reinterpret_cast<const float4*>(&s_cos[t][piece * 4]), s = *reinterpret_cast<const float4*>(&s_sin[t][piece * 4]);
-          const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+      if (turns && kind != kValue) {
+        const float4 c4 = *reinterpret_cast<const float4*>(&s_cos[row >> 3][4 * piece]), s4 = *reinterpret_cast<const float4*>(&s_sin[row >> 3][4 * piece]);
+        const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+        if (halves) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float u = x[2 * i], w = x[2 * i + 1];
-            x[2 * i] = u * cc[i] - w * ss[i];
-            x[2 * i + 1] = w * cc[i] + u * ss[i];
-          }
-        }
-      } else if (a.half) {
-        const bool low = piece < a.half;
-        const int other = piece >= 2 * a.half ? 0 : low ? a.half : -a.half, lane = tid & 31, i0 = turns ? (low ? piece : piece - a.half) * 8 : 0;
-        float y[8];
+          for (int z = 0; z < 4; ++z) turn_pair(x[z], x[z + 4], c[z], s[z]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], lane + other);
-        if (turns) {
-#pragma unroll
-          for (int i = 0; i < 8; i += 4) {
-            const float4 c = *reinterpret_cast<const float4*>(&s_cos[t][i0 + i]), s = *reinterpret_cast<const float4*>(&s_sin[t][i0 + i]);
-            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-            for (int z = 0; z < 4; ++z) x[i + z] = fmaf(x[i + z], cc[z], low ? -y[i + z] * ss[z] : y[i + z] * ss[z]);
-          }
+          for (int z = 0; z < 4; ++z) turn_pair(x[2 * z], x[2 * z + 1], c[z], s[z]);
         }
       }
-      raw[j] = pack8<T>(x);
-    }
-    if (kRotate && (query || (key && !a.cache))) {
-      if (p.pos >= 0) {
-        uint16_t* to = query ? a.q_out + tok[j] * a.qo_token + r * a.qo_head : a.k_out + tok[j] * a.ko_token + (r - a.nq) * a.ko_head;
-        *reinterpret_cast<uint4*>(to + piece * 8) = raw[j];
+      if (kind != kValue) {
+        raw[j][0] = make_uint2(pack<T>(x[0], x[1]), pack<T>(x[2], x[3]));
+        raw[j][1] = make_uint2(pack<T>(x[4], x[5]), pack<T>(x[6], x[7]));
       }
     }
-    const int row = ((r - a.nq) << a.shift) + p.at;  // of the page, where this is a key or a value with a place
-    if (kHeld) {
-      float x[8];
-      widen8<T>(raw[j], x);
+    if (kHeld && __any_sync(0xffffffffu, kind != kQuery)) {
+      widen4<T>(raw[j][0], x);
+      widen4<T>(raw[j][1], x + 4);
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
+      for (int z = 0; z < 8; ++z) {
+        const uint32_t b = __float_as_uint(x[z]) & 0x7fffffffu;
         top = max(top, b < 0x7f800000u ? b : 0u);
       }
 #pragma unroll
       for (int o = 1; o < L; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (!query && p.page >= 0) {
+      if (kind != kQuery && dst) {
         const int e = exponent_of(top);
-        char* page = a.cache + p.page * a.page_bytes;
-        *reinterpret_cast<uint2*>(page + (int64_t)row * HD + piece * 8) = to_e4m3(x, __uint_as_float((uint32_t)(254 - e) << 23));
-        if (piece == 0) page[((int64_t)2 * a.nkv << a.shift) * HD + row] = (char)e;
+        const uint2 w = to_e4m3(x, __uint_as_float((uint32_t)(254 - e) << 23));
+        if (kRotate) {
+          *reinterpret_cast<uint32_t*>(dst + o0) = w.x;
+          *reinterpret_cast<uint32_t*>(dst + o1) = w.y;
+        } else {
+          *reinterpret_cast<uint2*>(dst + o0) = w;
+        }
+        if (piece == 0) *s_exponent[i] = (char)e;
       }
-    } else if (!query && a.cache && p.page >= 0) {
-      *reinterpret_cast<uint4*>(a.cache + p.page * a.page_bytes + (int64_t)row * (HD * 2) + piece * 16) = raw[j];
+    }
+    if ((!kHeld || kind == kQuery) && dst) {
+      *reinterpret_cast<uint2*>(dst + 2 * o0) = raw[j][0];
+      *reinterpret_cast<uint2*>(dst + 2 * o1) = raw[j][1];
     }
   }
 }
@@ -311,72 +359,81 @@ k_rows_in(const __grid_constant__ RowsArgs a) {
 template <class T, int HD, bool kHeld>
 __global__ void __launch_bounds__(kThreads)
 k_rows_out(const __grid_constant__ RowsArgs a) {
-  using R = Rows<HD>;
-  constexpr int L = R::kLanes;
-  __shared__ Place s_place[R::kTokens];
+  using R = Rows<HD, 16>;
+  constexpr int L = R::kLanes, kVecs = R::kVecs;
+  extern __shared__ int s_cu[];
+  __shared__ const char* s_src[R::kBlock];  // nullptr: not there
+  __shared__ uint16_t* s_dst[R::kBlock];
+  __shared__ const uint8_t* s_exponent[kHeld ? R::kBlock : 1];
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
-  const int tid = threadIdx.x, piece = tid % L;
-  const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock, last = min(total, first + R::kBlock) - 1;
-  const int t0 = (int)(first / a.rows), tokens = (int)(last / a.rows) - t0 + 1;
-  for (int t = tid; t < tokens; t += kThreads) s_place[t] = place_of(a, t0 + t);
+  keep_starts(a, s_cu);
   __syncthreads();
-  uint4 raw[kVecs];
+  const int tid = threadIdx.x, piece = tid % L, slot = tid / L;
+  const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock;
+  const int rows = (int)(min(total, first + R::kBlock) - first);
+  if (tid < rows) {
+    const int t = (int)((first + tid) / a.rows), r = (int)(first + tid - (uint32_t)t * a.rows);
+    const Place p = place_of(a, s_cu, t);
+    const char* page = a.cache + p.page * a.page_bytes;
+    const int64_t at = ((int64_t)r << a.shift) + p.at;
+    s_src[tid] = p.page < 0 ? nullptr : page + at * (kHeld ? HD : HD * 2);
+    if (kHeld) s_exponent[tid] = reinterpret_cast<const uint8_t*>(page) + ((int64_t)2 * a.nkv << a.shift) * HD + at;
+    s_dst[tid] = r < a.nkv ? a.k + t * a.k_token + r * a.k_head : a.v + t * a.v_token + (r - a.nkv) * a.v_head;
+  }
+  __syncthreads();
+  uint4 raw[kVecs][kHeld ? 1 : 2];
   float power[kVecs];
   uint16_t* to[kVecs];
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
-    const uint32_t row = first + j * R::kTurn + tid / L;
+    const int i = j * R::kTurn + slot;
     to[j] = nullptr;
-    if (row > last) continue;
-    const int t = (int)(row / a.rows), r = (int)(row - (uint32_t)t * a.rows);
-    const Place p = s_place[t - t0];
-    if (p.page < 0) continue;
-    to[j] = (r < a.nkv ? a.k + t * a.k_token + r * a.k_head : a.v + t * a.v_token + (r - a.nkv) * a.v_head) + piece * 8;
-    const char* page = a.cache + p.page * a.page_bytes;
-    const int at = (r << a.shift) + p.at;
-    if (kHeld) {
-      const uint2 w = *reinterpret_cast<const uint2*>(page + (int64_t)at * HD + piece * 8);
-      raw[j] = make_uint4(w.x, w.y, 0, 0);
-      power[j] = __uint_as_float((uint32_t)(uint8_t)page[((int64_t)2 * a.nkv << a.shift) * HD + at] << 23);
+    const char* src = i < rows ? s_src[i] : nullptr;
+    if (!src) continue;
+    to[j] = s_dst[i] + piece * 16;
+    if constexpr (kHeld) {
+      raw[j][0] = *reinterpret_cast<const uint4*>(src + piece * 16);
+      power[j] = __uint_as_float((uint32_t)*s_exponent[i] << 23);
     } else {
-      raw[j] = *reinterpret_cast<const uint4*>(page + (int64_t)at * (HD * 2) + piece * 16);
+      raw[j][0] = *reinterpret_cast<const uint4*>(src + piece * 32);
+      raw[j][1] = *reinterpret_cast<const uint4*>(src + piece * 32 + 16);
     }
   }
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
     if (!to[j]) continue;
-    if (kHeld) {
-      float x[8];
-      const uint32_t w[4] = {raw[j].x & 0xffffu, raw[j].x >> 16, raw[j].y & 0xffffu, raw[j].y >> 16};
+    if constexpr (kHeld) {
+      const uint32_t w[4] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w};
+      uint32_t o[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w[i], __NV_E4M3);
+      for (int i = 0; i < 8; ++i) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (i & 1) * 16), __NV_E4M3);
         const float2 f = __half22float2(__half2(h));
-        x[2 * i] = f.x * power[j];
-        x[2 * i + 1] = f.y * power[j];
+        o[i] = pack<T>(to_finite<T>(f.x * power[j]), to_finite<T>(f.y * power[j]));
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = x[i] > largest<T>() ? largest<T>() : x[i] < -largest<T>() ? -largest<T>() : x[i];  // NaN stays
-      raw[j] = pack8<T>(x);
+      *reinterpret_cast<uint4*>(to[j]) = make_uint4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<uint4*>(to[j] + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+    } else {
+      *reinterpret_cast<uint4*>(to[j]) = raw[j][0];
+      *reinterpret_cast<uint4*>(to[j] + 8) = raw[j][1];
     }
-    *reinterpret_cast<uint4*>(to[j]) = raw[j];
   }
 }
 
 template <class T>
 cudaError_t launch_in(const RowsArgs& a, int hd, bool rotate, bool held, cudaStream_t s) {
-  const int block = hd == 128 ? Rows<128>::kBlock : Rows<64>::kBlock;
+  const int block = hd == 128 ? Rows<128, 8>::kBlock : Rows<64, 8>::kBlock;
   const dim3 grid((unsigned)(((int64_t)a.n_tokens * a.rows + block - 1) / block));
-  auto go = [&](auto kernel) { return launch_early(kernel, grid, kThreads, 0, s, a); };
+  auto go = [&](auto kernel) { return launch_early(kernel, grid, kThreads, a.cu ? (a.n + 1) * sizeof(int) : 0, s, a); };
   if (hd == 128) return !rotate ? go(k_rows_in<T, 128, false, true>) : held ? go(k_rows_in<T, 128, true, true>) : go(k_rows_in<T, 128, true, false>);
   return !rotate ? go(k_rows_in<T, 64, false, true>) : held ? go(k_rows_in<T, 64, true, true>) : go(k_rows_in<T, 64, true, false>);
 }
 template <class T>
 cudaError_t launch_out(const RowsArgs& a, int hd, bool held, cudaStream_t s) {
-  const int block = hd == 128 ? Rows<128>::kBlock : Rows<64>::kBlock;
+  const int block = hd == 128 ? Rows<128, 16>::kBlock : Rows<64, 16>::kBlock;
   const dim3 grid((unsigned)(((int64_t)a.n_tokens * a.rows + block - 1) / block));
-  auto go = [&](auto kernel) { return launch_early(kernel, grid, kThreads, 0, s, a); };
+  auto go = [&](auto kernel) { return launch_early(kernel, grid, kThreads, a.cu ? (a.n + 1) * sizeof(int) : 0, s, a); };
   if (hd == 128) return held ? go(k_rows_out<T, 128, true>) : go(k_rows_out<T, 128, false>);
   return held ? go(k_rows_out<T, 64, true>) : go(k_rows_out<T, 64, false>);
 }
@@ -404,6 +461,7 @@ const char* rotation_error(const np_rotation* r, int head_dim) {
 const char* tokens_error(int32_t n_tokens, const int32_t* cu, int32_t n) {
   if (n < 0 || n_tokens < 0) return "n and n_tokens must not be negative";
   if (!cu && n_tokens != n) return "without cu there is one token for each sequence";
+  if (cu && n > NP_KV_MAX_SEQS) return "n outside [0, NP_KV_MAX_SEQS]";
   return nullptr;
 }
 
@@ -440,7 +498,7 @@ void put_cache(RowsArgs& a, const np_kv_desc* d, const void* cache, int layer, c
   a.nkv = d->n_kv_heads;
 }
 constexpr const char* kTooMany = "too many rows for one call";
-bool too_many(const RowsArgs& a) { return (int64_t)a.n_tokens * a.rows > 0x7fffffffLL - 2 * Rows<64>::kBlock; }
+bool too_many(const RowsArgs& a) { return (int64_t)a.n_tokens * a.rows > 0x7fffffffLL - 2 * Rows<64, 16>::kBlock; }
 
 // What every call over a cache checks; 1: there is nothing to do.
 int enter(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* k, const np_rows* v, int32_t n_tokens,

@@ -100,6 +100,7 @@ def test_rotate_refuses_bad_arguments(lib):
     assert call(dtype=2) == BAD and call(dtype=16) == BAD and call(hd=96) == BAD and call(hq=0) == BAD and call(hkv=0) == BAD and call(hkv=1025) == BAD
     assert call(rot=None) == BAD and call(tokens=-1) == BAD and call(n=-1) == BAD and call(start=None) == BAD
     assert call(cu=None) == BAD and _said(lib, "one token for each")
+    assert call(n=1025) == BAD and _said(lib, "NP_KV_MAX_SEQS")
     for name in ("q", "k", "qo", "ko"):
         for field, value in (("data", None), ("data", P + 8), ("token_stride", 12), ("head_stride", -8)):
             assert call(**{name: _rows(**{field: value})}) == BAD

@@ -344,7 +344,7 @@ __device__ __forceinline__ void join_shared(const DecodeArgs& a, int tokens, int
 // three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16 sequences of 2000, five
 // 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
 constexpr int blocks_per_sm(int hd, int form) {
-  return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 2 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
+  return form == kHeldEight ? 3 : form == kHeldSixteen ? (hd == 64 ? 3 : 2) : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
 }
 
 // In 8 bits sums are of 2^(s - m + kHeldShift): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.
@@ -372,6 +372,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   constexpr bool kWide = kForm == kSixteen, kHeld = kForm == kHeldEight || kForm == kHeldSixteen;
   constexpr int HB = kForm == kSixteen || kForm == kHeldSixteen ? 16 : 8;  // heads of a block, at most
   constexpr int NT = HB / 8, NH = kHeld ? 2 * NT : 2;  // in 8 bits: eights of heads; heads of a lane's scores
+  constexpr int SC = kHeld && HD == 64 ? 2 : 1;         // sixteens of tokens of a chunk
+  constexpr int kTileTokens = kTile * SC, kUnitsBefore = kStart / SC;  // tokens of a tile, what a group's start counts
   constexpr int KV = kHeld ? HD / 64 : HD / 32;        // 16-byte pieces of a key row per lane
   constexpr int VW = HD / 32;                          // in 8 bits: words of a value row per lane
   constexpr int VC = HD / 64;        // 16-byte pieces of a value row per lane
@@ -385,7 +387,10 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   __shared__ __align__(16) float s_o[kWarps][HB][SO];
   __shared__ __align__(8) uint64_t s_full[kWarps][kSlots];  // a warp's ring is its own
   extern __shared__ __align__(1024) unsigned char s_dyn[];
-  __shared__ __align__(16) unsigned char s_q[HB * QR];
+  __shared__ __align__(16) unsigned char s_q[kHeld ? 16 : HB * QR];
+  // In 8 bits: the queries in fp16, sixteen bytes to a lane as the products read them, and what a head's scores are to be multiplied with
+  __shared__ __align__(16) unsigned char s_qh[kHeld ? HB * HD * 2 : 16];
+  __shared__ __align__(8) float s_up[HB];
   __shared__ float s_ml[kWarps][HB][2];
   __shared__ int64_t s_wsum[kWarps];
   __shared__ int s_last;
@@ -430,7 +435,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   if (a.n <= 32) {  // every warp by itself: all write the same
     int len = 0, seq = -1;
     if (lane < a.n) len = own_len(lane, &seq);
-    int64_t inc = len > 0 ? ((int64_t)len + kTile - 1) / kTile + kStart : 0;
+    int64_t inc = len > 0 ? ((int64_t)len + kTileTokens - 1) / kTileTokens + kUnitsBefore : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
@@ -444,7 +449,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       const int i = base + tid;
       int len = 0, seq = -1;
       if (i < a.n) len = own_len(i, &seq);
-      int64_t inc = len > 0 ? ((int64_t)len + kTile - 1) / kTile + kStart : 0;
+      int64_t inc = len > 0 ? ((int64_t)len + kTileTokens - 1) / kTileTokens + kUnitsBefore : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
@@ -530,12 +535,12 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       const int64_t ra = r0 - pair * units, rb = min(units, ra + (w1 - w0));
       p.first_w = w0 - ra;
       w0 += rb - ra;
-      p.ta = (int)max((int64_t)0, ra - kStart);
-      p.tb = (int)max((int64_t)0, rb - kStart);
+      p.ta = (int)max((int64_t)0, ra - kUnitsBefore);
+      p.tb = (int)max((int64_t)0, rb - kUnitsBefore);
       if (p.ta == p.tb) continue;  // the start alone: whoever has the first tile begins
       p.row = row;
       p.pair = pair;
-      p.tiles = (int)(units - kStart);
+      p.tiles = (int)(units - kUnitsBefore);
       int seq;
       p.len = own_len(row, &seq);
       const int kvh = pair / a.blocks_of_heads, hb = pair - kvh * a.blocks_of_heads;
@@ -551,8 +556,15 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     return false;
   };
 
-  uint4 qf[QV], kf[2][KV], vf[kHeld ? 1 : 4][VC];
-  uint32_t vw[kHeld ? 4 : 1][VW], ex[kHeld ? 4 : 1];  // in 8 bits: values; exponents of keys and values of tokens g and g + 8
+  uint4 qf[QV], kf[kHeld ? 1 : 2][KV], vf[kHeld ? 1 : 4][VC];
+  // In 8 bits: keys of tokens g and g + 8 of each sixteen, values of 2t, 2t + 1, 2t + 8 and 2t + 9, exponents of keys and (from bit 8 on) values of
+  // token `lane`; how many tokens of each sixteen there are, where they are, and their pages, of this chunk and the next
+  uint4 kh[kHeld ? SC : 1][2][KV];
+  uint32_t vh[kHeld ? SC : 1][4][VW], ex = 0, ex_next = 0;
+  int have_h[SC], next_have_h[SC], page_h[SC];
+  uint32_t end_h = 0;       // tokens up to the end of the piece
+  bool next_whole = false;  // all tokens of the next chunk are there
+  int64_t next_at_h[SC];
   Piece p = {};
   int chunk_end, c, have, have_next, pg_next;  // chunks of 16 tokens
   int64_t at, at_next;
@@ -564,7 +576,6 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   const uint32_t lane_row = ((lane & 7) + (lane >> 4) * 8) * 128, lane_col = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
   auto tiles_at = [&](uint32_t base, int step) { return base + lane_row + (step >> 2) * 2048 + (((step & 3) << 5) ^ lane_col); };
   // where the chunk's page starts, and how many of its tokens there are (0: nothing to read)
-  uint32_t ex_next[4] = {0, 0, 0, 0};
   auto chunk_of = [&](int chunk, int pg, int& n, int64_t& off) {
     n = 0;
     off = 0;
@@ -574,25 +585,76 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       return;
     }
     n = (int)min((int64_t)16, p.len - (int64_t)chunk * 16);
-    const int place = (chunk * 16) & ((1 << a.shift) - 1);
-    off = pg * page_bytes + (int64_t)place * kRowBytes;
-    if constexpr (kHeld) {
-      const uint8_t* e = reinterpret_cast<const uint8_t*>(p.ebase) + pg * page_bytes + place + g;
-      const int64_t values = (int64_t)a.n_kv_heads << a.shift;
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const bool there = g + 8 * r < n;
-        ex_next[r] = there ? __ldg(e + 8 * r) : 0u;
-        ex_next[2 + r] = there ? __ldg(e + 8 * r + values) : 0u;
-      }
-    }
+    off = pg * page_bytes + (int64_t)((chunk * 16) & ((1 << a.shift) - 1)) * (HD * 2);
   };
   auto page_of = [&](int chunk) { return chunk < chunk_end ? p.pages[(int)(((int64_t)chunk * 16) >> a.shift)] : 0; };
-  auto keep_exponents = [&] {
-    if constexpr (kHeld) {
+  // in 8 bits: the pages of a chunk's sixteens (0 where there are no tokens)
+  auto pages_of_held = [&](int chunk) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ex[i] = ex_next[i];
+    for (int x = 0; x < SC; ++x) {
+      const uint32_t tok = ((uint32_t)chunk * SC + x) * 16;
+      page_h[x] = tok < end_h ? p.pages[tok >> a.shift] : 0;
     }
+  };
+  // asks for the exponents of the chunk with the pages page_h, and works out where the rest of it is
+  auto ask_held = [&](int chunk) {
+    next_whole = true;
+    const char* e = nullptr;
+    bool mine = false;
+#pragma unroll
+    for (int x = 0; x < SC; ++x) {
+      const uint32_t tok = ((uint32_t)chunk * SC + x) * 16, place = tok & ((1u << a.shift) - 1);
+      next_have_h[x] = tok < end_h ? (int)min(16u, end_h - tok) : 0;
+      if ((unsigned)page_h[x] >= (unsigned)a.n_pages) {
+        atomicOr(a.status, NP_KV_S_PAGE);
+        next_have_h[x] = page_h[x] = 0;
+      }
+      next_whole &= next_have_h[x] == 16;
+      const int64_t page = page_h[x] * page_bytes;
+      next_at_h[x] = page + place * HD;
+      if (SC == 1 || lane >> 4 == x) {
+        e = p.ebase + page + (place + (lane & 15));
+        mine = lane < 16 * SC && (lane & 15) < next_have_h[x];
+      }
+    }
+    ex_next = 0;
+    if (mine) ex_next = (uint8_t)__ldg(e) | (uint32_t)(uint8_t)__ldg(e + ((int64_t)a.n_kv_heads << a.shift)) << 8;
+  };
+  auto load_k_held = [&] {
+#pragma unroll
+    for (int x = 0; x < SC; ++x) {
+      const char* k = p.kbase + next_at_h[x] + (g * HD + t * 16);
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < KV; ++j) {
+          if (next_whole) {
+            kh[x][r][j] = npd::ldg_stream(k + r * 8 * HD + j * 64);
+          } else {
+            kh[x][r][j] = make_uint4(0, 0, 0, 0);
+            if (g + 8 * r < next_have_h[x]) kh[x][r][j] = npd::ldg_stream(k + r * 8 * HD + j * 64);
+          }
+        }
+    }
+  };
+  auto load_v_held = [&] {
+#pragma unroll
+    for (int x = 0; x < SC; ++x) {
+      const char* v = p.vbase + next_at_h[x] + (2 * t * HD + g * (HD / 8));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int tok = (r & 1) + (r >> 1) * 8;
+        if (next_whole) {
+          load_words(v + tok * HD, vh[x][r]);
+        } else {
+#pragma unroll
+          for (int w = 0; w < VW; ++w) vh[x][r][w] = 0;
+          if (2 * t + tok < next_have_h[x]) load_words(v + tok * HD, vh[x][r]);
+        }
+      }
+      have_h[x] = next_have_h[x];
+    }
+    ex = ex_next;
   };
   auto load_k = [&](int n, int64_t off) {
 #pragma unroll
@@ -600,23 +662,17 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
       for (int j = 0; j < KV; ++j) {
         kf[r][j] = make_uint4(0, 0, 0, 0);
-        if (g + 8 * r < n) kf[r][j] = npd::ldg_stream(p.kbase + off + (g + 8 * r) * kRowBytes + (t + 4 * j) * 16);
+        if (g + 8 * r < n) kf[r][j] = npd::ldg_stream(p.kbase + off + (g + 8 * r) * (HD * 2) + (t + 4 * j) * 16);
       }
   };
   auto load_v = [&](int n, int64_t off) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
-      if constexpr (kHeld) {
 #pragma unroll
-        for (int x = 0; x < VW; ++x) vw[r][x] = 0;
-        if (tok < n) load_words(p.vbase + off + tok * HD + g * (HD / 8), vw[r]);
-      } else {
-#pragma unroll
-        for (int x = 0; x < VC; ++x) {
-          vf[r][x] = make_uint4(0, 0, 0, 0);
-          if (tok < n) vf[r][x] = npd::ldg_stream(p.vbase + off + tok * (HD * 2) + (g + 8 * x) * 16);
-        }
+      for (int x = 0; x < VC; ++x) {
+        vf[r][x] = make_uint4(0, 0, 0, 0);
+        if (tok < n) vf[r][x] = npd::ldg_stream(p.vbase + off + tok * (HD * 2) + (g + 8 * x) * 16);
       }
     }
   };
@@ -636,11 +692,16 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   };
   // asks for the queries and the first keys and values of a piece
   auto begin = [&] {
-    chunk_end = (int)min(((int64_t)p.len + 15) >> 4, (int64_t)p.tb * kWarps);
+    chunk_end = (int)min(((int64_t)p.len + 16 * SC - 1) / (16 * SC), (int64_t)p.tb * kWarps);
     c = p.ta * kWarps + wid;
-    int pg[kSlots + 1];
+    int pg[kSlots + 1] = {};
+    if constexpr (kHeld) {
+      end_h = (uint32_t)min((int64_t)p.len, (int64_t)p.tb * kTileTokens);
+      pages_of_held(c);
+    } else {
 #pragma unroll
-    for (int i = 0; i < (kWide ? kSlots : 1) + 1; ++i) pg[i] = page_of(c + i * kWarps);
+      for (int i = 0; i < (kWide ? kSlots : 1) + 1; ++i) pg[i] = page_of(c + i * kWarps);
+    }
 #pragma unroll
     for (int j = 0; j < QV; ++j) {
       const int x = j * kThreads + tid, h = x / (HD / 8), d = x % (HD / 8) * 8;
@@ -652,9 +713,13 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
       for (int i = 0; i < kSlots; ++i) waiting[i] = ask(c + i * kWarps, pg[i]);
       pg_next = pg[kSlots];
+    } else if constexpr (kHeld) {
+      ask_held(c);
+      load_k_held();
+      load_v_held();
+      pages_of_held(c + kWarps);
     } else {
       chunk_of(c, pg[0], have, at);
-      keep_exponents();
       load_k(have, at);
       load_v(have, at);
       pg_next = pg[1];
@@ -672,6 +737,29 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
     for (int j = 0; j < QV; ++j) {
       const int x = j * kThreads + tid, h = x / (HD / 8), d = x % (HD / 8);
+      if constexpr (kHeld) {  // in fp16, times a power of two that brings the largest finite one of a head to 2^14
+        float2 f[4];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f[i] = widen2<T>(word(qf[j], i));
+          const uint32_t b0 = __float_as_uint(f[i].x) & 0x7fffffffu, b1 = __float_as_uint(f[i].y) & 0x7fffffffu;
+          top = max(top, max(b0 < 0x7f800000u ? b0 : 0u, b1 < 0x7f800000u ? b1 : 0u));
+        }
+#pragma unroll
+        for (int y = 1; y < HD / 8; y <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, y));
+        const int e = max((int)(top >> 23), 29) - 14;  // biased exponent of the power of two to divide by: 15 to 240
+        const float by = __uint_as_float((uint32_t)(254 - e) << 23), back = __uint_as_float((uint32_t)e << 23);
+        if (h < HB) {
+          __half2 r[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = __floats2half2_rn(f[i].x * by, f[i].y * by);
+          // the halves of sixteen values d / 2, at lane 4 * (h % 8) + d / 2 % 4
+          *reinterpret_cast<uint4*>(s_qh + (h >> 3) * (HD * 16) + (((d >> 3) * 2 + (d & 1)) * 32 + (h & 7) * 4 + (d >> 1 & 3)) * 16) = *reinterpret_cast<const uint4*>(r);
+          if (d == 0) s_up[h] = fminf(fmaxf(a.scale2 * back, FLT_MIN), FLT_MAX);
+        }
+        continue;
+      }
       if (h < HB) *reinterpret_cast<uint4*>(s_q + h * QR + d * 16) = qf[j];
     }
   };
@@ -697,37 +785,6 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
         for (int i = 0; i < 4; ++i) qr[j][i] = *reinterpret_cast<const uint32_t*>(s_q + (g + (i & 1) * 8) * QR + j * 32 + t * 4 + (i >> 1) * 16);
     }
-    // In 8 bits: the queries in fp16, times a power of two that brings the largest finite one of a head to 2^14, and what scores of heads
-    // 2t and 2t + 1 (and those eight further) are to be multiplied with.
-    uint32_t qh[kHeld ? NT : 1][kHeld ? HD / 8 : 1];
-    float up[NH];
-    if constexpr (kHeld) {
-#pragma unroll
-      for (int x = 0; x < NT; ++x) {
-        const unsigned char* row = s_q + (g + 8 * x) * QR;
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < HD / 8; ++j) {
-          qh[x][j] = *reinterpret_cast<const uint32_t*>(row + (t + 4 * (j >> 3)) * 32 + (j & 7) * 4);
-          const float2 f = widen2<T>(qh[x][j]);
-          const uint32_t b0 = __float_as_uint(f.x) & 0x7fffffffu, b1 = __float_as_uint(f.y) & 0x7fffffffu;
-          top = max(top, max(b0 < 0x7f800000u ? b0 : 0u, b1 < 0x7f800000u ? b1 : 0u));
-        }
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int e = max((int)(top >> 23), 29) - 14;  // biased exponent of the power of two to divide by: 15 to 240
-        const float by = __uint_as_float((uint32_t)(254 - e) << 23), back = __uint_as_float((uint32_t)e << 23);
-#pragma unroll
-        for (int j = 0; j < HD / 8; ++j) {
-          const float2 f = widen2<T>(qh[x][j]);
-          const __half2 h = __floats2half2_rn(f.x * by, f.y * by);
-          qh[x][j] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-        const float mine = fminf(fmaxf(a.scale2 * back, FLT_MIN), FLT_MAX);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) up[2 * x + i] = __shfl_sync(0xffffffffu, mine, (2 * t + i) * 4);
-      }
-    }
     // the maxima of the two heads grow to `top`, what has been added up is rescaled (by(i, factor) for the accumulators of head i), `use` is
     // what to take off
     auto raise = [&](const auto& top, auto& use, auto by) {
@@ -749,43 +806,63 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       }
     };
     if constexpr (kHeld) {
-      for (; c < chunk_end; c += kWarps) {
-        chunk_of(c + kWarps, pg_next, have_next, at_next);
-        pg_next = page_of(c + 2 * kWarps);
-        // ---- S^T = K Q^T, without their powers of two
-        float s[NT][4];
+      float up[NH];
 #pragma unroll
-        for (int x = 0; x < NT; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
+      for (int i = 0; i < NH; ++i) up[i] = s_up[(i >> 1) * 8 + 2 * t + (i & 1)];
+      for (; c < chunk_end; c += kWarps) {
+        ask_held(c + kWarps);
+        pages_of_held(c + 2 * kWarps);
+        // ---- S^T = K Q^T, without their powers of two
+        float s[SC][NT][4];
+#pragma unroll
+        for (int y = 0; y < SC; ++y)
+#pragma unroll
+          for (int x = 0; x < NT; ++x) s[y][x][0] = s[y][x][1] = s[y][x][2] = s[y][x][3] = 0.f;
 #pragma unroll
         for (int j = 0; j < KV; ++j)
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t a0, a1, a2, a3;
-            widen4(word(kf[0][j], w), a0, a2);
-            widen4(word(kf[1][j], w), a1, a3);
+          for (int half = 0; half < 2; ++half) {
+            uint4 q[NT];
 #pragma unroll
-            for (int x = 0; x < NT; ++x) Half2<__half>::mma(s[x], a0, a1, a2, a3, qh[x][8 * j + 2 * w], qh[x][8 * j + 2 * w + 1]);
+            for (int x = 0; x < NT; ++x) q[x] = *reinterpret_cast<const uint4*>(s_qh + x * (HD * 16) + ((j * 2 + half) * 32 + lane) * 16);
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+#pragma unroll
+              for (int y = 0; y < SC; ++y) {
+                uint32_t a0, a1, a2, a3;
+                widen4(word(kh[y][0][j], 2 * half + w), a0, a2);
+                widen4(word(kh[y][1][j], 2 * half + w), a1, a3);
+#pragma unroll
+                for (int x = 0; x < NT; ++x) Half2<__half>::mma(s[y][x], a0, a1, a2, a3, w ? q[x].z : q[x].x, w ? q[x].w : q[x].y);
+              }
           }
-        load_k(have_next, at_next);
-        // ---- softmax: s[x][0], s[x][1] are token g, s[x][2], s[x][3] token g + 8; heads 8x + 2t and 8x + 2t + 1.  A token's values are times
-        // 2^lv: their weight is 2^(s + lv - m), m the largest s + lv, and the sum is of 2^(s - m).
-        float lv[2], top[NH], use[NH];
+        load_k_held();
+        // ---- softmax: s[y][x][0], s[y][x][1] are token g of a sixteen, s[y][x][2], s[y][x][3] token g + 8; heads 8x + 2t and 8x + 2t + 1.  A
+        // token's values are times 2^lv: their weight is 2^(s + lv - m), m the largest s + lv, and the sum is of 2^(s - m).
+        float lv[SC][2], top[NH], use[NH];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const float power = __uint_as_float(ex[r] << 23);
-          const bool there = g + 8 * r < have;
-          lv[r] = (float)(int)ex[2 + r] - 127.f;
+        for (int i = 0; i < NH; ++i) top[i] = -INFINITY;
 #pragma unroll
-          for (int x = 0; x < NT; ++x)
+        for (int y = 0; y < SC; ++y)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) s[x][2 * r + i] = there ? s[x][2 * r + i] * up[2 * x + i] * power : -INFINITY;
-        }
+          for (int r = 0; r < 2; ++r) {
+            const uint32_t e = __shfl_sync(0xffffffffu, ex, 16 * y + g + 8 * r);
+            const float power = __uint_as_float((e & 0xffu) << 23);
+            const bool there = g + 8 * r < have_h[y];
+            lv[y][r] = (float)(int)(e >> 8) - 127.f;
 #pragma unroll
-        for (int i = 0; i < NH; ++i) {
-          top[i] = fmaxf(s[i >> 1][i & 1] + lv[0], s[i >> 1][(i & 1) + 2] + lv[1]);
+            for (int x = 0; x < NT; ++x)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const float z = s[y][x][2 * r + i] * up[2 * x + i] * power;
+                s[y][x][2 * r + i] = there ? z : -INFINITY;
+                top[2 * x + i] = fmaxf(top[2 * x + i], s[y][x][2 * r + i] + lv[y][r]);
+              }
+          }
+#pragma unroll
+        for (int i = 0; i < NH; ++i)
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
-        }
         raise(top, use, [&](int i, float f) {
 #pragma unroll
           for (int v = 0; v < HD / 16; ++v) {
@@ -793,42 +870,42 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
             o[(i >> 1) * (HD / 16) + v][(i & 1) + 2] *= f;
           }
         });
-        uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
-        for (int x = 0; x < NT; ++x)
+        for (int y = 0; y < SC; ++y) {
+          uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            float w[2];
+          for (int x = 0; x < NT; ++x)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float e = s[x][2 * r + i] - use[2 * x + i];
-              l[2 * x + i] += exp2_fast(e + kHeldShift);
-              w[i] = exp2_fast(e + lv[r]);
+            for (int r = 0; r < 2; ++r) {
+              float w[2];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const float e = s[y][x][2 * r + i] - use[2 * x + i];
+                l[2 * x + i] += exp2_fast(e + kHeldShift);
+                w[i] = exp2_fast(e + lv[y][r]);
+              }
+              uint32_t hi, lo;
+              Half2<__half>::split(w[0], w[1], hi, lo);
+              ph[x][r] = transpose8x8(hi);
+              pl[x][r] = transpose8x8(lo);
             }
-            uint32_t hi, lo;
-            Half2<__half>::split(w[0], w[1], hi, lo);
-            ph[x][r] = transpose8x8(hi);
-            pl[x][r] = transpose8x8(lo);
-          }
-        // ---- O^T += V^T W^T
+          // ---- O^T += V^T W^T
 #pragma unroll
-        for (int w = 0; w < VW; ++w)
+          for (int w = 0; w < VW; ++w)
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const uint32_t order = half ? 0x7362 : 0x5140;
-            uint32_t a0, a1, a2, a3;
-            widen4(__byte_perm(vw[0][w], vw[1][w], order), a0, a1);
-            widen4(__byte_perm(vw[2][w], vw[3][w], order), a2, a3);
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t order = half ? 0x7362 : 0x5140;
+              uint32_t a0, a1, a2, a3;
+              widen4(__byte_perm(vh[y][0][w], vh[y][1][w], order), a0, a1);
+              widen4(__byte_perm(vh[y][2][w], vh[y][3][w], order), a2, a3);
 #pragma unroll
-            for (int x = 0; x < NT; ++x) {
-              Half2<__half>::mma(o[x * (HD / 16) + 2 * w + half], a0, a1, a2, a3, ph[x][0], ph[x][1]);
-              Half2<__half>::mma(o[x * (HD / 16) + 2 * w + half], a0, a1, a2, a3, pl[x][0], pl[x][1]);
+              for (int x = 0; x < NT; ++x) {
+                Half2<__half>::mma(o[x * (HD / 16) + 2 * w + half], a0, a1, a2, a3, ph[x][0], ph[x][1]);
+                Half2<__half>::mma(o[x * (HD / 16) + 2 * w + half], a0, a1, a2, a3, pl[x][0], pl[x][1]);
+              }
             }
-          }
-        load_v(have_next, at_next);
-        keep_exponents();
-        have = have_next;
-        at = at_next;
+        }
+        load_v_held();
       }
     } else if constexpr (!kWide) {
       for (; c < chunk_end; c += kWarps) {
@@ -1027,7 +1104,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       mend<T, HD>(a, odd, e.row, kTail ? s_first[e.row] : 0, e.pair, e.ta, e.tb, e.h0, e.heads, whole ? nullptr : a.part_o + (size_t)slot * HB * HD, reinterpret_cast<int*>(&s_o[0][0][0]));
     if (!whole) {
       // ---- the last block to arrive joins up to kJoin neighbouring pieces; the last of those that did joins what they got
-      const int c0 = block_of(e.first_w + kStart), c1 = block_of(e.first_w + kStart + e.tiles - 1), pieces = c1 - c0 + 1;
+      const int c0 = block_of(e.first_w + kUnitsBefore), c1 = block_of(e.first_w + kUnitsBefore + e.tiles - 1), pieces = c1 - c0 + 1;
       auto slot_of = [&](int b) { return (2 * b + (b == c0)) * HB; };
       // true in the block that is the last of n to arrive at a count, which is zero again then
       auto last_of = [&](unsigned int* count, int n) {

@@ -36,7 +36,6 @@ struct Rows {
   static constexpr int kTurn = kThreads / kLanes;            // rows of a block at a time
   static constexpr int kVecs = kValues / kEach;
   static constexpr int kBlock = kTurn * kVecs;
-  static constexpr int kTokens = kBlock / 2 + 2;             // of a block at most: a token has two rows or more
 };
 
 struct RowsArgs {
@@ -189,7 +188,7 @@ template <class T, int HD, bool kRotate, bool kHeld>
 __global__ void __launch_bounds__(kThreads)
 k_rows_in(const __grid_constant__ RowsArgs a) {
   using R = Rows<HD, 8>;
-  constexpr int L = R::kLanes, kVecs = R::kVecs;
+  constexpr int L = R::kLanes, kVecs = R::kVecs, kTokens = R::kBlock / 2 + 2;  // of a block at most: a token has two rows or more
   extern __shared__ int s_cu[];
   __shared__ const uint16_t* s_src[R::kBlock];
   __shared__ char* s_dst[R::kBlock];              // nullptr: the row is not written
@@ -197,7 +196,7 @@ k_rows_in(const __grid_constant__ RowsArgs a) {
   __shared__ int s_row[R::kBlock];                // token of the block << 3 | whether it is normed << 2 | kind
   __shared__ __align__(16) float s_gain[kRotate ? 2 : 1][HD];
   __shared__ double s_freq[kRotate ? HD / 2 : 1];  // turns per position
-  __shared__ __align__(16) float s_cos[kRotate ? R::kTokens : 1][HD / 2], s_sin[kRotate ? R::kTokens : 1][HD / 2];
+  __shared__ __align__(16) float s_cos[kRotate ? kTokens : 1][HD / 2], s_sin[kRotate ? kTokens : 1][HD / 2];
   const int tid = threadIdx.x, piece = tid % L, slot = tid / L;
   const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock;
   const int rows = (int)(min(total, first + R::kBlock) - first);

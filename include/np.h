@@ -749,7 +749,8 @@ int np_kv_shared(const np_kv_desc* desc, const np_kv_tables* tables, const int32
  *   shared     dev [n_groups]: tokens, from np_kv_shared, or any multiple of page_tokens up to that; 0: nothing.  The pages of the group's first row
  *              with a sequence are read for all of its rows.  Where a group's rows do not all have that many tokens, or they do not fill
  *              pages, it shares nothing (NP_KV_S_LENGTH)
- *   workspace  as np_attn_decode's, np_attn_shared_workspace_bytes long at least; the two calls may share one
+ *   workspace  dev, 16-byte aligned, np_attn_shared_workspace_bytes long at least; zeroed before its first use and left ready for the next call
+ *              of any size; not one that np_attn_decode uses.  Calls (and graphs) that share one must not overlap on the GPU
  * n_heads / n_kv_heads <= NP_ATTN_MAX_GROUP.  Over an e4m3 cache every row is computed by itself, as np_attn_decode does. */
 int np_attn_shared_workspace_bytes(const np_kv_desc* desc, int32_t n_heads, int32_t n, uint64_t* out);
 int np_attn_decode_shared(const np_kv_desc* desc, const void* cache, int32_t layer, const np_kv_tables* tables, const np_rows* q,

@@ -76,7 +76,8 @@ struct DecodeArgs {
   int64_t q_token, q_head, o_token, o_head;  // elements
   float* lse;
   unsigned int* count;       // [2 * kMaxBlocks] partial results that have arrived, at the place of their first; zero between calls
-  unsigned int* pair_count;  // [n * pairs] the same of joined ones
+  unsigned int* pair_count;  // [n * pairs], pair_step apart: the same of joined ones
+  int pair_step;
   float* part_ml;            // [2 * kMaxBlocks][HB][2]
   float* part_o;             // [2 * kMaxBlocks][HB][HD]
   float scale2;              // scale * log2(e)
@@ -88,6 +89,9 @@ struct DecodeArgs {
 
 // How keys and values get to the products: in the rows' type, up to eight or sixteen heads of a group at once; in 8 bits, the same.
 enum Form { kEight, kSixteen, kHeldEight, kHeldSixteen };
+// What is computed: rows by themselves; rows behind the tokens that their group shares, joined to another kernel's partial results of those;
+// rows and what their groups share, of which the last part to arrive is joined to the others.
+enum Mode { kAlone, kBehind, kBoth };
 
 template <class T>
 struct Half2;
@@ -203,24 +207,20 @@ __device__ __forceinline__ constexpr uint32_t infinity_bits() {
 }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
-// By a whole block: results of tiles [ta, tb) of (row, pair) that are not finite, where V has anything of that kind among them.  Weights are
-// above 0, so an infinity stays one, and two of different signs or a NaN make a NaN; what the sums made of finite values stays.  V is looked
-// through once for all heads, eight values to a thread.  `odd`: bit k if the thread is to look at the four values of its turn k over heads and
-// head_dim; part_o: of the partial result, nullptr: out.  seen: HD ints of shared memory that are free.  One of 131071 tokens a NaN, 64
-// heads over 8: 201 us a call in place of 93. (One block that looks through all of V behind the join: 10 ms.)
+// By a whole block: what values that are not finite there are among V's of tokens [ta * kTile, len) of a piece, for each of head_dim (bit 0 a NaN, 8
+// inf, 16 -inf).  Weights are above 0, so an infinity stays one, and two of different signs or a NaN make a NaN; what the sums made of finite values
+// stays.  V is looked through once for all heads, eight values to a thread.  seen: HD ints of shared memory that are free.  One of 131071 tokens a
+// NaN, 64 heads over 8: 201 us a call in place of 93. (One block that looks through all of V behind the join: 10 ms.)
 template <class T, int HD>
-__device__ __noinline__ void mend(const DecodeArgs& a, uint32_t odd, int row, int first, int pair, int ta, int tb, int h0, int heads, float* part_o, int* seen) {
+__device__ __noinline__ void look_through(const DecodeArgs& a, const int32_t* pages, int kvh, int ta, int64_t len, int* seen) {
   constexpr int kCols = HD / 8, kStep = kThreads / kCols, kAhead = 4;
   constexpr uint32_t kInf = infinity_bits<T>();
   const int tid = threadIdx.x;
   for (int d = tid; d < HD; d += kThreads) seen[d] = 0;
   __syncthreads();
-  int seq;
-  const int64_t len = min((int64_t)row_len(a, row, &seq) - first, (int64_t)tb * kTile);
   const int col = tid % kCols;
-  const int32_t* pages = a.table + (size_t)seq * a.max_pages + (first >> a.shift);
   const int64_t head_bytes = (int64_t)(HD * 2) << a.shift;
-  const char* v = a.cache + (a.n_kv_heads + pair / a.blocks_of_heads) * head_bytes + col * 16;
+  const char* v = a.cache + (a.n_kv_heads + kvh) * head_bytes + col * 16;
   uint32_t bits = 0;  // value x of the column: 1 << x a NaN, 256 << x inf, 65536 << x -inf
   for (int64_t j0 = (int64_t)ta * kTile + tid / kCols; j0 < len; j0 += kAhead * kStep) {
     int pg[kAhead];
@@ -244,20 +244,10 @@ __device__ __noinline__ void mend(const DecodeArgs& a, uint32_t odd, int row, in
   for (int x = 0; bits && x < 8; ++x)
     if (const int what = bits >> x & 0x10101) atomicOr(&seen[col * 8 + x], what);
   __syncthreads();
-  for (int x = tid; odd && x < heads * (HD / 4); x += kThreads, odd >>= 1) {
-    if (!(odd & 1u)) continue;
-    const int h = x / (HD / 4), d = x % (HD / 4) * 4;
-    uint16_t* out = a.out + row * a.o_token + (int64_t)(h0 + h) * a.o_head + d;
-    float* part = part_o + h * HD + d;
-    for (int i = 0; i < 4; ++i) {
-      const int what = seen[d + i];
-      if (!what) continue;
-      const uint32_t now = what == 0x100 ? kInf : what == 0x10000 ? kInf | 0x8000u : 0x7fffu;
-      if (part_o == nullptr) out[i] = (uint16_t)now;
-      else __stcg(&part[i], what == 0x100 ? INFINITY : what == 0x10000 ? -INFINITY : __uint_as_float(0x7fffffffu));
-    }
-  }
-  __syncthreads();
+}
+// What a result that such values go into is, as fp32; 0: as it was.
+__device__ __forceinline__ float made_of(int seen) {
+  return seen == 0 ? 0.f : seen == 0x100 ? INFINITY : seen == 0x10000 ? -INFINITY : __uint_as_float(0x7fffffffu);
 }
 
 // Four values of joined partial results that are not finite: factors that are 0 make a NaN of an infinity, so they are what the partial results
@@ -294,6 +284,10 @@ __device__ __forceinline__ void join_shared(const DecodeArgs& a, int tokens, int
   const int64_t tiles = (tokens + kSharedTile - 1) / kSharedTile, w = plan.first_w + ((int64_t)kvh * plan.row_blocks + block) * tiles;
   auto block_of = [&](int64_t x) { return (int)(x < line.more * (line.each + 1) ? divide(x, line.each + 1) : line.more + divide(x - line.more * (line.each + 1), line.each)); };
   const int c0 = block_of(w), c1 = block_of(w + tiles - 1);
+  const Record* whole = s.records + ((int64_t)i * a.n_heads + h);  // where one block has done all of them
+  auto slot_of = [&](int b) { return (int64_t)(2 * b + (b == c0)) * s.part_rows + row; };
+  auto ml_of = [&](int b) { return c0 == c1 ? whole->ml[0] : s.part_ml + slot_of(b) * 2; };
+  auto o_of = [&](int b) { return (c0 == c1 ? whole->o[0] : s.part_o + slot_of(b) * HD) + d; };
   constexpr int kAhead = 4;
   const float own[4] = {acc.x, acc.y, acc.z, acc.w};
   for (int b0 = c0; b0 <= c1; b0 += kAhead) {
@@ -304,9 +298,8 @@ __device__ __forceinline__ void join_shared(const DecodeArgs& a, int tokens, int
       ml[y] = make_float2(-INFINITY, 0.f);
       v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (b0 + y > c1) continue;
-      const int64_t slot = c0 == c1 ? (int64_t)i * a.n_heads + h : (int64_t)(2 * (b0 + y) + (b0 + y == c0)) * s.part_rows + row;
-      ml[y] = __ldcg(reinterpret_cast<const float2*>((c0 == c1 ? s.row_ml : s.part_ml) + slot * 2));
-      v[y] = __ldcg(reinterpret_cast<const float4*>((c0 == c1 ? s.row_o : s.part_o) + slot * HD + d));
+      ml[y] = __ldcg(reinterpret_cast<const float2*>(ml_of(b0 + y)));
+      v[y] = __ldcg(reinterpret_cast<const float4*>(o_of(b0 + y)));
     }
     float now = top;
 #pragma unroll
@@ -331,8 +324,7 @@ __device__ __forceinline__ void join_shared(const DecodeArgs& a, int tokens, int
   for (int x = 0; x < 4; ++x) {
     float kept = not_finite(own[x]) ? own[x] : 0.f;
     for (int b = c0; b <= c1; ++b) {
-      const int64_t slot = c0 == c1 ? (int64_t)i * a.n_heads + h : (int64_t)(2 * b + (b == c0)) * s.part_rows + row;
-      const float v = __ldcg((c0 == c1 ? s.row_o : s.part_o) + slot * HD + d + x);
+      const float v = __ldcg(o_of(b) + x);
       if (not_finite(v)) kept += v;
     }
     if (not_finite(kept)) *to[x] = kept;
@@ -344,13 +336,39 @@ __device__ __forceinline__ void join_shared(const DecodeArgs& a, int tokens, int
 // three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16 sequences of 2000, five
 // 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
 constexpr int blocks_per_sm(int hd, int form) {
-  return form == kHeldEight ? 3 : form == kHeldSixteen ? (hd == 64 ? 3 : 2) : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
+  return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 2 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
 }
 
 // In 8 bits sums are of 2^(s - m + kHeldShift): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.
 constexpr float kHeldShift = 30.f, kHeldUp = 0x1p30f;
 
-constexpr uint32_t kTailBytes = NP_KV_MAX_SEQS * 6;  // of what kTail keeps of the groups
+// What a block knows of groups, in dynamic shared memory: for each row the tokens that it shares and its group; kBoth: for each group what it is, and
+// the units of groups and rows.
+struct GroupInfo {
+  int tokens;
+  int16_t lo, hi;  // its rows
+  int seq;         // whose pages are read
+};
+struct GroupRoom {
+  int64_t* end;
+  int* first;
+  GroupInfo* info;
+  uint16_t* group;
+  uint32_t bytes;
+  __host__ __device__ GroupRoom(unsigned char* base, bool both, int n, int n_groups) {
+    uint32_t at = 0;
+    auto take = [&](uint32_t size) {
+      unsigned char* p = base + at;
+      at += (size + 15) & ~15u;
+      return p;
+    };
+    end = reinterpret_cast<int64_t*>(take(both ? (n + n_groups) * 8 : 0));
+    first = reinterpret_cast<int*>(take(n * 4));
+    info = reinterpret_cast<GroupInfo*>(take(both ? n_groups * sizeof(GroupInfo) : 0));
+    group = reinterpret_cast<uint16_t*>(take(n * 2));
+    bytes = at;
+  }
+};
 
 constexpr int kSlots = 2;  // sixteen heads: chunks of a warp on their way
 
@@ -365,10 +383,10 @@ struct WarpWaits {
   }
 };
 
-// kTail: rows begin behind the tokens that their group shares, whose partial results are joined to theirs.
-template <class T, int HD, int kForm, bool kTail>
+template <class T, int HD, int kForm, int kMode>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kForm))
 k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
+  constexpr bool kTail = kMode == kBehind, kTogether = kMode == kBoth;
   constexpr bool kWide = kForm == kSixteen, kHeld = kForm == kHeldEight || kForm == kHeldSixteen;
   constexpr int HB = kForm == kSixteen || kForm == kHeldSixteen ? 16 : 8;  // heads of a block, at most
   constexpr int NT = HB / 8, NH = kHeld ? 2 * NT : 2;  // in 8 bits: eights of heads; heads of a lane's scores
@@ -383,7 +401,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   constexpr uint32_t kHalf = 16 * HD * 2, kSlot = 2 * kHalf;
   // Bytes from query to query, values from head to head of a warp's result, in shared memory: reads and stores meet all banks
   constexpr int QR = HD * 2 + (kWide ? 16 : 64), SO = HD + (kWide ? 8 : 0);
-  __shared__ int64_t s_end[NP_KV_MAX_SEQS];             // tiles of the rows up to and including this one
+  __shared__ int64_t s_ends[kTogether ? 1 : NP_KV_MAX_SEQS];
   __shared__ __align__(16) float s_o[kWarps][HB][SO];
   __shared__ __align__(8) uint64_t s_full[kWarps][kSlots];  // a warp's ring is its own
   extern __shared__ __align__(1024) unsigned char s_dyn[];
@@ -395,8 +413,10 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   __shared__ int64_t s_wsum[kWarps];
   __shared__ int s_last;
   __shared__ volatile int s_lost[kWarps];  // a wait of the warp was given up
-  int* const s_first = reinterpret_cast<int*>(s_dyn);                                    // kTail: tokens that the row's group shares
-  uint16_t* const s_group = reinterpret_cast<uint16_t*>(s_dyn + NP_KV_MAX_SEQS * 4);     // and the group
+  __shared__ int s_done[kTogether ? HB : 1];
+  const int n_groups = kTogether ? a.shared.n_groups : 0, items = n_groups + a.n;  // items: groups, then rows
+  const GroupRoom room(s_dyn, kTogether, a.n, n_groups);
+  int64_t* const s_end = kTogether ? room.end : s_ends;  // units of the items up to and including this one
   if (kWide && (threadIdx.x & 31) == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
     for (int i = 0; i < kSlots; ++i) npp::mbar_init(&s_full[threadIdx.x >> 5][i], 1);
@@ -410,46 +430,63 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
   const int pairs = a.n_kv_heads * a.blocks_of_heads;   // (key-value head, block of its query heads)
 
-  if constexpr (kTail) {
-    for (int i = tid; i < a.n; i += kThreads) s_first[i] = 0;
+  if constexpr (kTail || kTogether) {
+    for (int i = tid; i < a.n; i += kThreads) room.first[i] = 0;
     __syncthreads();
     for (int x = wid; x < a.shared.n_groups; x += kWarps) {
       int lo, hi, seq;
       group_rows(a.shared, a.n, x, &lo, &hi);
       const int tokens = group_tokens(a.shared, x, lo, hi, a.seqs, a.lens, a.max_seqs, a.max_pages, a.shift, a.status, &seq);
       for (int i = lo + lane; i < hi; i += 32) {
-        s_first[i] = tokens;
-        s_group[i] = (uint16_t)x;
+        room.first[i] = tokens;
+        room.group[i] = (uint16_t)x;
       }
+      if (kTogether && lane == 0) room.info[x] = GroupInfo{tokens, (int16_t)lo, (int16_t)hi, seq};
     }
     __syncthreads();
   }
   // tokens of row i of the call that are its own
   auto own_len = [&](int i, int* seq) {
     const int len = row_len(a, i, seq);
-    return kTail && len > 0 ? len - s_first[i] : len;
+    return (kTail || kTogether) && len > 0 ? len - room.first[i] : len;
+  };
+  // blocks of columns, (row, query head) pairs of one key-value head, of a group
+  auto column_blocks = [&](const GroupInfo& x) { return ((x.hi - x.lo) * a.group + HB - 1) / HB; };
+  // units of an item; kTogether: of all its pairs
+  auto units_of = [&](int i) {
+    int seq;
+    int len;
+    int64_t of = 1;
+    if (kTogether && i < n_groups) {
+      const GroupInfo x = room.info[i];
+      len = x.tokens;
+      of = (int64_t)a.n_kv_heads * column_blocks(x);
+    } else {
+      len = own_len(i - n_groups, &seq);
+      if (kTogether) {
+        of = pairs;
+        if (len <= 0 && row_len(a, i - n_groups, &seq) == 0) room.first[i - n_groups] = 0;  // no sequence: it shares nothing
+      }
+    }
+    return len > 0 ? (((int64_t)len + kTileTokens - 1) / kTileTokens + kUnitsBefore) * of : 0;
   };
 
   // ---- units (tiles, and a group's start) of every row, summed up; rows without tokens are answered here
   int64_t run = 0;
-  if (a.n <= 32) {  // every warp by itself: all write the same
-    int len = 0, seq = -1;
-    if (lane < a.n) len = own_len(lane, &seq);
-    int64_t inc = len > 0 ? ((int64_t)len + kTileTokens - 1) / kTileTokens + kUnitsBefore : 0;
+  if (items <= 32) {  // every warp by itself: all write the same
+    int64_t inc = lane < items ? units_of(lane) : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += up;
     }
-    if (lane < a.n) s_end[lane] = inc;
+    if (lane < items) s_end[lane] = inc;
     run = __shfl_sync(0xffffffffu, inc, 31);
     __syncwarp();
   } else {
-    for (int base = 0; base < a.n; base += kThreads) {
+    for (int base = 0; base < items; base += kThreads) {
       const int i = base + tid;
-      int len = 0, seq = -1;
-      if (i < a.n) len = own_len(i, &seq);
-      int64_t inc = len > 0 ? ((int64_t)len + kTileTokens - 1) / kTileTokens + kUnitsBefore : 0;
+      int64_t inc = i < items ? units_of(i) : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
@@ -458,7 +495,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       if (lane == 31) s_wsum[wid] = inc;
       __syncthreads();
       for (int w = 0; w < wid; ++w) inc += s_wsum[w];
-      if (i < a.n) s_end[i] = run + inc;
+      if (i < items) s_end[i] = run + inc;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) run += s_wsum[w];
       __syncthreads();
@@ -467,7 +504,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   // four values of a head's result; its log of the sum with the first
   auto result = [&](int i, int h, int d, float4 acc, float top, float sum) {
     if constexpr (kTail) {
-      if (s_first[i] > 0) join_shared<HD>(a, s_first[i], s_group[i], i, h, d, acc, top, sum);
+      if (room.first[i] > 0) join_shared<HD>(a, room.first[i], room.group[i], i, h, d, acc, top, sum);
     }
     const float use = top == -INFINITY ? 0.f : top;
     const bool none = sum == 0.f;
@@ -479,10 +516,13 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     *reinterpret_cast<uint2*>(a.out + i * a.o_token + (int64_t)h * a.o_head + d) = r;
     if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = none ? -INFINITY : (kHeld ? use - kHeldShift : use) * kLn2 + logf(sum);
   };
+  // kTogether: where the parts of (row i, head h) meet
+  auto record = [&](int64_t i, int h) { return a.shared.records + (i * a.n_heads + h); };
   for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
-    if (s_end[i] != (i ? s_end[i - 1] : 0)) continue;
+    if (s_end[n_groups + i] != (n_groups + i ? s_end[n_groups + i - 1] : 0)) continue;
     int seq;
-    if (kTail && s_first[i] > 0 && row_len(a, i, &seq) > 0) {  // all of its tokens are shared
+    if (kTogether && room.first[i] > 0) continue;  // all of its tokens are shared
+    if (kTail && room.first[i] > 0 && row_len(a, i, &seq) > 0) {
       for (int x = tid; x < a.n_heads * (HD / 4); x += kThreads) result(i, x / (HD / 4), x % (HD / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
       continue;
     }
@@ -493,7 +533,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     }
   }
   // the line's W units over G blocks: the first `more` blocks take each + 1 of them, the others each
-  const int64_t W = run * pairs;
+  const int per = kTogether ? 1 : pairs;
+  const int64_t W = run * per;
   const int G = (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
   if ((int)blockIdx.x >= G) {
     if (kTail) npp::pdl_wait_prior();
@@ -505,10 +546,10 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   const int64_t w1 = w0 + each + (blockIdx.x < more ? 1 : 0);
   int row = 0;
   {
-    int lo = 0, hi = a.n - 1;  // the first row whose units end after w0
+    int lo = 0, hi = items - 1;  // the first item whose units end after w0
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (s_end[mid] * pairs > w0) hi = mid;
+      if (s_end[mid] * per > w0) hi = mid;
       else lo = mid + 1;
     }
     row = lo;
@@ -517,8 +558,9 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   constexpr int kRowBytes = kHeld ? HD : HD * 2;
   const int64_t head_bytes = (int64_t)kRowBytes << a.shift, page_bytes = a.page_bytes;
   const int64_t exponents = 2 * a.n_kv_heads * head_bytes;  // in 8 bits: of a page, from its start
-  struct Piece {  // tiles [ta, tb) of one (row, pair)
-    int row, pair, h0, heads, len, tiles, ta, tb;
+  struct Piece {  // tiles [ta, tb) of one (row, pair), or of a group and a block of its columns: from h0 on, of key-value head kvh
+    int row, pair, kvh, h0, heads, len, tiles, ta, tb;
+    bool of_group;
     int64_t first_w;  // of its pair, on the line
     const int32_t* pages;
     int first_row;    // of its key-value head in a page
@@ -529,8 +571,11 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   // the next piece with tokens from w0 on; false: none is left
   auto next_piece = [&](Piece& p) {
     while (w0 < w1) {
-      while (s_end[row] * pairs <= w0) ++row;
-      const int64_t before = row ? s_end[row - 1] : 0, units = s_end[row] - before, r0 = w0 - before * pairs;
+      while (s_end[row] * per <= w0) ++row;
+      p.of_group = kTogether && row < n_groups;
+      const GroupInfo of = p.of_group ? room.info[row] : GroupInfo{};
+      const int64_t before = row ? s_end[row - 1] : 0, r0 = w0 - before * per;
+      const int64_t units = !kTogether ? s_end[row] - before : divide(s_end[row] - before, p.of_group ? a.n_kv_heads * column_blocks(of) : pairs);
       const int pair = (int)divide(r0, units);
       const int64_t ra = r0 - pair * units, rb = min(units, ra + (w1 - w0));
       p.first_w = w0 - ra;
@@ -538,15 +583,27 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       p.ta = (int)max((int64_t)0, ra - kUnitsBefore);
       p.tb = (int)max((int64_t)0, rb - kUnitsBefore);
       if (p.ta == p.tb) continue;  // the start alone: whoever has the first tile begins
-      p.row = row;
+      p.row = row - n_groups;
       p.pair = pair;
       p.tiles = (int)(units - kUnitsBefore);
-      int seq;
-      p.len = own_len(row, &seq);
-      const int kvh = pair / a.blocks_of_heads, hb = pair - kvh * a.blocks_of_heads;
-      p.h0 = kvh * a.group + hb * HB;
-      p.heads = min(HB, a.group - hb * HB);
-      p.pages = a.table + (size_t)seq * a.max_pages + (kTail ? s_first[row] >> a.shift : 0);
+      int seq, kvh;
+      if (p.of_group) {
+        const int blocks = column_blocks(of);
+        kvh = pair / blocks;
+        p.row = of.lo;
+        p.len = of.tokens;
+        p.h0 = (pair - kvh * blocks) * HB;
+        p.heads = min(HB, (of.hi - of.lo) * a.group - p.h0);
+        p.pages = a.table + (size_t)of.seq * a.max_pages;
+      } else {
+        p.len = own_len(p.row, &seq);
+        kvh = pair / a.blocks_of_heads;
+        const int hb = pair - kvh * a.blocks_of_heads;
+        p.h0 = kvh * a.group + hb * HB;
+        p.heads = min(HB, a.group - hb * HB);
+        p.pages = a.table + (size_t)seq * a.max_pages + (kTail || kTogether ? room.first[p.row] >> a.shift : 0);
+      }
+      p.kvh = kvh;
       p.first_row = kvh << a.shift;
       p.kbase = a.cache + kvh * head_bytes;
       p.vbase = p.kbase + a.n_kv_heads * head_bytes;
@@ -571,7 +628,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   int waiting[kSlots];                 // tokens of the chunks in this warp's ring
   npp::WarpRing<kSlots> uses;
   WarpWaits waits = {&s_lost[wid], a.status};
-  const uint32_t ring = ((npp::smem_addr(s_dyn) + (kTail ? kTailBytes : 0) + 1023) & ~1023u) + wid * kSlots * kSlot;
+  const uint32_t ring = ((npp::smem_addr(s_dyn) + (kMode == kAlone ? 0u : room.bytes) + 1023) & ~1023u) + wid * kSlots * kSlot;
   // what a lane reads with load_tiles: rows (tokens) 0-7 and 8-15 of two neighbouring 16-byte columns, 128-byte swizzle
   const uint32_t lane_row = ((lane & 7) + (lane >> 4) * 8) * 128, lane_col = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
   auto tiles_at = [&](uint32_t base, int step) { return base + lane_row + (step >> 2) * 2048 + (((step & 3) << 5) ^ lane_col); };
@@ -706,7 +763,15 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     for (int j = 0; j < QV; ++j) {
       const int x = j * kThreads + tid, h = x / (HD / 8), d = x % (HD / 8) * 8;
       qf[j] = make_uint4(0, 0, 0, 0);
-      if (h < p.heads) qf[j] = *reinterpret_cast<const uint4*>(a.q + p.row * a.q_token + (int64_t)(p.h0 + h) * a.q_head + d);
+      if (h < p.heads) {
+        int64_t i = p.row, head = p.h0 + h;
+        if (kTogether && p.of_group) {  // columns go through the rows' heads
+          const int at = p.h0 + h, member = at / a.group;
+          i += member;
+          head = p.kvh * a.group + at - member * a.group;
+        }
+        qf[j] = *reinterpret_cast<const uint4*>(a.q + i * a.q_token + head * a.q_head + d);
+      }
     }
     if constexpr (kWide) {
       __syncwarp();  // all lanes have read what the ring held
@@ -1074,6 +1139,22 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     __syncthreads();
     if (any) keep_queries();
     const bool whole = e.ta == 0 && e.tb == e.tiles;
+    const bool meets = kTogether && (e.of_group || room.first[e.row] > 0);  // its result is a part
+    auto record_of = [&](int h) {
+      if (!e.of_group) return record(e.row, e.h0 + h);
+      const int at = e.h0 + h, member = at / a.group;
+      return record(e.row + member, e.kvh * a.group + at - member * a.group);
+    };
+    auto emit = [&](int h, int d, float4 acc, float top, float sum) {
+      if (kTogether && meets) {
+        Record* r = record_of(h);
+        const int part = e.of_group ? 0 : 1;
+        __stcg(reinterpret_cast<float4*>(&r->o[part][d]), sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : acc);
+        if (d == 0) __stcg(reinterpret_cast<float2*>(r->ml[part]), make_float2(top, sum));
+        return;
+      }
+      result(e.row, e.h0 + h, d, acc, top, sum);
+    };
     const int slot = 2 * blockIdx.x + (e.ta == 0 ? 1 : 0);
     uint32_t odd = 0, turn = 1;  // bit k: the values of turn k below are not finite, and the sum does not say why
     for (int x = tid; x < e.heads * (HD / 4); x += kThreads, turn <<= 1) {
@@ -1093,15 +1174,41 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       }
       if (odd_four(acc) && !not_finite(sum) && !(whole && sum == 0.f)) odd |= turn;
       if (whole) {
-        result(e.row, e.h0 + h, d, acc, top, sum);
+        emit(h, d, acc, top, sum);
       } else {
         __stcg(reinterpret_cast<float4*>(&a.part_o[((size_t)slot * HB + h) * HD + d]), acc);
         if (d == 0) __stcg(reinterpret_cast<float2*>(&a.part_ml[(slot * HB + h) * 2]), make_float2(top, sum));
       }
     }
-    if (kHeld) __syncthreads();  // e4m3 has no infinities, and a NaN stays one by itself
-    else if (__syncthreads_or(odd))  // s_o and s_ml are free from here on, the next piece's queries are where all warps read them
-      mend<T, HD>(a, odd, e.row, kTail ? s_first[e.row] : 0, e.pair, e.ta, e.tb, e.h0, e.heads, whole ? nullptr : a.part_o + (size_t)slot * HB * HD, reinterpret_cast<int*>(&s_o[0][0][0]));
+    if (kHeld) {
+      __syncthreads();  // e4m3 has no infinities, and a NaN stays one by itself
+    } else if (__syncthreads_or(odd)) {  // s_o and s_ml are free from here on, the next piece's queries are where all warps read them
+      int* const seen = reinterpret_cast<int*>(&s_o[0][0][0]);
+      int seq, len, from = 0;
+      if (kTogether && e.of_group) {
+        const GroupInfo of = room.info[room.group[e.row]];
+        seq = of.seq;
+        len = of.tokens;
+      } else {
+        len = own_len(e.row, &seq);
+        if (kMode != kAlone) from = room.first[e.row];
+      }
+      look_through<T, HD>(a, a.table + (size_t)seq * a.max_pages + (from >> a.shift), kTogether ? e.kvh : e.pair / a.blocks_of_heads, e.ta,
+                          min((int64_t)len, (int64_t)e.tb * kTile), seen);
+      for (int x = tid; odd && x < e.heads * (HD / 4); x += kThreads, odd >>= 1) {
+        if (!(odd & 1u)) continue;
+        const int h = x / (HD / 4), d = x % (HD / 4) * 4;
+        for (int i = d; i < d + 4; ++i) {
+          const float now = made_of(seen[i]);
+          if (now == 0.f) continue;
+          if (!whole) __stcg(&a.part_o[((size_t)slot * HB + h) * HD + i], now);
+          else if (kTogether && meets) __stcg(&record_of(h)->o[e.of_group ? 0 : 1][i], now);
+          else a.out[e.row * a.o_token + (int64_t)(e.h0 + h) * a.o_head + i] = (uint16_t)(infinity_bits<T>() | (now > 0.f ? 0u : now < 0.f ? 0x8000u : 0x7fffu));
+        }
+      }
+      __syncthreads();
+    }
+    bool finished = whole;  // by this block
     if (!whole) {
       // ---- the last block to arrive joins up to kJoin neighbouring pieces; the last of those that did joins what they got
       const int c0 = block_of(e.first_w + kUnitsBefore), c1 = block_of(e.first_w + kUnitsBefore + e.tiles - 1), pieces = c1 - c0 + 1;
@@ -1157,7 +1264,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
           __syncwarp();  // b's place is read by the HD / 4 lanes of a head, all of this warp: they are done
           if (!there) continue;
           if (final) {
-            result(e.row, e.h0 + h, d, acc, top, sum);
+            emit(h, d, acc, top, sum);
           } else {
             const int sl = slot_of(b) + h;
             __stcg(reinterpret_cast<float4*>(&a.part_o[(size_t)sl * HD + d]), acc);
@@ -1168,7 +1275,59 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       const int mine = ((int)blockIdx.x - c0) / kJoin, groups = (pieces + kJoin - 1) / kJoin, b0 = c0 + mine * kJoin;
       if (last_of(&a.count[2 * b0 + (b0 == c0)], min(kJoin, pieces - mine * kJoin))) {
         join(b0, min(kJoin, pieces - mine * kJoin), 1, groups == 1);
-        if (groups > 1 && last_of(&a.pair_count[(size_t)e.row * pairs + e.pair], groups)) join(c0, groups, kJoin, true);
+        finished = groups == 1;
+        unsigned int* count = a.pair_count + ((size_t)e.row * pairs + e.pair) * a.pair_step;
+        if (kMode != kAlone) count = e.of_group ? &record(e.row, e.pair)->group_count : &record(e.row, e.h0)->pair_count;
+        if (groups > 1 && last_of(count, groups)) {
+          join(c0, groups, kJoin, true);
+          finished = true;
+        }
+      }
+    }
+    if constexpr (kTogether) {
+      if (finished && meets) {
+        // ---- a part of one row, or of a group's up to HB rows: the last part of a row and key-value head to arrive joins them
+        const int m0 = e.of_group ? e.h0 / a.group : 0, rows = e.of_group ? (e.h0 + e.heads - 1) / a.group - m0 + 1 : 1;
+        auto has_own = [&](int i) { return s_end[n_groups + i] != s_end[n_groups + i - 1]; };
+        __threadfence();
+        __syncthreads();
+        if (tid < rows) {
+          const int i = e.row + m0 + tid;
+          bool last = false;
+          if (room.first[i] > 0 && (!e.of_group || room.group[i] == room.group[e.row])) {
+            const int member = i - room.info[room.group[i]].lo;
+            const int parts = ((member + 1) * a.group - 1) / HB - member * a.group / HB + 1 + (has_own(i) ? a.blocks_of_heads : 0);
+            unsigned int* count = &record(i, e.kvh * a.group)->count;
+            last = atomicAdd(count, 1u) + 1u == (unsigned)parts;
+            if (last) *count = 0u;
+          }
+          s_done[tid] = last;
+        }
+        __syncthreads();
+        __threadfence();
+        for (int x = tid; x < rows * a.group * (HD / 4); x += kThreads) {
+          const int at = x / (HD / 4), d = x % (HD / 4) * 4, r = at / a.group, i = e.row + m0 + r, h = e.kvh * a.group + at - r * a.group;
+          if (!s_done[r]) continue;
+          const Record* from = record(i, h);
+          const bool own = has_own(i);
+          const float2 m0 = __ldcg(reinterpret_cast<const float2*>(from->ml[0])), m1 = own ? __ldcg(reinterpret_cast<const float2*>(from->ml[1])) : make_float2(-INFINITY, 0.f);
+          const float4 v0 = __ldcg(reinterpret_cast<const float4*>(&from->o[0][d]));
+          const float4 v1 = own ? __ldcg(reinterpret_cast<const float4*>(&from->o[1][d])) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float top = fmaxf(m0.x, m1.x), use = top == -INFINITY ? 0.f : top, f0 = exp2_fast(m0.x - use), f1 = exp2_fast(m1.x - use);
+          const float sum = f0 * m0.y + f1 * m1.y;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          add(acc, f0, v0);
+          add(acc, f1, v1);
+          if (odd_four(acc) && !not_finite(sum)) {  // a factor that is 0 makes a NaN of an infinity
+            auto kept = [](float now, float u, float w) {
+              const float both = (not_finite(u) ? u : 0.f) + (not_finite(w) ? w : 0.f);
+              return not_finite(both) ? both : now;
+            };
+            acc = make_float4(kept(acc.x, v0.x, v1.x), kept(acc.y, v0.y, v1.y), kept(acc.z, v0.z, v1.z), kept(acc.w, v0.w, v1.w));
+          }
+          result(i, h, d, acc, top, sum);
+        }
+        __syncthreads();
       }
     }
   }
@@ -1195,23 +1354,24 @@ bool make_map(CUtensorMap* map, const DecodeArgs& a, int hd) {
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class T, int HD, int kForm, bool kTail>
+template <class T, int HD, int kForm, int kMode>
 cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int sms, cudaStream_t s) {
-  size_t room = kTail ? kTailBytes : 0;
-  if (kForm == kSixteen) {
+  size_t room = kMode == kAlone ? 0 : GroupRoom(nullptr, kMode == kBoth, a.n, a.shared.n_groups).bytes;
+  if (kForm == kSixteen) room += (size_t)kWarps * kSlots * 16 * HD * 4 + 1024;
+  if (kForm == kSixteen || kMode == kBoth) {
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kForm, kTail>), &done);
+    const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kForm, kMode>), &done);
     if (e != cudaSuccess) return e;
-    room += (size_t)kWarps * kSlots * 16 * HD * 4 + 1024;
   }
   const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(HD, kForm) * sms));
-  return launch_early(k_attn_decode<T, HD, kForm, kTail>, grid, kThreads, room, s, map, a);
+  return launch_early(k_attn_decode<T, HD, kForm, kMode>, grid, kThreads, room, s, map, a);
 }
 template <class T, int HD>
-cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hb, bool held, bool tail, int sms, cudaStream_t s) {
-  if (held) return hb == 8 ? launch<T, HD, kHeldEight, false>(map, a, sms, s) : launch<T, HD, kHeldSixteen, false>(map, a, sms, s);
-  if (tail) return hb == 8 ? launch<T, HD, kEight, true>(map, a, sms, s) : launch<T, HD, kSixteen, true>(map, a, sms, s);
-  return hb == 8 ? launch<T, HD, kEight, false>(map, a, sms, s) : launch<T, HD, kSixteen, false>(map, a, sms, s);
+cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hb, bool held, int mode, int sms, cudaStream_t s) {
+  if (held) return hb == 8 ? launch<T, HD, kHeldEight, kAlone>(map, a, sms, s) : launch<T, HD, kHeldSixteen, kAlone>(map, a, sms, s);
+  if (mode == kBehind) return hb == 8 ? launch<T, HD, kEight, kBehind>(map, a, sms, s) : launch<T, HD, kSixteen, kBehind>(map, a, sms, s);
+  if (mode == kBoth) return hb == 8 ? launch<T, HD, kEight, kBoth>(map, a, sms, s) : launch<T, HD, kSixteen, kBoth>(map, a, sms, s);
+  return hb == 8 ? launch<T, HD, kEight, kAlone>(map, a, sms, s) : launch<T, HD, kSixteen, kAlone>(map, a, sms, s);
 }
 
 // [(m, l) of the partial results][their O][counts]: the counts start at the same place for every description and n, and the
@@ -1231,7 +1391,7 @@ const char* heads_error(const np_kv_desc* d, int n_heads, int n) {
 
 }  // namespace
 
-uint64_t decode_space_bytes(int n_kv_heads, int group, int n) { return space_bytes(n_kv_heads, group, n); }
+uint64_t decode_parts_bytes() { return kSpacePairs; }
 
 int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads, const int32_t* seqs, int32_t n,
            float scale2, const np_rows* out, float* lse, void* workspace, const SharedArgs* shared, int sms, cudaStream_t s) {
@@ -1253,7 +1413,7 @@ int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_ta
   a.n_heads = n_heads;
   a.n_kv_heads = d->n_kv_heads;
   a.group = n_heads / d->n_kv_heads;
-  const int hb = heads_per_block(a.group);
+  const int hb = heads_per_block(shared && shared->n_groups && shared->together ? std::max(a.group, shared->columns) : a.group);
   a.blocks_of_heads = (a.group + hb - 1) / hb;
   a.scale2 = scale2;
   a.shift = log2_of(d->page_tokens);
@@ -1266,12 +1426,18 @@ int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_ta
   a.part_o = reinterpret_cast<float*>(ws + kSpaceO);
   a.count = reinterpret_cast<unsigned int*>(ws + kSpaceCounts);
   a.pair_count = reinterpret_cast<unsigned int*>(ws + kSpacePairs);
-  const bool held = held_in_8(d), tail = shared != nullptr;
+  a.pair_step = 1;
+  if (shared && shared->n_groups == 0) {  // nothing is shared, but the workspace is of that kind
+    a.pair_count = &shared->records->pair_count;
+    a.pair_step = sizeof(Record) / 4;
+  }
+  const bool held = held_in_8(d);
+  const int mode = !shared || shared->n_groups == 0 ? kAlone : shared->together ? kBoth : kBehind;
   CUtensorMap map = {};
   if (hb == 16 && !held && !make_map(&map, a, d->head_dim)) return fail(NP_E_INVAL, "a cache that a tensor map does not describe");
   cudaError_t e;
-  if (row_type(d) == NP_T_BF16) e = d->head_dim == 128 ? launch<__nv_bfloat16, 128>(map, a, hb, held, tail, sms, s) : launch<__nv_bfloat16, 64>(map, a, hb, held, tail, sms, s);
-  else e = d->head_dim == 128 ? launch<__half, 128>(map, a, hb, held, tail, sms, s) : launch<__half, 64>(map, a, hb, held, tail, sms, s);
+  if (row_type(d) == NP_T_BF16) e = d->head_dim == 128 ? launch<__nv_bfloat16, 128>(map, a, hb, held, mode, sms, s) : launch<__nv_bfloat16, 64>(map, a, hb, held, mode, sms, s);
+  else e = d->head_dim == 128 ? launch<__half, 128>(map, a, hb, held, mode, sms, s) : launch<__half, 64>(map, a, hb, held, mode, sms, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);
 }
 

@@ -1,6 +1,5 @@
-// What the two kernels of np_attn_decode_shared have in common: which groups of rows share how many tokens, and where the first kernel
-// (np_attn_shared.cu: the shared tokens, for all rows of a group at once) leaves its results for the second (np_attn_decode.cu: each row's own tokens,
-// and the join).
+// What the kernels of np_attn_decode_shared have in common: which groups of rows share how many tokens, and where the kernel of the shared tokens
+// (np_attn_shared.cu) leaves its results for that of the rows' own (np_attn_decode.cu), which does both where groups are small.
 #pragma once
 
 #include <stdint.h>
@@ -23,17 +22,29 @@ struct __align__(16) LinePlan {
   int64_t each, more;
 };
 
+// Where the parts of a (row, query head) meet, and counts of what has arrived, which are zero between calls.  Of one size for all calls, so that
+// what one call leaves in a workspace is never another's count.
+struct __align__(32) Record {
+  float o[2][128];            // sums of the shared tokens and of the row's own
+  float ml[2][2];             // their maxima (base two) and sums
+  unsigned int count;         // at a key-value head's first query head: parts of the row
+  unsigned int pair_count;    // at the first query head of a block of them: joined pieces of the row's own tokens
+  unsigned int group_count;   // in a group's first row, by the number of the block of columns: joined pieces of the shared tokens
+  unsigned int unused;
+};
+
 struct SharedArgs {
   const int32_t* cu;       // [n_groups + 1]
   const int32_t* tokens;   // [n_groups] that a group shares
   int n_groups;
-  int members;             // rows of the call in a block of rows
-  int tile_members;        // and in each tile of 128 query rows
+  bool together;           // one kernel for both
+  int columns;             // together: (row, query head) pairs of a group and key-value head, about
+  Record* records;         // [n][n_heads]
+  // the two kernels apart: rows of the call in a block of rows, and in each tile of 128 query rows
+  int members, tile_members;
   LinePlan* line;
   GroupPlan* plan;         // [n_groups]
-  float* row_ml;           // [n][n_heads][2]   maximum (base two) and sum, of rows that one block has done alone
-  float* row_o;            // [n][n_heads][HD]
-  float* part_ml;          // [2 * blocks][rows of a block][2]   of the others
+  float* part_ml;          // [2 * blocks][rows of a block][2]   of blocks that have not done all of a block of rows' tiles (the others: records)
   float* part_o;           // [2 * blocks][rows of a block][HD]
   int part_rows;
 };

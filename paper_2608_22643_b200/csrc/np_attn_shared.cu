@@ -107,10 +107,10 @@ __device__ __forceinline__ int page_of(const Args& a, const Piece& p, int j, int
   return lane < 8 && j < p.t1 && tok < p.tokens ? p.pages[tok >> a.shift] : -1;
 }
 
-// Rows whose O is not finite though their sum is, by their warp: what the values make infinite or NaN is so (weights are above 0).  at: a
-// row's place in part.
+// Rows whose O is not finite though their sum is, by their warp: what the values make infinite or NaN is so (weights are above 0).  mine: a
+// lane's row's O.
 template <bool kBf16, int HD>
-__device__ __noinline__ void mend_rows(const Args& a, const Piece& p, uint32_t rows, float* part, int64_t at, int lane) {
+__device__ __noinline__ void mend_rows(const Args& a, const Piece& p, uint32_t rows, float* mine, int lane) {
   constexpr int N = HD / 32;
   int odd[N];  // 1 a NaN, 2 inf, 4 -inf
 #pragma unroll
@@ -130,7 +130,7 @@ __device__ __noinline__ void mend_rows(const Args& a, const Piece& p, uint32_t r
   }
   __syncwarp();  // the rows are stored
   for (; rows; rows &= rows - 1) {
-    float* o = part + __shfl_sync(0xffffffffu, at, __ffs(rows) - 1) * HD + lane;
+    float* o = reinterpret_cast<float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), __ffs(rows) - 1)) + lane;
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (odd[i]) __stcg(o + i * 32, odd[i] == 2 ? INFINITY : odd[i] == 4 ? -INFINITY : __uint_as_float(0x7fffffffu));
@@ -461,10 +461,10 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       if (!ok) break;
       // ---- the partial result
       fence_after();
-      const int64_t at = p.whole ? (int64_t)(p.row0 + member) * a.n_heads + p.kvh * a.group + in_group
-                                 : (int64_t)(2 * blockIdx.x + (p.t0 == 0)) * a.shared.part_rows + i * kRows + row;
-      float* part_o = p.whole ? a.shared.row_o : a.shared.part_o;
-      float* part_ml = p.whole ? a.shared.row_ml : a.shared.part_ml;
+      Record* const record = a.shared.records + ((int64_t)(p.row0 + member) * a.n_heads + p.kvh * a.group + in_group);
+      const int64_t at = (int64_t)(2 * blockIdx.x + (p.t0 == 0)) * a.shared.part_rows + i * kRows + row;
+      float* const part_o = p.whole ? record->o[0] : a.shared.part_o + at * HD;
+      float* const part_ml = p.whole ? record->ml[0] : a.shared.part_ml + at * 2;
       uint32_t big = 0;
 #pragma unroll 1
       for (int c = 0; c < HD; c += 32) {
@@ -487,12 +487,12 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           uint32_t v[8];
 #pragma unroll
           for (int y = 0; y < 8; ++y) v[y] = o[x + y];
-          store32(part_o + at * HD + c + x, v);
+          store32(part_o + c + x, v);
         }
       }
-      if (valid) *reinterpret_cast<float2*>(part_ml + at * 2) = make_float2(m, l);
+      if (valid) *reinterpret_cast<float2*>(part_ml) = make_float2(m, l);
       const uint32_t odd = __ballot_sync(0xffffffffu, valid && big >= 0x7f800000u && !not_finite(l));
-      if (odd) mend_rows<kBf16, HD>(a, p, odd, part_o, at, lane);
+      if (odd) mend_rows<kBf16, HD>(a, p, odd, part_o, lane);
     }
   }
   fence_before();
@@ -531,26 +531,29 @@ cudaError_t launch(const CUtensorMap& q, const CUtensorMap& kv, const Args& a, i
   return tiles == 2 ? launch<kBf16, 64, 2>(q, kv, a, sms, s) : launch<kBf16, 64, 1>(q, kv, a, sms, s);
 }
 
-// [np_attn_decode's][how the line is dealt out][plans][maxima and sums of rows][their O][of blocks' parts][their O]
+// [partial results and counts of np_attn_decode.cu][how the line is dealt out][plans][maxima and sums of blocks' parts][their O][records]: all but the
+// last are at the same place for every call.
 struct Space {
-  uint64_t line, plan, row_ml, row_o, part_ml, part_o, bytes;
-  Space(const np_kv_desc* d, int n_heads, int n) {
+  uint64_t line, plan, part_ml, part_o, records, bytes;
+  Space(int n_heads, int n) {
     uint64_t at = 0;
     auto take = [&at](uint64_t bytes) {
       const uint64_t from = (at + 255) & ~(uint64_t)255;
       at = from + bytes;
       return from;
     };
-    take(decode_space_bytes(d->n_kv_heads, n_heads / d->n_kv_heads, n));
+    take(decode_parts_bytes());
     line = take(sizeof(LinePlan));
     plan = take((uint64_t)NP_KV_MAX_SEQS * sizeof(GroupPlan));
-    row_ml = take((uint64_t)n * n_heads * 8);
-    row_o = take((uint64_t)n * n_heads * d->head_dim * 4);
     part_ml = take((uint64_t)2 * kSharedBlocks * kRows * 8);
-    part_o = take((uint64_t)2 * kSharedBlocks * kRows * d->head_dim * 4);
+    part_o = take((uint64_t)2 * kSharedBlocks * kRows * 128 * 4);
+    records = take((uint64_t)n * n_heads * sizeof(Record));
     bytes = at;
   }
 };
+
+// Columns, (row, query head) pairs of a group and key-value head, that one kernel does beside the rows' own tokens; more take the tensor cores' way.
+constexpr int kFewColumns = 16;
 
 const char* shared_heads_error(const np_kv_desc* d, int n_heads, int n) {
   if (const char* m = decode_heads_error(d, n_heads, n)) return m;
@@ -568,7 +571,7 @@ int np_attn_shared_workspace_bytes(const np_kv_desc* d, int32_t n_heads, int32_t
   if (const char* m = desc_error(d)) return fail(NP_E_INVAL, m);
   if (const char* m = shared_heads_error(d, n_heads, n)) return fail(NP_E_INVAL, m);
   if (!out) return fail(NP_E_INVAL, "NULL argument");
-  *out = Space(d, n_heads, n).bytes;
+  *out = Space(n_heads, n).bytes;
   return NP_OK;
 }
 
@@ -583,14 +586,22 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   float scale2;
   if (const char* m = decode_error(d, cache, layer, t, q, n_heads, n, scale, out, workspace, &scale2)) return fail(NP_E_INVAL, m);
   if (n_groups > 0 && (!cu || !shared)) return fail(NP_E_INVAL, "NULL argument");
-  const Space space(d, n_heads, n);
+  const Space space(n_heads, n);
   if (workspace_bytes < space.bytes) return fail(NP_E_INVAL, "workspace is smaller than np_attn_shared_workspace_bytes says");
   int sms;
   if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (n_groups == 0 || held_in_8(d)) return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, nullptr, sms, s);
+  if (held_in_8(d)) n_groups = 0;
   char* ws = static_cast<char*>(workspace);
+  const int group = n_heads / d->n_kv_heads, columns = n_groups ? (int)std::min<int64_t>(1 << 20, ((int64_t)n * group + n_groups - 1) / n_groups) : 0;
   Args a = {};
+  a.shared.cu = cu;
+  a.shared.tokens = shared;
+  a.shared.n_groups = n_groups;
+  a.shared.records = reinterpret_cast<Record*>(ws + space.records);
+  a.shared.columns = columns;
+  a.shared.together = columns <= kFewColumns;
+  if (a.shared.together) return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s);
   a.page_bytes = page_bytes(d);
   a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * a.page_bytes;
   a.table = t->page_table;
@@ -600,23 +611,18 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   a.n = n;
   a.n_heads = n_heads;
   a.n_kv_heads = d->n_kv_heads;
-  a.group = n_heads / d->n_kv_heads;
+  a.group = group;
   a.shift = log2_of(d->page_tokens);
   a.n_pages = d->n_pages;
   a.max_seqs = d->max_seqs;
   a.max_pages = d->max_pages;
   a.scale2 = scale2;
   // two tiles of rows where an average group fills more than one
-  const int tile_members = kRows / a.group, tiles = (int64_t)n > (int64_t)n_groups * tile_members ? 2 : 1;
-  a.shared.cu = cu;
-  a.shared.tokens = shared;
-  a.shared.n_groups = n_groups;
+  const int tile_members = kRows / group, tiles = (int64_t)n > (int64_t)n_groups * tile_members ? 2 : 1;
   a.shared.tile_members = tile_members;
   a.shared.members = tiles * tile_members;
   a.shared.line = reinterpret_cast<LinePlan*>(ws + space.line);
   a.shared.plan = reinterpret_cast<GroupPlan*>(ws + space.plan);
-  a.shared.row_ml = reinterpret_cast<float*>(ws + space.row_ml);
-  a.shared.row_o = reinterpret_cast<float*>(ws + space.row_o);
   a.shared.part_ml = reinterpret_cast<float*>(ws + space.part_ml);
   a.shared.part_o = reinterpret_cast<float*>(ws + space.part_o);
   a.shared.part_rows = tiles * kRows;

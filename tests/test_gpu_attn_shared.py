@@ -211,10 +211,11 @@ def test_a_cache_of_8_bits():
     assert torch.equal(out, want)
 
 
-def test_one_workspace_serves_both_calls_and_replays():
-    """Captured with np_kv_shared before it, replayed in turn with np_attn_decode over the same workspace while the branches grow."""
+def test_captured_with_what_is_shared():
+    """Captured with np_kv_shared before it and np_attn_decode behind it, replayed while the branches grow."""
     c, seqs, cu = _branches(BF, 2, 64, 16, [400, 640], [[20, 0, 4], [3, 0]])
     ws = _workspace(c, 8, 5)
+    other = torch.zeros(nb.np_attn_workspace_bytes(c.desc, 8, 5), dtype=torch.uint8, device="cuda")
     q = torch.randn(5, 8, 64, device="cuda").to(BF)
     out, plain, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(5, 8, device="cuda")
     held, cu_dev, seq_dev = c.dev([0, 0]), c.dev(cu), c.dev(seqs)
@@ -223,7 +224,7 @@ def test_one_workspace_serves_both_calls_and_replays():
     with torch.cuda.graph(g, stream=s):
         nb.np_kv_shared(c.desc, c.tables, seq_dev, cu_dev, held, stream=s)
         nb.np_attn_decode_shared(c.desc, c.cache, 0, c.tables, q, out, ws, cu_dev, held, seqs=seq_dev, lse=lse, stream=s)
-        nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, plain, ws, seqs=seq_dev, stream=s)
+        nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, plain, other, seqs=seq_dev, stream=s)
     for t in range(5):
         c.grow(seqs, [t, 17, 0, 1, 2], seed=t)
         q.copy_(torch.randn(q.shape, device="cuda").to(BF))
@@ -277,6 +278,21 @@ def test_calls_one_behind_the_other():
         torch.cuda.synchronize()
         assert torch.equal(want, outs[layer])
         check_rows(want, lse, qs[layer], lambda i: c.tokens(layer, seqs[i]), 0.125, True)
+
+
+def test_one_workspace_serves_calls_of_all_sizes():
+    """Few rows and many, small groups and large ones, both head sizes, 8 bits and nothing shared, one behind the other over one workspace."""
+    small, seqs, cu = _branches(BF, 2, 64, 16, [3000, 300], [[20, 700, 4], [3, 0]])
+    large, seqs2, cu2 = _branches(HF, 4, 128, 64, [2000], [[30, 5, 0] * 30])
+    held, seqs3, cu3 = _branches(BF, 2, 64, 16, [4000], [[20, 0, 4]], make=Held)
+    ws = torch.zeros(max(nb.np_attn_shared_workspace_bytes(small.desc, 40, 5), nb.np_attn_shared_workspace_bytes(large.desc, 16, 90)), dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        _run(small, 2, seqs, cu, small.dev([2992, 288]), ws=ws)
+        _run(large, 16, seqs2, cu2, large.dev([1984]), ws=ws)
+        _run(held, 40, seqs3, cu3, held.dev([4000]), ws=ws)
+        _run(small, 40, seqs, cu, small.dev([2992, 288]), ws=ws)
+        _run(small, 4, seqs, [0], small.dev([]), ws=ws)
+        _run(large, 4, seqs2, cu2, large.dev([64]), ws=ws)
 
 
 # ---- what is shared ---------------------------------------------------------------------

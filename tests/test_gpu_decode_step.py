@@ -64,6 +64,7 @@ def test_prompts_branches_and_steps(make, dtype, hq, hkv, hd, P):
     n = len(dst)
     seqs, groups, shared = c.dev(dst), c.dev(range(0, n + 1, ways)), c.dev([0] * 3)
     ws = torch.zeros(nb.np_attn_shared_workspace_bytes(c.desc, hq, n), dtype=torch.uint8, device="cuda")
+    other = torch.zeros(nb.np_attn_workspace_bytes(c.desc, hq, n), dtype=torch.uint8, device="cuda")
     for _ in range(steps):
         start, at = c.reserve(dst, [1] * n)
         nb.np_kv_shared(c.desc, c.tables, seqs, groups, shared)
@@ -71,7 +72,7 @@ def test_prompts_branches_and_steps(make, dtype, hq, hkv, hd, P):
             q, _, _ = enter(layer, seqs, None, start, at)
             out, lse, plain = torch.empty_like(q), torch.empty(n, hq, device="cuda"), torch.empty_like(q)
             nb.np_attn_decode_shared(c.desc, c.cache, layer, c.tables, q, out, ws, groups, shared, seqs=seqs, lse=lse)
-            nb.np_attn_decode(c.desc, c.cache, layer, c.tables, q, plain, ws, seqs=seqs)
+            nb.np_attn_decode(c.desc, c.cache, layer, c.tables, q, plain, other, seqs=seqs)
             torch.cuda.synchronize()
             kept = [c.tokens(layer, s) for s in dst]
             if held:

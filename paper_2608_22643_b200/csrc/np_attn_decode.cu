@@ -84,14 +84,14 @@ struct DecodeArgs {
   int n, n_heads, n_kv_heads, group, blocks_of_heads;  // heads of a group: blocks_of_heads pieces of HB
   int shift, n_pages, max_seqs, max_pages;
   int64_t page_bytes;
-  SharedArgs shared;  // kTail: tokens that other rows share, and their partial results
+  SharedArgs shared;  // not kAlone: what groups of rows share
 };
 
 // How keys and values get to the products: in the rows' type, up to eight or sixteen heads of a group at once; in 8 bits, the same.
 enum Form { kEight, kSixteen, kHeldEight, kHeldSixteen };
-// What is computed: rows by themselves; rows behind the tokens that their group shares, joined to another kernel's partial results of those;
-// rows and what their groups share, of which the last part to arrive is joined to the others.
-enum Mode { kAlone, kBehind, kBoth };
+// What is computed: rows by themselves; what rows have behind the tokens that their group shares, which is left for a join; rows and what their
+// groups share, of which the last part to arrive is joined to the others.
+enum Mode { kAlone, kOwn, kBoth };
 
 template <class T>
 struct Half2;
@@ -272,65 +272,6 @@ __device__ __noinline__ float4 keep_infinite(float4 acc, const float* part, int6
   return acc;
 }
 
-// The partial results of the `tokens` that row i and its group share join those of its own: four values of head h, its maximum and its sum.
-template <int HD>
-__device__ __forceinline__ void join_shared(const DecodeArgs& a, int tokens, int group, int i, int h, int d, float4& acc, float& top, float& sum) {
-  npp::pdl_wait_prior();
-  const SharedArgs& s = a.shared;
-  const GroupPlan plan = s.plan[group];
-  const LinePlan line = *s.line;
-  const int kvh = h / a.group, member = i - plan.row0, block = member / s.members, in_block = member - block * s.members, tile = in_block / s.tile_members;
-  const int row = tile * kSharedTile + (in_block - tile * s.tile_members) * a.group + h - kvh * a.group;
-  const int64_t tiles = (tokens + kSharedTile - 1) / kSharedTile, w = plan.first_w + ((int64_t)kvh * plan.row_blocks + block) * tiles;
-  auto block_of = [&](int64_t x) { return (int)(x < line.more * (line.each + 1) ? divide(x, line.each + 1) : line.more + divide(x - line.more * (line.each + 1), line.each)); };
-  const int c0 = block_of(w), c1 = block_of(w + tiles - 1);
-  const Record* whole = s.records + ((int64_t)i * a.n_heads + h);  // where one block has done all of them
-  auto slot_of = [&](int b) { return (int64_t)(2 * b + (b == c0)) * s.part_rows + row; };
-  auto ml_of = [&](int b) { return c0 == c1 ? whole->ml[0] : s.part_ml + slot_of(b) * 2; };
-  auto o_of = [&](int b) { return (c0 == c1 ? whole->o[0] : s.part_o + slot_of(b) * HD) + d; };
-  constexpr int kAhead = 4;
-  const float own[4] = {acc.x, acc.y, acc.z, acc.w};
-  for (int b0 = c0; b0 <= c1; b0 += kAhead) {
-    float2 ml[kAhead];
-    float4 v[kAhead];
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y) {
-      ml[y] = make_float2(-INFINITY, 0.f);
-      v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (b0 + y > c1) continue;
-      ml[y] = __ldcg(reinterpret_cast<const float2*>(ml_of(b0 + y)));
-      v[y] = __ldcg(reinterpret_cast<const float4*>(o_of(b0 + y)));
-    }
-    float now = top;
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y) now = fmaxf(now, ml[y].x);
-    const float use = now == -INFINITY ? 0.f : now, f0 = exp2_fast(top - use);
-    top = now;
-    sum *= f0;
-    acc = make_float4(acc.x * f0, acc.y * f0, acc.z * f0, acc.w * f0);
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y) {
-      const float f = exp2_fast(ml[y].x - use);
-      sum += f * ml[y].y;
-      acc.x += f * v[y].x;
-      acc.y += f * v[y].y;
-      acc.z += f * v[y].z;
-      acc.w += f * v[y].w;
-    }
-  }
-  if (not_finite(sum) || !(not_finite(acc.x) || not_finite(acc.y) || not_finite(acc.z) || not_finite(acc.w))) return;
-  // factors that are 0 make a NaN of an infinity: what is not finite is what the parts that are not add up to
-  float* const to[4] = {&acc.x, &acc.y, &acc.z, &acc.w};
-  for (int x = 0; x < 4; ++x) {
-    float kept = not_finite(own[x]) ? own[x] : 0.f;
-    for (int b = c0; b <= c1; ++b) {
-      const float v = __ldcg(o_of(b) + x);
-      if (not_finite(v)) kept += v;
-    }
-    if (not_finite(kept)) *to[x] = kept;
-  }
-}
-
 // Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
 // accumulators.  us with one more and with this many (sixteen heads: with keys and values in registers): 128 values, eight heads, four blocks 113 (the long sequence) and 186 (64 of 1000),
 // three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16 sequences of 2000, five
@@ -342,18 +283,13 @@ constexpr int blocks_per_sm(int hd, int form) {
 // In 8 bits sums are of 2^(s - m + kHeldShift): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.
 constexpr float kHeldShift = 30.f, kHeldUp = 0x1p30f;
 
-// What a block knows of groups, in dynamic shared memory: for each row the tokens that it shares and its group; kBoth: for each group what it is, and
-// the units of groups and rows.
-struct GroupInfo {
-  int tokens;
-  int16_t lo, hi;  // its rows
-  int seq;         // whose pages are read
-};
+// What a block knows of groups, in dynamic shared memory: for each row its tokens, how many of them it shares, its group and sequence; kBoth: the
+// units of groups and rows.
 struct GroupRoom {
   int64_t* end;
-  int* first;
+  int *len, *first;
   GroupInfo* info;
-  uint16_t* group;
+  int16_t *group, *seq;
   uint32_t bytes;
   __host__ __device__ GroupRoom(unsigned char* base, bool both, int n, int n_groups) {
     uint32_t at = 0;
@@ -363,9 +299,11 @@ struct GroupRoom {
       return p;
     };
     end = reinterpret_cast<int64_t*>(take(both ? (n + n_groups) * 8 : 0));
+    len = reinterpret_cast<int*>(take(n * 4));
     first = reinterpret_cast<int*>(take(n * 4));
-    info = reinterpret_cast<GroupInfo*>(take(both ? n_groups * sizeof(GroupInfo) : 0));
-    group = reinterpret_cast<uint16_t*>(take(n * 2));
+    info = reinterpret_cast<GroupInfo*>(take(n_groups * sizeof(GroupInfo)));
+    group = reinterpret_cast<int16_t*>(take(n * 2));
+    seq = reinterpret_cast<int16_t*>(take(n * 2));
     bytes = at;
   }
 };
@@ -386,7 +324,7 @@ struct WarpWaits {
 template <class T, int HD, int kForm, int kMode>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kForm))
 k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
-  constexpr bool kTail = kMode == kBehind, kTogether = kMode == kBoth;
+  constexpr bool kShares = kMode != kAlone, kTogether = kMode == kBoth;
   constexpr bool kWide = kForm == kSixteen, kHeld = kForm == kHeldEight || kForm == kHeldSixteen;
   constexpr int HB = kForm == kSixteen || kForm == kHeldSixteen ? 16 : 8;  // heads of a block, at most
   constexpr int NT = HB / 8, NH = kHeld ? 2 * NT : 2;  // in 8 bits: eights of heads; heads of a lane's scores
@@ -415,7 +353,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   __shared__ volatile int s_lost[kWarps];  // a wait of the warp was given up
   __shared__ int s_done[kTogether ? HB : 1];
   const int n_groups = kTogether ? a.shared.n_groups : 0, items = n_groups + a.n;  // items: groups, then rows
-  const GroupRoom room(s_dyn, kTogether, a.n, n_groups);
+  const GroupRoom room(s_dyn, kTogether, a.n, kShares ? a.shared.n_groups : 0);
   int64_t* const s_end = kTogether ? room.end : s_ends;  // units of the items up to and including this one
   if (kWide && (threadIdx.x & 31) == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
@@ -423,32 +361,47 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     s_lost[threadIdx.x >> 5] = 0;
     npp::fence_barrier_init();
   }
-  // The kernel of the shared tokens lets this one begin when all that came before it is done; its own results are waited for where they are
-  // needed, and by every block before it leaves.
-  if (!kTail) npp::pdl_wait_prior();
+  // The kernel of the shared tokens lets this one begin when all that came before it is done, and has nothing that this one needs; but what comes
+  // next waits for this one alone, so every block waits for that kernel before it leaves.
+  if (kMode != kOwn) npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
   const int pairs = a.n_kv_heads * a.blocks_of_heads;   // (key-value head, block of its query heads)
 
-  if constexpr (kTail || kTogether) {
+  if constexpr (kShares) {
+    for (int i = tid; i < a.n; i += kThreads) {
+      int seq;
+      const int len = row_len(a, i, &seq);
+      const bool known = seq >= 0 && seq < a.max_seqs;
+      room.len[i] = len;
+      room.seq[i] = (int16_t)(known ? seq : -1);
+      room.first[i] = len > 0 || !known ? len : a.lens[seq];  // as the tables say
+    }
+    for (int x = tid; x < a.shared.n_groups; x += kThreads) room.info[x] = group_at(a.shared, a.n, x);
+    __syncthreads();
+    for (int x = wid; x < a.shared.n_groups; x += kWarps) {
+      GroupInfo of = room.info[x];
+      check_group(of, room.seq, room.first, a.max_pages, a.shift, a.status);
+      __syncwarp();
+      if (lane == 0) room.info[x] = of;
+    }
+    __syncthreads();
     for (int i = tid; i < a.n; i += kThreads) room.first[i] = 0;
     __syncthreads();
     for (int x = wid; x < a.shared.n_groups; x += kWarps) {
-      int lo, hi, seq;
-      group_rows(a.shared, a.n, x, &lo, &hi);
-      const int tokens = group_tokens(a.shared, x, lo, hi, a.seqs, a.lens, a.max_seqs, a.max_pages, a.shift, a.status, &seq);
-      for (int i = lo + lane; i < hi; i += 32) {
-        room.first[i] = tokens;
-        room.group[i] = (uint16_t)x;
+      const GroupInfo of = room.info[x];
+      for (int i = of.lo + lane; i < of.hi; i += 32) {
+        room.first[i] = room.len[i] > 0 ? of.tokens : 0;
+        room.group[i] = (int16_t)x;
       }
-      if (kTogether && lane == 0) room.info[x] = GroupInfo{tokens, (int16_t)lo, (int16_t)hi, seq};
     }
     __syncthreads();
   }
   // tokens of row i of the call that are its own
   auto own_len = [&](int i, int* seq) {
-    const int len = row_len(a, i, seq);
-    return (kTail || kTogether) && len > 0 ? len - room.first[i] : len;
+    if (!kShares) return row_len(a, i, seq);
+    *seq = room.seq[i];
+    return room.len[i] - room.first[i];
   };
   // blocks of columns, (row, query head) pairs of one key-value head, of a group
   auto column_blocks = [&](const GroupInfo& x) { return ((x.hi - x.lo) * a.group + HB - 1) / HB; };
@@ -463,10 +416,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       of = (int64_t)a.n_kv_heads * column_blocks(x);
     } else {
       len = own_len(i - n_groups, &seq);
-      if (kTogether) {
-        of = pairs;
-        if (len <= 0 && row_len(a, i - n_groups, &seq) == 0) room.first[i - n_groups] = 0;  // no sequence: it shares nothing
-      }
+      if (kTogether) of = pairs;
     }
     return len > 0 ? (((int64_t)len + kTileTokens - 1) / kTileTokens + kUnitsBefore) * of : 0;
   };
@@ -503,9 +453,6 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   }
   // four values of a head's result; its log of the sum with the first
   auto result = [&](int i, int h, int d, float4 acc, float top, float sum) {
-    if constexpr (kTail) {
-      if (room.first[i] > 0) join_shared<HD>(a, room.first[i], room.group[i], i, h, d, acc, top, sum);
-    }
     const float use = top == -INFINITY ? 0.f : top;
     const bool none = sum == 0.f;
     const float inv = none ? 0.f : 1.f / sum;
@@ -516,16 +463,11 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     *reinterpret_cast<uint2*>(a.out + i * a.o_token + (int64_t)h * a.o_head + d) = r;
     if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = none ? -INFINITY : (kHeld ? use - kHeldShift : use) * kLn2 + logf(sum);
   };
-  // kTogether: where the parts of (row i, head h) meet
+  // where the parts of (row i, head h) meet
   auto record = [&](int64_t i, int h) { return a.shared.records + (i * a.n_heads + h); };
   for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
     if (s_end[n_groups + i] != (n_groups + i ? s_end[n_groups + i - 1] : 0)) continue;
-    int seq;
-    if (kTogether && room.first[i] > 0) continue;  // all of its tokens are shared
-    if (kTail && room.first[i] > 0 && row_len(a, i, &seq) > 0) {
-      for (int x = tid; x < a.n_heads * (HD / 4); x += kThreads) result(i, x / (HD / 4), x % (HD / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
-      continue;
-    }
+    if (kShares && room.first[i] > 0) continue;  // all of its tokens are shared
     for (int e = tid; e < a.n_heads * (HD / 8); e += kThreads) {
       const int h = e / (HD / 8), d = e % (HD / 8) * 8;
       *reinterpret_cast<uint4*>(a.out + i * a.o_token + h * a.o_head + d) = make_uint4(0, 0, 0, 0);
@@ -537,7 +479,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   const int64_t W = run * per;
   const int G = (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
   if ((int)blockIdx.x >= G) {
-    if (kTail) npp::pdl_wait_prior();
+    if (kMode == kOwn) npp::pdl_wait_prior();
     return;
   }
   const int64_t each = divide(W, G), more = W - each * G;
@@ -601,7 +543,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         const int hb = pair - kvh * a.blocks_of_heads;
         p.h0 = kvh * a.group + hb * HB;
         p.heads = min(HB, a.group - hb * HB);
-        p.pages = a.table + (size_t)seq * a.max_pages + (kTail || kTogether ? room.first[p.row] >> a.shift : 0);
+        p.pages = a.table + (size_t)seq * a.max_pages + (kShares ? room.first[p.row] >> a.shift : 0);
       }
       p.kvh = kvh;
       p.first_row = kvh << a.shift;
@@ -628,7 +570,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   int waiting[kSlots];                 // tokens of the chunks in this warp's ring
   npp::WarpRing<kSlots> uses;
   WarpWaits waits = {&s_lost[wid], a.status};
-  const uint32_t ring = ((npp::smem_addr(s_dyn) + (kMode == kAlone ? 0u : room.bytes) + 1023) & ~1023u) + wid * kSlots * kSlot;
+  const uint32_t ring = ((npp::smem_addr(s_dyn) + (kShares ? room.bytes : 0u) + 1023) & ~1023u) + wid * kSlots * kSlot;
   // what a lane reads with load_tiles: rows (tokens) 0-7 and 8-15 of two neighbouring 16-byte columns, 128-byte swizzle
   const uint32_t lane_row = ((lane & 7) + (lane >> 4) * 8) * 128, lane_col = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
   auto tiles_at = [&](uint32_t base, int step) { return base + lane_row + (step >> 2) * 2048 + (((step & 3) << 5) ^ lane_col); };
@@ -1139,14 +1081,14 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     __syncthreads();
     if (any) keep_queries();
     const bool whole = e.ta == 0 && e.tb == e.tiles;
-    const bool meets = kTogether && (e.of_group || room.first[e.row] > 0);  // its result is a part
+    const bool meets = kShares && (e.of_group || room.first[e.row] > 0);  // its result is a part
     auto record_of = [&](int h) {
       if (!e.of_group) return record(e.row, e.h0 + h);
       const int at = e.h0 + h, member = at / a.group;
       return record(e.row + member, e.kvh * a.group + at - member * a.group);
     };
     auto emit = [&](int h, int d, float4 acc, float top, float sum) {
-      if (kTogether && meets) {
+      if (kShares && meets) {
         Record* r = record_of(h);
         const int part = e.of_group ? 0 : 1;
         __stcg(reinterpret_cast<float4*>(&r->o[part][d]), sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : acc);
@@ -1191,7 +1133,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         len = of.tokens;
       } else {
         len = own_len(e.row, &seq);
-        if (kMode != kAlone) from = room.first[e.row];
+        if (kShares) from = room.first[e.row];
       }
       look_through<T, HD>(a, a.table + (size_t)seq * a.max_pages + (from >> a.shift), kTogether ? e.kvh : e.pair / a.blocks_of_heads, e.ta,
                           min((int64_t)len, (int64_t)e.tb * kTile), seen);
@@ -1202,7 +1144,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
           const float now = made_of(seen[i]);
           if (now == 0.f) continue;
           if (!whole) __stcg(&a.part_o[((size_t)slot * HB + h) * HD + i], now);
-          else if (kTogether && meets) __stcg(&record_of(h)->o[e.of_group ? 0 : 1][i], now);
+          else if (kShares && meets) __stcg(&record_of(h)->o[e.of_group ? 0 : 1][i], now);
           else a.out[e.row * a.o_token + (int64_t)(e.h0 + h) * a.o_head + i] = (uint16_t)(infinity_bits<T>() | (now > 0.f ? 0u : now < 0.f ? 0x8000u : 0x7fffu));
         }
       }
@@ -1277,7 +1219,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         join(b0, min(kJoin, pieces - mine * kJoin), 1, groups == 1);
         finished = groups == 1;
         unsigned int* count = a.pair_count + ((size_t)e.row * pairs + e.pair) * a.pair_step;
-        if (kMode != kAlone) count = e.of_group ? &record(e.row, e.pair)->group_count : &record(e.row, e.h0)->pair_count;
+        if (kShares) count = e.of_group ? &record(e.row, e.pair)->group_count : &record(e.row, e.h0)->pair_count;
         if (groups > 1 && last_of(count, groups)) {
           join(c0, groups, kJoin, true);
           finished = true;
@@ -1335,7 +1277,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     uint32_t patience = npp::kSpinLimit;
     npp::drain_ring(s_full[wid], kSlots, uses.slot(uses.asked), uses.parity(uses.asked), patience);
   }
-  if (kTail) npp::pdl_wait_prior();
+  if (kMode == kOwn) npp::pdl_wait_prior();
 }
 
 // Heads of a block.  Sixteen read keys and values once for up to sixteen heads, eight have more warps: 64 sequences of 2000 tokens, 64
@@ -1358,7 +1300,7 @@ template <class T, int HD, int kForm, int kMode>
 cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int sms, cudaStream_t s) {
   size_t room = kMode == kAlone ? 0 : GroupRoom(nullptr, kMode == kBoth, a.n, a.shared.n_groups).bytes;
   if (kForm == kSixteen) room += (size_t)kWarps * kSlots * 16 * HD * 4 + 1024;
-  if (kForm == kSixteen || kMode == kBoth) {
+  if (kForm == kSixteen || kMode != kAlone) {
     static std::atomic<uint64_t> done{0};
     const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kForm, kMode>), &done);
     if (e != cudaSuccess) return e;
@@ -1369,7 +1311,7 @@ cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int sms, cudaStr
 template <class T, int HD>
 cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hb, bool held, int mode, int sms, cudaStream_t s) {
   if (held) return hb == 8 ? launch<T, HD, kHeldEight, kAlone>(map, a, sms, s) : launch<T, HD, kHeldSixteen, kAlone>(map, a, sms, s);
-  if (mode == kBehind) return hb == 8 ? launch<T, HD, kEight, kBehind>(map, a, sms, s) : launch<T, HD, kSixteen, kBehind>(map, a, sms, s);
+  if (mode == kOwn) return hb == 8 ? launch<T, HD, kEight, kOwn>(map, a, sms, s) : launch<T, HD, kSixteen, kOwn>(map, a, sms, s);
   if (mode == kBoth) return hb == 8 ? launch<T, HD, kEight, kBoth>(map, a, sms, s) : launch<T, HD, kSixteen, kBoth>(map, a, sms, s);
   return hb == 8 ? launch<T, HD, kEight, kAlone>(map, a, sms, s) : launch<T, HD, kSixteen, kAlone>(map, a, sms, s);
 }
@@ -1432,7 +1374,7 @@ int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_ta
     a.pair_step = sizeof(Record) / 4;
   }
   const bool held = held_in_8(d);
-  const int mode = !shared || shared->n_groups == 0 ? kAlone : shared->together ? kBoth : kBehind;
+  const int mode = !shared || shared->n_groups == 0 ? kAlone : shared->together ? kBoth : kOwn;
   CUtensorMap map = {};
   if (hb == 16 && !held && !make_map(&map, a, d->head_dim)) return fail(NP_E_INVAL, "a cache that a tensor map does not describe");
   cudaError_t e;

@@ -12,10 +12,14 @@ constexpr int kSharedTile = 128;       // tokens of a tile of the first kernel
 constexpr int kSharedBlocks = 320;     // its blocks, at most
 constexpr int kSharedSlotRows = 256;   // rows of a block's partial result, at most
 
-// Of a group: where its tiles begin on the line of work, its first row, and its blocks of rows.
-struct __align__(16) GroupPlan {
-  int64_t first_w;
-  int32_t row0, row_blocks;
+constexpr int kSharedGroups = 512;     // groups that it keeps in mind, at most
+
+// Of a row: where on the line of work its shared tokens' tiles begin, of key-value head 0, and how far it is to the next head's; their number; its
+// first query head's place among the rows of a block's partial result; whether it shares anything, and has tokens of its own.
+struct __align__(32) RowPlan {
+  int64_t first_w, step;
+  int32_t tiles, place;
+  bool shares, own;
 };
 // How the line is dealt out: the first `more` blocks take each + 1 tiles of it, the others each.
 struct __align__(16) LinePlan {
@@ -43,40 +47,37 @@ struct SharedArgs {
   // the two kernels apart: rows of the call in a block of rows, and in each tile of 128 query rows
   int members, tile_members;
   LinePlan* line;
-  GroupPlan* plan;         // [n_groups]
+  RowPlan* plan;           // [n]
   float* part_ml;          // [2 * blocks][rows of a block][2]   of blocks that have not done all of a block of rows' tiles (the others: records)
   float* part_o;           // [2 * blocks][rows of a block][HD]
   int part_rows;
 };
 
-// Rows [lo, hi) of a group.
-__device__ __forceinline__ void group_rows(const SharedArgs& s, int n, int g, int* lo, int* hi) {
-  *lo = min(max(s.cu[g], 0), n);
-  *hi = max(*lo, min(s.cu[g + 1], n));
+// What is known of a group: the tokens that it shares, its rows [lo, hi) of the call, and the sequence whose pages are read for them.
+struct GroupInfo {
+  int tokens;
+  int16_t lo, hi;
+  int seq;
+};
+__device__ __forceinline__ GroupInfo group_at(const SharedArgs& s, int n, int g) {
+  const int lo = min(max(s.cu[g], 0), n), hi = max(lo, min(s.cu[g + 1], n));
+  return GroupInfo{s.tokens[g], (int16_t)lo, (int16_t)hi, -1};
 }
-
-// By a whole warp: the tokens that group g shares; 0 where it has no row with a sequence, or (NP_KV_S_LENGTH) where its rows do not all have
-// that many or they do not fill pages.  *seq: the sequence of its first row that has one.
-__device__ __forceinline__ int group_tokens(const SharedArgs& s, int g, int lo, int hi, const int32_t* seqs, const int32_t* lens, int max_seqs, int max_pages,
-                                            int shift, int32_t* status, int* seq) {
-  const int lane = threadIdx.x & 31, tokens = s.tokens[g];
-  *seq = -1;
-  if (tokens == 0 || lo == hi) return 0;
-  bool good = tokens > 0 && (tokens & ((1 << shift) - 1)) == 0 && (tokens >> shift) <= max_pages;
-  for (int i0 = lo; i0 < hi; i0 += 32) {
-    const int i = i0 + lane, q = i < hi ? (seqs ? seqs[i] : i) : -1;
-    const bool has = q >= 0 && q < max_seqs;
-    if (has) good &= lens[q] >= tokens;
-    const uint32_t all = __ballot_sync(0xffffffffu, has);
-    if (*seq < 0 && all) *seq = __shfl_sync(0xffffffffu, q, __ffs(all) - 1);
+// By a whole warp: the group's sequence is that of its first row that has one; it shares nothing if there is none, or (NP_KV_S_LENGTH) if its rows do
+// not all have that many tokens or they do not fill pages.  Of row i: seqs[i] (-1: none) and lens[i], as the tables say.
+__device__ __forceinline__ void check_group(GroupInfo& x, const int16_t* seqs, const int* lens, int max_pages, int shift, int32_t* status) {
+  const int lane = threadIdx.x & 31;
+  if (x.tokens == 0) return;
+  bool good = x.tokens > 0 && (x.tokens & ((1 << shift) - 1)) == 0 && (x.tokens >> shift) <= max_pages;
+  for (int i0 = x.lo; i0 < x.hi; i0 += 32) {
+    const int i = i0 + lane, seq = i < x.hi ? seqs[i] : -1;
+    if (seq >= 0) good &= lens[i] >= x.tokens;
+    const uint32_t all = __ballot_sync(0xffffffffu, seq >= 0);
+    if (x.seq < 0 && all) x.seq = __shfl_sync(0xffffffffu, seq, __ffs(all) - 1);
   }
   good = __all_sync(0xffffffffu, good);
-  if (*seq < 0) return 0;
-  if (!good) {
-    if (lane == 0) atomicOr(status, NP_KV_S_LENGTH);
-    return 0;
-  }
-  return tokens;
+  if (!good && x.seq >= 0 && lane == 0) atomicOr(status, NP_KV_S_LENGTH);
+  if (!good || x.seq < 0) x.tokens = 0;
 }
 
 __device__ __forceinline__ int64_t divide_up(int64_t a, int b) { return (a + b - 1) / b; }

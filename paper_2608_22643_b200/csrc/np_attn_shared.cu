@@ -73,21 +73,25 @@ struct Piece {
   bool whole;
   const int32_t* pages;
 };
-template <int kTiles>
+// The line of work, in shared memory.
+struct Groups {
+  int64_t end[kSharedGroups];  // tiles of the groups up to and including this one
+  int tokens[kSharedGroups];
+  int16_t lo[kSharedGroups], hi[kSharedGroups], seq[kSharedGroups];
+};
 struct Line {
   const Args& a;
-  const int64_t* ends;  // of the groups
-  int64_t w, end;       // what is left of this block's stretch
+  const Groups& groups;
+  int64_t w, end;  // what is left of this block's stretch
   int g;
-  // by a whole warp; false: nothing is left
+  // false: nothing is left
   __device__ __forceinline__ bool next(Piece& p) {
     if (w >= end) return false;
-    while (ends[g] <= w) ++g;
-    const int64_t first = g ? ends[g - 1] : 0;
-    int lo, hi, seq;
-    group_rows(a.shared, a.n, g, &lo, &hi);
-    p.tokens = group_tokens(a.shared, g, lo, hi, a.seqs, a.lens, a.max_seqs, a.max_pages, a.shift, a.status, &seq);
-    const int tiles = (int)divide_up(p.tokens, kRows), blocks = (hi - lo + a.shared.members - 1) / a.shared.members;
+    while (groups.end[g] <= w) ++g;
+    const int64_t first = g ? groups.end[g - 1] : 0;
+    const int lo = groups.lo[g], hi = groups.hi[g];
+    p.tokens = groups.tokens[g];
+    const int tiles = (p.tokens + kRows - 1) / kRows, blocks = (hi - lo + a.shared.members - 1) / a.shared.members;
     const int64_t item = (w - first) / tiles;
     p.t0 = (int)(w - first - item * tiles);
     p.t1 = (int)min((int64_t)tiles, p.t0 + (end - w));
@@ -96,7 +100,7 @@ struct Line {
     p.kvh = (int)(item / blocks);
     p.row0 = lo + (int)(item - (int64_t)p.kvh * blocks) * a.shared.members;
     p.rows = min(a.shared.members, hi - p.row0);
-    p.pages = a.table + (size_t)seq * a.max_pages;
+    p.pages = a.table + (size_t)groups.seq[g] * a.max_pages;
     return true;
   }
 };
@@ -142,56 +146,12 @@ __global__ void __launch_bounds__(Shape<HD, kTiles>::kThreads, 3 - kTiles)
 k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ Args a) {
   using S = Shape<HD, kTiles>;
   extern __shared__ __align__(1024) unsigned char tsm[];
-  __shared__ int64_t s_end[NP_KV_MAX_SEQS];  // tiles of the groups up to and including this one
+  __shared__ Groups s_groups;
   __shared__ __align__(8) uint64_t full[S::kStages], empty[S::kStages], q_full, q_empty, s_full[kTiles], p_half[kTiles], p_full[kTiles], o_full[kTiles], o_empty[kTiles];
   __shared__ uint32_t s_tmem;
   __shared__ int s_ok;  // 0: a wait has run out
-  npp::pdl_wait_prior();
-  npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int n_groups = a.shared.n_groups;
-
-  // ---- the line of work
-  for (int g = wid; g < n_groups; g += S::kThreads / 32) {
-    int lo, hi, seq;
-    group_rows(a.shared, a.n, g, &lo, &hi);
-    const int tokens = group_tokens(a.shared, g, lo, hi, a.seqs, a.lens, a.max_seqs, a.max_pages, a.shift, a.status, &seq);
-    const int blocks = (hi - lo + a.shared.members - 1) / a.shared.members;
-    if (lane == 0) {
-      s_end[g] = divide_up(tokens, kRows) * blocks * a.n_kv_heads;
-      if (blockIdx.x == 0) {
-        a.shared.plan[g].row0 = lo;
-        a.shared.plan[g].row_blocks = blocks;
-      }
-    }
-  }
-  __syncthreads();
-  if (wid == 0) {
-    int64_t run = 0;
-    for (int g0 = 0; g0 < n_groups; g0 += 32) {
-      const int64_t mine = g0 + lane < n_groups ? s_end[g0 + lane] : 0;
-      int64_t inc = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += up;
-      }
-      if (g0 + lane < n_groups) {
-        s_end[g0 + lane] = run + inc;
-        if (blockIdx.x == 0) a.shared.plan[g0 + lane].first_w = run + inc - mine;
-      }
-      run += __shfl_sync(0xffffffffu, inc, 31);
-    }
-  }
-  __syncthreads();
-  const int64_t W = s_end[n_groups - 1];
-  const int G = (int)min((int64_t)gridDim.x, W);
-  if ((int)blockIdx.x >= G) return;
-  const int64_t each = W / G, more = W - each * G;
-  if (blockIdx.x == 0 && tid == 0) *a.shared.line = LinePlan{each, more};
-  Line<kTiles> line = {a, s_end, blockIdx.x * each + min((int64_t)blockIdx.x, more), 0, 0};
-  line.end = line.w + each + (blockIdx.x < more ? 1 : 0);
-
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tsm) + 1023) & ~(uintptr_t)1023);
   unsigned char* q_sm = base;
   unsigned char* ring = base + kTiles * S::kTileBytes;
@@ -212,6 +172,68 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     npp::fence_barrier_init();
     s_ok = 1;
   }
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+
+  // ---- the line of work.  Rows' sequences and lengths lie where the queries will be.
+  int* const lens = reinterpret_cast<int*>(q_sm);
+  int16_t* const seqs = reinterpret_cast<int16_t*>(q_sm + NP_KV_MAX_SEQS * 4);
+  for (int i = tid; i < a.n; i += S::kThreads) {
+    const int seq = a.seqs ? a.seqs[i] : i;
+    const bool known = seq >= 0 && seq < a.max_seqs;
+    seqs[i] = (int16_t)(known ? seq : -1);
+    lens[i] = known ? a.lens[seq] : 0;
+  }
+  __syncthreads();
+  auto tiles_in = [](int tokens) { return (tokens + kRows - 1) / kRows; };
+  for (int g = wid; g < n_groups; g += S::kThreads / 32) {
+    GroupInfo x = group_at(a.shared, a.n, g);
+    check_group(x, seqs, lens, a.max_pages, a.shift, a.status);
+    if (lane == 0) {
+      s_groups.end[g] = (int64_t)tiles_in(x.tokens) * ((x.hi - x.lo + a.shared.members - 1) / a.shared.members) * a.n_kv_heads;
+      s_groups.tokens[g] = x.tokens;
+      s_groups.lo[g] = x.lo;
+      s_groups.hi[g] = x.hi;
+      s_groups.seq[g] = (int16_t)x.seq;
+    }
+  }
+  __syncthreads();
+  if (wid == 0) {
+    int64_t run = 0;
+    for (int g0 = 0; g0 < n_groups; g0 += 32) {
+      int64_t inc = g0 + lane < n_groups ? s_groups.end[g0 + lane] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+      }
+      if (g0 + lane < n_groups) s_groups.end[g0 + lane] = run + inc;
+      run += __shfl_sync(0xffffffffu, inc, 31);
+    }
+  }
+  __syncthreads();
+  const int64_t W = s_groups.end[n_groups - 1];
+  const int G = (int)min((int64_t)gridDim.x, W);
+  const int64_t each = G ? W / G : 0, more = W - each * G;
+  if (blockIdx.x == 0) {  // for the join
+    if (tid == 0) *a.shared.line = LinePlan{each, more};
+    for (int i = tid; i < a.n; i += S::kThreads) a.shared.plan[i].shares = false;
+    __syncthreads();
+    for (int g = wid; g < n_groups; g += S::kThreads / 32) {
+      const int lo = s_groups.lo[g], tokens = s_groups.tokens[g], tiles = tiles_in(tokens), blocks = (s_groups.hi[g] - lo + a.shared.members - 1) / a.shared.members;
+      if (tokens == 0) continue;
+      for (int i = lo + lane; i < s_groups.hi[g]; i += 32) {
+        const int block = (i - lo) / a.shared.members, in_block = i - lo - block * a.shared.members, tile = in_block / a.shared.tile_members;
+        const bool there = seqs[i] >= 0 && ((int64_t)lens[i] + (1 << a.shift) - 1) >> a.shift <= a.max_pages;  // else its result is an empty row's
+        a.shared.plan[i] = RowPlan{(g ? s_groups.end[g - 1] : 0) + (int64_t)block * tiles, (int64_t)blocks * tiles, tiles,
+                                   tile * kRows + (in_block - tile * a.shared.tile_members) * a.group, there, there && lens[i] > tokens};
+      }
+    }
+  }
+  if ((int)blockIdx.x >= G) return;
+  Line line = {a, s_groups, blockIdx.x * each + min((int64_t)blockIdx.x, more), 0, 0};
+  line.end = line.w + each + (blockIdx.x < more ? 1 : 0);
+  npp::fence_proxy_async();  // copies will write over what the block has read
   if (wid == S::kLoadWarp && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_kv) : "memory");
@@ -503,6 +525,91 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   }
 }
 
+// The parts of rows that share tokens: a thread has four values of a row and query head.  They come from up to a few dozen blocks, a line of the
+// L2 each, so a thread asks for eight at a time; 64 rows of 64 heads, nine blocks: TIME us.
+constexpr int kJoinThreads = 256, kJoinAhead = 8;
+
+template <bool kBf16, int HD>
+__global__ void __launch_bounds__(kJoinThreads)
+k_attn_shared_join(const __grid_constant__ Args a, uint16_t* out, int64_t o_token, int64_t o_head, float* lse) {
+  npp::pdl_wait_prior();
+  npp::pdl_launch_dependents();
+  const int64_t x = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
+  const unsigned at = (unsigned)(x / (HD / 4));  // at most 2^27
+  const int d = (int)(x % (HD / 4)) * 4, i = (int)(at / a.n_heads), h = (int)(at - (unsigned)i * a.n_heads);
+  if (i >= a.n) return;
+  const RowPlan plan = a.shared.plan[i];
+  const LinePlan line = *a.shared.line;
+  if (!plan.shares) return;
+  const Record* const record = a.shared.records + ((int64_t)i * a.n_heads + h);
+  const int kvh = h / a.group, place = plan.place + h - kvh * a.group;
+  const int64_t w = plan.first_w + kvh * plan.step;
+  auto block_of = [&](int64_t y) { return (int)(y < line.more * (line.each + 1) ? y / (line.each + 1) : line.more + (y - line.more * (line.each + 1)) / line.each); };
+  const int c0 = block_of(w), c1 = block_of(w + plan.tiles - 1), parts = c1 - c0 + 1 + plan.own;
+  // the parts: of the blocks, or of the one that has done all shared tokens, and the row's own
+  auto part = [&](int y, const float** ml, const float** o) {
+    if (y == c1 - c0 + 1 || c0 == c1) {
+      const int of = y == c1 - c0 + 1;
+      *ml = record->ml[of];
+      *o = record->o[of] + d;
+    } else {
+      const int64_t slot = (int64_t)(2 * (c0 + y) + (y == 0)) * a.shared.part_rows + place;
+      *ml = a.shared.part_ml + slot * 2;
+      *o = a.shared.part_o + slot * HD + d;
+    }
+  };
+  float top = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int y0 = 0; y0 < parts; y0 += kJoinAhead) {
+    float2 ml[kJoinAhead];
+    float4 v[kJoinAhead];
+#pragma unroll
+    for (int y = 0; y < kJoinAhead; ++y) {
+      ml[y] = make_float2(-INFINITY, 0.f);
+      v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (y0 + y >= parts) continue;
+      const float *pm, *po;
+      part(y0 + y, &pm, &po);
+      ml[y] = __ldcg(reinterpret_cast<const float2*>(pm));
+      v[y] = __ldcg(reinterpret_cast<const float4*>(po));
+    }
+    float now = top;
+#pragma unroll
+    for (int y = 0; y < kJoinAhead; ++y) now = fmaxf(now, ml[y].x);
+    const float use = now == -INFINITY ? 0.f : now, f0 = exp2_fast(top - use);
+    top = now;
+    sum *= f0;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) acc[z] *= f0;
+#pragma unroll
+    for (int y = 0; y < kJoinAhead; ++y) {
+      const float f = exp2_fast(ml[y].x - use);
+      sum += f * ml[y].y;
+      acc[0] += f * v[y].x;
+      acc[1] += f * v[y].y;
+      acc[2] += f * v[y].z;
+      acc[3] += f * v[y].w;
+    }
+  }
+  if (!not_finite(sum) && (not_finite(acc[0]) || not_finite(acc[1]) || not_finite(acc[2]) || not_finite(acc[3]))) {
+    // factors that are 0 make a NaN of an infinity: what is not finite is what the parts that are not add up to
+    for (int z = 0; z < 4; ++z) {
+      float kept = 0.f;
+      for (int y = 0; y < parts; ++y) {
+        const float *pm, *po;
+        part(y, &pm, &po);
+        const float u = __ldcg(po + z);
+        if (not_finite(u)) kept += u;
+      }
+      if (not_finite(kept)) acc[z] = kept;
+    }
+  }
+  const bool none = sum == 0.f;
+  const float inv = none ? 0.f : 1.f / sum;
+  *reinterpret_cast<uint2*>(out + i * o_token + h * o_head + d) =
+      none ? make_uint2(0, 0) : make_uint2(pack<kBf16>(acc[0] * inv, acc[1] * inv), pack<kBf16>(acc[2] * inv, acc[3] * inv));
+  if (lse && d == 0) lse[at] = none ? -INFINITY : (top == -INFINITY ? 0.f : top) * kLn2 + logf(sum);
+}
+
 // A layer of the cache as (64 values, rows of a page's heads, halves of head_dim, keys and values, pages); a box is one half of up to 128
 // rows of a page.
 bool make_map(CUtensorMap* map, const Args& a, int hd) {
@@ -544,7 +651,7 @@ struct Space {
     };
     take(decode_parts_bytes());
     line = take(sizeof(LinePlan));
-    plan = take((uint64_t)NP_KV_MAX_SEQS * sizeof(GroupPlan));
+    plan = take((uint64_t)NP_KV_MAX_SEQS * sizeof(RowPlan));
     part_ml = take((uint64_t)2 * kSharedBlocks * kRows * 8);
     part_o = take((uint64_t)2 * kSharedBlocks * kRows * 128 * 4);
     records = take((uint64_t)n * n_heads * sizeof(Record));
@@ -600,7 +707,7 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   a.shared.n_groups = n_groups;
   a.shared.records = reinterpret_cast<Record*>(ws + space.records);
   a.shared.columns = columns;
-  a.shared.together = columns <= kFewColumns;
+  a.shared.together = columns <= kFewColumns || n_groups > kSharedGroups;
   if (a.shared.together) return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s);
   a.page_bytes = page_bytes(d);
   a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * a.page_bytes;
@@ -622,16 +729,22 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   a.shared.tile_members = tile_members;
   a.shared.members = tiles * tile_members;
   a.shared.line = reinterpret_cast<LinePlan*>(ws + space.line);
-  a.shared.plan = reinterpret_cast<GroupPlan*>(ws + space.plan);
+  a.shared.plan = reinterpret_cast<RowPlan*>(ws + space.plan);
   a.shared.part_ml = reinterpret_cast<float*>(ws + space.part_ml);
   a.shared.part_o = reinterpret_cast<float*>(ws + space.part_o);
   a.shared.part_rows = tiles * kRows;
   CUtensorMap mq, mkv;
   if (!make_rows_map(&mq, *q, d->head_dim, n_heads, n, a.group, tile_members) || !make_map(&mkv, a, d->head_dim))
     return fail(NP_E_INVAL, "rows or a cache that a tensor map does not describe");
-  const cudaError_t e = row_type(d) == NP_T_BF16 ? launch<true>(mq, mkv, a, d->head_dim, tiles, sms, s) : launch<false>(mq, mkv, a, d->head_dim, tiles, sms, s);
+  cudaError_t e = row_type(d) == NP_T_BF16 ? launch<true>(mq, mkv, a, d->head_dim, tiles, sms, s) : launch<false>(mq, mkv, a, d->head_dim, tiles, sms, s);
   if (e != cudaSuccess) return fail_cuda(e);
-  return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s);
+  if (int rc = decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s)) return rc;
+  const dim3 grid((unsigned)(((int64_t)n * n_heads * (d->head_dim / 4) + kJoinThreads - 1) / kJoinThreads));
+  uint16_t* to = static_cast<uint16_t*>(out->data);
+  auto join = [&](auto kernel) { return launch_early(kernel, grid, kJoinThreads, 0, s, a, to, out->token_stride, out->head_stride, lse); };
+  if (row_type(d) == NP_T_BF16) e = d->head_dim == 128 ? join(k_attn_shared_join<true, 128>) : join(k_attn_shared_join<true, 64>);
+  else e = d->head_dim == 128 ? join(k_attn_shared_join<false, 128>) : join(k_attn_shared_join<false, 64>);
+  return e == cudaSuccess ? NP_OK : fail_cuda(e);
 }
 
 }  // extern "C"

@@ -481,8 +481,8 @@ k_kv_compact_small(Pool p, int32_t* refs_out, int32_t* __restrict__ n_live, Copy
   copy_and_rewrite(a, w);
 }
 
-// The tokens in full pages that all rows of a group begin with: a block per group.  Pages are compared a block's threads at a time with those of
-// the group's first sequence, up to the first that differ.
+// The tokens in full pages that all rows of a group begin with: a block per group, a warp per sequence, whose pages are compared with those of the
+// group's first.
 constexpr int kSharedThreads = 512;
 
 __global__ void __launch_bounds__(kSharedThreads)
@@ -516,27 +516,32 @@ k_kv_shared(Pool p, const int32_t* __restrict__ seqs, int n, const int32_t* __re
     s_seq[i - lo] = seq;
   }
   __syncthreads();
-  const int members = hi - lo, first = s_first, full = s_members > 1 ? s_full : 0;
-  int common = full;
-  for (int j0 = 0; j0 < full; j0 += kSharedThreads) {
-    const int j = j0 + tid;
-    bool differs = false;
-    if (j < full) {
-      const int page = p.table[(size_t)s_seq[first] * p.max_pages + j];
-      differs = (unsigned)page >= (unsigned)p.n_pages;
-#pragma unroll 8
-      for (int i = first + 1; i < members; ++i) {
-        const int seq = s_seq[i];
-        differs |= seq >= 0 && p.table[(size_t)seq * p.max_pages + j] != page;
+  const int members = hi - lo, first = s_first, full = s_members > 1 ? s_full : 0, lane = tid & 31, wid = tid >> 5;
+  // a warp takes a sequence at a time, and of its pages what has not been found to differ yet
+  constexpr int kAhead = 4;
+  auto common = [&] { return __shfl_sync(0xffffffffu, *static_cast<volatile int*>(&s_full), 0); };  // the same for all lanes
+  for (int i = first + wid; i < members && full > 0; i += kSharedThreads / 32) {
+    const int seq = s_seq[i];
+    if (seq < 0) continue;
+    const int32_t *mine = p.table + (size_t)seq * p.max_pages, *theirs = p.table + (size_t)s_seq[first] * p.max_pages;
+    for (int j0 = 0; j0 < common(); j0 += 32 * kAhead) {
+      int u[kAhead], v[kAhead];
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        const int j = j0 + 32 * y + lane;
+        u[y] = j < full ? mine[j] : 0;
+        v[y] = j < full ? theirs[j] : 0;
       }
-    }
-    if (differs) atomicMin(&s_full, j);
-    if (__syncthreads_or(differs)) {
-      common = s_full;
-      break;
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        const uint32_t differ = __ballot_sync(0xffffffffu, j0 + 32 * y + lane < full && (u[y] != v[y] || (unsigned)u[y] >= (unsigned)p.n_pages));
+        if (differ && lane == 0) atomicMin(&s_full, j0 + 32 * y + __ffs(differ) - 1);
+      }
+      __syncwarp();
     }
   }
-  if (tid == 0) shared[blockIdx.x] = common << p.shift;
+  __syncthreads();
+  if (tid == 0) shared[blockIdx.x] = (full > 0 ? s_full : 0) << p.shift;
 }
 
 struct AppendArgs {

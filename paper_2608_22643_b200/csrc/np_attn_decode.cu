@@ -63,6 +63,7 @@ constexpr int kMinTiles = 2;
 constexpr int kStart = 2;
 // Partial results that are joined at a time.  The long sequence: 93.0 us; with 4 94.9, 16 99.4 (registers).
 constexpr int kJoin = 8;
+constexpr int kFewTiles = 8;
 constexpr int kMaxBlocks = 640;       // blocks of a launch (the workspace holds two partial results of each)
 
 struct DecodeArgs {
@@ -474,18 +475,27 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = -INFINITY;
     }
   }
+  // Rows' own tokens behind shared ones are often few: where none has more than kFewTiles tiles, a block does a (row, pair) and then the next that is no
+  // other block's, instead of parts of one, which would meet through memory.
+  bool by_pair = false;
+  if constexpr (kMode == kOwn) {
+    bool many = false;
+    for (int i = tid; i < a.n; i += kThreads) many |= s_end[i] - (i ? s_end[i - 1] : 0) > kFewTiles + kUnitsBefore;
+    by_pair = !__syncthreads_or(many);
+  }
+  int64_t next_pair = blockIdx.x;
   // the line's W units over G blocks: the first `more` blocks take each + 1 of them, the others each
   const int per = kTogether ? 1 : pairs;
   const int64_t W = run * per;
-  const int G = (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
+  const int G = by_pair ? (int)gridDim.x : (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
   if ((int)blockIdx.x >= G) {
     if (kMode == kOwn) npp::pdl_wait_prior();
     return;
   }
   const int64_t each = divide(W, G), more = W - each * G;
   auto block_of = [&](int64_t w) { return (int)(w < more * (each + 1) ? divide(w, each + 1) : more + divide(w - more * (each + 1), each)); };
-  int64_t w0 = blockIdx.x * each + min((int64_t)blockIdx.x, more);
-  const int64_t w1 = w0 + each + (blockIdx.x < more ? 1 : 0);
+  int64_t w0 = by_pair ? 0 : blockIdx.x * each + min((int64_t)blockIdx.x, more);
+  const int64_t w1 = by_pair ? W : w0 + each + (blockIdx.x < more ? 1 : 0);
   int row = 0;
   {
     int lo = 0, hi = items - 1;  // the first item whose units end after w0
@@ -513,13 +523,21 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   // the next piece with tokens from w0 on; false: none is left
   auto next_piece = [&](Piece& p) {
     while (w0 < w1) {
+      if (kMode == kOwn && by_pair) {
+        if (next_pair >= (int64_t)a.n * pairs) return false;
+        row = (int)(next_pair / pairs);
+        const int64_t from = row ? s_end[row - 1] : 0, each_pair = s_end[row] - from;
+        w0 = from * pairs + (next_pair - (int64_t)row * pairs) * each_pair;
+        next_pair += gridDim.x;
+        if (each_pair == 0) continue;
+      }
       while (s_end[row] * per <= w0) ++row;
       p.of_group = kTogether && row < n_groups;
       const GroupInfo of = p.of_group ? room.info[row] : GroupInfo{};
       const int64_t before = row ? s_end[row - 1] : 0, r0 = w0 - before * per;
       const int64_t units = !kTogether ? s_end[row] - before : divide(s_end[row] - before, p.of_group ? a.n_kv_heads * column_blocks(of) : pairs);
       const int pair = (int)divide(r0, units);
-      const int64_t ra = r0 - pair * units, rb = min(units, ra + (w1 - w0));
+      const int64_t ra = r0 - pair * units, rb = by_pair ? units : min(units, ra + (w1 - w0));
       p.first_w = w0 - ra;
       w0 += rb - ra;
       p.ta = (int)max((int64_t)0, ra - kUnitsBefore);

@@ -184,16 +184,21 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     seqs[i] = (int16_t)(known ? seq : -1);
     lens[i] = known ? a.lens[seq] : 0;
   }
+  for (int g = tid; g < n_groups; g += S::kThreads) {
+    const GroupInfo x = group_at(a.shared, a.n, g);
+    s_groups.tokens[g] = x.tokens;
+    s_groups.lo[g] = x.lo;
+    s_groups.hi[g] = x.hi;
+  }
   __syncthreads();
   auto tiles_in = [](int tokens) { return (tokens + kRows - 1) / kRows; };
   for (int g = wid; g < n_groups; g += S::kThreads / 32) {
-    GroupInfo x = group_at(a.shared, a.n, g);
+    GroupInfo x = {s_groups.tokens[g], s_groups.lo[g], s_groups.hi[g], -1};
     check_group(x, seqs, lens, a.max_pages, a.shift, a.status);
+    __syncwarp();
     if (lane == 0) {
       s_groups.end[g] = (int64_t)tiles_in(x.tokens) * ((x.hi - x.lo + a.shared.members - 1) / a.shared.members) * a.n_kv_heads;
       s_groups.tokens[g] = x.tokens;
-      s_groups.lo[g] = x.lo;
-      s_groups.hi[g] = x.hi;
       s_groups.seq[g] = (int16_t)x.seq;
     }
   }

@@ -487,11 +487,16 @@ constexpr int kSharedThreads = 512;
 
 __global__ void __launch_bounds__(kSharedThreads)
 k_kv_shared(Pool p, const int32_t* __restrict__ seqs, int n, const int32_t* __restrict__ cu, int32_t* __restrict__ shared) {
-  __shared__ int s_seq[NP_KV_MAX_SEQS];
+  __shared__ int s_seq[NP_KV_MAX_SEQS], s_len[NP_KV_MAX_SEQS];
   __shared__ int s_full, s_members, s_first;
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x;
+  for (int i = tid; i < n; i += kSharedThreads) {  // all rows of the call, beside the group's place among them
+    const int seq = seqs ? seqs[i] : i;
+    s_seq[i] = seq;
+    s_len[i] = seq >= 0 && seq < p.max_seqs ? p.lens[seq] : 0;
+  }
   const int lo = min(max(cu[blockIdx.x], 0), n), hi = max(lo, min(cu[blockIdx.x + 1], n));
   if (tid == 0) {
     s_full = p.max_pages;
@@ -500,27 +505,24 @@ k_kv_shared(Pool p, const int32_t* __restrict__ seqs, int n, const int32_t* __re
   }
   __syncthreads();
   for (int i = lo + tid; i < hi; i += kSharedThreads) {
-    int seq = seqs ? seqs[i] : i, full = 0;
+    const int seq = s_seq[i];
     if (seq >= p.max_seqs) {
-      seq = -1;
       atomicOr(p.status, NP_KV_S_SEQ);
-    }
-    if (seq >= 0) {
-      const int len = p.lens[seq];
-      if (pages_of(p, len) < 0) atomicOr(p.status, NP_KV_S_LENGTH);
-      else full = len >> p.shift;
-      atomicMin(&s_full, full);
+      s_seq[i] = -1;
+    } else if (seq >= 0) {
+      const bool fits = pages_of(p, s_len[i]) >= 0;
+      if (!fits) atomicOr(p.status, NP_KV_S_LENGTH);
+      atomicMin(&s_full, fits ? s_len[i] >> p.shift : 0);
       atomicAdd(&s_members, 1);
-      atomicMin(&s_first, i - lo);
+      atomicMin(&s_first, i);
     }
-    s_seq[i - lo] = seq;
   }
   __syncthreads();
-  const int members = hi - lo, first = s_first, full = s_members > 1 ? s_full : 0, lane = tid & 31, wid = tid >> 5;
+  const int first = s_first, full = s_members > 1 ? s_full : 0, lane = tid & 31, wid = tid >> 5;
   // a warp takes a sequence at a time, and of its pages what has not been found to differ yet
   constexpr int kAhead = 4;
   auto common = [&] { return __shfl_sync(0xffffffffu, *static_cast<volatile int*>(&s_full), 0); };  // the same for all lanes
-  for (int i = first + wid; i < members && full > 0; i += kSharedThreads / 32) {
+  for (int i = first + wid; i < hi && full > 0; i += kSharedThreads / 32) {
     const int seq = s_seq[i];
     if (seq < 0) continue;
     const int32_t *mine = p.table + (size_t)seq * p.max_pages, *theirs = p.table + (size_t)s_seq[first] * p.max_pages;

@@ -138,7 +138,12 @@ def test_a_group_that_is_longer_than_its_sequences_of_another():
 
 def test_shared_pages_that_are_not_there():
     """A page number outside the pool among the shared ones: its tokens are not seen by any row."""
-    c, seqs, cu = _branches(BF, 2, 64, 16, [400], [[20, 0, 4]])
+    for ways in (3, 40):
+        _shared_pages_that_are_not_there(ways)
+
+
+def _shared_pages_that_are_not_there(ways):
+    c, seqs, cu = _branches(BF, 2, 64, 16, [400], [[20, 0, 4] + [1] * (ways - 3)])
     kept = {s: c.tokens(0, s) for s in seqs}
     c.table[:, 3] = c.desc.n_pages
     c.table[:, 20] = -1
@@ -177,12 +182,38 @@ def test_values_that_are_not_finite(dtype):
     assert (out[4] == 0).all() and (lse[4] == -float("inf")).all()
 
 
+@pytest.mark.parametrize("ways,hq", [(3, 2), (40, 2), (6, 8)])
+def test_infinities_among_shared_and_own_values(ways, hq):
+    """Small groups and large ones: an infinity of either kind of token stays one however small its weight, two of different signs make a NaN."""
+    c, seqs, cu = _branches(BF, 1, 64, 16, [800], [[20, 300] + [1] * (ways - 2)])
+    inf = float("inf")
+    pages, own = c.pool.pages[0], c.pool.pages[1][50:]
+    c.cache[0, pages[2], 1, 0, 5, 10] = inf
+    c.cache[0, pages[3], 1, 0, 5, 11] = -inf
+    c.cache[0, own[1], 1, 0, 3, 10] = -inf
+    c.cache[0, own[1], 1, 0, 3, 11] = -inf
+    c.cache[0, own[2], 1, 0, 3, 12] = inf
+    c.cache[0, own[0], 1, 0, 3, 13] = float("nan")
+    c.cache[0, pages[2:4], 0] *= 0.01                          # small weights beside large ones
+    q = (torch.randn(ways, hq, 64, device="cuda") * 12).to(BF)
+    out, lse = torch.empty_like(q), torch.empty(ways, hq, device="cuda")
+    nb.np_attn_decode_shared(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, hq, ways), c.dev(cu), c.dev([800]), seqs=c.dev(seqs), lse=lse)
+    torch.cuda.synchronize()
+    o = out.float()
+    others = [i for i in range(ways) if i != 1]
+    assert (o[others, :, 10] == inf).all() and (o[others, :, 11] == -inf).all()
+    assert torch.isnan(o[1, :, 10]).all() and (o[1, :, 11] == -inf).all() and (o[1, :, 12] == inf).all() and torch.isnan(o[1, :, 13]).all()
+    fine = [d for d in range(64) if d not in (10, 11, 12, 13)]
+    assert torch.isfinite(o[..., fine]).all() and torch.isfinite(o[others][..., 12:14]).all() and torch.isfinite(lse).all()
+
+
 def test_peaked_scores():
     """Scores that differ by hundreds, within the prefix and between it and the own tokens."""
-    c, seqs, cu = _branches(BF, 2, 128, 32, [1500], [[40, 300, 0, 7]])
-    _run(c, 16, seqs, cu, c.dev([1472]), spread=15.0)
-    c.cache[0, c.pool.pages[0][:30], 0] *= 0.01
-    _run(c, 16, seqs, cu, c.dev([1472]), spread=20.0)
+    for hq in (2, 16):
+        c, seqs, cu = _branches(BF, 2, 128, 32, [1500], [[40, 300, 0, 7]])
+        _run(c, hq, seqs, cu, c.dev([1472]), spread=15.0)
+        c.cache[0, c.pool.pages[0][:30], 0] *= 0.01
+        _run(c, hq, seqs, cu, c.dev([1472]), spread=20.0)
 
 
 def test_prefix_past_32_bit_offsets():

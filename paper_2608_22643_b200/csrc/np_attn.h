@@ -70,6 +70,9 @@ int append_held(const np_kv_desc* d, void* cache, int32_t layer, const np_kv_tab
 struct SharedArgs;
 int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads, const int32_t* seqs,
            int32_t n, float scale2, const np_rows* out, float* lse, void* workspace, const SharedArgs* shared, int sms, cudaStream_t s);
+// The rows' own tokens behind shared ones, and the join (np_attn_rest.cu).  cache: of the layer.
+int decode_rest(const np_kv_desc* d, const char* cache, const np_kv_tables* t, const np_rows* q, int32_t n_heads, const int32_t* seqs, int32_t n, float scale2,
+                const np_rows* out, float* lse, const SharedArgs& shared, int sms, cudaStream_t s);
 uint64_t decode_parts_bytes();  // of the workspace's first part, the same for all calls
 const char* decode_heads_error(const np_kv_desc* d, int n_heads, int n);
 const char* decode_error(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tables* t, const np_rows* q, int32_t n_heads, int32_t n,

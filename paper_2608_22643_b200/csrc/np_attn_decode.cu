@@ -37,15 +37,11 @@
 // between a warp's loads: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, 53.8 us, 74 % (69 % with keys and values
 // in registers, 55 % with 16-byte asynchronous copies in place of TMA, 70 % with the chunks beyond asked into the L2 ahead, 74 % with
 // keys and values as two copies).
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <algorithm>
-#include <cmath>
-#include <type_traits>
 
 #include "np_attn.h"
 #include "np_attn_groups.cuh"
+#include "np_attn_mma.cuh"
 #include "np_device.cuh"
 #include "np_internal.h"
 #include "np_pipe.cuh"
@@ -63,7 +59,6 @@ constexpr int kMinTiles = 2;
 constexpr int kStart = 2;
 // Partial results that are joined at a time.  The long sequence: 93.0 us; with 4 94.9, 16 99.4 (registers).
 constexpr int kJoin = 8;
-constexpr int kFewTiles = 8;
 constexpr int kMaxBlocks = 640;       // blocks of a launch (the workspace holds two partial results of each)
 
 struct DecodeArgs {
@@ -85,61 +80,12 @@ struct DecodeArgs {
   int n, n_heads, n_kv_heads, group, blocks_of_heads;  // heads of a group: blocks_of_heads pieces of HB
   int shift, n_pages, max_seqs, max_pages;
   int64_t page_bytes;
-  SharedArgs shared;  // not kAlone: what groups of rows share
+  SharedArgs shared;  // kTogether: what groups of rows share
 };
 
 // How keys and values get to the products: in the rows' type, up to eight or sixteen heads of a group at once; in 8 bits, the same.
 enum Form { kEight, kSixteen, kHeldEight, kHeldSixteen };
-// What is computed: rows by themselves; what rows have behind the tokens that their group shares, which is left for a join; rows and what their
-// groups share, of which the last part to arrive is joined to the others.
-enum Mode { kAlone, kOwn, kBoth };
 
-template <class T>
-struct Half2;
-template <>
-struct Half2<__nv_bfloat16> {
-  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-  // (x, y) rounded, and what the rounding left, rounded
-  static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-    const float2 f = __bfloat1622float2(h);
-    const __nv_bfloat162 l = __floats2bfloat162_rn(x - f.x, y - f.y);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
-  }
-  static __device__ __forceinline__ uint16_t round(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
-};
-template <>
-struct Half2<__half> {
-  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-  static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
-    const __half2 h = __floats2half2_rn(x, y);
-    const float2 f = __half22float2(h);
-    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
-  }
-  static __device__ __forceinline__ uint16_t round(float x) { return __half_as_ushort(__float2half_rn(x)); }
-};
-
-__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
-  uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // Four 8 x 8 tiles of 16-bit values; lane 8 i + j has the address of row j of tile i.
 __device__ __forceinline__ void load_tiles(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -166,7 +112,6 @@ __device__ __forceinline__ void tma_load_chunk(uint32_t dst, const CUtensorMap* 
                "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(page), "r"(npp::smem_addr(bar))
                : "memory");
 }
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // 16 or 8 bytes that are used once
 __device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[4]) {
@@ -178,11 +123,6 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[4]) {
 }
 __device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[2]) {
   asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-}
-
-// a / b, by 32 bits where they do
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
-  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
 // Tokens of row i of the call; 0 where there are none to read.
@@ -200,55 +140,6 @@ __device__ __forceinline__ int row_len(const DecodeArgs& a, int i, int* seq_out)
     return 0;
   }
   return len;
-}
-
-template <class T>
-__device__ __forceinline__ constexpr uint32_t infinity_bits() {
-  return std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
-}
-__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
-
-// By a whole block: what values that are not finite there are among V's of tokens [ta * kTile, len) of a piece, for each of head_dim (bit 0 a NaN, 8
-// inf, 16 -inf).  Weights are above 0, so an infinity stays one, and two of different signs or a NaN make a NaN; what the sums made of finite values
-// stays.  V is looked through once for all heads, eight values to a thread.  seen: HD ints of shared memory that are free.  One of 131071 tokens a
-// NaN, 64 heads over 8: 201 us a call in place of 93. (One block that looks through all of V behind the join: 10 ms.)
-template <class T, int HD>
-__device__ __noinline__ void look_through(const DecodeArgs& a, const int32_t* pages, int kvh, int ta, int64_t len, int* seen) {
-  constexpr int kCols = HD / 8, kStep = kThreads / kCols, kAhead = 4;
-  constexpr uint32_t kInf = infinity_bits<T>();
-  const int tid = threadIdx.x;
-  for (int d = tid; d < HD; d += kThreads) seen[d] = 0;
-  __syncthreads();
-  const int col = tid % kCols;
-  const int64_t head_bytes = (int64_t)(HD * 2) << a.shift;
-  const char* v = a.cache + (a.n_kv_heads + kvh) * head_bytes + col * 16;
-  uint32_t bits = 0;  // value x of the column: 1 << x a NaN, 256 << x inf, 65536 << x -inf
-  for (int64_t j0 = (int64_t)ta * kTile + tid / kCols; j0 < len; j0 += kAhead * kStep) {
-    int pg[kAhead];
-    uint4 w[kAhead];
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y) pg[y] = j0 + y * kStep < len ? pages[(j0 + y * kStep) >> a.shift] : -1;
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y) {
-      w[y] = make_uint4(0, 0, 0, 0);
-      if ((unsigned)pg[y] < (unsigned)a.n_pages)
-        w[y] = npd::ldg_stream(v + (int64_t)pg[y] * 2 * a.n_kv_heads * head_bytes + ((j0 + y * kStep) & ((1 << a.shift) - 1)) * (HD * 2));
-    }
-#pragma unroll
-    for (int y = 0; y < kAhead; ++y)
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const uint32_t b = word(w[y], x >> 1) >> (x & 1) * 16 & 0xffffu;
-        if ((b & kInf) == kInf) bits |= (b & 0x7fffu) != kInf ? 1u << x : b == kInf ? 256u << x : 65536u << x;
-      }
-  }
-  for (int x = 0; bits && x < 8; ++x)
-    if (const int what = bits >> x & 0x10101) atomicOr(&seen[col * 8 + x], what);
-  __syncthreads();
-}
-// What a result that such values go into is, as fp32; 0: as it was.
-__device__ __forceinline__ float made_of(int seen) {
-  return seen == 0 ? 0.f : seen == 0x100 ? INFINITY : seen == 0x10000 ? -INFINITY : __uint_as_float(0x7fffffffu);
 }
 
 // Four values of joined partial results that are not finite: factors that are 0 make a NaN of an infinity, so they are what the partial results
@@ -284,22 +175,22 @@ constexpr int blocks_per_sm(int hd, int form) {
 // In 8 bits sums are of 2^(s - m + kHeldShift): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.
 constexpr float kHeldShift = 30.f, kHeldUp = 0x1p30f;
 
-// What a block knows of groups, in dynamic shared memory: for each row its tokens, how many of them it shares, its group and sequence; kBoth: the
-// units of groups and rows.
+// What a block knows of groups, in dynamic shared memory: for each row its tokens, how many of them it shares, its group and sequence; and the units of
+// groups and rows.
 struct GroupRoom {
   int64_t* end;
   int *len, *first;
   GroupInfo* info;
   int16_t *group, *seq;
   uint32_t bytes;
-  __host__ __device__ GroupRoom(unsigned char* base, bool both, int n, int n_groups) {
+  __host__ __device__ GroupRoom(unsigned char* base, int n, int n_groups) {
     uint32_t at = 0;
     auto take = [&](uint32_t size) {
       unsigned char* p = base + at;
       at += (size + 15) & ~15u;
       return p;
     };
-    end = reinterpret_cast<int64_t*>(take(both ? (n + n_groups) * 8 : 0));
+    end = reinterpret_cast<int64_t*>(take((n + n_groups) * 8));
     len = reinterpret_cast<int*>(take(n * 4));
     first = reinterpret_cast<int*>(take(n * 4));
     info = reinterpret_cast<GroupInfo*>(take(n_groups * sizeof(GroupInfo)));
@@ -322,10 +213,11 @@ struct WarpWaits {
   }
 };
 
-template <class T, int HD, int kForm, int kMode>
+// kTogether: groups' shared tokens are items of work beside the rows, whose own begin behind them; the last part of a row to arrive is joined to the
+// others.
+template <class T, int HD, int kForm, bool kTogether>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(HD, kForm))
 k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
-  constexpr bool kShares = kMode != kAlone, kTogether = kMode == kBoth;
   constexpr bool kWide = kForm == kSixteen, kHeld = kForm == kHeldEight || kForm == kHeldSixteen;
   constexpr int HB = kForm == kSixteen || kForm == kHeldSixteen ? 16 : 8;  // heads of a block, at most
   constexpr int NT = HB / 8, NH = kHeld ? 2 * NT : 2;  // in 8 bits: eights of heads; heads of a lane's scores
@@ -354,7 +246,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   __shared__ volatile int s_lost[kWarps];  // a wait of the warp was given up
   __shared__ int s_done[kTogether ? HB : 1];
   const int n_groups = kTogether ? a.shared.n_groups : 0, items = n_groups + a.n;  // items: groups, then rows
-  const GroupRoom room(s_dyn, kTogether, a.n, kShares ? a.shared.n_groups : 0);
+  const GroupRoom room(s_dyn, kTogether ? a.n : 0, n_groups);
   int64_t* const s_end = kTogether ? room.end : s_ends;  // units of the items up to and including this one
   if (kWide && (threadIdx.x & 31) == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
@@ -362,14 +254,12 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     s_lost[threadIdx.x >> 5] = 0;
     npp::fence_barrier_init();
   }
-  // The kernel of the shared tokens lets this one begin when all that came before it is done, and has nothing that this one needs; but what comes
-  // next waits for this one alone, so every block waits for that kernel before it leaves.
-  if (kMode != kOwn) npp::pdl_wait_prior();
+  npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
   const int pairs = a.n_kv_heads * a.blocks_of_heads;   // (key-value head, block of its query heads)
 
-  if constexpr (kShares) {
+  if constexpr (kTogether) {
     for (int i = tid; i < a.n; i += kThreads) {
       int seq;
       const int len = row_len(a, i, &seq);
@@ -400,7 +290,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   }
   // tokens of row i of the call that are its own
   auto own_len = [&](int i, int* seq) {
-    if (!kShares) return row_len(a, i, seq);
+    if (!kTogether) return row_len(a, i, seq);
     *seq = room.seq[i];
     return room.len[i] - room.first[i];
   };
@@ -468,34 +358,22 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   auto record = [&](int64_t i, int h) { return a.shared.records + (i * a.n_heads + h); };
   for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
     if (s_end[n_groups + i] != (n_groups + i ? s_end[n_groups + i - 1] : 0)) continue;
-    if (kShares && room.first[i] > 0) continue;  // all of its tokens are shared
+    if (kTogether && room.first[i] > 0) continue;  // all of its tokens are shared
     for (int e = tid; e < a.n_heads * (HD / 8); e += kThreads) {
       const int h = e / (HD / 8), d = e % (HD / 8) * 8;
       *reinterpret_cast<uint4*>(a.out + i * a.o_token + h * a.o_head + d) = make_uint4(0, 0, 0, 0);
       if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = -INFINITY;
     }
   }
-  // Rows' own tokens behind shared ones are often few: where none has more than kFewTiles tiles, a block does a (row, pair) and then the next that is no
-  // other block's, instead of parts of one, which would meet through memory.
-  bool by_pair = false;
-  if constexpr (kMode == kOwn) {
-    bool many = false;
-    for (int i = tid; i < a.n; i += kThreads) many |= s_end[i] - (i ? s_end[i - 1] : 0) > kFewTiles + kUnitsBefore;
-    by_pair = !__syncthreads_or(many);
-  }
-  int64_t next_pair = blockIdx.x;
   // the line's W units over G blocks: the first `more` blocks take each + 1 of them, the others each
   const int per = kTogether ? 1 : pairs;
   const int64_t W = run * per;
-  const int G = by_pair ? (int)gridDim.x : (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
-  if ((int)blockIdx.x >= G) {
-    if (kMode == kOwn) npp::pdl_wait_prior();
-    return;
-  }
+  const int G = (int)min((int64_t)gridDim.x, (W + kMinTiles - 1) / kMinTiles);
+  if ((int)blockIdx.x >= G) return;
   const int64_t each = divide(W, G), more = W - each * G;
   auto block_of = [&](int64_t w) { return (int)(w < more * (each + 1) ? divide(w, each + 1) : more + divide(w - more * (each + 1), each)); };
-  int64_t w0 = by_pair ? 0 : blockIdx.x * each + min((int64_t)blockIdx.x, more);
-  const int64_t w1 = by_pair ? W : w0 + each + (blockIdx.x < more ? 1 : 0);
+  int64_t w0 = blockIdx.x * each + min((int64_t)blockIdx.x, more);
+  const int64_t w1 = w0 + each + (blockIdx.x < more ? 1 : 0);
   int row = 0;
   {
     int lo = 0, hi = items - 1;  // the first item whose units end after w0
@@ -523,21 +401,13 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   // the next piece with tokens from w0 on; false: none is left
   auto next_piece = [&](Piece& p) {
     while (w0 < w1) {
-      if (kMode == kOwn && by_pair) {
-        if (next_pair >= (int64_t)a.n * pairs) return false;
-        row = (int)(next_pair / pairs);
-        const int64_t from = row ? s_end[row - 1] : 0, each_pair = s_end[row] - from;
-        w0 = from * pairs + (next_pair - (int64_t)row * pairs) * each_pair;
-        next_pair += gridDim.x;
-        if (each_pair == 0) continue;
-      }
       while (s_end[row] * per <= w0) ++row;
       p.of_group = kTogether && row < n_groups;
       const GroupInfo of = p.of_group ? room.info[row] : GroupInfo{};
       const int64_t before = row ? s_end[row - 1] : 0, r0 = w0 - before * per;
       const int64_t units = !kTogether ? s_end[row] - before : divide(s_end[row] - before, p.of_group ? a.n_kv_heads * column_blocks(of) : pairs);
       const int pair = (int)divide(r0, units);
-      const int64_t ra = r0 - pair * units, rb = by_pair ? units : min(units, ra + (w1 - w0));
+      const int64_t ra = r0 - pair * units, rb = min(units, ra + (w1 - w0));
       p.first_w = w0 - ra;
       w0 += rb - ra;
       p.ta = (int)max((int64_t)0, ra - kUnitsBefore);
@@ -561,7 +431,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         const int hb = pair - kvh * a.blocks_of_heads;
         p.h0 = kvh * a.group + hb * HB;
         p.heads = min(HB, a.group - hb * HB);
-        p.pages = a.table + (size_t)seq * a.max_pages + (kShares ? room.first[p.row] >> a.shift : 0);
+        p.pages = a.table + (size_t)seq * a.max_pages + (kTogether ? room.first[p.row] >> a.shift : 0);
       }
       p.kvh = kvh;
       p.first_row = kvh << a.shift;
@@ -588,7 +458,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   int waiting[kSlots];                 // tokens of the chunks in this warp's ring
   npp::WarpRing<kSlots> uses;
   WarpWaits waits = {&s_lost[wid], a.status};
-  const uint32_t ring = ((npp::smem_addr(s_dyn) + (kShares ? room.bytes : 0u) + 1023) & ~1023u) + wid * kSlots * kSlot;
+  const uint32_t ring = ((npp::smem_addr(s_dyn) + (kTogether ? room.bytes : 0u) + 1023) & ~1023u) + wid * kSlots * kSlot;
   // what a lane reads with load_tiles: rows (tokens) 0-7 and 8-15 of two neighbouring 16-byte columns, 128-byte swizzle
   const uint32_t lane_row = ((lane & 7) + (lane >> 4) * 8) * 128, lane_col = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
   auto tiles_at = [&](uint32_t base, int step) { return base + lane_row + (step >> 2) * 2048 + (((step & 3) << 5) ^ lane_col); };
@@ -1099,14 +969,14 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     __syncthreads();
     if (any) keep_queries();
     const bool whole = e.ta == 0 && e.tb == e.tiles;
-    const bool meets = kShares && (e.of_group || room.first[e.row] > 0);  // its result is a part
+    const bool meets = kTogether && (e.of_group || room.first[e.row] > 0);  // its result is a part
     auto record_of = [&](int h) {
       if (!e.of_group) return record(e.row, e.h0 + h);
       const int at = e.h0 + h, member = at / a.group;
       return record(e.row + member, e.kvh * a.group + at - member * a.group);
     };
     auto emit = [&](int h, int d, float4 acc, float top, float sum) {
-      if (kShares && meets) {
+      if (kTogether && meets) {
         Record* r = record_of(h);
         const int part = e.of_group ? 0 : 1;
         __stcg(reinterpret_cast<float4*>(&r->o[part][d]), sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : acc);
@@ -1151,9 +1021,10 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         len = of.tokens;
       } else {
         len = own_len(e.row, &seq);
-        if (kShares) from = room.first[e.row];
+        if (kTogether) from = room.first[e.row];
       }
-      look_through<T, HD>(a, a.table + (size_t)seq * a.max_pages + (from >> a.shift), kTogether ? e.kvh : e.pair / a.blocks_of_heads, e.ta,
+      look_through<T, HD>(Layer{a.cache, a.n_kv_heads, a.shift, a.n_pages}, a.table + (size_t)seq * a.max_pages + (from >> a.shift),
+                          kTogether ? e.kvh : e.pair / a.blocks_of_heads, (int64_t)e.ta * kTile,
                           min((int64_t)len, (int64_t)e.tb * kTile), seen);
       for (int x = tid; odd && x < e.heads * (HD / 4); x += kThreads, odd >>= 1) {
         if (!(odd & 1u)) continue;
@@ -1162,7 +1033,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
           const float now = made_of(seen[i]);
           if (now == 0.f) continue;
           if (!whole) __stcg(&a.part_o[((size_t)slot * HB + h) * HD + i], now);
-          else if (kShares && meets) __stcg(&record_of(h)->o[e.of_group ? 0 : 1][i], now);
+          else if (kTogether && meets) __stcg(&record_of(h)->o[e.of_group ? 0 : 1][i], now);
           else a.out[e.row * a.o_token + (int64_t)(e.h0 + h) * a.o_head + i] = (uint16_t)(infinity_bits<T>() | (now > 0.f ? 0u : now < 0.f ? 0x8000u : 0x7fffu));
         }
       }
@@ -1237,7 +1108,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         join(b0, min(kJoin, pieces - mine * kJoin), 1, groups == 1);
         finished = groups == 1;
         unsigned int* count = a.pair_count + ((size_t)e.row * pairs + e.pair) * a.pair_step;
-        if (kShares) count = e.of_group ? &record(e.row, e.pair)->group_count : &record(e.row, e.h0)->pair_count;
+        if (kTogether) count = e.of_group ? &record(e.row, e.pair)->group_count : &record(e.row, e.h0)->pair_count;
         if (groups > 1 && last_of(count, groups)) {
           join(c0, groups, kJoin, true);
           finished = true;
@@ -1295,7 +1166,6 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     uint32_t patience = npp::kSpinLimit;
     npp::drain_ring(s_full[wid], kSlots, uses.slot(uses.asked), uses.parity(uses.asked), patience);
   }
-  if (kMode == kOwn) npp::pdl_wait_prior();
 }
 
 // Heads of a block.  Sixteen read keys and values once for up to sixteen heads, eight have more warps: 64 sequences of 2000 tokens, 64
@@ -1314,24 +1184,23 @@ bool make_map(CUtensorMap* map, const DecodeArgs& a, int hd) {
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class T, int HD, int kForm, int kMode>
+template <class T, int HD, int kForm, bool kTogether>
 cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int sms, cudaStream_t s) {
-  size_t room = kMode == kAlone ? 0 : GroupRoom(nullptr, kMode == kBoth, a.n, a.shared.n_groups).bytes;
+  size_t room = kTogether ? GroupRoom(nullptr, a.n, a.shared.n_groups).bytes : 0;
   if (kForm == kSixteen) room += (size_t)kWarps * kSlots * 16 * HD * 4 + 1024;
-  if (kForm == kSixteen || kMode != kAlone) {
+  if (kForm == kSixteen || kTogether) {
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kForm, kMode>), &done);
+    const cudaError_t e = npi::allow_shared(reinterpret_cast<const void*>(k_attn_decode<T, HD, kForm, kTogether>), &done);
     if (e != cudaSuccess) return e;
   }
   const dim3 grid(std::min(kMaxBlocks, blocks_per_sm(HD, kForm) * sms));
-  return launch_early(k_attn_decode<T, HD, kForm, kMode>, grid, kThreads, room, s, map, a);
+  return launch_early(k_attn_decode<T, HD, kForm, kTogether>, grid, kThreads, room, s, map, a);
 }
 template <class T, int HD>
-cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hb, bool held, int mode, int sms, cudaStream_t s) {
-  if (held) return hb == 8 ? launch<T, HD, kHeldEight, kAlone>(map, a, sms, s) : launch<T, HD, kHeldSixteen, kAlone>(map, a, sms, s);
-  if (mode == kOwn) return hb == 8 ? launch<T, HD, kEight, kOwn>(map, a, sms, s) : launch<T, HD, kSixteen, kOwn>(map, a, sms, s);
-  if (mode == kBoth) return hb == 8 ? launch<T, HD, kEight, kBoth>(map, a, sms, s) : launch<T, HD, kSixteen, kBoth>(map, a, sms, s);
-  return hb == 8 ? launch<T, HD, kEight, kAlone>(map, a, sms, s) : launch<T, HD, kSixteen, kAlone>(map, a, sms, s);
+cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int hb, bool held, bool together, int sms, cudaStream_t s) {
+  if (held) return hb == 8 ? launch<T, HD, kHeldEight, false>(map, a, sms, s) : launch<T, HD, kHeldSixteen, false>(map, a, sms, s);
+  if (together) return hb == 8 ? launch<T, HD, kEight, true>(map, a, sms, s) : launch<T, HD, kSixteen, true>(map, a, sms, s);
+  return hb == 8 ? launch<T, HD, kEight, false>(map, a, sms, s) : launch<T, HD, kSixteen, false>(map, a, sms, s);
 }
 
 // [(m, l) of the partial results][their O][counts]: the counts start at the same place for every description and n, and the
@@ -1373,7 +1242,7 @@ int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_ta
   a.n_heads = n_heads;
   a.n_kv_heads = d->n_kv_heads;
   a.group = n_heads / d->n_kv_heads;
-  const int hb = heads_per_block(shared && shared->n_groups && shared->together ? std::max(a.group, shared->columns) : a.group);
+  const int hb = heads_per_block(shared && shared->n_groups > 0 ? std::max(a.group, shared->columns) : a.group);
   a.blocks_of_heads = (a.group + hb - 1) / hb;
   a.scale2 = scale2;
   a.shift = log2_of(d->page_tokens);
@@ -1392,12 +1261,12 @@ int decode(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_ta
     a.pair_step = sizeof(Record) / 4;
   }
   const bool held = held_in_8(d);
-  const int mode = !shared || shared->n_groups == 0 ? kAlone : shared->together ? kBoth : kOwn;
+  const bool together = shared && shared->n_groups > 0;
   CUtensorMap map = {};
   if (hb == 16 && !held && !make_map(&map, a, d->head_dim)) return fail(NP_E_INVAL, "a cache that a tensor map does not describe");
   cudaError_t e;
-  if (row_type(d) == NP_T_BF16) e = d->head_dim == 128 ? launch<__nv_bfloat16, 128>(map, a, hb, held, mode, sms, s) : launch<__nv_bfloat16, 64>(map, a, hb, held, mode, sms, s);
-  else e = d->head_dim == 128 ? launch<__half, 128>(map, a, hb, held, mode, sms, s) : launch<__half, 64>(map, a, hb, held, mode, sms, s);
+  if (row_type(d) == NP_T_BF16) e = d->head_dim == 128 ? launch<__nv_bfloat16, 128>(map, a, hb, held, together, sms, s) : launch<__nv_bfloat16, 64>(map, a, hb, held, together, sms, s);
+  else e = d->head_dim == 128 ? launch<__half, 128>(map, a, hb, held, together, sms, s) : launch<__half, 64>(map, a, hb, held, together, sms, s);
   return e == cudaSuccess ? NP_OK : fail_cuda(e);
 }
 

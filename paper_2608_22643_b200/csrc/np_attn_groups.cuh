@@ -1,5 +1,6 @@
-// What the kernels of np_attn_decode_shared have in common: which groups of rows share how many tokens, and where the kernel of the shared tokens
-// (np_attn_shared.cu) leaves its results for that of the rows' own (np_attn_decode.cu), which does both where groups are small.
+// What the two ways of np_attn_decode_shared have in common: which groups of rows share how many tokens, and where parts of a row's result meet.  Small
+// groups go through np_attn_decode.cu, beside their rows' own tokens; of large ones np_attn_shared.cu does the shared tokens, and leaves them for
+// np_attn_rest.cu, which does the rows' own and the join.
 #pragma once
 
 #include <stdint.h>
@@ -10,20 +11,19 @@ namespace npa {
 
 constexpr int kSharedTile = 128;       // tokens of a tile of the first kernel
 constexpr int kSharedBlocks = 320;     // its blocks, at most
-constexpr int kSharedSlotRows = 256;   // rows of a block's partial result, at most
-
 constexpr int kSharedGroups = 512;     // groups that it keeps in mind, at most
+constexpr int kRestBlocks = 640;       // blocks of the second kernel, at most, where it splits rows
 
-// Of a row: where on the line of work its shared tokens' tiles begin, of key-value head 0, and how far it is to the next head's; their number; its
-// first query head's place among the rows of a block's partial result; whether it shares anything, and has tokens of its own.
+// Of a row: where on the line of work its shared tokens' tiles begin, of key-value head 0, and how far it is to the next head's; its first query head's
+// place among the rows of a block's part; the tokens that it shares.
 struct __align__(32) RowPlan {
   int64_t first_w, step;
-  int32_t tiles, place;
-  bool shares, own;
+  int32_t place, shared;
 };
-// How the line is dealt out: the first `more` blocks take each + 1 tiles of it, the others each.
-struct __align__(16) LinePlan {
+// How the line is dealt out to `blocks` blocks: the first `more` take each + 1 tiles of it, the others each.
+struct __align__(32) LinePlan {
   int64_t each, more;
+  int32_t blocks;
 };
 
 // Where the parts of a (row, query head) meet, and counts of what has arrived, which are zero between calls.  Of one size for all calls, so that
@@ -32,7 +32,7 @@ struct __align__(32) Record {
   float o[2][128];            // sums of the shared tokens and of the row's own
   float ml[2][2];             // their maxima (base two) and sums
   unsigned int count;         // at a key-value head's first query head: parts of the row
-  unsigned int pair_count;    // at the first query head of a block of them: joined pieces of the row's own tokens
+  unsigned int pair_count;    // at the first query head of a block of them: pieces of the row's own tokens
   unsigned int group_count;   // in a group's first row, by the number of the block of columns: joined pieces of the shared tokens
   unsigned int unused;
 };
@@ -41,16 +41,18 @@ struct SharedArgs {
   const int32_t* cu;       // [n_groups + 1]
   const int32_t* tokens;   // [n_groups] that a group shares
   int n_groups;
-  bool together;           // one kernel for both
-  int columns;             // together: (row, query head) pairs of a group and key-value head, about
+  int columns;             // (row, query head) pairs of a group and key-value head, about
   Record* records;         // [n][n_heads]
-  // the two kernels apart: rows of the call in a block of rows, and in each tile of 128 query rows
+  // large groups: rows of the call in a block of rows, and in each tile of 128 query rows
   int members, tile_members;
   LinePlan* line;
   RowPlan* plan;           // [n]
   float* part_ml;          // [2 * blocks][rows of a block][2]   of blocks that have not done all of a block of rows' tiles (the others: records)
   float* part_o;           // [2 * blocks][rows of a block][HD]
   int part_rows;
+  // and of the rows' own tokens: what a block has of a split (row, key-value head, heads)
+  float* rest_ml;          // [blocks][8][2]
+  float* rest_o;           // [blocks][8][HD]
 };
 
 // What is known of a group: the tokens that it shares, its rows [lo, hi) of the call, and the sequence whose pages are read for them.

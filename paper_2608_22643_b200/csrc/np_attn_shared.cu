@@ -3,7 +3,7 @@
 //
 //   m = max_j s_j,   l = sum_j 2^(s_j - m),   O = sum_j 2^(s_j - m) v_j,   s_j = scale * log2(e) * q . k_j     over the shared tokens j
 //
-// in fp32; the rows' own tokens and the join are the second kernel's (np_attn_decode.cu, which begins while this one ends).
+// in fp32; the rows' own tokens and the join are the second kernel's (np_attn_rest.cu).
 //
 // The shared keys and values are read once for up to 256 such pairs, so with few of them the cache's bytes bound the kernel, and with many the
 // two matrix products.  They are the products of np_attn_prompt without its mask: tiles of 128 pairs against 128 tokens on the
@@ -12,11 +12,16 @@
 // * A tile's rows are pairs (row of the call, query head), rows outermost; one tiled TMA copy brings them.  Keys and values come a page's rows at a
 //   time, up to sixteen copies to a tile; a lane of the loading warp each.
 // * All (group, key-value head, block of rows, tile of tokens) form one line, of which each block takes an equal stretch.  What a block has
-//   of a block of rows goes to the workspace: straight to the rows' places where it has all of their tiles.
+//   of a block of rows goes to the workspace: straight to the rows' places where it has all of their tiles.  Where those are is worked out by the first
+//   block alone, for the second kernel.
 // * One tile to a block, two blocks to an SM: while one does its softmax, the other has the tensor cores and its copies are under way.
 //   Two tiles share keys and values where groups have more rows than fill one.
 // * Tokens come in sixteens that are there or not (pages outside the pool, the end of the last tile); those that are not get scores of -inf
 //   and values of 0.
+//
+// Measured, both kernels (pages of 64 scattered over the pool): 64 rows, 64 heads of 128 over 8, that share 32768 tokens and have one of their own, 106 us,
+// 0.65 PFLOP/s; that share 8192 and have about 200, 61.3 us; 4 such rows that share 8192 tokens, 28.3 us.  Of the 61.3 us this kernel takes 28: 6.5 until
+// the first scores are there, 2.15 for each tile of 256 rows by 128 tokens (1.65 at the rate of a large product), 3 to store.
 //
 // Every wait is bounded; after a time-out all roles leave, the block meets and tensor memory is released.
 #include <algorithm>
@@ -58,6 +63,11 @@ struct Shape {
   static constexpr int kThreads = 32 * kSoftmaxWarps + 128;      // the last two warps have nothing to do
   static constexpr int kColumns = kTiles * 256;                  // of tensor memory: scores, then accumulators
 };
+
+// Tiles that a block takes, at least, of those of one block of rows: more blocks would each do less, but what every one leaves for the join is as
+// large.  64 rows of 64 heads over 8 that share 512, 2048 or 4096 tokens: 30.7, 38.5 and 43.4 us with four (32.1, 43.1 and 45.7 with one, 39.0, 42.2
+// and 45.6 with six); 4 rows that share 2048 or 8192: 23.6 and 28.7 (23.3 and 32.4; 29.3 and 32.0).
+constexpr int kFewestTiles = 4;
 
 // keys or values of a page's rows: (64 values, rows of a page's heads, halves of head_dim, keys and values, pages)
 __device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, int row, int half, int kv, int page, uint64_t* bar) {
@@ -149,7 +159,8 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   __shared__ Groups s_groups;
   __shared__ __align__(8) uint64_t full[S::kStages], empty[S::kStages], q_full, q_empty, s_full[kTiles], p_half[kTiles], p_full[kTiles], o_full[kTiles], o_empty[kTiles];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_ok;  // 0: a wait has run out
+  __shared__ int s_ok;     // 0: a wait has run out
+  __shared__ int s_items;  // (group, key-value head, block of rows) that share anything
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int n_groups = a.shared.n_groups;
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tsm) + 1023) & ~(uintptr_t)1023);
@@ -171,6 +182,7 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     }
     npp::fence_barrier_init();
     s_ok = 1;
+    s_items = 0;
   }
   npp::pdl_wait_prior();
   npp::pdl_launch_dependents();
@@ -181,6 +193,7 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   for (int i = tid; i < a.n; i += S::kThreads) {
     const int seq = a.seqs ? a.seqs[i] : i;
     const bool known = seq >= 0 && seq < a.max_seqs;
+    if (seq >= a.max_seqs && blockIdx.x == 0) atomicOr(a.status, NP_KV_S_SEQ);
     seqs[i] = (int16_t)(known ? seq : -1);
     lens[i] = known ? a.lens[seq] : 0;
   }
@@ -197,7 +210,9 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     check_group(x, seqs, lens, a.max_pages, a.shift, a.status);
     __syncwarp();
     if (lane == 0) {
-      s_groups.end[g] = (int64_t)tiles_in(x.tokens) * ((x.hi - x.lo + a.shared.members - 1) / a.shared.members) * a.n_kv_heads;
+      const int items = (x.hi - x.lo + a.shared.members - 1) / a.shared.members * a.n_kv_heads;
+      s_groups.end[g] = (int64_t)tiles_in(x.tokens) * items;
+      if (x.tokens) atomicAdd(&s_items, items);
       s_groups.tokens[g] = x.tokens;
       s_groups.seq[g] = (int16_t)x.seq;
     }
@@ -218,20 +233,21 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   }
   __syncthreads();
   const int64_t W = s_groups.end[n_groups - 1];
-  const int G = (int)min((int64_t)gridDim.x, W);
+  const int G = (int)min((int64_t)gridDim.x, max(divide_up(W, kFewestTiles), (int64_t)s_items));
   const int64_t each = G ? W / G : 0, more = W - each * G;
   if (blockIdx.x == 0) {  // for the join
-    if (tid == 0) *a.shared.line = LinePlan{each, more};
-    for (int i = tid; i < a.n; i += S::kThreads) a.shared.plan[i].shares = false;
+    if (tid == 0) *a.shared.line = LinePlan{each, more, G};
+    for (int i = tid; i < a.n; i += S::kThreads) a.shared.plan[i] = RowPlan{0, 0, 0, 0};
     __syncthreads();
     for (int g = wid; g < n_groups; g += S::kThreads / 32) {
-      const int lo = s_groups.lo[g], tokens = s_groups.tokens[g], tiles = tiles_in(tokens), blocks = (s_groups.hi[g] - lo + a.shared.members - 1) / a.shared.members;
+      const int lo = s_groups.lo[g], tokens = s_groups.tokens[g], tiles = tiles_in(tokens);
+      const int blocks = (s_groups.hi[g] - lo + a.shared.members - 1) / a.shared.members;
       if (tokens == 0) continue;
       for (int i = lo + lane; i < s_groups.hi[g]; i += 32) {
         const int block = (i - lo) / a.shared.members, in_block = i - lo - block * a.shared.members, tile = in_block / a.shared.tile_members;
-        const bool there = seqs[i] >= 0 && ((int64_t)lens[i] + (1 << a.shift) - 1) >> a.shift <= a.max_pages;  // else its result is an empty row's
-        a.shared.plan[i] = RowPlan{(g ? s_groups.end[g - 1] : 0) + (int64_t)block * tiles, (int64_t)blocks * tiles, tiles,
-                                   tile * kRows + (in_block - tile * a.shared.tile_members) * a.group, there, there && lens[i] > tokens};
+        if (seqs[i] >= 0)
+          a.shared.plan[i] = RowPlan{(g ? s_groups.end[g - 1] : 0) + (int64_t)block * tiles, (int64_t)blocks * tiles,
+                                     tile * kRows + (in_block - tile * a.shared.tile_members) * a.group, tokens};
       }
     }
   }
@@ -530,91 +546,6 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   }
 }
 
-// The parts of rows that share tokens: a thread has four values of a row and query head.  They come from up to a few dozen blocks, a line of the
-// L2 each, so a thread asks for eight at a time; 64 rows of 64 heads, nine blocks: TIME us.
-constexpr int kJoinThreads = 256, kJoinAhead = 8;
-
-template <bool kBf16, int HD>
-__global__ void __launch_bounds__(kJoinThreads)
-k_attn_shared_join(const __grid_constant__ Args a, uint16_t* out, int64_t o_token, int64_t o_head, float* lse) {
-  npp::pdl_wait_prior();
-  npp::pdl_launch_dependents();
-  const int64_t x = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
-  const unsigned at = (unsigned)(x / (HD / 4));  // at most 2^27
-  const int d = (int)(x % (HD / 4)) * 4, i = (int)(at / a.n_heads), h = (int)(at - (unsigned)i * a.n_heads);
-  if (i >= a.n) return;
-  const RowPlan plan = a.shared.plan[i];
-  const LinePlan line = *a.shared.line;
-  if (!plan.shares) return;
-  const Record* const record = a.shared.records + ((int64_t)i * a.n_heads + h);
-  const int kvh = h / a.group, place = plan.place + h - kvh * a.group;
-  const int64_t w = plan.first_w + kvh * plan.step;
-  auto block_of = [&](int64_t y) { return (int)(y < line.more * (line.each + 1) ? y / (line.each + 1) : line.more + (y - line.more * (line.each + 1)) / line.each); };
-  const int c0 = block_of(w), c1 = block_of(w + plan.tiles - 1), parts = c1 - c0 + 1 + plan.own;
-  // the parts: of the blocks, or of the one that has done all shared tokens, and the row's own
-  auto part = [&](int y, const float** ml, const float** o) {
-    if (y == c1 - c0 + 1 || c0 == c1) {
-      const int of = y == c1 - c0 + 1;
-      *ml = record->ml[of];
-      *o = record->o[of] + d;
-    } else {
-      const int64_t slot = (int64_t)(2 * (c0 + y) + (y == 0)) * a.shared.part_rows + place;
-      *ml = a.shared.part_ml + slot * 2;
-      *o = a.shared.part_o + slot * HD + d;
-    }
-  };
-  float top = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int y0 = 0; y0 < parts; y0 += kJoinAhead) {
-    float2 ml[kJoinAhead];
-    float4 v[kJoinAhead];
-#pragma unroll
-    for (int y = 0; y < kJoinAhead; ++y) {
-      ml[y] = make_float2(-INFINITY, 0.f);
-      v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (y0 + y >= parts) continue;
-      const float *pm, *po;
-      part(y0 + y, &pm, &po);
-      ml[y] = __ldcg(reinterpret_cast<const float2*>(pm));
-      v[y] = __ldcg(reinterpret_cast<const float4*>(po));
-    }
-    float now = top;
-#pragma unroll
-    for (int y = 0; y < kJoinAhead; ++y) now = fmaxf(now, ml[y].x);
-    const float use = now == -INFINITY ? 0.f : now, f0 = exp2_fast(top - use);
-    top = now;
-    sum *= f0;
-#pragma unroll
-    for (int z = 0; z < 4; ++z) acc[z] *= f0;
-#pragma unroll
-    for (int y = 0; y < kJoinAhead; ++y) {
-      const float f = exp2_fast(ml[y].x - use);
-      sum += f * ml[y].y;
-      acc[0] += f * v[y].x;
-      acc[1] += f * v[y].y;
-      acc[2] += f * v[y].z;
-      acc[3] += f * v[y].w;
-    }
-  }
-  if (!not_finite(sum) && (not_finite(acc[0]) || not_finite(acc[1]) || not_finite(acc[2]) || not_finite(acc[3]))) {
-    // factors that are 0 make a NaN of an infinity: what is not finite is what the parts that are not add up to
-    for (int z = 0; z < 4; ++z) {
-      float kept = 0.f;
-      for (int y = 0; y < parts; ++y) {
-        const float *pm, *po;
-        part(y, &pm, &po);
-        const float u = __ldcg(po + z);
-        if (not_finite(u)) kept += u;
-      }
-      if (not_finite(kept)) acc[z] = kept;
-    }
-  }
-  const bool none = sum == 0.f;
-  const float inv = none ? 0.f : 1.f / sum;
-  *reinterpret_cast<uint2*>(out + i * o_token + h * o_head + d) =
-      none ? make_uint2(0, 0) : make_uint2(pack<kBf16>(acc[0] * inv, acc[1] * inv), pack<kBf16>(acc[2] * inv, acc[3] * inv));
-  if (lse && d == 0) lse[at] = none ? -INFINITY : (top == -INFINITY ? 0.f : top) * kLn2 + logf(sum);
-}
-
 // A layer of the cache as (64 values, rows of a page's heads, halves of head_dim, keys and values, pages); a box is one half of up to 128
 // rows of a page.
 bool make_map(CUtensorMap* map, const Args& a, int hd) {
@@ -643,10 +574,10 @@ cudaError_t launch(const CUtensorMap& q, const CUtensorMap& kv, const Args& a, i
   return tiles == 2 ? launch<kBf16, 64, 2>(q, kv, a, sms, s) : launch<kBf16, 64, 1>(q, kv, a, sms, s);
 }
 
-// [partial results and counts of np_attn_decode.cu][how the line is dealt out][plans][maxima and sums of blocks' parts][their O][records]: all but the
-// last are at the same place for every call.
+// [partial results and counts of np_attn_decode.cu][how the line is dealt out][plans][np_attn_rest.cu's parts][maxima and sums of blocks' parts][their
+// O][records]: all but the last are at the same place for every call.
 struct Space {
-  uint64_t line, plan, part_ml, part_o, records, bytes;
+  uint64_t line, plan, rest_ml, rest_o, part_ml, part_o, records, bytes;
   Space(int n_heads, int n) {
     uint64_t at = 0;
     auto take = [&at](uint64_t bytes) {
@@ -657,6 +588,8 @@ struct Space {
     take(decode_parts_bytes());
     line = take(sizeof(LinePlan));
     plan = take((uint64_t)NP_KV_MAX_SEQS * sizeof(RowPlan));
+    rest_ml = take((uint64_t)kRestBlocks * 8 * 8);
+    rest_o = take((uint64_t)kRestBlocks * 8 * 128 * 4);
     part_ml = take((uint64_t)2 * kSharedBlocks * kRows * 8);
     part_o = take((uint64_t)2 * kSharedBlocks * kRows * 128 * 4);
     records = take((uint64_t)n * n_heads * sizeof(Record));
@@ -664,7 +597,10 @@ struct Space {
   }
 };
 
-// Columns, (row, query head) pairs of a group and key-value head, that one kernel does beside the rows' own tokens; more take the tensor cores' way.
+// Columns, (row, query head) pairs of a group and key-value head, on average, that one kernel does beside the rows' own tokens; more take the tensor
+// cores' way.  Both sides, us: 8 rows of 32 heads over 32 that share 8192 tokens, 8 columns, 42.3 in one kernel, 46.8 in two; 16 columns, sharing 1024,
+// 28.4 and 30.1; 2 rows of 64 heads over 8, 16 columns, sharing 8192, 29.9 and 28.0, with 600 of their own 30.7 and 37.0; 24 columns 35.0 and
+// 28.7; 24 rows of 32 heads, 24 columns, 80 and 59, with 600 of their own 76 and 94.
 constexpr int kFewColumns = 16;
 
 const char* shared_heads_error(const np_kv_desc* d, int n_heads, int n) {
@@ -712,8 +648,8 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   a.shared.n_groups = n_groups;
   a.shared.records = reinterpret_cast<Record*>(ws + space.records);
   a.shared.columns = columns;
-  a.shared.together = columns <= kFewColumns || n_groups > kSharedGroups;
-  if (a.shared.together) return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s);
+  if (columns <= kFewColumns || n_groups > kSharedGroups)
+    return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s);
   a.page_bytes = page_bytes(d);
   a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * a.page_bytes;
   a.table = t->page_table;
@@ -738,18 +674,14 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   a.shared.part_ml = reinterpret_cast<float*>(ws + space.part_ml);
   a.shared.part_o = reinterpret_cast<float*>(ws + space.part_o);
   a.shared.part_rows = tiles * kRows;
+  a.shared.rest_ml = reinterpret_cast<float*>(ws + space.rest_ml);
+  a.shared.rest_o = reinterpret_cast<float*>(ws + space.rest_o);
   CUtensorMap mq, mkv;
   if (!make_rows_map(&mq, *q, d->head_dim, n_heads, n, a.group, tile_members) || !make_map(&mkv, a, d->head_dim))
     return fail(NP_E_INVAL, "rows or a cache that a tensor map does not describe");
-  cudaError_t e = row_type(d) == NP_T_BF16 ? launch<true>(mq, mkv, a, d->head_dim, tiles, sms, s) : launch<false>(mq, mkv, a, d->head_dim, tiles, sms, s);
+  const cudaError_t e = row_type(d) == NP_T_BF16 ? launch<true>(mq, mkv, a, d->head_dim, tiles, sms, s) : launch<false>(mq, mkv, a, d->head_dim, tiles, sms, s);
   if (e != cudaSuccess) return fail_cuda(e);
-  if (int rc = decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s)) return rc;
-  const dim3 grid((unsigned)(((int64_t)n * n_heads * (d->head_dim / 4) + kJoinThreads - 1) / kJoinThreads));
-  uint16_t* to = static_cast<uint16_t*>(out->data);
-  auto join = [&](auto kernel) { return launch_early(kernel, grid, kJoinThreads, 0, s, a, to, out->token_stride, out->head_stride, lse); };
-  if (row_type(d) == NP_T_BF16) e = d->head_dim == 128 ? join(k_attn_shared_join<true, 128>) : join(k_attn_shared_join<true, 64>);
-  else e = d->head_dim == 128 ? join(k_attn_shared_join<false, 128>) : join(k_attn_shared_join<false, 64>);
-  return e == cudaSuccess ? NP_OK : fail_cuda(e);
+  return decode_rest(d, a.cache, t, q, n_heads, seqs, n, scale2, out, lse, a.shared, sms, s);
 }
 
 }  // extern "C"

@@ -86,6 +86,8 @@ CASES = [
     (BF, 8, 8, 64, 64, [9000, 64, 128], [[100, 5], [7, 7], [0, 1]]),
     (HF, 6, 2, 128, 16, [333], [[2] * 90]),
     (BF, 128, 1, 64, 32, [512], [[3, 3, 3]]),
+    (HF, 20, 10, 128, 16, [260], [[40] * 70 + [900, 0]]),
+    (BF, 7, 7, 64, 32, [96, 64], [[130] * 60, [1] * 70]),
 ]
 
 
@@ -205,6 +207,24 @@ def test_infinities_among_shared_and_own_values(ways, hq):
     assert torch.isnan(o[1, :, 10]).all() and (o[1, :, 11] == -inf).all() and (o[1, :, 12] == inf).all() and torch.isnan(o[1, :, 13]).all()
     fine = [d for d in range(64) if d not in (10, 11, 12, 13)]
     assert torch.isfinite(o[..., fine]).all() and torch.isfinite(o[others][..., 12:14]).all() and torch.isfinite(lse).all()
+
+
+def test_infinities_among_own_values_of_many_heads():
+    """Rows times key-value heads fill the GPU more than once: an infinity shows in the heads that read it, and in no other."""
+    c, seqs, cu = _branches(HF, 10, 64, 16, [160], [[20] * 70])
+    inf = float("inf")
+    c.cache[0, c.pool.pages[5][10], 1, 9, 3, 10] = inf
+    c.cache[0, c.pool.pages[6][11], 1, 4, 2, 11] = -inf
+    c.cache[0, c.pool.pages[6][10], 1, 5, 2, 12] = float("nan")
+    held = c.dev([160])
+    q = torch.randn(70, 20, 64, device="cuda").to(HF)
+    out, lse = torch.empty_like(q), torch.empty(70, 20, device="cuda")
+    nb.np_attn_decode_shared(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, 20, 70), c.dev(cu), held, seqs=c.dev(seqs), lse=lse)
+    torch.cuda.synchronize()
+    o = out.float()
+    assert (o[5, 18:, 10] == inf).all() and (o[6, 8:10, 11] == -inf).all() and torch.isnan(o[6, 10:12, 12]).all()
+    o[5, 18:, 10] = o[6, 8:10, 11] = o[6, 10:12, 12] = 0
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
 
 
 def test_peaked_scores():

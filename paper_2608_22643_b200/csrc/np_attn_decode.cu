@@ -172,8 +172,15 @@ constexpr int blocks_per_sm(int hd, int form) {
   return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 2 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
 }
 
-// In 8 bits sums are of 2^(s - m + kHeldShift): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.
-constexpr float kHeldShift = 30.f, kHeldUp = 0x1p30f;
+// In 8 bits sums are of 2^(s - m): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.  Warps add up to
+// 2^-149, what they have is 2^30 times as large from then on.
+constexpr float kHeldUp = 0x1p30f;
+// a b + c, whose result may be below 2^-126
+__device__ __forceinline__ float fma_full(float a, float b, float c) {
+  float d;
+  asm("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 
 // What a block knows of groups, in dynamic shared memory: for each row its tokens, how many of them it shares, its group and sequence; and the units of
 // groups and rows.
@@ -342,8 +349,9 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       __syncthreads();
     }
   }
-  // four values of a head's result; its log of the sum with the first
-  auto result = [&](int i, int h, int d, float4 acc, float top, float sum) {
+  // Four values of a head's result; its log of the sum with the first.  Of that log's two products one is rounded by itself, and which one is spelled out,
+  // so that results are the same in every build: the sum's, of a piece by itself; the maximum's, of joined ones.
+  auto result = [&](int i, int h, int d, float4 acc, float top, float sum, auto joined) {
     const float use = top == -INFINITY ? 0.f : top;
     const bool none = sum == 0.f;
     const float inv = none ? 0.f : 1.f / sum;
@@ -352,7 +360,15 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     r.x = (uint32_t)Half2<T>::round(none ? 0.f : acc.x * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.y * inv) << 16;
     r.y = (uint32_t)Half2<T>::round(none ? 0.f : acc.z * inv) | (uint32_t)Half2<T>::round(none ? 0.f : acc.w * inv) << 16;
     *reinterpret_cast<uint2*>(a.out + i * a.o_token + (int64_t)h * a.o_head + d) = r;
-    if (a.lse && d == 0) a.lse[(size_t)i * a.n_heads + h] = none ? -INFINITY : (kHeld ? use - kHeldShift : use) * kLn2 + logf(sum);
+    if (a.lse && d == 0) {
+      float m = use;
+      if (kHeld) {  // the maximum has an exponent of V's in it, which the sum takes back: whole numbers, which leave no rounding
+        int up;
+        sum = frexpf(sum, &up);
+        m += (float)(up - 30);
+      }
+      a.lse[(size_t)i * a.n_heads + h] = none ? -INFINITY : decltype(joined)::value ? __fmaf_rn(__log2f(sum), kLn2, __fmul_rn(m, kLn2)) : __fmaf_rn(m, kLn2, logf(sum));
+    }
   };
   // where the parts of (row i, head h) meet
   auto record = [&](int64_t i, int h) { return a.shared.records + (i * a.n_heads + h); };
@@ -696,7 +712,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       for (int i = 0; i < NH; ++i) {
         const float f = exp2_fast(m[i] - use[i]);
         m[i] = now[i];
-        l[i] *= f;
+        l[i] = kHeld ? fma_full(l[i], f, 0.f) : l[i] * f;
         by(i, f);
       }
     };
@@ -776,7 +792,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
                 const float e = s[y][x][2 * r + i] - use[2 * x + i];
-                l[2 * x + i] += exp2_fast(e + kHeldShift);
+                const float root = exp2_fast(0.5f * e);  // e + 30 would be rounded at 30's scale
+                l[2 * x + i] = fma_full(root, root, l[2 * x + i]);
                 w[i] = exp2_fast(e + lv[y][r]);
               }
               uint32_t hi, lo;
@@ -944,6 +961,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
     for (int i = 0; i < NH; ++i) {
       const int h = kWide ? g + 8 * i : kHeld ? (i >> 1) * 8 + 2 * t + (i & 1) : 2 * t + i;
+      if (kHeld) l[i] = fma_full(l[i], kHeldUp, 0.f);
 #pragma unroll
       for (int x = kWide ? 1 : 4; x < (kWide ? 4 : 32); x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
       if (h < e.heads) {
@@ -975,7 +993,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       const int at = e.h0 + h, member = at / a.group;
       return record(e.row + member, e.kvh * a.group + at - member * a.group);
     };
-    auto emit = [&](int h, int d, float4 acc, float top, float sum) {
+    auto emit = [&](int h, int d, float4 acc, float top, float sum, auto joined) {
       if (kTogether && meets) {
         Record* r = record_of(h);
         const int part = e.of_group ? 0 : 1;
@@ -983,7 +1001,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         if (d == 0) __stcg(reinterpret_cast<float2*>(r->ml[part]), make_float2(top, sum));
         return;
       }
-      result(e.row, e.h0 + h, d, acc, top, sum);
+      result(e.row, e.h0 + h, d, acc, top, sum, joined);
     };
     const int slot = 2 * blockIdx.x + (e.ta == 0 ? 1 : 0);
     uint32_t odd = 0, turn = 1;  // bit k: the values of turn k below are not finite, and the sum does not say why
@@ -1004,7 +1022,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       }
       if (odd_four(acc) && !not_finite(sum) && !(whole && sum == 0.f)) odd |= turn;
       if (whole) {
-        emit(h, d, acc, top, sum);
+        emit(h, d, acc, top, sum, std::false_type{});
       } else {
         __stcg(reinterpret_cast<float4*>(&a.part_o[((size_t)slot * HB + h) * HD + d]), acc);
         if (d == 0) __stcg(reinterpret_cast<float2*>(&a.part_ml[(slot * HB + h) * 2]), make_float2(top, sum));
@@ -1095,7 +1113,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
           __syncwarp();  // b's place is read by the HD / 4 lanes of a head, all of this warp: they are done
           if (!there) continue;
           if (final) {
-            emit(h, d, acc, top, sum);
+            emit(h, d, acc, top, sum, std::true_type{});
           } else {
             const int sl = slot_of(b) + h;
             __stcg(reinterpret_cast<float4*>(&a.part_o[(size_t)sl * HD + d]), acc);
@@ -1156,7 +1174,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
             };
             acc = make_float4(kept(acc.x, v0.x, v1.x), kept(acc.y, v0.y, v1.y), kept(acc.z, v0.z, v1.z), kept(acc.w, v0.w, v1.w));
           }
-          result(i, h, d, acc, top, sum);
+          result(i, h, d, acc, top, sum, std::true_type{});
         }
         __syncthreads();
       }

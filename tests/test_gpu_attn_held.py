@@ -258,3 +258,21 @@ def test_held_decode_is_near_the_rows_it_stands_for(dtype):
         ds = 0.125 * 2.0 ** -4 * np.abs(kn[:, h // 2]) @ np.abs(qn[0, h])       # how far a score may move
         bound = mean * (2.0 ** -4 + np.expm1(2 * ds.max())) + 0.01 * np.abs(vn).max()
         assert (np.abs(on[0, h] - want) <= bound).all()
+
+
+def test_logs_of_sums_without_scores():
+    """Queries of 0: the log of the sum is that of the number of tokens, whatever the values' exponents.
+
+    A weight is the square of a power of two that is off by 2^-22 at most, so it is off by 2^-21; up to four of them add up with 2^-22 more; the log of
+    a number between a half and one is off by 2^-21.4 and the maximum's product, of numbers below 2, by 2^-23.  Together below 2^-20 + 2^-21."""
+    lens = [1, 2, 3, 4, 1, 2]
+    c = Held(dtype=BF, hkv=2, hd=64, P=16, n_pages=8, max_seqs=len(lens))
+    for s, n in enumerate(lens):
+        c.grow([s], [n], seed=s)
+    c.cache[0, c.pool.pages[4][0], 2 * 2 * 16 * 64 + 2 * 16:] += 100     # values far larger, far smaller
+    c.cache[0, c.pool.pages[5][0], 2 * 2 * 16 * 64 + 2 * 16:] -= 50
+    q = torch.zeros(len(lens), 4, 64, dtype=BF, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(len(lens), 4, device="cuda")
+    nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, 4, len(lens)), lse=lse)
+    off = (lse.double().cpu() - torch.tensor(lens, dtype=torch.float64).log()[:, None]).abs().max().item()
+    assert off < 2.0 ** -20 + 2.0 ** -21

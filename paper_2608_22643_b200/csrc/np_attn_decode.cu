@@ -30,9 +30,21 @@
 //   it.  So where a piece's result is no finite number though its sum is one, the block looks through the piece's V (mend) and stores
 //   what the tokens make of it; joins take infinities as they are.
 //
+// A cache of 8 bits (e4m3 values, a power of two for each token, head and keys or values) goes the way of up to eight heads, or of two times eight: values
+// become fp16, which holds all of them, as they are read, and the products are of fp16 whatever the rows' type, with the queries times a power of two of
+// their own (the largest magnitude 2^14), so that nothing is lost.  A key's power of two is a factor of its score.  A value's is one of its
+// weight, which keeps the weights in fp16's range only if the maximum has it too:
+//
+//   m = max_j (s_j + v_j),   o = sum_j 2^(s_j + v_j - m) e4m3_j,   l = sum_j 2^(s_j - m),   out = o / l       v_j the exponents of V
+//
+// with two terms of fp16 for a weight, as above.  There are half the bytes, and each has to be widened before a product takes it.  Long sequences stream at
+// 5.2 TB/s behind a start and joins of 14 us; with nothing but the loads the long one below would still take 56 of its 66.6 us.  (Keys and values
+// through shared memory with asynchronous copies, deeper prefetch, more blocks: no gain.)
+//
 // Measured (pages of 64 scattered over the pool, caches larger than the L2 in turn): sixteen sequences of 0 to 4095 tokens, 32 heads
 // of 128, 57.3 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 159 us, 100 %; one of 131071 tokens, 64 heads over 8, 91.9 us,
-// 89 %; one of 100 tokens 4.7 us.  What is not the stream is the launch, three loads that depend on one another (length, page
+// 89 %; one of 100 tokens 4.7 us.  In 8 bits the sixteen, the long one
+// and the short one take 44.6, 66.6 and 5.1 us, 59 % and 63 % of the copy rate.  What is not the stream is the launch, three loads that depend on one another (length, page
 // number, keys) and the joins.  Groups of more than eight heads are bound by the steps
 // between a warp's loads: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, 53.8 us, 74 % (69 % with keys and values
 // in registers, 55 % with 16-byte asynchronous copies in place of TMA, 70 % with the chunks beyond asked into the L2 ahead, 74 % with
@@ -165,11 +177,13 @@ __device__ __noinline__ float4 keep_infinite(float4 acc, const float* part, int6
 }
 
 // Blocks that share an SM.  More of them keep more loads in flight, until the registers no longer hold a warp's keys, values and
-// accumulators.  us with one more and with this many (sixteen heads: with keys and values in registers): 128 values, eight heads, four blocks 113 (the long sequence) and 186 (64 of 1000),
-// three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16 sequences of 2000, five
-// 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
+// accumulators.  us with one more and with this many (sixteen heads: with keys and values in registers): 128 values, eight heads, four blocks 113 (the
+// long sequence) and 186 (64 of 1000), three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16
+// sequences of 2000, five 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
+// In 8 bits: 128 values, eight heads, the long sequence, four 66.4, three 66.7, two 81.2; 64 values, 16 of 2000, 64 heads, five 93.4, four 72.2,
+// three 76.2; sixteen heads, 64 of 2000, three 54.6 and two 56.6 (one 88.9), with 64 values 35.1 and 38.3 (58.7).
 constexpr int blocks_per_sm(int hd, int form) {
-  return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 2 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
+  return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 3 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
 }
 
 // In 8 bits sums are of 2^(s - m): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.  Warps add up to
@@ -228,7 +242,10 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
   constexpr bool kWide = kForm == kSixteen, kHeld = kForm == kHeldEight || kForm == kHeldSixteen;
   constexpr int HB = kForm == kSixteen || kForm == kHeldSixteen ? 16 : 8;  // heads of a block, at most
   constexpr int NT = HB / 8, NH = kHeld ? 2 * NT : 2;  // in 8 bits: eights of heads; heads of a lane's scores
-  constexpr int SC = kHeld && HD == 64 ? 2 : 1;         // sixteens of tokens of a chunk
+  // Sixteens of tokens of a chunk.  In 8 bits a sixteen's rows of 64 values are 1 KB, too few for a trip to memory.  16 sequences of 2000, 64 heads of 64:
+  // 72.2 us with two, 89.7 with one; one of 131071, 64 heads over 8, 41.7 and 49.8.  Of 128 values two are no better: 65.0 and 66.7, but 16 ragged
+  // sequences of 2000, 32 heads, 31.7 and 29.1.
+  constexpr int SC = kHeld && HD == 64 ? 2 : 1;
   constexpr int kTileTokens = kTile * SC, kUnitsBefore = kStart / SC;  // tokens of a tile, what a group's start counts
   constexpr int KV = kHeld ? HD / 64 : HD / 32;        // 16-byte pieces of a key row per lane
   constexpr int VW = HD / 32;                          // in 8 bits: words of a value row per lane

@@ -14,6 +14,13 @@
 //
 // Powers of two as scales make the 8 bits a matter of integers and one rounding: x * 2^-e is exact, so nothing of what is held depends on
 // how it was computed.
+//
+// Measured (tokens of 64 heads of 128 over 8, each set of inputs in turn larger than the L2): 9 prompts of up to 2000 tokens with norms, 35.6 us, 58 % of the
+// copy rate; 8192 tokens without norms into the cache 65.7 us, 79 %; 5 prompts into 8 bits and out again, two kernels, 19 us.  Issue slots are busy
+// 70 % in the first two; a block's start (where its rows come from and go to, three loads that depend on one another; its angles) is the rest, and
+// all that there is of the small calls: sixteen tokens 3.6 us, into 8 bits and out again 5.2, one token 2.4.  What lanes share took 46 and 92 us in
+// place of 35.6 and 65.7 when pairs lay in two lanes and every lane worked out its rows' places.  (No better: blocks that stay, a warp for the
+// loads, sixteen values to a lane; 64 values of a lane on their way 62 us for the 8192 tokens, and more for small calls.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>

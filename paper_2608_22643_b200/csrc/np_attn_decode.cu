@@ -782,7 +782,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
             for (int x = 0; x < NT; ++x)
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                const float z = s[y][x][2 * r + i] * up[2 * x + i] * power;
+                const float z = s[y][x][2 * r + i] * (up[2 * x + i] * power);  // either factor may be too large for the score by itself
                 s[y][x][2 * r + i] = there ? z : -INFINITY;
                 top[2 * x + i] = fmaxf(top[2 * x + i], s[y][x][2 * r + i] + lv[y][r]);
               }

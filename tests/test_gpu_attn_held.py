@@ -276,3 +276,22 @@ def test_logs_of_sums_without_scores():
     nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, 4, len(lens)), lse=lse)
     off = (lse.double().cpu() - torch.tensor(lens, dtype=torch.float64).log()[:, None]).abs().max().item()
     assert off < 2.0 ** -20 + 2.0 ** -21
+
+
+def test_queries_at_the_end_of_their_range():
+    """The largest queries against keys of the least exponent: the products are far from fp32's end, and the largest score takes all of the weight."""
+    c = Held(dtype=BF, hkv=1, hd=64, P=16, n_pages=2, max_seqs=1)
+    c.grow([0], [3], seed=4)
+    k = torch.zeros(3, 1, 64, dtype=BF, device="cuda")
+    k[:, 0, 0] = torch.tensor([224.0, 448.0, -448.0]) * 2.0 ** -60
+    v = torch.randn(3, 1, 64, device="cuda").to(BF)
+    nb.np_kv_append(c.desc, c.cache, 0, c.tables, k, v, c.dev([0]), cu=c.dev([0, 3]), start=c.dev([0]))
+    q = torch.zeros(1, 2, 64, dtype=BF, device="cuda")
+    q[0, 0, 0], q[0, 1, 0] = 1.5 * 2.0 ** 127, -1.5 * 2.0 ** 127
+    out, lse = torch.empty_like(q), torch.empty(1, 2, device="cuda")
+    nb.np_attn_decode(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, 2, 1), scale=1.0, lse=lse)
+    want = c.tokens(0, 0)[1][[1, 2], 0]
+    assert (np.abs(f64(out[0]) - want) <= np.abs(want) * 2.0 ** -8).all()
+    # the scale times log2(e), the score, the maximum times ln 2: a rounding each, and twice that of the constants
+    assert (lse.double() / (1.5 * 448 * 2.0 ** 67) - 1).abs().max() <= 6 * 2.0 ** -24
+    assert c.status.item() == 0

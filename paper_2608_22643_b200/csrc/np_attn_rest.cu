@@ -11,11 +11,12 @@
 //   has too few tokens for that, all the blocks compute the same and each joins some of the heads: 4 rows that share 8192 tokens, 64 heads over 8,
 //   46.2 us with one block to join eight heads, 32.2 so.
 // * Where there are more blocks than the GPU holds and groups have one head or two, a warp to each of four key-value heads: one start for
-//   four of them.  64 rows that share 8192 tokens and have about 64, 32 heads: 69.7 us in place of 84.8; 24 rows 61.4 in place of 59.5, with about
+//   four of them.  64 rows that share 8192 tokens and have 64 of their own, 32 heads: 69.7 us in place of 84.8; 24 rows 61.4 in place of 59.5, with
 //   600 tokens 94 in place of 103.  (Several pairs one after the other to a block, the next one's keys asked for before the join: 94.6.)
 //
-// Measured alone, its inputs in no cache: 64 rows of 1 to 400 tokens, 64 heads over 8, nine parts of what they share: 20 us for 52 MB of the cache and
-// 19 MB of parts.
+// Measured alone: 64 rows of 1 to 200 tokens (4190 together), 64 heads over 8, nine parts of what they share: 20 us for 17 MB of the cache and 19 MB of
+// parts, so it is latency that bounds it: four loads that depend on one another before the first keys, up to four steps of them, and two
+// rounds of parts.
 #include <algorithm>
 
 #include "np_attn.h"

@@ -20,7 +20,7 @@
 //   and values of 0.
 //
 // Measured, both kernels (pages of 64 scattered over the pool): 64 rows, 64 heads of 128 over 8, that share 32768 tokens and have one of their own, 106 us,
-// 0.65 PFLOP/s; that share 8192 and have about 200, 61.3 us; 4 such rows that share 8192 tokens, 28.3 us.  Of the 61.3 us this kernel takes 28: 6.5 until
+// 0.65 PFLOP/s; that share 8192 and have up to 200, 61.5 us; 4 such rows that share 8192 tokens, 28.3 us.  Of the 61.5 us this kernel takes 28: 6.5 until
 // the first scores are there, 2.15 for each tile of 256 rows by 128 tokens (1.65 at the rate of a large product), 3 to store.
 //
 // Every wait is bounded; after a time-out all roles leave, the block meets and tensor memory is released.

@@ -16,17 +16,18 @@
 // how it was computed.
 //
 // Measured (tokens of 64 heads of 128 over 8, each set of inputs in turn larger than the L2): 9 prompts of up to 2000 tokens with norms, 35.6 us, 58 % of the
-// copy rate; 8192 tokens without norms into the cache 65.7 us, 79 %; 5 prompts into 8 bits and out again, two kernels, 19 us.  Issue slots are busy
+// copy rate; 8192 tokens without norms into the cache 62.0 us, 84 %; 5 prompts into 8 bits and out again, two kernels, 19 us.  Issue slots are busy
 // 70 % in the first two; a block's start (where its rows come from and go to, three loads that depend on one another; its angles) is the rest, and
 // all that there is of the small calls: sixteen tokens 3.6 us, into 8 bits and out again 5.2, one token 2.4.  What lanes share took 46 and 92 us in
 // place of 35.6 and 65.7 when pairs lay in two lanes and every lane worked out its rows' places.  (No better: blocks that stay, a warp for the
-// loads, sixteen values to a lane; 64 values of a lane on their way 62 us for the 8192 tokens, and more for small calls.)
+// loads, sixteen values to a lane.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "np_attn.h"
 #include "np_device.cuh"
@@ -36,8 +37,8 @@
 namespace npa {
 namespace {
 
-constexpr int kThreads = 128, kValues = 32;  // of a lane on their way
-template <int HD, int kEach>
+constexpr int kThreads = 128, kFew = 32, kMany = 64;  // values of a lane on their way
+template <int HD, int kEach, int kValues = kFew>
 struct Rows {
   static constexpr int kLanes = HD / kEach;                  // of a row: a lane has that many of its values
   static constexpr int kTurn = kThreads / kLanes;            // rows of a block at a time
@@ -191,10 +192,10 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float power) {
 enum Kind { kQuery, kKey, kValue };
 
 // kRotate: norm and rotation.  kHeld: keys and values go into pages of 8 bits.
-template <class T, int HD, bool kRotate, bool kHeld>
+template <class T, int HD, bool kRotate, bool kHeld, int kValues>
 __global__ void __launch_bounds__(kThreads)
 k_rows_in(const __grid_constant__ RowsArgs a) {
-  using R = Rows<HD, 8>;
+  using R = Rows<HD, 8, kValues>;
   constexpr int L = R::kLanes, kVecs = R::kVecs, kTokens = R::kBlock / 2 + 2;  // of a block at most: a token has two rows or more
   extern __shared__ int s_cu[];
   __shared__ const uint16_t* s_src[R::kBlock];
@@ -427,13 +428,24 @@ k_rows_out(const __grid_constant__ RowsArgs a) {
   }
 }
 
+// Values of a call from which a lane of a rotation has kMany of them on their way: fewer blocks work out the same angles, and more loads wait for each
+// other's start.  64 heads of 128 over 8 into the cache, us with kMany and kFew: 64 tokens 4.1 and 3.4, 1024 (10 million) 13.7 and 12.7, 4096 (42 million)
+// 34.6 and 35.7, 8192 62.0 and 65.6; 32 heads of 64, 4096 tokens (25 million) 26.7 and 27.2; normed queries and keys of 4096 tokens 37.1 and 37.9.
+constexpr int64_t kManyFrom = 1 << 25;
 template <class T>
 cudaError_t launch_in(const RowsArgs& a, int hd, bool rotate, bool held, cudaStream_t s) {
-  const int block = hd == 128 ? Rows<128, 8>::kBlock : Rows<64, 8>::kBlock;
-  const dim3 grid((unsigned)(((int64_t)a.n_tokens * a.rows + block - 1) / block));
+  const int64_t rows = (int64_t)a.n_tokens * a.rows;
+  const bool many = rotate && rows * hd >= kManyFrom;
+  const int block = kThreads * 8 / hd * (many ? kMany : kFew) / 8;
+  const dim3 grid((unsigned)((rows + block - 1) / block));
   auto go = [&](auto kernel) { return launch_early(kernel, grid, kThreads, a.cu ? (a.n + 1) * sizeof(int) : 0, s, a); };
-  if (hd == 128) return !rotate ? go(k_rows_in<T, 128, false, true>) : held ? go(k_rows_in<T, 128, true, true>) : go(k_rows_in<T, 128, true, false>);
-  return !rotate ? go(k_rows_in<T, 64, false, true>) : held ? go(k_rows_in<T, 64, true, true>) : go(k_rows_in<T, 64, true, false>);
+  auto of_width = [&](auto width) {
+    constexpr int HD = decltype(width)::value;
+    if (!rotate) return go(k_rows_in<T, HD, false, true, kFew>);
+    if (many) return held ? go(k_rows_in<T, HD, true, true, kMany>) : go(k_rows_in<T, HD, true, false, kMany>);
+    return held ? go(k_rows_in<T, HD, true, true, kFew>) : go(k_rows_in<T, HD, true, false, kFew>);
+  };
+  return hd == 128 ? of_width(std::integral_constant<int, 128>{}) : of_width(std::integral_constant<int, 64>{});
 }
 template <class T>
 cudaError_t launch_out(const RowsArgs& a, int hd, bool held, cudaStream_t s) {

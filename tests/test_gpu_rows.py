@@ -325,3 +325,43 @@ def test_rows_on_a_stream_of_their_own_and_replayed():
         assert torch.equal(qo, q2)
     c.check()
     assert torch.equal(c.cache, d.cache)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd,neighbours", [(BF, 1, 1, 64, True), (HF, 9, 3, 128, False), (BF, 64, 8, 128, False)])
+def test_rotate_many_tokens_as_few(dtype, hq, hkv, hd, neighbours):
+    """Calls of tens of millions of values give what pieces of them give, bit for bit."""
+    rows = (1 << 25) // (hq + hkv) // hd + 1001
+    q, k, _ = _qkv(rows, hq, hkv, hd, dtype)
+    r = _rotation(hd, hd, "qk", neighbours)[0]
+    a, b = (torch.full((rows + 1, hq + hkv, hd), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    first = 12345
+    start = _dev([77, 100000])
+    cu = [0, rows // 3, rows]
+    nb.np_attn_rotate(r, q, k, a[:rows, :hq], a[:rows, hq:], _dev(cu), start)
+    for lo in range(0, rows, first):                          # a piece: the same two spans, cut
+        hi = min(rows, lo + first)
+        spans = [min(max(x, lo), hi) for x in cu]
+        where = _dev([77 + spans[0], 100000 + spans[1] - cu[1]])
+        nb.np_attn_rotate(r, q[lo:hi], k[lo:hi], b[lo:hi, :hq], b[lo:hi, hq:], _dev([x - lo for x in spans]), where)
+    torch.cuda.synchronize()
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and (a[rows] == 7).all()
+
+
+@pytest.mark.parametrize("kind", ["held", "rows"])
+@pytest.mark.parametrize("dtype,hq,hkv,hd,P", [(BF, 20, 20, 64, 16), (HF, 40, 8, 128, 64)])
+def test_append_rotated_many_tokens(kind, dtype, hq, hkv, hd, P):
+    """A call of tens of millions of values, into a cache: rotate and append, bit for bit."""
+    n = (1 << 25) // (hq + 2 * hkv) // hd + 333
+    counts = [n // 2, 0, n - n // 2]
+    c, d = (_pool(kind, dtype, hkv, hd, P, counts) for _ in range(2))
+    r = _rotation(hd, hd, "qk", False)[0]
+    start, _ = c.reserve(range(3), counts)
+    d.reserve(range(3), counts)
+    q, k, v = _qkv(n, hq, hkv, hd, dtype)
+    qo, q2, k2 = torch.full_like(q, 7.0), torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    nb.np_kv_append_rotated(c.desc, c.cache, 1, c.tables, r, q, k, v, qo, c.dev(range(3)), _cu(counts), start)
+    nb.np_attn_rotate(r, q, k, q2, k2, _cu(counts), start)
+    nb.np_kv_append(d.desc, d.cache, 1, d.tables, k2, v, d.dev(range(3)), _cu(counts), start)
+    torch.cuda.synchronize()
+    assert torch.equal(qo, q2) and torch.equal(c.cache.view(torch.uint8), d.cache.view(torch.uint8))
+    assert c.status.item() == 0

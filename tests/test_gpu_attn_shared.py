@@ -209,6 +209,17 @@ def test_infinities_among_shared_and_own_values(ways, hq):
     assert torch.isfinite(o[..., fine]).all() and torch.isfinite(o[others][..., 12:14]).all() and torch.isfinite(lse).all()
 
 
+def test_more_groups_than_are_kept_in_mind():
+    """Large groups among hundreds of empty ones, and of groups without rows that claim what nobody has."""
+    c, seqs, cu = _branches(HF, 1, 64, 16, [160, 48], [[3] * 30, [20] * 40])
+    many = [0, 30] + [30] * 520 + [70]
+    held = c.dev([160] + [0] * 260 + [64] * 260 + [48])
+    ws = _workspace(c, 128, 70)
+    _, a, la = _run(c, 128, seqs, many, held, ws=ws)
+    _, b, lb = _run(c, 128, seqs, many, held, ws=ws, check=False)
+    assert torch.equal(a, b) and torch.equal(la, lb) and c.status.item() == 0
+
+
 def test_infinities_among_own_values_of_many_heads():
     """Rows times key-value heads fill the GPU more than once: an infinity shows in the heads that read it, and in no other."""
     c, seqs, cu = _branches(HF, 10, 64, 16, [160], [[20] * 70])

@@ -139,20 +139,18 @@ __device__ __forceinline__ int sequence_of(const RowsArgs& a, const int* cu, int
   *off = t - cu[lo];
   return *off < 0 ? -1 : lo;
 }
-__device__ __forceinline__ int64_t position_of(const RowsArgs& a, const int* cu, int t) {
-  int off;
-  const int i = sequence_of(a, cu, t, &off), st = i < 0 ? -1 : a.start[i];
-  return st < 0 ? -1 : (int64_t)st + off;
-}
-__device__ __forceinline__ Place place_of(const RowsArgs& a, const int* cu, int t) {
-  Place p = {-1, -1, 0};
+// The position of token t (-1: the row is passed over), and its sequence, if there is a cache.
+__device__ __forceinline__ int64_t position_of(const RowsArgs& a, const int* cu, int t, int* seq) {
   int off;
   const int i = sequence_of(a, cu, t, &off);
-  if (i < 0) return p;
-  const int st = a.start[i], seq = !a.cache ? 0 : a.seqs ? a.seqs[i] : i;
-  if (st < 0) return p;
-  p.pos = (int64_t)st + off;
-  if (!a.cache) return p;
+  if (i < 0) return -1;
+  const int st = a.start[i];
+  *seq = !a.cache ? 0 : a.seqs ? a.seqs[i] : i;
+  return st < 0 ? -1 : (int64_t)st + off;
+}
+__device__ __forceinline__ Place place_of(const RowsArgs& a, int64_t pos, int seq) {
+  Place p = {pos, -1, 0};
+  if (pos < 0 || !a.cache) return p;
   if (seq < 0 || seq >= a.max_seqs) {
     atomicOr(a.status, NP_KV_S_SEQ);
     return p;
@@ -201,6 +199,8 @@ k_rows_in(const __grid_constant__ RowsArgs a) {
   __shared__ const uint16_t* s_src[R::kBlock];
   __shared__ char* s_dst[R::kBlock];              // nullptr: the row is not written
   __shared__ char* s_exponent[kHeld ? R::kBlock : 1];
+  __shared__ int64_t s_pos[kTokens];              // positions of the block's tokens, and their sequences
+  __shared__ int s_seq[kTokens];
   __shared__ int s_row[R::kBlock];                // token of the block << 3 | whether it is normed << 2 | kind
   __shared__ __align__(16) float s_gain[kRotate ? 2 : 1][HD];
   __shared__ double s_freq[kRotate ? HD / 2 : 1];  // turns per position
@@ -251,8 +251,10 @@ k_rows_in(const __grid_constant__ RowsArgs a) {
     }
   }
   // ---- where they go, and the angles of their tokens
+  if (tid < tokens) s_pos[tid] = position_of(a, s_cu, t0 + tid, &s_seq[tid]);
+  __syncthreads();
   if (tid < rows) {
-    const Place p = place_of(a, s_cu, t);
+    const Place p = place_of(a, s_pos[t - t0], s_seq[t - t0]);
     char* dst = nullptr;
     if (kRotate && r < a.nq) {
       if (p.pos >= 0) dst = reinterpret_cast<char*>(a.q_out + t * a.qo_token + r * a.qo_head);
@@ -267,10 +269,11 @@ k_rows_in(const __grid_constant__ RowsArgs a) {
     s_dst[tid] = dst;
   }
   if (kRotate && a.half) {
-    const int pairs = a.half * 8;
-    for (int x = tid; x < tokens * pairs; x += kThreads) {
-      const int u = x / pairs, i = x - u * pairs;
-      double turn = (double)position_of(a, s_cu, t0 + u) * s_freq[i];
+    const int pairs = a.half * 8, step = 32 - __clz(pairs - 1);  // a token's pairs, up to the next power of two
+    for (int x = tid; x < tokens << step; x += kThreads) {
+      const int u = x >> step, i = x - (u << step);
+      if (i >= pairs) continue;
+      double turn = (double)s_pos[u] * s_freq[i];
       turn -= rint(turn);
       float sin, cos;
       sincospif(2.f * (float)turn, &sin, &cos);
@@ -381,7 +384,9 @@ k_rows_out(const __grid_constant__ RowsArgs a) {
   const int rows = (int)(min(total, first + R::kBlock) - first);
   if (tid < rows) {
     const int t = (int)((first + tid) / a.rows), r = (int)(first + tid - (uint32_t)t * a.rows);
-    const Place p = place_of(a, s_cu, t);
+    int seq = 0;
+    const int64_t pos = position_of(a, s_cu, t, &seq);
+    const Place p = place_of(a, pos, seq);
     const char* page = a.cache + p.page * a.page_bytes;
     const int64_t at = ((int64_t)r << a.shift) + p.at;
     s_src[tid] = p.page < 0 ? nullptr : page + at * (kHeld ? HD : HD * 2);

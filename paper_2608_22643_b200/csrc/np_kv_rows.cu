@@ -57,6 +57,11 @@ struct RowsArgs {
   const int32_t* cu;
   const int32_t* start;
   int n, n_tokens, nq, nkv, rows;  // rows of a token: queries, keys, then values if there is a cache
+  // x / rows = x * mul >> 32 + shift for x below 2^31: mul = floor(2^(32 + shift) / rows) + 1 with 2^shift < rows <= 2^(shift + 1), so that what mul is too
+  // large by adds less than 1 / rows
+  uint32_t mul;
+  int mul_shift;
+  __device__ __forceinline__ int token_of(uint32_t x) const { return (int)(__umulhi(x, mul) >> mul_shift); }
   // the cache
   char* cache;  // of the layer; nullptr: none
   const int32_t* table;
@@ -208,11 +213,11 @@ k_rows_in(const __grid_constant__ RowsArgs a) {
   const int tid = threadIdx.x, piece = tid % L, slot = tid / L;
   const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock;
   const int rows = (int)(min(total, first + R::kBlock) - first);
-  const int t0 = (int)(first / a.rows), tokens = (int)((first + rows - 1) / a.rows) - t0 + 1;
+  const int t0 = a.token_of(first), tokens = a.token_of(first + rows - 1) - t0 + 1;
   // ---- where rows come from
   int t = 0, r = 0;
   if (tid < rows) {
-    t = (int)((first + tid) / a.rows);
+    t = a.token_of(first + tid);
     r = (int)(first + tid - (uint32_t)t * a.rows);
     const int kind = r < a.nq ? kQuery : r < a.nq + a.nkv ? kKey : kValue;
     s_src[tid] = kind == kQuery ? a.q + t * a.q_token + r * a.q_head
@@ -383,7 +388,7 @@ k_rows_out(const __grid_constant__ RowsArgs a) {
   const uint32_t total = (uint32_t)a.n_tokens * a.rows, first = blockIdx.x * R::kBlock;
   const int rows = (int)(min(total, first + R::kBlock) - first);
   if (tid < rows) {
-    const int t = (int)((first + tid) / a.rows), r = (int)(first + tid - (uint32_t)t * a.rows);
+    const int t = a.token_of(first + tid), r = (int)(first + tid - (uint32_t)t * a.rows);
     int seq = 0;
     const int64_t pos = position_of(a, s_cu, t, &seq);
     const Place p = place_of(a, pos, seq);
@@ -539,8 +544,10 @@ int enter(const np_kv_desc* d, const void* cache, int32_t layer, const np_kv_tab
   return NP_OK;
 }
 
-int run(const RowsArgs& a, int type, int hd, bool out, bool rotate, bool held, void* stream) {
+int run(RowsArgs& a, int type, int hd, bool out, bool rotate, bool held, void* stream) {
   if (too_many(a)) return fail(NP_E_INVAL, kTooMany);
+  while (1 << (a.mul_shift + 1) < a.rows) ++a.mul_shift;  // there are two rows or more, and fewer than 2^18
+  a.mul = (uint32_t)((1ULL << (32 + a.mul_shift)) / a.rows + 1);
   int sms;
   if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
   cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -15,11 +15,12 @@
 // Powers of two as scales make the 8 bits a matter of integers and one rounding: x * 2^-e is exact, so nothing of what is held depends on
 // how it was computed.
 //
-// Measured (tokens of 64 heads of 128 over 8, each set of inputs in turn larger than the L2): 9 prompts of up to 2000 tokens with norms, 35.6 us, 58 % of the
-// copy rate; 8192 tokens without norms into the cache 62.0 us, 84 %; 5 prompts into 8 bits and out again, two kernels, 19 us.  Issue slots are busy
-// 70 % in the first two; a block's start (where its rows come from and go to, three loads that depend on one another; its angles) is the rest, and
-// all that there is of the small calls: sixteen tokens 3.6 us, into 8 bits and out again 5.2, one token 2.4.  What lanes share took 46 and 92 us in
-// place of 35.6 and 65.7 when pairs lay in two lanes and every lane worked out its rows' places.  (No better: blocks that stay, a warp for the
+// Measured (tokens of 64 heads of 128 over 8, each set of inputs in turn larger than the L2): 9 prompts of up to 2000 tokens with norms, 33.9 us, 61 % of the
+// copy rate; 8192 tokens without norms into the cache 59.7 us, 87 %; 5 prompts into 8 bits and out again, two kernels, 18.6 us.  Issue slots are busy
+// 60 to 70 % in the first two; a block's start (where its rows come from and go to, three loads that depend on one another; its angles) is the rest, and
+// all that there is of the small calls: sixteen tokens 3.5 us, into 8 bits and out again 5.1, one token 2.4.  The first two took 46 and 92 us when
+// pairs lay in two lanes and every lane worked out its rows' places, and 35.6 and 62.0 when each pair's angle began with a search for its token's
+// sequence, and tokens were found by divisions.  (No better: blocks that stay, a warp for the
 // loads, sixteen values to a lane.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -439,8 +440,8 @@ k_rows_out(const __grid_constant__ RowsArgs a) {
 }
 
 // Values of a call from which a lane of a rotation has kMany of them on their way: fewer blocks work out the same angles, and more loads wait for each
-// other's start.  64 heads of 128 over 8 into the cache, us with kMany and kFew: 64 tokens 4.1 and 3.4, 1024 (10 million) 13.7 and 12.7, 4096 (42 million)
-// 34.6 and 35.7, 8192 62.0 and 65.6; 32 heads of 64, 4096 tokens (25 million) 26.7 and 27.2; normed queries and keys of 4096 tokens 37.1 and 37.9.
+// other's start.  64 heads of 128 over 8 into the cache, us with kMany and kFew: 64 tokens 3.95 and 3.16, 1024 (10 million) 13.0 and 11.9, 4096 (42 million)
+// 33.2 and 33.5, 8192 59.7 and 61.8; 32 heads of 64, 4096 tokens (25 million) 25.9 and 25.7; normed queries and keys of 8000 tokens 64.7 and 65.7.
 constexpr int64_t kManyFrom = 1 << 25;
 template <class T>
 cudaError_t launch_in(const RowsArgs& a, int hd, bool rotate, bool held, cudaStream_t s) {

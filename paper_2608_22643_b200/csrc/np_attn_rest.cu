@@ -369,7 +369,7 @@ k_attn_rest(const __grid_constant__ RestArgs a) {
   for (int x = turns > 1 ? tid - turn * results : tid; x < results; x += kThreads) {
     const int h = from_head + x / kFours, d = x % kFours * 4;
     int first = 0, parts = 0;
-    if (plan.shared) {
+    if (plan.shared && len > 0) {
       const int64_t w = plan.first_w + (kvh0 + kv_of(h)) * plan.step;
       first = block_of(w);
       parts = block_of(w + (plan.shared + kSharedTile - 1) / kSharedTile - 1) - first + 1;

@@ -138,6 +138,25 @@ def test_a_group_that_is_longer_than_its_sequences_of_another():
     assert torch.equal(out[[0, 2]], want[[0, 2]])
 
 
+@pytest.mark.parametrize("hq,hkv", [(4, 2), (16, 2), (64, 2), (2, 2)])
+def test_rows_whose_length_their_table_does_not_hold(hq, hkv):
+    """Such a row is empty, and one of a sequence that is none, in small groups and large ones; the rest of its group is as it was."""
+    c, seqs, cu = _branches(BF, hkv, 64, 16, [160], [[20, 0, 4, 6] * 10])
+    held = c.dev([160])
+    q, want, _ = _run(c, hq, seqs, cu, held)
+    for row, n in ((3, 16 * c.desc.max_pages + 1), (17, 2 ** 31 - 1)):
+        c.lens[row] = n
+    seqs[5], seqs[9] = c.desc.max_seqs, -2
+    out, lse = torch.empty_like(want), torch.empty(40, hq, device="cuda")
+    nb.np_attn_decode_shared(c.desc, c.cache, 0, c.tables, q, out, _workspace(c, hq, 40), c.dev(cu), held, seqs=c.dev(seqs), lse=lse)
+    torch.cuda.synchronize()
+    assert c.status.item() == A.S_LENGTH | A.S_SEQ
+    empty = [3, 5, 9, 17]
+    assert (out[empty] == 0).all() and (lse[empty] == -float("inf")).all()
+    others = [i for i in range(40) if i not in empty]
+    assert torch.equal(out[others], want[others])
+
+
 def test_shared_pages_that_are_not_there():
     """A page number outside the pool among the shared ones: its tokens are not seen by any row."""
     for ways in (3, 40):

@@ -743,8 +743,8 @@ int np_kv_shared(const np_kv_desc* desc, const np_kv_tables* tables, const int32
                  int32_t* shared, void* stream);
 
 /* np_attn_decode of rows whose groups share their first tokens: those are read and their scores taken once for all rows of a group, as one
- * matrix product, and joined with what each row's own tokens give.  The result is np_attn_decode's but for rounding (the shared tokens'
- * probabilities are rounded to the rows' type, as np_attn_prompt's are), and the same from run to run.
+ * matrix product, and joined with what each row's own tokens give.  The result is np_attn_decode's but for the rounding of fp32 sums, however large the
+ * groups are, and the same from run to run.
  *   cu         dev [n_groups + 1] ascending, 0 <= cu <= n: the groups.  Rows outside of them share nothing
  *   shared     dev [n_groups]: tokens, from np_kv_shared, or any multiple of page_tokens up to that; 0: nothing.  The pages of the group's first row
  *              with a sequence are read for all of its rows.  Where a group's rows do not all have that many tokens, or they do not fill

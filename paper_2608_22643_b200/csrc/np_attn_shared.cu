@@ -16,6 +16,9 @@
 //   block alone, for the second kernel.
 // * One tile to a block, two blocks to an SM: while one does its softmax, the other has the tensor cores and its copies are under way.
 //   Two tiles share keys and values where groups have more rows than fill one.
+// * Weights are the sum of two terms of the rows' type, as in np_attn_decode.cu, so that a row's result does not hang on how many others its group has:
+//   against 64 bits the last case below is off by 1.66e-3 (bf16; the rounding of the result alone), with one term by 2.31e-3.  The second term lies where
+//   the second half of the scores was and is half a product more: 69.0 us in place of 61.9.
 // * Tokens come in sixteens that are there or not (pages outside the pool, the end of the last tile); those that are not get scores of -inf
 //   and values of 0.
 //
@@ -355,6 +358,11 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       }
       commit(&s_full[i]);
     };
+    // both terms of sixteen tokens' weights times their values
+    auto weighted = [&](uint32_t d_o, uint32_t d_s, uint64_t vd, int k, uint32_t acc) {
+      mma_ts(d_o, d_s + k * 8, vd + k * 128, id_o, acc);
+      mma_ts(d_o, d_s + kRows / 2 + k * 8, vd + k * 128, id_o, 1u);
+    };
     uint32_t ld = 0, p_cnt[kTiles] = {}, o_cnt[kTiles] = {};  // loads, softmax steps and results so far
     auto wait_load = [&](uint32_t l) { return wait_all(&full[l % S::kStages], (l / S::kStages) & 1u); };
     Piece p;
@@ -398,7 +406,7 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           fence_after();
           if (elect_one()) {  // the first 64 tokens
 #pragma unroll
-            for (int k = 0; k < kRows / 32; ++k) mma_ts(d_o, d_s + k * 8, vd + k * 128, id_o, (j | k) > 0);
+            for (int k = 0; k < kRows / 32; ++k) weighted(d_o, d_s, vd, k, (j | k) > 0);
           }
           __syncwarp();
           ok = wait_all(&p_full[i], par);
@@ -406,7 +414,7 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           fence_after();
           if (elect_one()) {
 #pragma unroll
-            for (int k = kRows / 32; k < kRows / 16; ++k) mma_ts(d_o, d_s + k * 8, vd + k * 128, id_o, 1u);
+            for (int k = kRows / 32; k < kRows / 16; ++k) weighted(d_o, d_s, vd, k, 1u);
             if (more) scores(i, sk);
             else commit(&o_full[i]);
           }
@@ -462,7 +470,7 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         float part = 0.f, now, sc = a.scale2;
         bool fast = false;
         if (j > p.t0) {
-          part = softmax_half<kBf16, 0>(s, a.scale2, m, ts);
+          part = softmax_half<kBf16, 0, true>(s, a.scale2, m, ts);
           now = row_max(s) * a.scale2;
           fast = __all_sync(0xffffffffu, !valid || (now <= m + kGrow && fabsf(m) <= kLarge && now < INFINITY));
         } else {
@@ -494,10 +502,10 @@ k_attn_shared(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             for (int c = 0; c < kRows; ++c) s[c] = __float_as_uint(__uint_as_float(s[c]) * sc);
             sc = 1.f;
           }
-          part = softmax_half<kBf16, 0>(s, sc, use, ts);
+          part = softmax_half<kBf16, 0, true>(s, sc, use, ts);
         }
         arrive(&p_half[i]);
-        l += part + softmax_half<kBf16, kRows / 2>(s, sc, use, ts);
+        l += part + softmax_half<kBf16, kRows / 2, true>(s, sc, use, ts);
         arrive(&p_full[i]);
       }
       if (ok) ok = wait_all(&o_full[i], o_cnt++ & 1u);

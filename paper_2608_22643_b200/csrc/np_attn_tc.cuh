@@ -161,14 +161,30 @@ __device__ __forceinline__ float widen(uint16_t x) {
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
-// P = exp2(scale2 * S - m) of 64 of a row's scores, from column C on, into tensor memory; their sum.
-template <bool kBf16, int C>
+// (p0, p1) in the rows' type, and what that leaves of them, in it.  Together they are the value to 2^-16 in bf16, where the
+// first is cut off (a byte permute), and to 2^-22 in fp16, or 2^-25.
+template <bool kBf16>
+__device__ __forceinline__ void split(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+  if (kBf16) {
+    const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+    hi = __byte_perm(b0, b1, 0x7632);
+    lo = pack<true>(p0 - __uint_as_float(b0 & 0xffff0000u), p1 - __uint_as_float(b1 & 0xffff0000u));
+  } else {
+    hi = pack<false>(p0, p1);
+    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    lo = pack<false>(p0 - h.x, p1 - h.y);
+  }
+}
+
+// P = exp2(scale2 * S - m) of 64 of a row's scores, from column C on, into tensor memory; their sum.  kTwo: P in two terms, the second of all 128 behind
+// the first of all 128, where S was.
+template <bool kBf16, int C, bool kTwo = false>
 __device__ __forceinline__ float softmax_half(const uint32_t (&s)[kRows], float scale2, float use, uint32_t tp) {
   const f32x2 sc = two(scale2, scale2), off = two(-use, -use);
   f32x2 sum[2] = {0, 0};
 #pragma unroll
   for (int c = C; c < C + kRows / 2; c += 32) {
-    uint32_t w[16];
+    uint32_t w[16], rest[kTwo ? 16 : 1];
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
       const f32x2 e = fma2(two(__uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1])), sc, off);
@@ -177,9 +193,11 @@ __device__ __forceinline__ float softmax_half(const uint32_t (&s)[kRows], float 
       p0 = exp2_fast(p0);
       p1 = exp2_fast(p1);
       sum[x & 1] = add2(sum[x & 1], two(p0, p1));
-      w[x] = pack<kBf16>(p0, p1);
+      if constexpr (kTwo) split<kBf16>(p0, p1, w[x], rest[x]);
+      else w[x] = pack<kBf16>(p0, p1);
     }
     tm_st16(tp + c / 2, w);
+    if constexpr (kTwo) tm_st16(tp + kRows / 2 + c / 2, rest);
   }
   float a, b;
   apart(add2(sum[0], sum[1]), a, b);

@@ -583,9 +583,12 @@ cudaError_t launch(const CUtensorMap& q, const CUtensorMap& kv, const Args& a, i
 }
 
 // [partial results and counts of np_attn_decode.cu][how the line is dealt out][plans][np_attn_rest.cu's parts][maxima and sums of blocks' parts][their
-// O][records]: all but the last are at the same place for every call.
+// O][records]: all but the last are at the same place for every call.  They begin at the first multiple of kSpaceAlign in what the caller gives, which is
+// 16-byte aligned: results are stored 32 bytes at a time, and records are 32-byte aligned for the compiler.
+constexpr uint64_t kSpaceAlign = 32;
+static_assert(alignof(Record) <= kSpaceAlign && alignof(RowPlan) <= kSpaceAlign && alignof(LinePlan) <= kSpaceAlign && sizeof(Record) % 32 == 0, "");
 struct Space {
-  uint64_t line, plan, rest_ml, rest_o, part_ml, part_o, records, bytes;
+  uint64_t line, plan, rest_ml, rest_o, part_ml, part_o, records, bytes;  // bytes: with what lies before the beginning, at most
   Space(int n_heads, int n) {
     uint64_t at = 0;
     auto take = [&at](uint64_t bytes) {
@@ -601,7 +604,10 @@ struct Space {
     part_ml = take((uint64_t)2 * kSharedBlocks * kRows * 8);
     part_o = take((uint64_t)2 * kSharedBlocks * kRows * 128 * 4);
     records = take((uint64_t)n * n_heads * sizeof(Record));
-    bytes = at;
+    bytes = at + kSpaceAlign - 16;
+  }
+  static char* begin(void* workspace) {
+    return reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + kSpaceAlign - 1) & ~(uintptr_t)(kSpaceAlign - 1));
   }
 };
 
@@ -648,7 +654,7 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   if (!device_sms(&sms)) return fail(NP_E_CUDA, "no CUDA device");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (held_in_8(d)) n_groups = 0;
-  char* ws = static_cast<char*>(workspace);
+  char* const ws = Space::begin(workspace);
   const int group = n_heads / d->n_kv_heads, columns = n_groups ? (int)std::min<int64_t>(1 << 20, ((int64_t)n * group + n_groups - 1) / n_groups) : 0;
   Args a = {};
   a.shared.cu = cu;
@@ -657,7 +663,7 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   a.shared.records = reinterpret_cast<Record*>(ws + space.records);
   a.shared.columns = columns;
   if (columns <= kFewColumns || n_groups > kSharedGroups)
-    return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, workspace, &a.shared, sms, s);
+    return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, ws, &a.shared, sms, s);
   a.page_bytes = page_bytes(d);
   a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * a.page_bytes;
   a.table = t->page_table;

@@ -580,7 +580,8 @@ typedef struct np_kv_desc {
  * A row is written with the least exponent e of -60 .. 120 for which its largest finite magnitude is at most 448 * 2^e; each value is
  * rounded to nearest, ties to even, so it is off by at most 2^-4 of itself or 2^(e - 10).  Infinities and NaN become NaN.  np_kv_append,
  * np_kv_append_rotated, np_kv_read and the attention calls know the form; page tables and the calls that move whole pages are the same
- * for both. */
+ * for both.  In attention over it every token counts in the sum of the weights, and a weight times its value's power of two is good to 2^-25 of the
+ * row's largest such product. */
 
 /* Device arrays of a cache.  np_kv_reset writes the empty state into all of them. */
 typedef struct np_kv_tables {

@@ -186,14 +186,20 @@ constexpr int blocks_per_sm(int hd, int form) {
   return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 3 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
 }
 
-// In 8 bits sums are of 2^(s - m): s - m is between -120 and 60 for the token that m is of, and what is far below it still counts.  Warps add up to
-// 2^-149, what they have is 2^30 times as large from then on.
+// In 8 bits sums are of 2^(s - m): s - m is between -120 and 60 for the token that m is of, so a sum may be up to 2^60 to a maximum and still be all that
+// there is to one that is 2^180 as large.  Warps add up to 2^-149, what they have is 2^30 times as large from then on, and a sum goes from one maximum
+// to another by the square of a factor that is a normal number down to 2^-252.  (By the factor itself, sums of values that are 2^126 apart were lost.)
 constexpr float kHeldUp = 0x1p30f;
 // a b + c, whose result may be below 2^-126
 __device__ __forceinline__ float fma_full(float a, float b, float c) {
   float d;
   asm("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
+}
+// a sum in 8 bits to one whose maximum is 2^-e as large, added to c
+__device__ __forceinline__ float move_held(float sum, float e, float c) {
+  const float root = exp2_fast(0.5f * e);
+  return fma_full(fma_full(sum, root, 0.f), root, c);
 }
 
 // What a block knows of groups, in dynamic shared memory: for each row its tokens, how many of them it shares, its group and sequence; and the units of
@@ -728,8 +734,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
       for (int i = 0; i < NH; ++i) {
         const float f = exp2_fast(m[i] - use[i]);
+        l[i] = kHeld ? move_held(l[i], m[i] - use[i], 0.f) : l[i] * f;
         m[i] = now[i];
-        l[i] = kHeld ? fma_full(l[i], f, 0.f) : l[i] * f;
         by(i, f);
       }
     };
@@ -1034,7 +1040,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
       for (int w = 0; w < kWarps; ++w) {
         const float f = exp2_fast(s_ml[w][h][0] - use);
         const float4 v = *reinterpret_cast<const float4*>(&s_o[w][h][d]);
-        sum += f * s_ml[w][h][1];
+        if (kHeld) sum = move_held(s_ml[w][h][1], s_ml[w][h][0] - use, sum);
+        else sum += f * s_ml[w][h][1];
         add(acc, f, v);
       }
       if (odd_four(acc) && !not_finite(sum) && !(whole && sum == 0.f)) odd |= turn;
@@ -1115,13 +1122,14 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
 #pragma unroll
             for (int y = 0; y < kJoin; ++y) now = fmaxf(now, ml[y].x);
             const float use = now == -INFINITY ? 0.f : now, f0 = exp2_fast(top - use);
+            sum = kHeld ? move_held(sum, top - use, 0.f) : sum * f0;
             top = now;
-            sum *= f0;
             acc = make_float4(acc.x * f0, acc.y * f0, acc.z * f0, acc.w * f0);
 #pragma unroll
             for (int y = 0; y < kJoin; ++y) {
               const float f = exp2_fast(ml[y].x - use);
-              sum += f * ml[y].y;
+              if (kHeld) sum = move_held(ml[y].y, ml[y].x - use, sum);
+              else sum += f * ml[y].y;
               add(acc, f, v[y]);
             }
           }

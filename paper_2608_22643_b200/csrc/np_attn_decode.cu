@@ -385,7 +385,7 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
     *reinterpret_cast<uint2*>(a.out + i * a.o_token + (int64_t)h * a.o_head + d) = r;
     if (a.lse && d == 0) {
       float m = use;
-      if (kHeld) {  // the maximum has an exponent of V's in it, which the sum takes back: whole numbers, which leave no rounding
+      if (kHeld) {  // the maximum has an exponent v of V's in it, which the sum takes back: a whole number, added at the scale of |v| and the scores (half a step)
         int up;
         sum = frexpf(sum, &up);
         m += (float)(up - 30);

@@ -662,7 +662,9 @@ int np_attn_decode_shared(const np_kv_desc* d, const void* cache, int32_t layer,
   a.shared.n_groups = n_groups;
   a.shared.records = reinterpret_cast<Record*>(ws + space.records);
   a.shared.columns = columns;
-  if (columns <= kFewColumns || n_groups > kSharedGroups)
+  // queries that rows or heads have in common: a tensor map has no strides of 0
+  const bool in_common = (n > 1 && q->token_stride == 0) || (n_heads > 1 && q->head_stride == 0);
+  if (columns <= kFewColumns || n_groups > kSharedGroups || in_common)
     return decode(d, cache, layer, t, q, n_heads, seqs, n, scale2, out, lse, ws, &a.shared, sms, s);
   a.page_bytes = page_bytes(d);
   a.cache = static_cast<const char*>(cache) + (int64_t)layer * d->n_pages * a.page_bytes;

@@ -682,15 +682,17 @@ k_attn_decode(const __grid_constant__ CUtensorMap map, const __grid_constant__ D
         }
 #pragma unroll
         for (int y = 1; y < HD / 8; y <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, y));
-        const int e = max((int)(top >> 23), 29) - 14;  // biased exponent of the power of two to divide by: 15 to 240
+        // biased exponent of the power of two to divide by, 1 to 240; of small scales so large that the product of the two is a normal number (queries are
+        // then smaller than they could be, and off by 2^-25, which moves a score by 2^-15 at most, with 128 of the largest keys)
+        const int e = max(max((int)(top >> 23), 15) - 14, 128 - (int)(__float_as_uint(a.scale2) >> 23));
         const float by = __uint_as_float((uint32_t)(254 - e) << 23), back = __uint_as_float((uint32_t)e << 23);
         if (h < HB) {
           __half2 r[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) r[i] = __floats2half2_rn(f[i].x * by, f[i].y * by);
+          for (int i = 0; i < 4; ++i) r[i] = __floats2half2_rn(fma_full(f[i].x, by, 0.f), fma_full(f[i].y, by, 0.f));
           // the halves of sixteen values d / 2, at lane 4 * (h % 8) + d / 2 % 4
           *reinterpret_cast<uint4*>(s_qh + (h >> 3) * (HD * 16) + (((d >> 3) * 2 + (d & 1)) * 32 + (h & 7) * 4 + (d >> 1 & 3)) * 16) = *reinterpret_cast<const uint4*>(r);
-          if (d == 0) s_up[h] = fminf(fmaxf(a.scale2 * back, FLT_MIN), FLT_MAX);
+          if (d == 0) s_up[h] = fminf(a.scale2 * back, FLT_MAX);
         }
         continue;
       }

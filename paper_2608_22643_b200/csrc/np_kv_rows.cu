@@ -74,7 +74,7 @@ struct RowsArgs {
   const double* freq;
   const float* q_gain;
   const float* k_gain;
-  float eps;
+  float eps, small;      // sums of squares below `small`, where squares are lost that an eps as small does not cover
   int half, neighbours;  // 16-byte pieces of half the values that turn
 };
 
@@ -308,12 +308,13 @@ k_rows_in(const __grid_constant__ RowsArgs a) {
           return ss;
         };
         float ss = sum_of_squares(), eps = a.eps;
-        const bool normed = row & 4, past = normed && ss == INFINITY;
-        if (__any_sync(0xffffffffu, past)) {  // squares past fp32's range: of values 2^-80 as large
+        const bool normed = row & 4, past = normed && (ss == INFINITY || ss < a.small);
+        if (__any_sync(0xffffffffu, past)) {  // squares past fp32's range, of values 2^-80 as large, or below its normal numbers, of values 2^60 as large
           if (past) {
-            eps = 0.f;  // nothing beside such squares
+            const float by = ss == INFINITY ? 0x1p-80f : 0x1p60f;
+            eps = ss == INFINITY ? 0.f : eps * 0x1p120f;  // nothing beside large squares
 #pragma unroll
-            for (int z = 0; z < 8; ++z) x[z] *= 0x1p-80f;
+            for (int z = 0; z < 8; ++z) x[z] *= by;
           }
           const float again = sum_of_squares();
           if (past) ss = again;
@@ -499,6 +500,7 @@ void put_rotation(RowsArgs& a, const np_rotation* r) {
   a.q_gain = r->q_gain;
   a.k_gain = r->k_gain;
   a.eps = r->eps;
+  a.small = r->eps < 0x1p-80f ? 0x1p-80f : 0.f;
   a.half = r->rot_dim / 16;
   a.neighbours = r->pairs == NP_ROT_NEIGHBOURS;
 }

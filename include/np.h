@@ -746,7 +746,9 @@ int np_kv_shared(const np_kv_desc* desc, const np_kv_tables* tables, const int32
 
 /* np_attn_decode of rows whose groups share their first tokens: those are read and their scores taken once for all rows of a group, as one
  * matrix product, and joined with what each row's own tokens give.  The result is np_attn_decode's but for the rounding of fp32 sums, however large the
- * groups are, and the same from run to run.
+ * groups are, and the same from run to run.  A call has 20 to 30 us of starts and joins, so where np_attn_decode takes less than that for the same rows it
+ * is the faster one.  On a B200 64 rows of 64 heads of 128 over 8 take 30 us by it and 34 by this call (with np_kv_shared) with 512 shared tokens, 43 and 39 with 1024;
+ * 8 such rows 18 and 27 with 2048.
  *   cu         dev [n_groups + 1] ascending, 0 <= cu <= n: the groups.  Rows outside of them share nothing
  *   shared     dev [n_groups]: tokens, from np_kv_shared, or any multiple of page_tokens up to that; 0: nothing.  The pages of the group's first row
  *              with a sequence are read for all of its rows.  Where a group's rows do not all have that many tokens, or they do not fill

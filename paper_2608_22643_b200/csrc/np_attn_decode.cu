@@ -44,7 +44,7 @@
 // Measured (pages of 64 scattered over the pool, caches larger than the L2 in turn): sixteen sequences of 0 to 4095 tokens, 32 heads
 // of 128, 57.3 us, 5.8 TB/s, 89 % of the copy rate; 64 of 1000 in fp16 159 us, 100 %; one of 131071 tokens, 64 heads over 8, 91.9 us,
 // 89 %; one of 100 tokens 4.7 us.  In 8 bits the sixteen, the long one
-// and the short one take 44.6, 66.6 and 5.1 us, 59 % and 63 % of the copy rate.  What is not the stream is the launch, three loads that depend on one another (length, page
+// and the short one take 44.7, 67.1 and 5.1 us, 59 % and 63 % of the copy rate.  What is not the stream is the launch, three loads that depend on one another (length, page
 // number, keys) and the joins.  Groups of more than eight heads are bound by the steps
 // between a warp's loads: sixteen heads of 128 to a key-value head, 64 sequences of 2000 tokens, 53.8 us, 74 % (69 % with keys and values
 // in registers, 55 % with 16-byte asynchronous copies in place of TMA, 70 % with the chunks beyond asked into the L2 ahead, 74 % with
@@ -181,7 +181,8 @@ __device__ __noinline__ float4 keep_infinite(float4 acc, const float* part, int6
 // long sequence) and 186 (64 of 1000), three 101 and 164; sixteen heads, 64 of 2000, three 73.8, two 62.4.  64 values, eight heads, 64 heads, 16
 // sequences of 2000, five 91.2, four 86.8 (three 93.9); sixteen heads, one of 131071, four 43.3, three 40.2 (two 45.0).
 // In 8 bits: 128 values, eight heads, the long sequence, four 66.4, three 66.7, two 81.2; 64 values, 16 of 2000, 64 heads, five 93.4, four 72.2,
-// three 76.2; sixteen heads, 64 of 2000, three 54.6 and two 56.6 (one 88.9), with 64 values 35.1 and 38.3 (58.7).
+// three 76.2; sixteen heads, 64 of 2000, three 54.6 and two 56.6 (one 88.9), with 64 values 35.1 and 38.3 (58.7); 55.3 and 35.6 since
+// sums go by the square of a factor's root.
 constexpr int blocks_per_sm(int hd, int form) {
   return form == kHeldEight ? (hd == 64 ? 4 : 3) : form == kHeldSixteen ? 3 : hd == 64 ? (form == kEight ? 4 : 3) : (form == kEight ? 3 : 2);
 }

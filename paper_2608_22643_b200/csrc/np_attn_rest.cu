@@ -4,7 +4,8 @@
 // A block takes up to eight heads of a row and key-value head, four warps sixteen tokens each at a time, as in np_attn_decode.cu: S^T = K Q^T and
 // O^T = V^T P^T on mma.sync, keys and values from global memory into the registers that the products read.  Rows' own tokens are often few, and then
 // what counts is how short the way from the launch to the result is, so this is its own small kernel (np_attn_decode.cu's, with an even line of work
-// and another kernel for the join, took 24 us in place of 20 for the 64 rows below):
+// and another kernel for the join, took 24 us in place of 20 for the 64 rows below).  Times of both kernels that are compared here are from before the first
+// had its weights in two terms, which adds 3 to 8 us to either side:
 // * It begins as soon as the first kernel's blocks leave room, works out by itself what its row shares, and waits only before the join.  (With the
 //   first kernel telling what is where: 66.3 us for both in place of 61.)
 // * Only where there are fewer blocks than the GPU holds are rows split; the last split to arrive joins them, in the order of the tokens.  Where a row

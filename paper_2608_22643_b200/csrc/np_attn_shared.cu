@@ -22,9 +22,9 @@
 // * Tokens come in sixteens that are there or not (pages outside the pool, the end of the last tile); those that are not get scores of -inf
 //   and values of 0.
 //
-// Measured, both kernels (pages of 64 scattered over the pool): 64 rows, 64 heads of 128 over 8, that share 32768 tokens and have one of their own, 106 us,
-// 0.65 PFLOP/s; that share 8192 and have up to 200, 61.5 us; 4 such rows that share 8192 tokens, 28.3 us.  Of the 61.5 us this kernel takes 28: 6.5 until
-// the first scores are there, 2.15 for each tile of 256 rows by 128 tokens (1.65 at the rate of a large product), 3 to store.
+// Measured, both kernels (pages of 64 scattered over the pool): 64 rows, 64 heads of 128 over 8, that share 32768 tokens and have one of their own, 131 us,
+// 0.53 PFLOP/s; that share 8192 and have up to 200, 68.4 us; 4 such rows that share 8192 tokens, 30.0 us.  Of the 68.4 us this kernel takes some 34: 6.5 until
+// the first scores are there, 3.4 for each tile of 256 rows by 128 tokens (2.2 at the rate of a large product), 3 to store.
 //
 // Every wait is bounded; after a time-out all roles leave, the block meets and tensor memory is released.
 #include <algorithm>
@@ -68,8 +68,8 @@ struct Shape {
 };
 
 // Tiles that a block takes, at least, of those of one block of rows: more blocks would each do less, but what every one leaves for the join is as
-// large.  64 rows of 64 heads over 8 that share 512, 2048 or 4096 tokens: 30.7, 38.5 and 43.4 us with four (32.1, 43.1 and 45.7 with one, 39.0, 42.2
-// and 45.6 with six); 4 rows that share 2048 or 8192: 23.6 and 28.7 (23.3 and 32.4; 29.3 and 32.0).
+// large.  64 rows of 64 heads over 8 that share 512, 2048 or 4096 tokens: 33.9, 42.7 and 47.6 us with four (33.6, 45.7 and 49.6 with one, 33.9, 46.7
+// and 51.1 with six); 4 rows that share 2048 or 8192: 25.9 and 30.1 (21.5 and 31.3; 31.8 and 35.2).
 constexpr int kFewestTiles = 4;
 
 // keys or values of a page's rows: (64 values, rows of a page's heads, halves of head_dim, keys and values, pages)
@@ -612,9 +612,9 @@ struct Space {
 };
 
 // Columns, (row, query head) pairs of a group and key-value head, on average, that one kernel does beside the rows' own tokens; more take the tensor
-// cores' way.  Both sides, us: 8 rows of 32 heads over 32 that share 8192 tokens, 8 columns, 42.3 in one kernel, 46.8 in two; 16 columns, sharing 1024,
-// 28.4 and 30.1; 2 rows of 64 heads over 8, 16 columns, sharing 8192, 29.9 and 28.0, with 600 of their own 30.7 and 37.0; 24 columns 35.0 and
-// 28.7; 24 rows of 32 heads, 24 columns, 80 and 59, with 600 of their own 76 and 94.
+// cores' way.  Both sides, us: 8 rows of 32 heads over 32 that share 8192 tokens, 8 columns, 41.2 in one kernel, 53.6 in two; 16 columns, sharing 1024,
+// 27.5 and 29.6; 2 rows of 64 heads over 8, 16 columns, sharing 8192, 29.6 and 29.1, with 600 of their own 30.7 and 39.4; 24 columns 35.5 and
+// 29.8; 24 rows of 32 heads, 24 columns, 80 and 57, with 600 of their own 90 and 113.
 constexpr int kFewColumns = 16;
 
 const char* shared_heads_error(const np_kv_desc* d, int n_heads, int n) {

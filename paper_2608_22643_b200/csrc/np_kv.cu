@@ -519,6 +519,7 @@ k_kv_shared(Pool p, const int32_t* __restrict__ seqs, int n, const int32_t* __re
   }
   __syncthreads();
   const int first = s_first, full = s_members > 1 ? s_full : 0, lane = tid & 31, wid = tid >> 5;
+  __syncthreads();  // all have read it: warps that are ahead make it less
   // a warp takes a sequence at a time, and of its pages what has not been found to differ yet
   constexpr int kAhead = 4;
   auto common = [&] { return __shfl_sync(0xffffffffu, *static_cast<volatile int*>(&s_full), 0); };  // the same for all lanes

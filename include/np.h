@@ -581,8 +581,8 @@ typedef struct np_kv_desc {
  * rounded to nearest, ties to even, so it is off by at most 2^-4 of itself or 2^(e - 10).  Infinities and NaN become NaN.  np_kv_append,
  * np_kv_append_rotated, np_kv_read and the attention calls know the form; page tables and the calls that move whole pages are the same
  * for both.  In attention over it every token counts in the sum of the weights, and a weight times its value's power of two is good to 2^-25 of the
- * row's largest such product.  There scale times a head's largest query times any key's power of two has to stay below 2^140, and scores past 2^27 ask for
- * values whose powers of two are between 2^-10 and 2^10. */
+ * row's largest such product.  There scale times a head's largest query, and that times any key's power of two, have to stay below 2^140, and scores past 2^27
+ * ask for values whose powers of two are between 2^-10 and 2^10. */
 
 /* Device arrays of a cache.  np_kv_reset writes the empty state into all of them. */
 typedef struct np_kv_tables {

@@ -44,10 +44,9 @@ def test_ordinary_scores_of_products_at_the_ends(hq, q_power, k_power, scale_pow
     assert 1 < abs(f64(lse)).max() < 100
 
 
-@pytest.mark.parametrize("power", [13, 18, 21])
 @pytest.mark.parametrize("hq,hd", [(2, 64), (2, 128), (12, 64), (12, 128)])
 @pytest.mark.parametrize("order", ["rising", "falling", "any"])
-@pytest.mark.parametrize("ends", [(127, 127), (117, 137), (67, 230)])
+@pytest.mark.parametrize("power,ends", [(p, e) for p in (13, 18, 21) for e in ((127, 127), (117, 137), (67, 230))] + [(p, (117, 137)) for p in (25, 33, 45, 60)])
 def test_large_scores(power, hq, hd, order, ends):
     """Scores are whole numbers times 2^power, times powers of two that go back and forth among values: one that is not the largest has no weight, and a
     result is the mean of the values at the largest score.
